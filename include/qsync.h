@@ -24,7 +24,7 @@
  *    hipError_t of the failing call on this thread.
  *  - A tensor with rows*cols == 0 (or a GEMM with M*N == 0) is a successful no-op.
  *    A GEMM with K == 0 writes the bias (or zeros).
- *  - Inputs must be finite; behaviour on NaN/Inf is unspecified.
+ *  - Inputs must be finite; behaviour on NaN/Inf is unspecified, except where a call says otherwise.
  *  - Calls on different streams may run concurrently as long as their buffers are disjoint.
  */
 #ifndef QSYNC_H
@@ -40,8 +40,9 @@ extern "C" {
 /* Per-operator precision tag b_io (paper: problem (1); evaluation uses INT8, FP16, FP32). */
 typedef enum { QSYNC_INT8 = 8, QSYNC_FP16 = 16, QSYNC_FP32 = 32 } qsync_prec_t;
 
-/* Element type of a buffer. */
-typedef enum { QSYNC_F32 = 0, QSYNC_F16 = 1, QSYNC_I8 = 2, QSYNC_I32 = 3 } qsync_dtype_t;
+/* Element type of a buffer.  QSYNC_BF16 and QSYNC_I64: layer norm and logits only (qsync_layernorm_*, qsync_token_logprobs*,
+ * qsync_distill_topk); every other call answers QSYNC_ERR_BAD_ENUM to them. */
+typedef enum { QSYNC_F32 = 0, QSYNC_F16 = 1, QSYNC_I8 = 2, QSYNC_I32 = 3, QSYNC_BF16 = 4, QSYNC_I64 = 5 } qsync_dtype_t;
 
 /* Granularity of a scale: one per tensor ("layer-wise"), one per row, or one per column
  * ("channel-wise"; paper, Cost Mapper paragraph on quantization methods). */
@@ -594,6 +595,120 @@ typedef struct { double sumsq; double amax; int64_t D; } qsync_tensor_stats_t;
 int qsync_variance_increment(int kind, const qsync_tensor_stats_t* x, const qsync_tensor_stats_t* v,
                              const qsync_tensor_stats_t* grad_v, double q_x, double q_v, int k, double gamma,
                              int64_t d_o, int64_t d_L, double* sigma_fp, double* sigma_bp, double* omega);
+
+/*
+ * qsync_layernorm_fwd - layer norm over the columns of a matrix: what stands in front of a linear operator.
+ *
+ *   mean[r] = sum_c x[r,c] / cols        rstd[r] = 1 / sqrt(sum_c (x[r,c] - mean[r])^2 / cols + eps)
+ *   y[r,c]  = (x[r,c] - mean[r]) rstd[r] gamma[c] + beta[c]
+ *
+ * x          [rows, ld] of xdt (QSYNC_F32, QSYNC_F16 or QSYNC_BF16), ld >= cols.
+ * gamma_opt, beta_opt   cols floats each, or NULL (1 and 0).
+ * eps        finite and positive (QSYNC_ERR_UNSUPPORTED otherwise).
+ * y          out, packed [rows, cols] of ydt (the same three types), rounded once to nearest even.  It may be x itself when the
+ *            types agree and ld == cols; any other overlap is QSYNC_ERR_UNSUPPORTED.
+ * mean_opt, rstd_opt    out, rows floats each, or NULL: what qsync_layernorm_bwd reads.
+ * y_amax_opt device float or NULL: raised to max |y| as stored, under the rules of qsync_qlinear_fwd_amax, so that an INT8
+ *            operator fed by y takes its scale from it (qsync_scale_from_amax) without a pass over y.
+ * All statistics are fp32, the variance from differences to the mean.  Pointers need the alignment of their elements.
+ * A NaN or an infinity makes its own row NaN (or infinite) and no other.
+ */
+int qsync_layernorm_fwd(const void* x, int xdt, int64_t rows, int64_t cols, int64_t ld, const float* gamma_opt,
+                        const float* beta_opt, float eps, void* y, int ydt, float* mean_opt, float* rstd_opt,
+                        float* y_amax_opt, void* stream);
+
+/*
+ * qsync_layernorm_bwd - gradients of qsync_layernorm_fwd.  With xh = (x - mean) rstd and g = dy gamma:
+ *
+ *   dx[r,c] = rstd[r] (g[r,c] - sum_j g[r,j] / cols - xh[r,c] sum_j g[r,j] xh[r,j] / cols)
+ *   dgamma[c] = sum_r dy[r,c] xh[r,c]        dbeta[c] = sum_r dy[r,c]
+ *
+ * dy         [rows, lddy] of dydt, x [rows, ldx] of xdt; mean and rstd as qsync_layernorm_fwd left them.
+ * dx_opt     out, packed [rows, cols] of dxdt, or NULL.  It may be dy or x itself when the types agree and that tensor is packed;
+ *            any other overlap is QSYNC_ERR_UNSUPPORTED.
+ * dgamma_opt, dbeta_opt  out, cols floats each, or NULL; zeros when rows == 0.  Summed in fp32 in an order that depends on the
+ *            sizes alone.  One of the three outputs is required.
+ * workspace  at least qsync_layernorm_bwd_workspace_bytes(rows, cols) bytes, 16-byte aligned, no contents needed; NULL when
+ *            neither dgamma nor dbeta is wanted.
+ */
+int qsync_layernorm_bwd(const void* dy, int dydt, int64_t lddy, const void* x, int xdt, int64_t rows, int64_t cols, int64_t ldx,
+                        const float* gamma_opt, const float* mean, const float* rstd, void* dx_opt, int dxdt,
+                        float* dgamma_opt, float* dbeta_opt, void* workspace, size_t workspace_bytes, void* stream);
+size_t qsync_layernorm_bwd_workspace_bytes(int64_t rows, int64_t cols);
+
+/*
+ * qsync_token_logprobs - log probabilities of given tokens under the logits of a language model's head, with the entropy and the
+ * top alternatives of every position.  With p[r,:] = softmax(scale * logits[r,:]):
+ *
+ *   logp[r] = log p[r, tokens[r]]        entropy[r] = -sum_c p[r,c] log p[r,c]
+ *   top_index[r, 0..top_k-1] = the columns of the top_k largest logits in descending order, among equal ones the lower column
+ *   first;  top_logp[r,i] = log p[r, top_index[r,i]]
+ *
+ * logits     [rows, ld] of ldt (QSYNC_F32, QSYNC_F16 or QSYNC_BF16), ld >= cols, cols <= 2^30.
+ * scale      1 / temperature: finite and positive (QSYNC_ERR_UNSUPPORTED otherwise).
+ * tokens_opt rows integers of tdt (QSYNC_I32 or QSYNC_I64); required with logp_opt.  A negative token marks a position without
+ *            one: logp 0.  A token of cols or more: logp NaN; nothing is read there.
+ * logp_opt, entropy_opt   out, rows floats each, or NULL.
+ * stats_opt  out, [rows, 2] floats or NULL: the row's largest logit m and ln sum_c exp(scale (logits - m)), which
+ *            qsync_token_logprobs_bwd reads.
+ * top_k      0..64 (QSYNC_ERR_UNSUPPORTED beyond), at most cols; 0: top_logp_opt and top_index_opt are ignored, else required:
+ *            [rows, top_k] floats and int32.
+ * At least one output is required.
+ * workspace  at least qsync_token_logprobs_workspace_bytes(ldt, rows, cols, top_k) bytes, 16-byte aligned, no contents needed (what
+ *            is enough for some number of rows is enough for fewer).
+ * A logit of -inf (a masked one) has p = 0 and takes no part in the entropy.  A row of nothing else: logp and top_logp -inf, entropy
+ * 0, and as alternatives its first columns.  A logit of +inf or NaN makes the row's logp, entropy and top_logp NaN, and the columns of its
+ * alternatives unspecified (-1 or a column of the row).
+ */
+int qsync_token_logprobs(const void* logits, int ldt, int64_t rows, int64_t cols, int64_t ld, float scale,
+                         const void* tokens_opt, int tdt, float* logp_opt, float* entropy_opt, float* stats_opt, int top_k,
+                         float* top_logp_opt, int32_t* top_index_opt, void* workspace, size_t workspace_bytes, void* stream);
+size_t qsync_token_logprobs_workspace_bytes(int ldt, int64_t rows, int64_t cols, int top_k);
+
+/*
+ * qsync_token_logprobs_bwd - gradient of sum_r (dlogp[r] logp[r] + dentropy[r] entropy[r]) with respect to the logits:
+ *
+ *   dlogits[r,c] = scale (dlogp[r] ([c == tokens[r]] - p[r,c]) - dentropy[r] p[r,c] (log p[r,c] + entropy[r]))
+ *
+ * logits, ldt, rows, cols, ld, scale, tokens_opt, tdt  as in the forward call; stats and entropy as it left them.
+ * dlogp_opt  rows floats or NULL (0), with tokens_opt.  A position without a token has no gradient of logp; a token of cols or
+ *            more makes the row NaN.
+ * dentropy_opt rows floats or NULL (0), with entropy_opt.  One of the two is required.
+ * dlogits    out, packed [rows, cols] of ddt (the same three types), rounded once.  It may be the logits themselves when the types
+ *            agree and ld == cols; any other overlap is QSYNC_ERR_UNSUPPORTED.
+ * Masked logits (-inf) and rows of nothing else have a gradient of 0, and so have rows whose dlogp and dentropy are 0, whatever
+ * their logits hold.
+ */
+int qsync_token_logprobs_bwd(const void* logits, int ldt, int64_t rows, int64_t cols, int64_t ld, float scale,
+                             const void* tokens_opt, int tdt, const float* stats, const float* entropy_opt,
+                             const float* dlogp_opt, const float* dentropy_opt, void* dlogits, int ddt, void* stream);
+
+/*
+ * qsync_distill_topk - distillation of a student from a teacher's top logits, the loss and its gradient.  Of every position the
+ * teacher gives k columns with their logits (or log probabilities: a constant of the row does not matter).  With
+ * q[r,:] = softmax(scale * teacher[r,:]) over the k entries and p[r,:] = softmax(scale * logits[r,:]) over all columns:
+ *
+ *   loss[r]      = sum_i q[r,i] (log q[r,i] - log p[r, index[r,i]])
+ *   dlogits[r,c] = weight[r] scale (p[r,c] - sum over i with index[r,i] == c of q[r,i])       (gradient of sum_r weight[r] loss[r])
+ *
+ * logits     [rows, ld] of ldt (QSYNC_F32, QSYNC_F16 or QSYNC_BF16): the student's.  cols <= 2^30.
+ * scale      1 / temperature: finite and positive (QSYNC_ERR_UNSUPPORTED otherwise).
+ * teacher    packed [rows, k] of teacher_dt (the same three types); index packed [rows, k] of idt (QSYNC_I32 or QSYNC_I64).
+ *            k 1..256 (QSYNC_ERR_UNSUPPORTED beyond).  A negative index, or a teacher's logit of -inf, is no entry; a column that is
+ *            given twice counts twice.
+ * weight_opt rows floats or NULL (1): of the gradient only.  0: the row's gradient is 0 whatever its logits hold.
+ * loss       out, rows floats.
+ * dlogits_opt out, packed [rows, cols] of ddt (the same three types), rounded once, or NULL for the loss alone.  It may be the logits
+ *            themselves when the types agree and ld == cols; any other overlap is QSYNC_ERR_UNSUPPORTED.
+ * workspace  at least qsync_distill_topk_workspace_bytes(ldt, rows, cols) bytes, 16-byte aligned, no contents needed (what is
+ *            enough for some number of rows is enough for fewer).
+ * A row without entries: loss 0, gradient 0.  An index of cols or more, or a NaN of the teacher's: loss and gradient NaN; nothing is
+ * read or written there.  A student's row of -inf alone: loss +inf, gradient 0; p = 0 in any masked column.
+ */
+int qsync_distill_topk(const void* logits, int ldt, int64_t rows, int64_t cols, int64_t ld, float scale, const void* teacher,
+                       int teacher_dt, const void* index, int idt, int64_t k, const float* weight_opt, float* loss,
+                       void* dlogits_opt, int ddt, void* workspace, size_t workspace_bytes, void* stream);
+size_t qsync_distill_topk_workspace_bytes(int ldt, int64_t rows, int64_t cols);
 
 /* hipError_t (as int) of the last failing HIP call made by this thread, 0 if none. */
 int qsync_last_hip_error(void);

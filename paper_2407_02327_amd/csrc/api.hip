@@ -5,6 +5,8 @@
 #include "../../include/qsync_debug.h"
 #include "kernels.h"
 
+#include <cmath>
+#include <initializer_list>
 #include <limits>
 
 using namespace qsync;
@@ -24,6 +26,10 @@ int hip_status(hipError_t e)
 }
 
 bool is_float_dtype(int dt) { return dt == QSYNC_F32 || dt == QSYNC_F16; }
+// what layer norm and the calls on logits take
+bool is_row_dtype(int dt) { return dt == QSYNC_F32 || dt == QSYNC_F16 || dt == QSYNC_BF16; }
+bool is_index_dtype(int dt) { return dt == QSYNC_I32 || dt == QSYNC_I64; }
+int64_t dtype_bytes(int dt) { return dt == QSYNC_I64 ? 8 : dt == QSYNC_F32 || dt == QSYNC_I32 ? 4 : 2; }
 bool is_tag(int t) { return t == QSYNC_INT8 || t == QSYNC_FP16 || t == QSYNC_FP32; }
 bool is_gran(int g) { return g == QSYNC_PER_TENSOR || g == QSYNC_PER_ROW || g == QSYNC_PER_COL; }
 bool is_round(int r) { return r == QSYNC_ROUND_NEAREST || r == QSYNC_ROUND_STOCHASTIC || r == QSYNC_ROUND_FLOOR; }
@@ -65,6 +71,22 @@ bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes)
 {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return a && b && x < y + static_cast<uintptr_t>(b_bytes) && y < x + static_cast<uintptr_t>(a_bytes);
+}
+
+// elements at their own alignment (NULL is)
+bool elements_aligned(const void* p, int dt) { return reinterpret_cast<uintptr_t>(p) % static_cast<uintptr_t>(dtype_bytes(dt)) == 0; }
+bool floats_aligned(std::initializer_list<const float*> ps)
+{
+    for(const float* p : ps)
+        if(!elements_aligned(p, QSYNC_F32)) return false;
+    return true;
+}
+bool positive(float v) { return std::isfinite(v) && v > 0.0f; }
+// A packed result of row-wise kernels against one of their sources [rows, ld]: apart, or in its place element for element.
+bool in_place_or_apart(const void* out, int odt, const void* in, int idt, int64_t rows, int64_t cols, int64_t ld)
+{
+    if(out == in) return odt == idt && (ld == cols || rows == 1);
+    return !overlap(out, rows * cols * dtype_bytes(odt), in, ((rows - 1) * ld + cols) * dtype_bytes(idt));
 }
 
 // (Beside the last launch and with the cast of dY summing its columns, whole steps: FP16 2056x1000x1032 from fp32 gradients 61.7
@@ -985,6 +1007,127 @@ int qsync_dequantize(const void* a, int adt, int64_t rows, int64_t cols, int64_t
     return hip_status(launch_dequantize(a, adt == QSYNC_I32 ? kI32 : kI8, rows, cols, ld, row_scale_opt, col_scale_opt,
                                         tensor_scale, tensor_scale_dev_opt, col_bias_opt, y, ydt,
                                         static_cast<hipStream_t>(stream)));
+}
+
+// ---- layer norm, logits --------------------------------------------------------------------------
+int qsync_layernorm_fwd(const void* x, int xdt, int64_t rows, int64_t cols, int64_t ld, const float* gamma_opt, const float* beta_opt,
+                        float eps, void* y, int ydt, float* mean_opt, float* rstd_opt, float* y_amax_opt, void* stream)
+{
+    if(!x || !y) return QSYNC_ERR_NULL;
+    if(!is_row_dtype(xdt) || !is_row_dtype(ydt)) return QSYNC_ERR_BAD_ENUM;
+    if(!count_ok(rows, cols) || ld < cols || !count_ok(rows, ld)) return QSYNC_ERR_BAD_SHAPE;
+    if(!positive(eps)) return QSYNC_ERR_UNSUPPORTED;
+    if(rows == 0 || cols == 0) return QSYNC_OK;
+    if(!elements_aligned(x, xdt) || !elements_aligned(y, ydt) || !floats_aligned({gamma_opt, beta_opt, mean_opt, rstd_opt, y_amax_opt}))
+        return QSYNC_ERR_ALIGN;
+    if(!in_place_or_apart(y, ydt, x, xdt, rows, cols, ld)) return QSYNC_ERR_UNSUPPORTED;
+    return hip_status(launch_layernorm_fwd(x, xdt, rows, cols, ld, gamma_opt, beta_opt, eps, y, ydt, mean_opt, rstd_opt, y_amax_opt,
+                                           static_cast<hipStream_t>(stream)));
+}
+
+size_t qsync_layernorm_bwd_workspace_bytes(int64_t rows, int64_t cols)
+{
+    if(!count_ok(rows, cols) || rows == 0 || cols == 0) return 0;
+    return round256(layernorm_bwd_workspace_bytes(rows, cols));
+}
+
+int qsync_layernorm_bwd(const void* dy, int dydt, int64_t lddy, const void* x, int xdt, int64_t rows, int64_t cols, int64_t ldx,
+                        const float* gamma_opt, const float* mean, const float* rstd, void* dx_opt, int dxdt, float* dgamma_opt,
+                        float* dbeta_opt, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if(!dy || !x || !mean || !rstd || (!dx_opt && !dgamma_opt && !dbeta_opt)) return QSYNC_ERR_NULL;
+    if(!is_row_dtype(dydt) || !is_row_dtype(xdt) || (dx_opt && !is_row_dtype(dxdt))) return QSYNC_ERR_BAD_ENUM;
+    if(!count_ok(rows, cols) || lddy < cols || ldx < cols || !count_ok(rows, lddy) || !count_ok(rows, ldx)) return QSYNC_ERR_BAD_SHAPE;
+    if(cols == 0) return QSYNC_OK;
+    if(!elements_aligned(dy, dydt) || !elements_aligned(x, xdt) || (dx_opt && !elements_aligned(dx_opt, dxdt))
+       || !floats_aligned({gamma_opt, mean, rstd, dgamma_opt, dbeta_opt}))
+        return QSYNC_ERR_ALIGN;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if(rows == 0)
+    {
+        int rc = dgamma_opt ? hip_status(launch_zero_f32(dgamma_opt, cols, st)) : QSYNC_OK;
+        if(rc == QSYNC_OK && dbeta_opt) rc = hip_status(launch_zero_f32(dbeta_opt, cols, st));
+        return rc;
+    }
+    if(dgamma_opt || dbeta_opt)
+    {
+        if(!workspace || workspace_bytes < qsync_layernorm_bwd_workspace_bytes(rows, cols)) return QSYNC_ERR_WORKSPACE;
+        if(!aligned16(workspace)) return QSYNC_ERR_ALIGN;
+    }
+    if(dx_opt && (!in_place_or_apart(dx_opt, dxdt, dy, dydt, rows, cols, lddy) || !in_place_or_apart(dx_opt, dxdt, x, xdt, rows, cols, ldx)))
+        return QSYNC_ERR_UNSUPPORTED;
+    return hip_status(launch_layernorm_bwd(dy, dydt, lddy, x, xdt, rows, cols, ldx, gamma_opt, mean, rstd, dx_opt, dxdt, dgamma_opt,
+                                           dbeta_opt, workspace, st));
+}
+
+size_t qsync_token_logprobs_workspace_bytes(int ldt, int64_t rows, int64_t cols, int top_k)
+{
+    if(!is_row_dtype(ldt) || !count_ok(rows, cols) || rows == 0 || cols == 0 || cols > kLogitsMaxCols || top_k < 0 || top_k > kTopAlternatives)
+        return 0;
+    return round256(token_logprobs_workspace_bytes(ldt, rows, cols, top_k));
+}
+
+int qsync_token_logprobs(const void* logits, int ldt, int64_t rows, int64_t cols, int64_t ld, float scale, const void* tokens_opt,
+                         int tdt, float* logp_opt, float* entropy_opt, float* stats_opt, int top_k, float* top_logp_opt,
+                         int32_t* top_index_opt, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if(!logits || (logp_opt && !tokens_opt) || (top_k > 0 && (!top_logp_opt || !top_index_opt))) return QSYNC_ERR_NULL;
+    if(!logp_opt && !entropy_opt && !stats_opt && top_k <= 0) return QSYNC_ERR_NULL;
+    if(!is_row_dtype(ldt) || (logp_opt && !is_index_dtype(tdt))) return QSYNC_ERR_BAD_ENUM;
+    if(!count_ok(rows, cols) || ld < cols || !count_ok(rows, ld)) return QSYNC_ERR_BAD_SHAPE;
+    if(!positive(scale) || top_k < 0 || top_k > kTopAlternatives || cols > kLogitsMaxCols) return QSYNC_ERR_UNSUPPORTED;
+    if(rows == 0 || cols == 0) return QSYNC_OK;
+    if(top_k > cols) return QSYNC_ERR_BAD_SHAPE;
+    if(!elements_aligned(logits, ldt) || (logp_opt && !elements_aligned(tokens_opt, tdt)) || !floats_aligned({logp_opt, entropy_opt, stats_opt})
+       || (top_k > 0 && (!floats_aligned({top_logp_opt}) || !elements_aligned(top_index_opt, QSYNC_I32))))
+        return QSYNC_ERR_ALIGN;
+    if(!workspace || workspace_bytes < qsync_token_logprobs_workspace_bytes(ldt, rows, cols, top_k)) return QSYNC_ERR_WORKSPACE;
+    if(!aligned16(workspace)) return QSYNC_ERR_ALIGN;
+    return hip_status(launch_token_logprobs(logits, ldt, rows, cols, ld, scale, tokens_opt, tdt == QSYNC_I64, logp_opt, entropy_opt,
+                                            stats_opt, top_k, top_logp_opt, top_index_opt, workspace, static_cast<hipStream_t>(stream)));
+}
+
+int qsync_token_logprobs_bwd(const void* logits, int ldt, int64_t rows, int64_t cols, int64_t ld, float scale, const void* tokens_opt,
+                             int tdt, const float* stats, const float* entropy_opt, const float* dlogp_opt, const float* dentropy_opt,
+                             void* dlogits, int ddt, void* stream)
+{
+    if(!logits || !stats || !dlogits || (!dlogp_opt && !dentropy_opt) || (dlogp_opt && !tokens_opt) || (dentropy_opt && !entropy_opt))
+        return QSYNC_ERR_NULL;
+    if(!is_row_dtype(ldt) || !is_row_dtype(ddt) || (dlogp_opt && !is_index_dtype(tdt))) return QSYNC_ERR_BAD_ENUM;
+    if(!count_ok(rows, cols) || ld < cols || !count_ok(rows, ld)) return QSYNC_ERR_BAD_SHAPE;
+    if(!positive(scale) || cols > kLogitsMaxCols) return QSYNC_ERR_UNSUPPORTED;
+    if(rows == 0 || cols == 0) return QSYNC_OK;
+    if(!elements_aligned(logits, ldt) || !elements_aligned(dlogits, ddt) || (dlogp_opt && !elements_aligned(tokens_opt, tdt))
+       || !floats_aligned({stats, entropy_opt, dlogp_opt, dentropy_opt}))
+        return QSYNC_ERR_ALIGN;
+    if(!in_place_or_apart(dlogits, ddt, logits, ldt, rows, cols, ld)) return QSYNC_ERR_UNSUPPORTED;
+    return hip_status(launch_token_logprobs_bwd(logits, ldt, rows, cols, ld, scale, tokens_opt, tdt == QSYNC_I64, stats, entropy_opt, dlogp_opt,
+                                                dentropy_opt, dlogits, ddt, static_cast<hipStream_t>(stream)));
+}
+
+size_t qsync_distill_topk_workspace_bytes(int ldt, int64_t rows, int64_t cols)
+{
+    if(!is_row_dtype(ldt) || !count_ok(rows, cols) || rows == 0 || cols == 0 || cols > kLogitsMaxCols) return 0;
+    return round256(distill_topk_workspace_bytes(ldt, rows, cols));
+}
+
+int qsync_distill_topk(const void* logits, int ldt, int64_t rows, int64_t cols, int64_t ld, float scale, const void* teacher,
+                       int teacher_dt, const void* index, int idt, int64_t k, const float* weight_opt, float* loss, void* dlogits_opt,
+                       int ddt, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if(!logits || !teacher || !index || !loss) return QSYNC_ERR_NULL;
+    if(!is_row_dtype(ldt) || !is_row_dtype(teacher_dt) || !is_index_dtype(idt) || (dlogits_opt && !is_row_dtype(ddt))) return QSYNC_ERR_BAD_ENUM;
+    if(!count_ok(rows, cols) || ld < cols || !count_ok(rows, ld) || k < 1 || !count_ok(rows, k)) return QSYNC_ERR_BAD_SHAPE;
+    if(!positive(scale) || k > kTeacherEntries || cols > kLogitsMaxCols) return QSYNC_ERR_UNSUPPORTED;
+    if(rows == 0 || cols == 0) return QSYNC_OK;
+    if(!elements_aligned(logits, ldt) || !elements_aligned(teacher, teacher_dt) || !elements_aligned(index, idt)
+       || (dlogits_opt && !elements_aligned(dlogits_opt, ddt)) || !floats_aligned({weight_opt, loss}))
+        return QSYNC_ERR_ALIGN;
+    if(!workspace || workspace_bytes < qsync_distill_topk_workspace_bytes(ldt, rows, cols)) return QSYNC_ERR_WORKSPACE;
+    if(!aligned16(workspace)) return QSYNC_ERR_ALIGN;
+    if(dlogits_opt && !in_place_or_apart(dlogits_opt, ddt, logits, ldt, rows, cols, ld)) return QSYNC_ERR_UNSUPPORTED;
+    return hip_status(launch_distill_topk(logits, ldt, rows, cols, ld, scale, teacher, teacher_dt, index, idt == QSYNC_I64, static_cast<int>(k),
+                                          weight_opt, loss, dlogits_opt, ddt, workspace, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

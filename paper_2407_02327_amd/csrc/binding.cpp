@@ -66,7 +66,8 @@ void* pointer(PyObject* o)
     return reinterpret_cast<void*>(answer(o, "data_ptr"));      // (subclasses answer for themselves; a number has none)
 }
 
-int dtype_code(PyObject* o, at::ScalarType type)
+// `wide`: of a call that takes bfloat16 and 64-bit integers too
+int dtype_code(PyObject* o, at::ScalarType type, bool wide)
 {
     switch(type)
     {
@@ -74,6 +75,8 @@ int dtype_code(PyObject* o, at::ScalarType type)
     case at::kHalf: return QSYNC_F16;
     case at::kChar: return QSYNC_I8;
     case at::kInt: return QSYNC_I32;
+    case at::kBFloat16: if(wide) return QSYNC_BF16; break;
+    case at::kLong: if(wide) return QSYNC_I64; break;
     default: break;
     }
     PyObject* dt = PyObject_GetAttrString(o, "dtype");
@@ -82,7 +85,7 @@ int dtype_code(PyObject* o, at::ScalarType type)
 }
 
 // ... of what is no tensor but has a dtype
-int dtype_code(PyObject* o)
+int dtype_code(PyObject* o, bool wide)
 {
     PyObject* dt = PyObject_GetAttrString(o, "dtype");
     if(!dt) throw PythonError();
@@ -91,7 +94,7 @@ int dtype_code(PyObject* o)
     const at::ScalarType type = known ? reinterpret_cast<THPDtype*>(dt)->scalar_type : at::ScalarType::Undefined;
     Py_DECREF(dt);
     if(!known) throw PythonError();
-    return dtype_code(o, type);
+    return dtype_code(o, type, wide);
 }
 
 void* stream_handle(PyObject* o)
@@ -128,7 +131,7 @@ void* stream_handle(PyObject* o)
     return reinterpret_cast<void*>(v);
 }
 
-template <typename T> T argument(PyObject* const* args, size_t i, bool last)
+template <typename T, bool WIDE> T argument(PyObject* const* args, size_t i, bool last)
 {
     PyObject* const o        = args[i];
     const bool      repeated = i > 0 && args[i - 1] == o;
@@ -144,8 +147,8 @@ template <typename T> T argument(PyObject* const* args, size_t i, bool last)
     }
     else if constexpr(std::is_same<T, int>::value)
     {
-        if(const at::Tensor* t = repeated ? as_tensor(o) : nullptr) return dtype_code(o, t->scalar_type());
-        return repeated && o != Py_None && !PyIndex_Check(o) ? dtype_code(o) : static_cast<int>(integer(o));
+        if(const at::Tensor* t = repeated ? as_tensor(o) : nullptr) return dtype_code(o, t->scalar_type(), WIDE);
+        return repeated && o != Py_None && !PyIndex_Check(o) ? dtype_code(o, WIDE) : static_cast<int>(integer(o));
     }
     else if constexpr(std::is_same<T, size_t>::value)
     {
@@ -157,13 +160,13 @@ template <typename T> T argument(PyObject* const* args, size_t i, bool last)
         return static_cast<T>(integer(o));
 }
 
-template <auto F> struct Call;
-template <typename... A, int (*F)(A...)> struct Call<F>
+template <auto F, bool WIDE> struct Call;
+template <typename... A, int (*F)(A...), bool WIDE> struct Call<F, WIDE>
 {
     static constexpr size_t N = sizeof...(A);
     template <size_t... I> static int run(PyObject* const* args, std::index_sequence<I...>)
     {
-        std::tuple<A...> a{argument<A>(args, I, I + 1 == N)...};
+        std::tuple<A...> a{argument<A, WIDE>(args, I, I + 1 == N)...};
         int              rc;
         Py_BEGIN_ALLOW_THREADS
         rc = std::apply(F, a);
@@ -195,7 +198,9 @@ PyObject* set_error(PyObject*, PyObject* f)
     Py_RETURN_NONE;
 }
 
-#define ENTRY(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&Call<name>::call)), METH_FASTCALL, nullptr}
+#define ENTRY_OF(name, wide) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&Call<name, wide>::call)), METH_FASTCALL, nullptr}
+#define ENTRY(name) ENTRY_OF(name, false)
+#define ENTRY_WIDE(name) ENTRY_OF(name, true)
 PyMethodDef methods[] = {
     {"set_error", set_error, METH_O, nullptr},
     ENTRY(qsync_absmax_scale), ENTRY(qsync_absmax_scale_static), ENTRY(qsync_quantize), ENTRY(qsync_absmax_quantize),
@@ -203,7 +208,8 @@ PyMethodDef methods[] = {
     ENTRY(qsync_qlinear_fwd_codes), ENTRY(qsync_transpose_i8), ENTRY(qsync_scale_from_amax), ENTRY(qsync_qlinear_bwd),
     ENTRY(qsync_qlinear_bwd_rm), ENTRY(qsync_qlinear_backward), ENTRY(qsync_qlinear_bwd_fp16_of_int8), ENTRY(qsync_conv3x3_fwd), ENTRY(qsync_conv3x3_fwd_amax),
     ENTRY(qsync_conv3x3_wgrad), ENTRY(qsync_conv3x3_prepare_weights), ENTRY(qsync_conv3x3_wflip), ENTRY(qsync_im2col3x3_i8),
-    ENTRY(qsync_prepare_weights), ENTRY(qsync_dequantize), {nullptr, nullptr, 0, nullptr}};
+    ENTRY(qsync_prepare_weights), ENTRY(qsync_dequantize), ENTRY_WIDE(qsync_layernorm_fwd), ENTRY_WIDE(qsync_layernorm_bwd),
+    ENTRY_WIDE(qsync_token_logprobs), ENTRY_WIDE(qsync_token_logprobs_bwd), ENTRY_WIDE(qsync_distill_topk), {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

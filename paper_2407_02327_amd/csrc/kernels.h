@@ -8,7 +8,7 @@
 
 namespace qsync {
 
-enum Dtype { kF32 = 0, kF16 = 1, kI8 = 2, kI32 = 3 };
+enum Dtype { kF32 = 0, kF16 = 1, kI8 = 2, kI32 = 3, kBF16 = 4, kI64 = 5 };
 enum Gran { kPerTensor = 0, kPerRow = 1, kPerCol = 2 };
 enum Round { kNearest = 0, kStochastic = 1, kFloor = 2 };
 
@@ -118,6 +118,30 @@ hipError_t launch_column_fold(const ColumnFoldArgs& fold, hipStream_t stream);
 // the tiled conversion does not serve the tensor
 hipError_t launch_convert_sums(const float* x, int64_t rows, int64_t cols, int outdt, void* q, void* qT, float* out, float* workspace,
                                ColumnFoldArgs* fold, bool* taken, hipStream_t stream);
+
+// ---- layer norm (layernorm.hip): x, y, dy, dx of kF32, kF16 or kBF16 -------------------
+hipError_t launch_layernorm_fwd(const void* x, int xdt, int64_t rows, int64_t cols, int64_t ld, const float* gamma, const float* beta,
+                                float eps, void* y, int ydt, float* mean, float* rstd, float* y_amax, hipStream_t st);
+size_t layernorm_bwd_workspace_bytes(int64_t rows, int64_t cols);
+hipError_t launch_layernorm_bwd(const void* dy, int dydt, int64_t lddy, const void* x, int xdt, int64_t rows, int64_t cols, int64_t ldx,
+                                const float* gamma, const float* mean, const float* rstd, void* dx, int dxdt, float* dgamma, float* dbeta,
+                                void* workspace, hipStream_t st);
+
+// ---- logits (logits.hip): of the same types; `wide`: 64-bit tokens or indices, else 32-bit ----
+constexpr int     kTopAlternatives  = 64;                // at most, of a position
+constexpr int     kTeacherEntries   = 256;               // at most, of a position
+constexpr int64_t kLogitsMaxCols    = int64_t(1) << 30;
+size_t token_logprobs_workspace_bytes(int zdt, int64_t rows, int64_t cols, int top);
+hipError_t launch_token_logprobs(const void* z, int zdt, int64_t rows, int64_t cols, int64_t ld, float scale, const void* tokens, bool wide,
+                                 float* logp, float* entropy, float* stats, int top, float* top_logp, int32_t* top_index, void* workspace,
+                                 hipStream_t st);
+hipError_t launch_token_logprobs_bwd(const void* z, int zdt, int64_t rows, int64_t cols, int64_t ld, float scale, const void* tokens, bool wide,
+                                     const float* stats, const float* entropy, const float* dlogp, const float* dentropy, void* dz, int ddt,
+                                     hipStream_t st);
+size_t distill_topk_workspace_bytes(int zdt, int64_t rows, int64_t cols);
+hipError_t launch_distill_topk(const void* z, int zdt, int64_t rows, int64_t cols, int64_t ld, float scale, const void* teacher, int tdt,
+                               const void* index, bool wide, int k, const float* weight, float* loss, void* dz, int ddt, void* workspace,
+                               hipStream_t st);
 
 // ---- GEMM  C[M,N] = epilogue( sum_k A[M,k] B[N,k] ) ------------------------------------
 // epilogue(acc) = float(acc) * (s0 * s1 * col_scale[n]) + col_bias[n]; absent factors are 1 / 0.

@@ -1,0 +1,214 @@
+// What the row-wise kernels (layer norm, logits) share: rows of fp32, binary16 or bfloat16 read and written in 16-byte vectors at
+// any element alignment, and reductions over 16 and 64 lanes on the data-parallel primitives.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "kernels.h"
+
+namespace qsync {
+
+namespace {
+
+typedef unsigned row_v4u32 __attribute__((ext_vector_type(4)));
+// A row of an odd number of 16-bit elements starts at any even address.  Global memory takes 16-byte accesses at any address here, so
+// one form serves every leading dimension: 2187 rows of 1001 fp32 elements are read at the same rate as 1024.
+typedef row_v4u32 row_v4u32_a2 __attribute__((aligned(2)));
+typedef row_v4u32 row_v4u32_a4 __attribute__((aligned(4)));
+
+template <typename T> struct RowType;
+template <> struct RowType<float>
+{
+    static constexpr int      N = 4, kCode = kF32;      // elements of a 16-byte vector
+    static constexpr uint32_t kMinusInf = 0xFF800000u;  // vector words of absent logits
+    typedef row_v4u32_a4 vec_t;
+    template <int E> __device__ static __forceinline__ float get(const row_v4u32& w) { return __uint_as_float(w[E]); }
+    __device__ static __forceinline__ row_v4u32 pack(const float (&v)[4])
+    {
+        return row_v4u32{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    }
+};
+template <> struct RowType<_Float16>
+{
+    static constexpr int      N = 8, kCode = kF16;
+    static constexpr uint32_t kMinusInf = 0xFC00FC00u;
+    typedef row_v4u32_a2 vec_t;
+    template <int E> __device__ static __forceinline__ float get(const row_v4u32& w)
+    {
+        return static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(E % 2 ? w[E / 2] >> 16 : w[E / 2])));
+    }
+    __device__ static __forceinline__ row_v4u32 pack(const float (&v)[8])      // to nearest even
+    {
+        row_v4u32 w;
+#pragma unroll
+        for(int i = 0; i < 4; ++i)
+            w[i] = static_cast<uint32_t>(__builtin_bit_cast(uint16_t, static_cast<_Float16>(v[2 * i])))
+                   | static_cast<uint32_t>(__builtin_bit_cast(uint16_t, static_cast<_Float16>(v[2 * i + 1]))) << 16;
+        return w;
+    }
+};
+template <> struct RowType<__bf16>
+{
+    static constexpr int      N = 8, kCode = kBF16;
+    static constexpr uint32_t kMinusInf = 0xFF80FF80u;
+    typedef row_v4u32_a2 vec_t;
+    template <int E> __device__ static __forceinline__ float get(const row_v4u32& w)
+    {
+        return __uint_as_float(E % 2 ? w[E / 2] & 0xFFFF0000u : w[E / 2] << 16);
+    }
+    __device__ static __forceinline__ row_v4u32 pack(const float (&v)[8])      // to nearest even
+    {
+        row_v4u32 w;
+#pragma unroll
+        for(int i = 0; i < 4; ++i)
+            w[i] = static_cast<uint32_t>(__builtin_bit_cast(uint16_t, static_cast<__bf16>(v[2 * i])))
+                   | static_cast<uint32_t>(__builtin_bit_cast(uint16_t, static_cast<__bf16>(v[2 * i + 1]))) << 16;
+        return w;
+    }
+};
+
+template <typename T> __device__ __forceinline__ row_v4u32 row_load(const T* p)
+{
+    return *reinterpret_cast<const typename RowType<T>::vec_t*>(p);
+}
+template <typename T> __device__ __forceinline__ void row_store(T* p, const row_v4u32& w)
+{
+    *reinterpret_cast<typename RowType<T>::vec_t*>(p) = w;
+}
+template <typename T> __device__ __forceinline__ float row_element(const T* p) { return static_cast<float>(*p); }
+
+// The first `valid` elements at p (the others: `fill`, a word of elements), nothing read beyond them.
+template <typename T> __device__ __forceinline__ row_v4u32 row_load_part(const T* p, int64_t valid, uint32_t fill)
+{
+    if(valid >= RowType<T>::N) return row_load(p);
+    row_v4u32 w{fill, fill, fill, fill};
+    if constexpr(sizeof(T) == 4)
+    {
+#pragma unroll
+        for(int e = 0; e < 4; ++e)
+            if(e < valid) w[e] = reinterpret_cast<const uint32_t*>(p)[e];
+    }
+    else
+    {
+#pragma unroll
+        for(int e = 0; e < 8; ++e)
+            if(e < valid)
+            {
+                const uint32_t h = reinterpret_cast<const uint16_t*>(p)[e];
+                w[e / 2] = e % 2 ? (w[e / 2] & 0xFFFFu) | h << 16 : (w[e / 2] & 0xFFFF0000u) | h;
+            }
+    }
+    return w;
+}
+template <typename T> __device__ __forceinline__ void row_store_part(T* p, const row_v4u32& w, int64_t valid)
+{
+    if(valid >= RowType<T>::N) { row_store(p, w); return; }
+    if constexpr(sizeof(T) == 4)
+    {
+#pragma unroll
+        for(int e = 0; e < 4; ++e)
+            if(e < valid) reinterpret_cast<uint32_t*>(p)[e] = w[e];
+    }
+    else
+    {
+#pragma unroll
+        for(int e = 0; e < 8; ++e)
+            if(e < valid) reinterpret_cast<uint16_t*>(p)[e] = static_cast<uint16_t>(e % 2 ? w[e / 2] >> 16 : w[e / 2]);
+    }
+}
+template <typename T> __device__ __forceinline__ void row_decode(const row_v4u32& w, float* v)
+{
+    v[0] = RowType<T>::template get<0>(w); v[1] = RowType<T>::template get<1>(w);
+    v[2] = RowType<T>::template get<2>(w); v[3] = RowType<T>::template get<3>(w);
+    if constexpr(RowType<T>::N == 8)
+    {
+        v[4] = RowType<T>::template get<4>(w); v[5] = RowType<T>::template get<5>(w);
+        v[6] = RowType<T>::template get<6>(w); v[7] = RowType<T>::template get<7>(w);
+    }
+}
+
+// Eight consecutive elements of a row, whatever their type: what a lane of the layer norm owns.
+template <typename T> struct Row8
+{
+    row_v4u32 w[8 / RowType<T>::N];
+    __device__ __forceinline__ void load(const T* p, int64_t valid)      // (absent elements: 0)
+    {
+#pragma unroll
+        for(int i = 0; i < 8 / RowType<T>::N; ++i) w[i] = row_load_part(p + i * RowType<T>::N, valid - i * RowType<T>::N, 0u);
+    }
+    __device__ __forceinline__ void decode(float (&v)[8]) const
+    {
+#pragma unroll
+        for(int i = 0; i < 8 / RowType<T>::N; ++i) row_decode<T>(w[i], v + i * RowType<T>::N);
+    }
+    __device__ __forceinline__ void encode(const float (&v)[8])
+    {
+        if constexpr(RowType<T>::N == 8) w[0] = RowType<T>::pack(v);
+        else
+        {
+            const float lo[4] = {v[0], v[1], v[2], v[3]}, hi[4] = {v[4], v[5], v[6], v[7]};
+            w[0] = RowType<T>::pack(lo);
+            w[1] = RowType<T>::pack(hi);
+        }
+    }
+    __device__ __forceinline__ void store(T* p, int64_t valid) const
+    {
+#pragma unroll
+        for(int i = 0; i < 8 / RowType<T>::N; ++i) row_store_part(p + i * RowType<T>::N, w[i], valid - i * RowType<T>::N);
+    }
+};
+// ... to a buffer whose type is known at run time only (the same for every lane); `stored` receives the values as rounded
+template <bool STORED> __device__ __forceinline__ void row8_store(void* base, int dtype, int64_t at, float (&v)[8], int64_t valid)
+{
+    auto put = [&](auto tag) {
+        typedef decltype(tag) T;
+        Row8<T> r;
+        r.encode(v);
+        r.store(static_cast<T*>(base) + at, valid);
+        if constexpr(STORED) r.decode(v);
+    };
+    if(dtype == kF16) put(_Float16{});
+    else if(dtype == kBF16) put(__bf16{});
+    else put(float{});
+}
+
+// ---- reductions: fixed order, the result in every lane ------------------------------------------------------------------------
+template <int CTRL, int ROWS = 0xF> __device__ __forceinline__ float dpp_move(float old, float v)
+{
+    return __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(old), __float_as_uint(v), CTRL, ROWS, 0xF, false));
+}
+constexpr int kRotate = 0x120;      // within 16 lanes, by the low digit
+__device__ __forceinline__ float row16_sum(float v)
+{
+    v += dpp_move<kRotate + 8>(0.0f, v);
+    v += dpp_move<kRotate + 4>(0.0f, v);
+    v += dpp_move<kRotate + 2>(0.0f, v);
+    v += dpp_move<kRotate + 1>(0.0f, v);
+    return v;
+}
+__device__ __forceinline__ float row16_max(float v)
+{
+    v = fmaxf(v, dpp_move<kRotate + 8>(v, v));
+    v = fmaxf(v, dpp_move<kRotate + 4>(v, v));
+    v = fmaxf(v, dpp_move<kRotate + 2>(v, v));
+    v = fmaxf(v, dpp_move<kRotate + 1>(v, v));
+    return v;
+}
+__device__ __forceinline__ float lane_value(float v, int lane)
+{
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
+}
+__device__ __forceinline__ float wave64_sum(float v)
+{
+    v = row16_sum(v);
+    return (lane_value(v, 0) + lane_value(v, 16)) + (lane_value(v, 32) + lane_value(v, 48));
+}
+__device__ __forceinline__ float wave64_max(float v)
+{
+    v = row16_max(v);
+    return fmaxf(fmaxf(lane_value(v, 0), lane_value(v, 16)), fmaxf(lane_value(v, 32), lane_value(v, 48)));
+}
+
+}  // namespace
+
+}  // namespace qsync

@@ -18,7 +18,7 @@ import torch
 
 INT8, FP16, FP32 = 8, 16, 32                       # qsync_prec_t
 QUANT_FIXED, QUANT_FLOAT = 0, 1                    # qsync_quant_kind_t
-F32, F16, I8, I32 = 0, 1, 2, 3                     # qsync_dtype_t
+F32, F16, I8, I32, BF16, I64 = 0, 1, 2, 3, 4, 5    # qsync_dtype_t (BF16, I64: layer norm and logits only)
 PER_TENSOR, PER_ROW, PER_COL = 0, 1, 2             # qsync_gran_t
 ROUND_NEAREST, ROUND_STOCHASTIC, ROUND_FLOOR = 0, 1, 2
 OK, ERR_NULL, ERR_BAD_ENUM, ERR_BAD_SHAPE, ERR_UNSUPPORTED, ERR_ALIGN, ERR_WORKSPACE, ERR_HIP = 0, -1, -2, -3, -4, -5, -6, -7
@@ -77,6 +77,14 @@ SIGNATURES = {
     "qsync_variance_increment": (_i, [_i, _vp, _vp, _vp, ctypes.c_double, ctypes.c_double, _i, ctypes.c_double, _i64, _i64,
                                       ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double),
                                       ctypes.POINTER(ctypes.c_double)]),
+    "qsync_layernorm_fwd": (_i, [_vp, _i, _i64, _i64, _i64, _vp, _vp, _f, _vp, _i, _vp, _vp, _vp, _vp]),
+    "qsync_layernorm_bwd": (_i, [_vp, _i, _i64, _vp, _i, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _i, _vp, _vp, _vp, _sz, _vp]),
+    "qsync_layernorm_bwd_workspace_bytes": (_sz, [_i64, _i64]),
+    "qsync_token_logprobs": (_i, [_vp, _i, _i64, _i64, _i64, _f, _vp, _i, _vp, _vp, _vp, _i, _vp, _vp, _vp, _sz, _vp]),
+    "qsync_token_logprobs_workspace_bytes": (_sz, [_i, _i64, _i64, _i]),
+    "qsync_token_logprobs_bwd": (_i, [_vp, _i, _i64, _i64, _i64, _f, _vp, _i, _vp, _vp, _vp, _vp, _vp, _i, _vp]),
+    "qsync_distill_topk": (_i, [_vp, _i, _i64, _i64, _i64, _f, _vp, _i, _vp, _i, _i64, _vp, _vp, _vp, _i, _vp, _sz, _vp]),
+    "qsync_distill_topk_workspace_bytes": (_sz, [_i, _i64, _i64]),
     "qsync_last_hip_error": (_i, []),
     "qsync_strerror": (ctypes.c_char_p, [_i]),
     "qsync_version": (_i, []),
@@ -86,6 +94,8 @@ for _name, (_res, _args) in SIGNATURES.items():
     _fn.restype, _fn.argtypes = _res, _args
 
 _DTYPE_OF = {torch.float32: F32, torch.float16: F16, torch.int8: I8, torch.int32: I32}
+
+_WIDE_DTYPE_OF = {**_DTYPE_OF, torch.bfloat16: BF16, torch.int64: I64}      # ... of layer norm and logits
 
 
 class QsyncError(RuntimeError):
@@ -304,6 +314,44 @@ def qsync_dequantize(a, rows, cols, ld, row_scale_opt, col_scale_opt, tensor_sca
                      stream=None, tensor_scale_dev_opt=None) -> None:
     _native.qsync_dequantize(a, a, rows, cols, ld, row_scale_opt, col_scale_opt, float(tensor_scale), tensor_scale_dev_opt,
                              col_bias_opt, y, y, stream)
+
+
+def qsync_layernorm_fwd(x, rows, cols, ld, gamma_opt, beta_opt, eps, y, mean_opt, rstd_opt, y_amax_opt=None, stream=None) -> None:
+    _native.qsync_layernorm_fwd(x, x, rows, cols, ld, gamma_opt, beta_opt, eps, y, y, mean_opt, rstd_opt, y_amax_opt, stream)
+
+
+def qsync_layernorm_bwd_workspace_bytes(rows: int, cols: int) -> int:
+    return lib.qsync_layernorm_bwd_workspace_bytes(rows, cols)
+
+
+def qsync_layernorm_bwd(dy, lddy, x, rows, cols, ldx, gamma_opt, mean, rstd, dx_opt, dgamma_opt, dbeta_opt, workspace, stream=None) -> None:
+    _native.qsync_layernorm_bwd(dy, dy, lddy, x, x, rows, cols, ldx, gamma_opt, mean, rstd, dx_opt, _or_f32(dx_opt), dgamma_opt, dbeta_opt,
+                                workspace, workspace, stream)
+
+
+def qsync_token_logprobs_workspace_bytes(logits_dtype_code: int, rows: int, cols: int, top_k: int) -> int:
+    return lib.qsync_token_logprobs_workspace_bytes(logits_dtype_code, rows, cols, top_k)
+
+
+def qsync_token_logprobs(logits, rows, cols, ld, scale, tokens_opt, logp_opt, entropy_opt, stats_opt, top_k, top_logp_opt, top_index_opt,
+                         workspace, stream=None) -> None:
+    _native.qsync_token_logprobs(logits, logits, rows, cols, ld, scale, tokens_opt, I64 if tokens_opt is None else tokens_opt, logp_opt,
+                                 entropy_opt, stats_opt, top_k, top_logp_opt, top_index_opt, workspace, workspace, stream)
+
+
+def qsync_token_logprobs_bwd(logits, rows, cols, ld, scale, tokens_opt, stats, entropy_opt, dlogp_opt, dentropy_opt, dlogits,
+                             stream=None) -> None:
+    _native.qsync_token_logprobs_bwd(logits, logits, rows, cols, ld, scale, tokens_opt, I64 if tokens_opt is None else tokens_opt, stats,
+                                     entropy_opt, dlogp_opt, dentropy_opt, dlogits, dlogits, stream)
+
+
+def qsync_distill_topk_workspace_bytes(logits_dtype_code: int, rows: int, cols: int) -> int:
+    return lib.qsync_distill_topk_workspace_bytes(logits_dtype_code, rows, cols)
+
+
+def qsync_distill_topk(logits, rows, cols, ld, scale, teacher, index, k, weight_opt, loss, dlogits_opt, workspace, stream=None) -> None:
+    _native.qsync_distill_topk(logits, logits, rows, cols, ld, scale, teacher, teacher, index, index, k, weight_opt, loss, dlogits_opt,
+                               _or_f32(dlogits_opt), workspace, workspace, stream)
 
 
 class TensorStatsC(ctypes.Structure):
