@@ -579,8 +579,8 @@ __device__ __forceinline__ Entry row_entries(const DistillArgs& p, int64_t row, 
     if(e.any && mass != 0.0f)
     {
         e.q = mass / total;
-        const float log_p = r.s == 0.0f ? -INFINITY : (e.z - r.m) * p.scale - ln_s;
-        part = e.q * ((t - top) * p.scale - logf(total) - log_p);
+        // q (log q - log p), the logit's part by itself: a mask of the lowest value times the scale need not be a finite logarithm
+        part = r.s == 0.0f ? INFINITY : e.q * ((t - top) * p.scale - logf(total) + ln_s) - (e.q * p.scale) * (e.z - r.m);
     }
     if(tid < p.k) { sh.column[tid] = e.column; sh.q[tid] = e.q; }
     loss = block_all<WG, false>(part, slots + 48);

@@ -54,6 +54,8 @@ def _vector(t: Optional[torch.Tensor], n: int, dtypes, what: str) -> None:
 
 
 def _one_device(op, **tensors) -> None:
+    if op.device.type != "cuda":
+        raise ValueError(f"the operator's buffers are on {op.device}: its kernels run on a GPU")
     for name, t in tensors.items():
         if t is not None and t.device != op.device:
             raise ValueError(f"{name} is on {t.device}, the operator's buffers on {op.device}")
