@@ -20,15 +20,14 @@ namespace qsync {
 
 namespace {
 
-constexpr int   kRowThreads = 256;
+constexpr int   kRowThreads = 256;        // a row, or a piece of one
 constexpr int   kUnroll     = 4;          // vectors of a lane in flight: a chunk
-constexpr int   kMaxChunks  = 16;         // chunks of a lane whose maxima the top search keeps in LDS
 constexpr float kLn2 = 0.693147180559945309f, kLog2e = 1.44269504088896341f;
 constexpr float kFar = -1.0e30f;          // stands for differences to the maximum that overflow: e^x is 0 there, and 0 * x is 0
 constexpr int   kTopMost = kTopAlternatives;      // a sorted list is a value per lane
-static_assert(kTopMost == kWaveSize && kTeacherEntries == kRowThreads, "a lane an alternative, a thread an entry");
+static_assert(kTopMost == kWaveSize, "an alternative per lane");
 
-template <typename T> constexpr int chunk_span() { return kRowThreads * RowType<T>::N * kUnroll; }      // elements of a workgroup's chunks
+template <typename T> constexpr int chunk_span(int threads) { return threads * RowType<T>::N * kUnroll; }      // elements of a workgroup's chunks
 
 struct Moments
 {
@@ -59,11 +58,14 @@ __device__ __forceinline__ int64_t index_at(const void* p, int wide, int64_t i)
 
 __device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
 
-// Joins the lanes' moments; the result in every lane.  `slots`: one per wavefront.
-template <int WG> __device__ __forceinline__ Moments join_lanes(Moments a, float k2, float4* slots)
+// Joins the lanes' moments; the result in every lane.  `slots`: one per wavefront.  FAR: what the references differ by is their difference
+// times k2; otherwise the difference of their products, which is what a lane's own terms are relative to (row_pass), and at the end the
+// rounding of the joined one's product is taken out of the sums.
+template <int WG, bool FAR> __device__ __forceinline__ Moments join_lanes(Moments a, float k2, float4* slots)
 {
+    auto apart = [&](float x, float m) { return FAR ? fmaxf((x - m) * k2, kFar) : x * k2 - m * k2; };
     const float m  = wave64_max(a.m);
-    const float dm = fmaxf((a.m - m) * k2, kFar), f = exp2_fast(dm);
+    const float dm = apart(a.m, m), f = exp2_fast(dm);
     a.w = wave64_sum((a.w + dm * a.s) * f);
     a.s = wave64_sum(a.s * f);
     if(threadIdx.x % kWaveSize == 0) slots[threadIdx.x / kWaveSize] = make_float4(m, a.s, a.w, 0.0f);
@@ -75,9 +77,15 @@ template <int WG> __device__ __forceinline__ Moments join_lanes(Moments a, float
     for(int i = 0; i < WG / kWaveSize; ++i)
     {
         const float4 o = slots[i];
-        const float  d = fmaxf((o.x - r.m) * k2, kFar), g = exp2_fast(d);
+        const float  d = apart(o.x, r.m), g = exp2_fast(d);
         r.s += o.y * g;
         r.w += (o.z + d * o.y) * g;
+    }
+    if constexpr(!FAR)
+    {
+        const float d = -fmaf(r.m, k2, -(r.m * k2)), g = exp2_fast(d);
+        r.w = (r.w + d * r.s) * g;
+        r.s *= g;
     }
     return r;
 }
@@ -89,28 +97,82 @@ struct LaneBest
     int   chunk = -1;
 };
 
-// One pass over the elements [begin, end) of a row.
-template <typename T, int WG, bool ENTROPY, bool TOP>
-__device__ __forceinline__ Moments row_pass(const T* z, int begin, int end, float k2, float* chunk_max, LaneBest& best)
+// A row's elements [begin, end): whole 16-byte lines of memory, taken as vectors, and the fewer than two lines' elements in front of and
+// behind them, one each for the first threads ("edge").  A row of an odd number of elements is so read and written in whole lines: 2048 x
+// 65535 bfloat16 63.0 -> 54.8 us, a distillation step over 4096 x 65535 363 -> 256.
+template <typename T> struct RowSpan
 {
-    constexpr int N = RowType<T>::N, SPAN = WG * N * kUnroll;
-    const int     len = end - begin, chunks = (len + SPAN - 1) / SPAN;
-    const T*      at  = z + begin + threadIdx.x * N;
+    const T* row;
+    int      begin, end, body, vectors;      // body: column of the first vector
+    __device__ RowSpan() {}
+    __device__ RowSpan(const T* r, int b, int e) : row(r), begin(b), end(e)
+    {
+        constexpr int N    = RowType<T>::N;
+        const int     past = static_cast<int>((reinterpret_cast<uintptr_t>(r + b) & 15u) / sizeof(T)), head = past ? N - past : 0;
+        body    = b + (head < e - b ? head : e - b);
+        vectors = (e - body) / N;
+    }
+    // the column of thread t's edge element, or -1
+    __device__ int edge(int t) const
+    {
+        if(t < body - begin) return begin + t;
+        const int behind = body + vectors * RowType<T>::N + t - (body - begin);
+        return behind < end ? behind : -1;
+    }
+    template <int WG> __device__ int chunks() const { return (vectors + WG * kUnroll - 1) / (WG * kUnroll); }
+    // the number of vector u of chunk c of thread t, and a vector's column
+    template <int WG> static __device__ int vector(int c, int u, int t) { return (c * kUnroll + u) * WG + t; }
+    // the vectors from number i on, without edges
+    __device__ RowSpan from(int i) const
+    {
+        RowSpan s;
+        s.row     = row;
+        s.vectors = vectors > i ? vectors - i : 0;
+        s.begin = s.body = column(i);
+        s.end = s.body + s.vectors * RowType<T>::N;
+        return s;
+    }
+    __device__ int column(int i) const { return body + i * RowType<T>::N; }
+    // (a row's address in scalar registers and 32-bit offsets: a row of 2^30 fp32 elements ends below 2^32 bytes)
+    __device__ __forceinline__ row_v4u32 load(int i) const
+    {
+        return row_load(reinterpret_cast<const T*>(reinterpret_cast<const uint8_t*>(row) + static_cast<uint32_t>(column(i)) * static_cast<uint32_t>(sizeof(T))));
+    }
+};
+
+// One pass over a span.  FAR: the differences to the maximum are taken first, so that any finite logits do; otherwise z k2 less the rounded
+// product m k2 is one operation, for rows whose maximum lies within 1e30 (a lane's reference does not go below -1e30: what lies there is 0
+// beside such a maximum).  The lanes' sums are then relative to that product; join_lanes keeps to it.
+template <typename T, int WG, bool ENTROPY, bool TOP, bool FAR>
+__device__ __forceinline__ Moments row_pass(const RowSpan<T>& z, float k2, float* chunk_max, LaneBest& best)
+{
+    constexpr int N = RowType<T>::N;
+    const int     tid = threadIdx.x, chunks = z.template chunks<WG>();
     row_v4u32     next[kUnroll];
     auto          fetch = [&](int c) {
-        const T* from = at + static_cast<int64_t>(c) * SPAN;
-        if((c + 1) * static_cast<int64_t>(SPAN) <= len)
+        if((c + 1) * kUnroll * WG <= z.vectors)
         {
 #pragma unroll
-            for(int u = 0; u < kUnroll; ++u) next[u] = row_load(from + u * WG * N);
+            for(int u = 0; u < kUnroll; ++u) next[u] = z.load(z.template vector<WG>(c, u, tid));
             return;
         }
-        const int left = len - c * SPAN - static_cast<int>(threadIdx.x) * N;
 #pragma unroll
-        for(int u = 0; u < kUnroll; ++u) next[u] = row_load_part(from + u * WG * N, left - u * WG * N, RowType<T>::kMinusInf);
+        for(int u = 0; u < kUnroll; ++u)
+        {
+            constexpr uint32_t absent = RowType<T>::kMinusInf;
+            next[u] = row_v4u32{absent, absent, absent, absent};
+            if(tid < z.vectors - z.template vector<WG>(c, u, 0)) next[u] = z.load(z.template vector<WG>(c, u, tid));
+        }
     };
-    Moments r{-FLT_MAX, 0.0f, 0.0f};
+    const int edge = z.edge(tid);
     if(chunks > 0) fetch(0);
+    Moments r{FAR ? -FLT_MAX : kFar, 0.0f, 0.0f};
+    if(edge >= 0)
+    {
+        const float v = row_element(z.row + edge);
+        r.m = fmaxf(r.m, v);
+        r.s = exp2_fast(FAR ? (v - r.m) * k2 : fmaf(v, k2, -(r.m * k2)));
+    }
     for(int c = 0; c < chunks; ++c)
     {
         float v[kUnroll * N];
@@ -122,24 +184,38 @@ __device__ __forceinline__ Moments row_pass(const T* z, int begin, int end, floa
         for(int i = 1; i < kUnroll * N; ++i) top = fmaxf(top, v[i]);
         if constexpr(TOP)
         {
-            chunk_max[c * WG + threadIdx.x] = top;
+            chunk_max[c * WG + tid] = top;
             best.chunk = top > best.value ? c : best.chunk;
             best.value = top > best.value ? top : best.value;
         }
-        const float m  = fmaxf(r.m, top);
-        const float dm = fmaxf((r.m - m) * k2, kFar), f = exp2_fast(dm);
+        const float m  = fmaxf(r.m, top), mk = m * k2;
+        const float dm = FAR ? fmaxf((r.m - m) * k2, kFar) : r.m * k2 - mk, f = exp2_fast(dm);
         if constexpr(ENTROPY) r.w = (r.w + dm * r.s) * f;
         r.s *= f;
         r.m = m;
 #pragma unroll
         for(int i = 0; i < kUnroll * N; ++i)
         {
-            const float d = (v[i] - m) * k2, e = exp2_fast(d);
+            const float d = FAR ? (v[i] - m) * k2 : fmaf(v[i], k2, -mk), e = exp2_fast(d);
             r.s += e;
             if constexpr(ENTROPY) r.w = fmaf(e, fmaxf(d, kFar), r.w);
         }
     }
     return r;
+}
+
+// The moments of a span, in every lane.
+template <typename T, int WG, bool ENTROPY, bool TOP>
+__device__ __forceinline__ Moments span_moments(const RowSpan<T>& z, float k2, float* chunk_max, LaneBest& best, float4* slots)
+{
+    if(k2 < 1.0e7f)
+    {
+        const Moments r = join_lanes<WG, false>(row_pass<T, WG, ENTROPY, TOP, false>(z, k2, chunk_max, best), k2, slots);
+        if(fabsf(r.m) < -kFar) return r;
+        __syncthreads();      // (all lanes have read the slots)
+    }
+    best = LaneBest{};
+    return join_lanes<WG, true>(row_pass<T, WG, ENTROPY, TOP, true>(z, k2, chunk_max, best), k2, slots);
 }
 
 // ---- top alternatives -------------------------------------------------------------------------------------------------------
@@ -160,22 +236,42 @@ __device__ __forceinline__ float key_value(uint64_t key)
 }
 __device__ __forceinline__ uint32_t key_column(uint64_t key) { return 0xFFFFFFFFu - static_cast<uint32_t>(key); }
 
-__device__ __forceinline__ uint64_t lane_xor(uint64_t v, int mask)
+// The value of the lane whose index differs in the bits of MASK, a power of two: on the data-parallel primitives and the row swaps,
+// which answer in a few cycles where a permutation through LDS takes a hundred (2048 x 32768 binary16, 8 alternatives: 42.0 -> 38.6 us).
+template <int MASK> __device__ __forceinline__ uint32_t lane_xor(uint32_t v)
 {
-    const uint32_t lo = __shfl_xor(static_cast<uint32_t>(v), mask, kWaveSize), hi = __shfl_xor(static_cast<uint32_t>(v >> 32), mask, kWaveSize);
-    return static_cast<uint64_t>(hi) << 32 | lo;
+    if constexpr(MASK == 1) return __builtin_amdgcn_update_dpp(v, v, 0xB1, 0xF, 0xF, false);             // quad_perm 1 0 3 2
+    else if constexpr(MASK == 2) return __builtin_amdgcn_update_dpp(v, v, 0x4E, 0xF, 0xF, false);        // quad_perm 2 3 0 1
+    else if constexpr(MASK == 4)
+    {   // four lanes on (row_shl) into the quads of even number, four lanes back (row_shr) into the others
+        const uint32_t r = __builtin_amdgcn_update_dpp(v, v, 0x104, 0xF, 0x5, false);
+        return __builtin_amdgcn_update_dpp(r, v, 0x114, 0xF, 0xA, false);
+    }
+    else if constexpr(MASK == 8) return __builtin_amdgcn_update_dpp(v, v, kRotate + 8, 0xF, 0xF, false);
+    else if constexpr(MASK == 16)
+    {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        return threadIdx.x & 16 ? r[0] : r[1];
+    }
+    else
+    {
+        static_assert(MASK == 32, "a power of two below 64");
+        const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return threadIdx.x & 32 ? r[0] : r[1];
+    }
+}
+template <int MASK> __device__ __forceinline__ uint64_t lane_xor(uint64_t v)
+{
+    return static_cast<uint64_t>(lane_xor<MASK>(static_cast<uint32_t>(v >> 32))) << 32 | lane_xor<MASK>(static_cast<uint32_t>(v));
 }
 // The keys of a wavefront in descending order of the lanes: bitonic sort, and its last stage alone.
-template <int SIZE> __device__ __forceinline__ void bitonic_stage(uint64_t& key)
+template <int SIZE, int J = SIZE / 2> __device__ __forceinline__ void bitonic_stage(uint64_t& key)
 {
-    const int lane = threadIdx.x % kWaveSize;
-#pragma unroll
-    for(int j = SIZE / 2; j >= 1; j /= 2)
-    {
-        const uint64_t other   = lane_xor(key, j);
-        const bool     larger  = ((lane & j) == 0) == ((lane & SIZE) == 0);
-        key = (key > other) == larger ? key : other;
-    }
+    const int      lane   = threadIdx.x % kWaveSize;
+    const uint64_t other  = lane_xor<J>(key);
+    const bool     larger = ((lane & J) == 0) == ((lane & SIZE) == 0);
+    key = (key > other) == larger ? key : other;
+    if constexpr(J > 1) bitonic_stage<SIZE, J / 2>(key);
 }
 __device__ __forceinline__ void sort_wave(uint64_t& key)
 {
@@ -199,98 +295,155 @@ __device__ __forceinline__ uint64_t lane_key(uint64_t v, int lane)
     return static_cast<uint64_t>(hi) << 32 | lo;
 }
 
-// LDS of a top search, behind the chunk maxima.
+// LDS of a top search beside the chunk maxima.
+constexpr int kGathered = 256;
 struct TopShared
 {
-    uint64_t list[kRowThreads / kWaveSize][kTopMost];
-    uint64_t gathered[kRowThreads / kWaveSize][2 * kTopMost];
-    int      count;
+    uint64_t claim[kRowThreads];
+    uint64_t list[4][kTopMost];
+    uint64_t gathered[kGathered];
+    uint64_t folding[4][2 * kTopMost];
+    uint64_t bound;
+    int      chosen, found;
 };
-constexpr size_t top_lds_bytes(int chunks)
-{
-    return sizeof(TopShared) + static_cast<size_t>(chunks) * kRowThreads * (sizeof(float) + sizeof(uint16_t));
-}
+// chunk maxima and the chosen chunks' numbers
+constexpr size_t top_lds_bytes(int chunks) { return static_cast<size_t>(chunks) * kRowThreads * (sizeof(float) + sizeof(uint16_t)); }
 
-// Joins the wavefronts' descending lists: every wavefront gets the largest 64.
-__device__ __forceinline__ uint64_t join_lists(uint64_t key, TopShared& sh)
+// The first wavefront joins `lists` descending lists, its own and those of the next wavefronts.
+__device__ __forceinline__ void join_lists(uint64_t& key, int lists, uint64_t (&list)[4][kTopMost])
 {
     const int lane = threadIdx.x % kWaveSize, wave = threadIdx.x / kWaveSize;
-    sh.list[wave][lane] = key;
+    if(wave > 0 && wave < lists) list[wave][kWaveSize - 1 - lane] = key;
     __syncthreads();
-    uint64_t all = sh.list[0][lane];
-#pragma unroll
-    for(int w = 1; w < kRowThreads / kWaveSize; ++w) merge_wave(all, sh.list[w][kWaveSize - 1 - lane]);
-    return all;
+    if(wave == 0)
+        for(int w = 1; w < lists; ++w) merge_wave(key, list[w][lane]);
 }
 
-// The `top` largest of [begin, end), descending over the lanes of every wavefront (0: fewer elements than that).
-// The k-th largest of the lanes' maxima is a bound that at least k elements reach; a chunk whose maximum stays below it is not looked
-// at again.  About k chunks (32 or 16 elements) remain of a row, and never more than the k best lanes have; they are read a second
-// time, out of a cache, and what reaches the bound is sorted.  The work beside the pass does not depend on the order of the logits, and the
-// order (value, then lower column) makes equal logits as good as different ones.
+// The `top` largest of a span, descending over the lanes of the first wavefront (0: fewer elements than that).
+// The k-th largest of the maxima of 64 or 256 groups of lanes is a bound that at least k elements reach; a chunk whose maximum stays
+// below it is not looked at again.  About k chunks (32 or 16 elements) remain of a row, and never more than the k best groups
+// have; they are read a second time, out of a cache, and what reaches the bound is sorted.  The work beside the pass hardly depends on
+// the order of the logits, and the order (value, then lower column) makes equal logits as good as different ones.
 template <typename T>
-__device__ __forceinline__ uint64_t row_top(const T* z, int begin, int end, int top, const LaneBest& best, const float* chunk_max,
-                                            uint16_t* chosen, TopShared& sh)
+__device__ __forceinline__ uint64_t row_top(const RowSpan<T>& z, int top, const LaneBest& best, const float* chunk_max, uint16_t* chosen, TopShared& sh)
 {
-    constexpr int N = RowType<T>::N, WG = kRowThreads, SPAN = WG * N * kUnroll;
-    const int     tid = threadIdx.x, lane = tid % kWaveSize, wave = tid / kWaveSize;
-    const int     first = begin + tid * N, chunks = (end - begin + SPAN - 1) / SPAN;
+    constexpr int N = RowType<T>::N, WG = kRowThreads, WAVES = WG / kWaveSize;
+    const int     tid = threadIdx.x, lane = tid % kWaveSize, wave = tid / kWaveSize, chunks = z.template chunks<WG>();
     // a lane's claim: an element of at least this value at this column or in front of it
     uint64_t claim = 0;
-    if(best.chunk >= 0) claim = rank_key(best.value, first + best.chunk * SPAN + (kUnroll - 1) * WG * N + N - 1);
-    else if(first < end) claim = rank_key(-INFINITY, first);
-    if(tid == 0) sh.count = 0;
-    sort_wave(claim);
-    const uint64_t bound = lane_key(join_lists(claim, sh), top - 1);
+    if(best.chunk >= 0) claim = rank_key(best.value, z.column(z.template vector<WG>(best.chunk, kUnroll - 1, tid)) + N - 1);
+    else if(tid < z.vectors) claim = rank_key(-INFINITY, z.column(tid));
+    sh.claim[tid] = claim;
+    if(tid == 0) sh.chosen = sh.found = 0;
+    __syncthreads();
+    const int lists = top <= kTopMost / 2 ? 1 : 4;      // groups of lanes, 64 or 256: the fewer, the more elements reach the bound
+    if(wave < lists)
+    {
+        claim = 0;
+        for(int w = wave; w < WAVES; w += lists)
+        {
+            const uint64_t other = sh.claim[w * kWaveSize + lane];
+            claim = claim > other ? claim : other;
+        }
+        sort_wave(claim);
+    }
+    if(lists > 1) join_lists(claim, lists, sh.list);
+    if(wave == 0) sh.bound = lane_key(claim, top - 1);
+    __syncthreads();
+    const uint64_t bound = sh.bound;
 
     for(int c = 0; c < chunks; ++c)
-        if(rank_key(chunk_max[c * WG + tid], first + c * SPAN) >= bound) chosen[atomicAdd(&sh.count, 1)] = static_cast<uint16_t>(c * WG + tid);
+        if(rank_key(chunk_max[c * WG + tid], z.column(z.template vector<WG>(c, 0, tid))) >= bound)
+            chosen[atomicAdd(&sh.chosen, 1)] = static_cast<uint16_t>(c * WG + tid);
     __syncthreads();
-    const int vectors = sh.count * kUnroll;
-    uint64_t  list    = 0, limit = bound;
-    uint64_t* mine    = sh.gathered[wave];
-    int       held    = 0;
-    auto      fold    = [&]() {
-        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-        uint64_t key = lane < held ? mine[lane] : 0;
-        const uint64_t rest = mine[kWaveSize + lane];
-        sort_wave(key);
-        const uint64_t reversed = static_cast<uint64_t>(__shfl(static_cast<uint32_t>(key >> 32), kWaveSize - 1 - lane, kWaveSize)) << 32
-                                  | __shfl(static_cast<uint32_t>(key), kWaveSize - 1 - lane, kWaveSize);
-        merge_wave(list, reversed);
-        const uint64_t last = lane_key(list, top - 1);
-        limit = last > limit ? last : limit;
-        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-        mine[lane] = rest;
-        held = held > kWaveSize ? held - kWaveSize : 0;
-    };
-    for(int i0 = wave * kWaveSize; i0 < vectors; i0 += WG)
-    {
-        const int i = i0 + lane;
-        row_v4u32 w{};
-        int       column = end;
-        if(i < vectors)
-        {
-            const int id = chosen[i / kUnroll], c = id / WG, t = id % WG;
-            column = begin + c * SPAN + (i % kUnroll) * WG * N + t * N;
-            if(column < end) w = row_load_part(z + column, end - column, RowType<T>::kMinusInf);
-        }
-        float v[N];
-        row_decode<T>(w, v);
-#pragma unroll
-        for(int e = 0; e < N; ++e)
-        {
-            const uint64_t key = rank_key(v[e], column + e);
-            const bool     in  = column + e < end && key >= limit;
+    const int vectors = sh.chosen * kUnroll;
+    // body(key, reaches the bound, how many lanes in front do, how many do) for the elements of the chosen chunks, in wavefronts, of which
+    // `of` share the vectors; the first one has the edges too
+    auto chosen_keys = [&](int of, uint64_t& limit, auto&& body) {
+        auto offer = [&](float v, int column, bool in) {
+            const uint64_t key = rank_key(v, static_cast<uint32_t>(column));
+            in = in && key >= limit;
             const uint64_t who = __ballot(in);
-            if(!who) continue;
-            if(in) mine[held + __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(who >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(who), 0))] = key;
-            held += __popcll(who);
-            if(held >= kWaveSize) fold();
+            if(who) body(key, in, __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(who >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(who), 0)),
+                         __popcll(who));
+        };
+        if(wave == 0)
+        {
+            const int edge = z.edge(lane);
+            offer(edge >= 0 ? row_element(z.row + edge) : 0.0f, edge, edge >= 0);
         }
+        for(int i0 = wave * kWaveSize; i0 < vectors; i0 += of * kWaveSize)
+        {
+            const int i = i0 + lane;
+            row_v4u32 w{};
+            int       vector = z.vectors;
+            if(i < vectors)
+            {
+                const int id = chosen[i / kUnroll];
+                vector = z.template vector<WG>(id / WG, i % kUnroll, id % WG);
+                if(vector < z.vectors) w = z.load(vector);
+            }
+            float v[N];
+            row_decode<T>(w, v);
+#pragma unroll
+            for(int e = 0; e < N; ++e) offer(v[e], z.column(vector) + e, vector < z.vectors);
+        }
+    };
+    uint64_t limit = bound, key = 0;
+    chosen_keys(WAVES, limit, [&](uint64_t k, bool in, int place, int count) {
+        int at = 0;
+        if(lane == 0) at = atomicAdd(&sh.found, count);
+        at = __builtin_amdgcn_readfirstlane(at) + place;
+        if(in && at < kGathered) sh.gathered[at] = k;
+    });
+    __syncthreads();
+    const int found = sh.found;
+    if(found <= kGathered)
+    {
+        const int full = (found + kWaveSize - 1) / kWaveSize;
+        if(wave < full)
+        {
+            const int i = wave * kWaveSize + lane;
+            key = i < found ? sh.gathered[i] : 0;
+            sort_wave(key);
+        }
+        if(full > 1) join_lists(key, full, sh.list);
+        return key;
     }
-    if(held > 0) fold();
-    return join_lists(list, sh);      // (every wavefront is past the lists' first use: a barrier lies between)
+    // more than there is room for (the best logits side by side): four wavefronts keep the largest 64 of theirs as they go
+    if(wave < 4)
+    {
+        uint64_t* mine   = sh.folding[wave];
+        int       held   = 0;
+        bool      folded = false;
+        auto      fold   = [&]() {
+            __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+            uint64_t       next = lane < held ? mine[lane] : 0;
+            const uint64_t rest = mine[kWaveSize + lane];
+            sort_wave(next);
+            if(folded)
+            {
+                mine[kWaveSize - 1 - lane] = next;
+                __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+                merge_wave(key, mine[lane]);
+                __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+            }
+            else key = next;
+            folded = true;
+            const uint64_t last = lane_key(key, top - 1);
+            limit = last > limit ? last : limit;
+            mine[lane] = rest;
+            held = held > kWaveSize ? held - kWaveSize : 0;
+        };
+        chosen_keys(4, limit, [&](uint64_t k, bool in, int place, int count) {
+            if(in) mine[held + place] = k;
+            held += count;
+            if(held >= kWaveSize) fold();
+        });
+        if(held > 0) fold();
+    }
+    join_lists(key, 4, sh.list);
+    return key;
 }
 
 // ---- log probabilities --------------------------------------------------------------------------------------------------------
@@ -333,26 +486,24 @@ __device__ __forceinline__ void write_logprobs(const LogitsArgs& p, int64_t row,
 // Item: a piece of a row.  One piece a row: the results; several: their moments and lists.
 template <typename T, bool ENTROPY, bool TOP> __global__ __launch_bounds__(kRowThreads) void logprobs_kernel(const LogitsArgs p)
 {
+    constexpr int WG = kRowThreads;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    __shared__ float4 slots[kRowThreads / kWaveSize];
-    TopShared&        sh        = *reinterpret_cast<TopShared*>(lds);
-    float*            chunk_max = reinterpret_cast<float*>(lds + sizeof(TopShared));
+    __shared__ float4 slots[WG / kWaveSize];
+    float*            chunk_max = reinterpret_cast<float*>(lds);
     const float       k2        = p.scale * kLog2e;
     const int64_t     items     = p.rows * p.pieces;
     for(int64_t item = blockIdx.x; item < items; item += gridDim.x)
     {
-        const int64_t row   = item / p.pieces;
-        const int     begin = static_cast<int>(item - row * p.pieces) * p.piece;
-        const int     end   = p.cols - begin < p.piece ? p.cols : begin + p.piece;
-        const T*      z     = static_cast<const T*>(p.z) + row * p.ld;
-        LaneBest      best;
-        Moments       r     = row_pass<T, kRowThreads, ENTROPY, TOP>(z, begin, end, k2, chunk_max, best);
-        uint64_t      key   = 0;
-        r = join_lanes<kRowThreads>(r, k2, slots);
+        const int64_t    row   = item / p.pieces;
+        const int        begin = static_cast<int>(item - row * p.pieces) * p.piece;
+        const RowSpan<T> z(static_cast<const T*>(p.z) + row * p.ld, begin, p.cols - begin < p.piece ? p.cols : begin + p.piece);
+        LaneBest         best;
+        const Moments    r   = span_moments<T, WG, ENTROPY, TOP>(z, k2, chunk_max, best, slots);
+        uint64_t         key = 0;
         if constexpr(TOP)
         {
-            const int chunks = (p.piece + chunk_span<T>() - 1) / chunk_span<T>();
-            key = row_top(z, begin, end, p.top, best, chunk_max, reinterpret_cast<uint16_t*>(chunk_max + chunks * kRowThreads), sh);
+            __shared__ TopShared sh;
+            key = row_top(z, p.top, best, chunk_max, reinterpret_cast<uint16_t*>(chunk_max + z.template chunks<WG>() * WG), sh);
         }
         if(threadIdx.x < kWaveSize)
         {
@@ -380,26 +531,34 @@ template <int WG> __device__ __forceinline__ Moments join_pieces(const float4* p
         r.s = r.s * fa + o.y * fb;
         r.m = m;
     }
-    return join_lanes<WG>(r, k2, slots);
+    return join_lanes<WG, true>(r, k2, slots);
 }
 
 template <typename T> __global__ __launch_bounds__(kRowThreads) void logprobs_join_kernel(const LogitsArgs p)
 {
-    __shared__ float4    slots[kRowThreads / kWaveSize];
-    __shared__ TopShared sh;
-    const int            lane = threadIdx.x % kWaveSize, wave = threadIdx.x / kWaveSize;
+    __shared__ float4   slots[kRowThreads / kWaveSize];
+    __shared__ uint64_t lists[4][kTopMost];
+    const int           lane = threadIdx.x % kWaveSize, wave = threadIdx.x / kWaveSize;
     for(int64_t row = blockIdx.x; row < p.rows; row += gridDim.x)
     {
         const Moments r    = join_pieces<kRowThreads>(p.part + row * p.pieces, p.pieces, p.scale * kLog2e, slots);
         uint64_t      list = 0;
         if(p.top > 0)
         {
-            for(int i = wave; i < p.pieces; i += kRowThreads / kWaveSize)
+            constexpr int   WAVES = kRowThreads / kWaveSize, AHEAD = 4;      // lists of a wavefront under way
+            const int       at    = kWaveSize - 1 - lane;
+            const uint64_t* keys  = p.part_keys + row * p.pieces * p.top + at;
+            for(int i = wave; i < p.pieces; i += AHEAD * WAVES)
             {
-                const int at = kWaveSize - 1 - lane;
-                merge_wave(list, at < p.top ? p.part_keys[(row * p.pieces + i) * p.top + at] : 0);
+                uint64_t next[AHEAD];
+#pragma unroll
+                for(int a = 0; a < AHEAD; ++a)
+                    next[a] = at < p.top && i + a * WAVES < p.pieces ? keys[static_cast<int64_t>(i + a * WAVES) * p.top] : 0;
+#pragma unroll
+                for(int a = 0; a < AHEAD; ++a)
+                    if(i + a * WAVES < p.pieces) merge_wave(list, next[a]);
             }
-            list = join_lists(list, sh);
+            join_lists(list, p.pieces < WAVES ? p.pieces : WAVES, lists);
         }
         if(threadIdx.x < kWaveSize) write_logprobs<T>(p, row, r, list);
         __syncthreads();
@@ -421,37 +580,51 @@ struct LogprobsGradArgs
     int          ddt;
 };
 
-// Walks over [begin, end) of a row in units of eight elements, two of them in flight a lane: body(column, values, valid).
-template <typename T, int WG, typename F> __device__ __forceinline__ void row_units(const T* z, int begin, int end, F&& body)
+// Walks over a span, 32 bytes of a lane in flight: body(column, values of a vector), edge(column, value).
+template <typename T, int WG, typename F, typename G> __device__ __forceinline__ void walk(const RowSpan<T>& z, F&& body, G&& edge)
 {
-    constexpr int U = 2, SPAN = WG * 8;
-    int           c = begin + static_cast<int>(threadIdx.x) * 8;
-    Row8<T>       next[U];
-#pragma unroll
-    for(int u = 0; u < U; ++u) next[u].load(z + c + u * SPAN, end - c - u * SPAN);
-    for(; c < end; c += U * SPAN)
-    {
-        float v[U][8];
-#pragma unroll
-        for(int u = 0; u < U; ++u) next[u].decode(v[u]);
-        if(c + U * SPAN < end)
-        {
-#pragma unroll
-            for(int u = 0; u < U; ++u) next[u].load(z + c + (U + u) * SPAN, end - c - (U + u) * SPAN);
-        }
+    constexpr int U = 2, N = RowType<T>::N;
+    int           i = threadIdx.x;
+    row_v4u32     next[U];
+    auto          fetch = [&](int from) {
 #pragma unroll
         for(int u = 0; u < U; ++u)
-            if(c + u * SPAN < end) body(c + u * SPAN, v[u], end - c - u * SPAN);
+            if(from + u * WG < z.vectors) next[u] = z.load(from + u * WG);
+    };
+    fetch(i);
+    const int e = z.edge(threadIdx.x);
+    if(e >= 0) edge(e, row_element(z.row + e));
+    for(; i < z.vectors; i += U * WG)
+    {
+        float v[U][N];
+#pragma unroll
+        for(int u = 0; u < U; ++u) row_decode<T>(next[u], v[u]);
+        fetch(i + U * WG);
+#pragma unroll
+        for(int u = 0; u < U; ++u)
+            if(i + u * WG < z.vectors) body(z.column(i + u * WG), v[u]);
     }
 }
-
-__device__ __forceinline__ void store_zeros(void* dz, int ddt, int64_t row_at, int begin, int end, int threads)
+// The result of f for every element of a span, to a buffer of type dtype whose row begins at `at`.
+template <typename T, int WG, typename F> __device__ __forceinline__ void map_span(const RowSpan<T>& z, void* out, int dtype, int64_t at, F&& f)
 {
-    for(int c = begin + static_cast<int>(threadIdx.x) * 8; c < end; c += threads * 8)
-    {
-        float o[8] = {};
-        row8_store<false>(dz, ddt, row_at + c, o, end - c);
-    }
+    constexpr int N = RowType<T>::N;
+    walk<T, WG>(
+        z,
+        [&](int c, float(&v)[N]) {
+            float o[N];
+#pragma unroll
+            for(int e = 0; e < N; ++e) o[e] = f(c + e, v[e]);
+            vector_store<T>(out, dtype, at + c, o);
+        },
+        [&](int c, float v) { element_store(out, dtype, at + c, f(c, v)); });
+}
+template <typename T, int WG> __device__ __forceinline__ void zero_span(const RowSpan<T>& z, void* out, int dtype, int64_t at)
+{
+    const float o[RowType<T>::N] = {};
+    for(int i = threadIdx.x; i < z.vectors; i += WG) vector_store<T>(out, dtype, at + z.column(i), o);
+    const int e = z.edge(threadIdx.x);
+    if(e >= 0) element_store(out, dtype, at + e, 0.0f);
 }
 
 template <typename T, bool ENTROPY> __global__ __launch_bounds__(kRowThreads) void logprobs_grad_kernel(const LogprobsGradArgs p)
@@ -473,29 +646,20 @@ template <typename T, bool ENTROPY> __global__ __launch_bounds__(kRowThreads) vo
             entropy = p.entropy[row];
         }
         if(given >= p.cols) g = NAN;      // (no column of it: the row says so)
-        const int64_t at = row * p.cols;
+        const int64_t    at = row * p.cols;
+        const RowSpan<T> z(static_cast<const T*>(p.z) + row * p.ld, begin, end);
         if(ln_s == -INFINITY || (g == 0.0f && h == 0.0f))
         {
-            store_zeros(p.dz, p.ddt, at, begin, end, kRowThreads);
+            zero_span<T, kRowThreads>(z, p.dz, p.ddt, at);
             continue;
         }
         const int   token = given < p.cols ? static_cast<int>(given) : -1;
         const float l2 = ln_s * kLog2e;
-        row_units<T, kRowThreads>(static_cast<const T*>(p.z) + row * p.ld, begin, end, [&](int c, float(&v)[8], int left) {
-            float o[8];
-#pragma unroll
-            for(int e = 0; e < 8; ++e)
-            {
-                const float d = (v[e] - m) * k2 - l2, q = exp2_fast(d);      // log2 p and p
-                o[e] = -(g * q);
-                if constexpr(ENTROPY) o[e] = fmaf(-(h * q), fmaf(fmaxf(d, kFar), kLn2, entropy), o[e]);
-            }
-            if(static_cast<unsigned>(token - c) < 8u)
-            {
-#pragma unroll
-                for(int e = 0; e < 8; ++e) o[e] += token - c == e ? g : 0.0f;
-            }
-            row8_store<false>(p.dz, p.ddt, at + c, o, left);
+        map_span<T, kRowThreads>(z, p.dz, p.ddt, at, [&](int c, float v) {
+            const float d = (v - m) * k2 - l2, q = exp2_fast(d);      // log2 p and p
+            float       o = -(g * q);
+            if constexpr(ENTROPY) o = fmaf(-(h * q), fmaf(fmaxf(d, kFar), kLn2, entropy), o);
+            return c == token ? o + g : o;
         });
     }
 }
@@ -519,143 +683,280 @@ struct DistillArgs
     float4*      part;
 };
 
-constexpr int kEntries = kTeacherEntries;      // one a thread
-
+// The teacher's entries of a row, prepared by the first wavefront: in LDS, so that they take no registers beside a row's.
 struct EntriesShared
 {
-    int    column[kEntries];
-    float  q[kEntries];
-    float4 slots[16];
+    int   column[kTeacherEntries];      // -1: none
+    float q[kTeacherEntries], log_q[kTeacherEntries], z[kTeacherEntries];
+    int   any, bad;                     // some entry has weight; a column beyond the vocabulary, or a NaN of the teacher's
 };
-
-// A thread's entry of the teacher's.
-struct Entry
+// The columns and the teacher's logits (in log_q) ...
+__device__ __forceinline__ void entries_fetch(const DistillArgs& p, int64_t row, EntriesShared& sh)
 {
-    int   column = -1;
-    float q = 0.0f, z = 0.0f;
-    bool  any = false;      // (of the row) some entry has weight
-    bool  bad = false;      // (of the row) a column beyond the vocabulary, or a NaN of the teacher's
-};
-
-template <int WG, bool MAX> __device__ __forceinline__ float block_all(float v, float* slots)
+    bool bad = false;
+#pragma unroll 1
+    for(int i = threadIdx.x; i < p.k; i += kWaveSize)
+    {
+        const int64_t e = row * p.k + i, c = index_at(p.index, p.wide, e);
+        const float   t = p.tdt == kF32 ? row_element(static_cast<const float*>(p.teacher) + e)
+                          : p.tdt == kF16 ? row_element(static_cast<const _Float16*>(p.teacher) + e)
+                                          : row_element(static_cast<const __bf16*>(p.teacher) + e);
+        const bool    in = c >= 0 && c < p.cols;
+        bad |= c >= p.cols || (in && t != t);
+        sh.column[i] = in ? static_cast<int>(c) : -1;
+        sh.log_q[i]  = in ? t : -INFINITY;
+    }
+    const uint64_t spoilt = __ballot(bad);
+    if(threadIdx.x == 0) sh.bad = spoilt != 0;
+}
+// ... then, behind the requests for the row itself, the student's logits and the teacher's probabilities.  (A lane reads what it wrote.)
+template <typename T> __device__ __forceinline__ void entries_prepare(const DistillArgs& p, const T* row, EntriesShared& sh)
 {
-    v = MAX ? wave64_max(v) : wave64_sum(v);
-    if(threadIdx.x % kWaveSize == 0) slots[threadIdx.x / kWaveSize] = v;
-    __syncthreads();
-    float t = slots[0];
-#pragma unroll
-    for(int w = 1; w < WG / kWaveSize; ++w) t = MAX ? fmaxf(t, slots[w]) : t + slots[w];
-    return t;
+    float top = -INFINITY, total = 0.0f;
+#pragma unroll 1
+    for(int i = threadIdx.x; i < p.k; i += kWaveSize)
+    {
+        const int c = sh.column[i];
+        sh.z[i] = c >= 0 ? row_element(row + c) : 0.0f;
+        top     = fmaxf(top, sh.log_q[i]);
+    }
+    top = wave64_max(top);
+    const bool any = top > -INFINITY;
+#pragma unroll 1
+    for(int i = threadIdx.x; i < p.k; i += kWaveSize)
+    {
+        const float q = any ? exp2_fast((sh.log_q[i] - top) * (p.scale * kLog2e)) : 0.0f;
+        sh.q[i] = q;
+        total += q;
+    }
+    total = wave64_sum(total);
+    const float log_total = logf(total);
+#pragma unroll 1
+    for(int i = threadIdx.x; i < p.k; i += kWaveSize)
+    {
+        sh.q[i]     = any ? sh.q[i] / total : 0.0f;
+        sh.log_q[i] = (sh.log_q[i] - top) * p.scale - log_total;
+    }
+    if(threadIdx.x == 0) sh.any = any;
+}
+// By the first wavefront: sum q (log q - log p), the logits' part by itself: a mask of the lowest value times the scale need not be a
+// finite logarithm.
+__device__ __forceinline__ float entries_loss(const DistillArgs& p, const Moments& r, float ln_s, const EntriesShared& sh)
+{
+    float sum = 0.0f;
+    for(int i = threadIdx.x; i < p.k; i += kWaveSize)
+    {
+        const float q = sh.q[i];
+        if(q != 0.0f) sum += r.s == 0.0f ? INFINITY : q * (sh.log_q[i] + ln_s) - (q * p.scale) * (sh.z[i] - r.m);
+    }
+    sum = wave64_sum(sum);
+    return sh.bad ? NAN : sum;
+}
+// By the first wavefront, over the probabilities of [begin, end), which are written: the entries' columns less the teacher's.  mass(z) is
+// weight scale p.
+template <typename F>
+__device__ __forceinline__ void entries_subtract(const DistillArgs& p, int64_t at, int begin, int end, float g, const EntriesShared& sh, F&& mass)
+{
+    for(int i = threadIdx.x; i < p.k; i += kWaveSize)
+    {
+        const int column = sh.column[i];
+        if(column < begin || column >= end) continue;
+        float of = 0.0f;      // of all entries of this column
+        for(int j = 0; j < p.k; ++j) of += sh.column[j] == column ? sh.q[j] : 0.0f;
+        const float v = mass(sh.z[i]) - g * of;
+        element_store(p.dz, p.ddt, at + column, v);
+    }
 }
 
-// Loads the entries, the teacher's probabilities and the row's loss.
-template <typename T, int WG>
-__device__ __forceinline__ Entry row_entries(const DistillArgs& p, int64_t row, const Moments& r, float ln_s, EntriesShared& sh, float& loss)
+// weight scale of a row's gradient; 0 where the whole row's is 0 whatever its logits hold
+__device__ __forceinline__ float row_factor(const DistillArgs& p, int64_t row, const Moments& r, const EntriesShared& sh)
 {
-    const int tid = threadIdx.x;
-    Entry     e;
-    float     t = -INFINITY, bad = 0.0f;
-    if(tid < p.k)
-    {
-        const int64_t at = row * p.k + tid, column = index_at(p.index, p.wide, at);
-        if(column >= p.cols) bad = 1.0f;
-        else if(column >= 0)
-        {
-            e.column = static_cast<int>(column);
-            t = p.tdt == kF32 ? row_element(static_cast<const float*>(p.teacher) + at)
-                : p.tdt == kF16 ? row_element(static_cast<const _Float16*>(p.teacher) + at)
-                                : row_element(static_cast<const __bf16*>(p.teacher) + at);
-            e.z = row_element(static_cast<const T*>(p.z) + row * p.ld + e.column);
-            if(t != t) bad = 1.0f;
-        }
-    }
-    float*      slots = reinterpret_cast<float*>(sh.slots);
-    const float top   = block_all<WG, true>(t, slots);
-    e.bad = block_all<WG, true>(bad, slots + 16) > 0.0f;
-    e.any = top > -INFINITY;
-    const float mass  = e.any ? exp2_fast((t - top) * (p.scale * kLog2e)) : 0.0f;
-    const float total = block_all<WG, false>(mass, slots + 32);
-    float       part  = 0.0f;
-    if(e.any && mass != 0.0f)
-    {
-        e.q = mass / total;
-        // q (log q - log p), the logit's part by itself: a mask of the lowest value times the scale need not be a finite logarithm
-        part = r.s == 0.0f ? INFINITY : e.q * ((t - top) * p.scale - logf(total) + ln_s) - (e.q * p.scale) * (e.z - r.m);
-    }
-    if(tid < p.k) { sh.column[tid] = e.column; sh.q[tid] = e.q; }
-    loss = block_all<WG, false>(part, slots + 48);
-    if(e.bad) loss = NAN;
-    return e;
-}
-
-// The gradient of [begin, end): the student's probabilities, then, over them, the entries' columns less the teacher's.
-template <typename T, int WG>
-__device__ __forceinline__ void row_gradient(const DistillArgs& p, int64_t row, int begin, int end, const Moments& r, float ln_s, const Entry& e,
-                                             const EntriesShared& sh)
-{
-    const float   weight = p.weight ? p.weight[row] : 1.0f;
-    const int64_t at     = row * p.cols;
-    float         g      = weight * p.scale;
-    if(e.bad && weight != 0.0f) g = NAN;
-    if(weight == 0.0f || r.s == 0.0f || !(e.any || e.bad))
-    {
-        store_zeros(p.dz, p.ddt, at, begin, end, WG);
-        return;
-    }
-    const float k2 = p.scale * kLog2e, l2 = ln_s * kLog2e;
-    row_units<T, WG>(static_cast<const T*>(p.z) + row * p.ld, begin, end, [&](int c, float(&v)[8], int left) {
-        float o[8];
-#pragma unroll
-        for(int i = 0; i < 8; ++i) o[i] = g * exp2_fast((v[i] - r.m) * k2 - l2);
-        row8_store<false>(p.dz, p.ddt, at + c, o, left);
-    });
-    __syncthreads();      // (behind the probabilities)
-    if(static_cast<int>(threadIdx.x) < p.k && e.column >= begin && e.column < end)
-    {
-        float q = 0.0f;      // of all entries of this column
-        for(int i = 0; i < p.k; ++i) q += sh.column[i] == e.column ? sh.q[i] : 0.0f;
-        const float v = g * (exp2_fast((e.z - r.m) * k2 - l2) - q);
-        if(p.ddt == kF16) static_cast<_Float16*>(p.dz)[at + e.column] = static_cast<_Float16>(v);
-        else if(p.ddt == kBF16) static_cast<__bf16*>(p.dz)[at + e.column] = static_cast<__bf16>(v);
-        else static_cast<float*>(p.dz)[at + e.column] = v;
-    }
+    const float weight = p.weight ? p.weight[row] : 1.0f;
+    if(weight == 0.0f || r.s == 0.0f || !(sh.any || sh.bad)) return 0.0f;
+    return sh.bad ? NAN : weight * p.scale;
 }
 
 __device__ __forceinline__ float log_sum(const Moments& r) { return r.s == 0.0f ? -INFINITY : logf(r.s); }
 
-// A row a workgroup: both passes, the second one out of a cache.
-template <typename T, int WG> __global__ __launch_bounds__(WG) void distill_row_kernel(const DistillArgs p)
+// The gradient of a span from logits that are read again.
+template <typename T, int WG>
+__device__ __forceinline__ void span_gradient(const DistillArgs& p, int64_t row, const RowSpan<T>& z, const Moments& r, const EntriesShared& sh)
 {
+    const int64_t at = row * p.cols;
+    const float   g  = row_factor(p, row, r, sh);
+    if(g == 0.0f)
+    {
+        zero_span<T, WG>(z, p.dz, p.ddt, at);
+        return;
+    }
+    const float k2 = p.scale * kLog2e, gs = g / r.s;
+    auto        mass = [&](float v) { return gs * exp2_fast((v - r.m) * k2); };
+    map_span<T, WG>(z, p.dz, p.ddt, at, [&](int, float v) { return mass(v); });
+    __syncthreads();      // (behind the probabilities)
+    if(threadIdx.x < kWaveSize) entries_subtract(p, at, z.begin, z.end, g, sh, mass);
+}
+
+// A row a workgroup, its logits in registers between the sums and the gradient: NV vectors of a thread, all under way at once.  What a
+// longer row has beyond them is read twice, the second time out of a cache.
+//   A step over 4096 x 65536 bfloat16 logits: 230 us, 4.7 TB/s of logits read once and gradient written once; with all of a row read
+//   twice 272 (512 threads) and 309 (256).
+// (Four wavefronts of a SIMD leave 128 registers.  The scheduling barriers keep the phases from being unrolled into more values than
+// that; the words are taken apart again in each phase, as fp32 values they would take twice the registers.)
+template <typename T, int WG, int NV, bool REST> __global__ __launch_bounds__(WG, 4) void distill_held_kernel(const DistillArgs p)
+{
+    constexpr int            N = RowType<T>::N, WAVES = WG / kWaveSize;
     __shared__ EntriesShared sh;
-    __shared__ float4        slots[WG / kWaveSize];
+    __shared__ float         largest[WAVES], sums[WAVES];
+    __shared__ float4        slots[WAVES];
+    const int                tid = threadIdx.x;
+    const bool               first = tid < kWaveSize;
     const float              k2 = p.scale * kLog2e;
     for(int64_t row = blockIdx.x; row < p.rows; row += gridDim.x)
     {
-        LaneBest      none;
-        const Moments r = join_lanes<WG>(row_pass<T, WG, false, false>(static_cast<const T*>(p.z) + row * p.ld, 0, p.cols, k2, nullptr, none), k2, slots);
-        const float   ln_s = log_sum(r);
-        float         loss;
-        const Entry   e = row_entries<T, WG>(p, row, r, ln_s, sh, loss);
-        if(threadIdx.x == 0) p.loss[row] = loss;
-        if(p.dz) row_gradient<T, WG>(p, row, 0, p.cols, r, ln_s, e, sh);
+        const RowSpan<T> z(static_cast<const T*>(p.z) + row * p.ld, 0, p.cols);
+        if(first) entries_fetch(p, row, sh);
+        row_v4u32 w[NV];
+        int       t = tid;
+        asm volatile("" : "+v"(t));      // (offsets that hang on it are not kept from row to row)
+#pragma unroll
+        for(int u = 0; u < NV; ++u)
+        {
+            constexpr uint32_t absent = RowType<T>::kMinusInf;
+            w[u] = row_v4u32{absent, absent, absent, absent};
+            if(t < z.vectors - u * WG) w[u] = z.load(u * WG + t);
+        }
+        const int   edge    = z.edge(tid);
+        const float at_edge = edge >= 0 ? row_element(z.row + edge) : -INFINITY;
+        if(first) entries_prepare(p, z.row, sh);
+        RowSpan<T> rest;
+        LaneBest   none;
+        Moments    r{-FLT_MAX, 0.0f, 0.0f};
+        if constexpr(REST)
+        {
+            rest = z.from(WG * NV);
+            r    = row_pass<T, WG, false, false, false>(rest, k2, nullptr, none);
+        }
+        const float rest_m = r.m;
+        r.m = fmaxf(r.m, at_edge);
+#pragma unroll
+        for(int u = 0; u < NV; ++u)
+        {
+            float v[N];
+            row_decode<T>(w[u], v);
+#pragma unroll
+            for(int i = 0; i < N; ++i) r.m = fmaxf(r.m, v[i]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        r.m = wave64_max(r.m);
+        if(tid % kWaveSize == 0) largest[tid / kWaveSize] = r.m;
+        __syncthreads();
+#pragma unroll
+        for(int i = 0; i < WAVES; ++i) r.m = fmaxf(r.m, largest[i]);
+        // as in row_pass, one operation where the maximum allows it; the product's rounding is common to the sum and the probabilities,
+        // and is taken out of the sum that the loss has
+        const bool  near = fabsf(r.m) < -kFar && k2 < 1.0e7f;
+        const float mk   = r.m * k2;
+        auto        again = [&]() {
+#pragma unroll
+            for(int u = 0; u < NV; ++u) asm volatile("" : "+v"(w[u]));
+            asm volatile("" : "+v"(t));
+        };
+        Moments exact;
+        if(near)
+        {
+            if constexpr(REST) r.s *= exp2_fast(rest_m * k2 - mk);
+            r.s += exp2_fast(fmaf(at_edge, k2, -mk));
+            again();
+#pragma unroll
+            for(int u = 0; u < NV; ++u)
+            {
+                float v[N];
+                row_decode<T>(w[u], v);
+#pragma unroll
+                for(int i = 0; i < N; ++i) r.s += exp2_fast(fmaf(v[i], k2, -mk));
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            r.s = wave64_sum(r.s);
+            if(tid % kWaveSize == 0) sums[tid / kWaveSize] = r.s;
+            __syncthreads();
+            r.s = 0.0f;
+#pragma unroll
+            for(int i = 0; i < WAVES; ++i) r.s += sums[i];
+            exact = r;
+            exact.s *= exp2_fast(-fmaf(r.m, k2, -mk));
+        }
+        else exact = r = span_moments<T, WG, false, false>(z, k2, nullptr, none, slots);
+        if(first)
+        {
+            const float loss = entries_loss(p, exact, log_sum(exact), sh);
+            if(tid == 0) p.loss[row] = loss;
+        }
+        const float g = row_factor(p, row, exact, sh);
+        if(near && g != 0.0f && p.ddt == RowType<T>::kCode)
+        {
+            T* const    out  = static_cast<T*>(p.dz) + row * p.cols;
+            const float gs   = g / r.s;
+            auto        mass = [&](float v) { return gs * exp2_fast(fmaf(v, k2, -mk)); };
+            again();
+#pragma unroll
+            for(int u = 0; u < NV; ++u)
+            {
+                float v[N];
+                row_decode<T>(w[u], v);
+#pragma unroll
+                for(int i = 0; i < N; ++i) v[i] = mass(v[i]);
+                if(t < z.vectors - u * WG)
+                    row_store(reinterpret_cast<T*>(reinterpret_cast<uint8_t*>(out) + static_cast<uint32_t>(z.column(u * WG + t)) * static_cast<uint32_t>(sizeof(T))),
+                              RowType<T>::pack(v));
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if(edge >= 0) out[edge] = static_cast<T>(mass(at_edge));
+            if constexpr(REST) map_span<T, WG>(rest, p.dz, p.ddt, row * p.cols, [&](int, float v) { return mass(v); });
+            __syncthreads();      // (behind the probabilities)
+            if(first) entries_subtract(p, row * p.cols, 0, p.cols, g, sh, mass);
+        }
+        else span_gradient<T, WG>(p, row, z, exact, sh);      // (rows of zeros or of extreme logits, other types)
         __syncthreads();
     }
 }
 
-// Few rows: the moments of the pieces ...
+// The loss alone, a row a workgroup.
+template <typename T> __global__ __launch_bounds__(kRowThreads) void distill_loss_kernel(const DistillArgs p)
+{
+    __shared__ EntriesShared sh;
+    __shared__ float4        slots[kRowThreads / kWaveSize];
+    const float              k2 = p.scale * kLog2e;
+    for(int64_t row = blockIdx.x; row < p.rows; row += gridDim.x)
+    {
+        const RowSpan<T> z(static_cast<const T*>(p.z) + row * p.ld, 0, p.cols);
+        if(threadIdx.x < kWaveSize)
+        {
+            entries_fetch(p, row, sh);
+            entries_prepare(p, z.row, sh);
+        }
+        LaneBest      none;
+        const Moments r = span_moments<T, kRowThreads, false, false>(z, k2, nullptr, none, slots);
+        if(threadIdx.x < kWaveSize)
+        {
+            const float loss = entries_loss(p, r, log_sum(r), sh);
+            if(threadIdx.x == 0) p.loss[row] = loss;
+        }
+        __syncthreads();
+    }
+}
+
+// Few long rows: the moments of the pieces ...
 template <typename T> __global__ __launch_bounds__(kRowThreads) void distill_pieces_kernel(const DistillArgs p)
 {
     __shared__ float4 slots[kRowThreads / kWaveSize];
-    const float       k2    = p.scale * kLog2e;
     const int64_t     items = p.rows * p.pieces;
     for(int64_t item = blockIdx.x; item < items; item += gridDim.x)
     {
-        const int64_t row   = item / p.pieces;
-        const int     begin = static_cast<int>(item - row * p.pieces) * p.piece;
-        const int     end   = p.cols - begin < p.piece ? p.cols : begin + p.piece;
-        LaneBest      none;
-        const Moments r = join_lanes<kRowThreads>(
-            row_pass<T, kRowThreads, false, false>(static_cast<const T*>(p.z) + row * p.ld, begin, end, k2, nullptr, none), k2, slots);
+        const int64_t    row   = item / p.pieces;
+        const int        begin = static_cast<int>(item - row * p.pieces) * p.piece;
+        const RowSpan<T> z(static_cast<const T*>(p.z) + row * p.ld, begin, p.cols - begin < p.piece ? p.cols : begin + p.piece);
+        LaneBest         none;
+        const Moments    r = span_moments<T, kRowThreads, false, false>(z, p.scale * kLog2e, nullptr, none, slots);
         if(threadIdx.x == 0) p.part[item] = make_float4(r.m, r.s, r.w, 0.0f);
         __syncthreads();
     }
@@ -668,17 +969,24 @@ template <typename T> __global__ __launch_bounds__(kRowThreads) void distill_joi
     const int64_t            items = p.dz ? p.rows * p.pieces : p.rows;
     for(int64_t item = blockIdx.x; item < items; item += gridDim.x)
     {
-        const int64_t row  = p.dz ? item / p.pieces : item;
-        const int     i    = p.dz ? static_cast<int>(item - row * p.pieces) : 0;
-        const Moments r    = join_pieces<kRowThreads>(p.part + row * p.pieces, p.pieces, p.scale * kLog2e, slots);
-        const float   ln_s = log_sum(r);
-        float         loss;
-        const Entry   e = row_entries<T, kRowThreads>(p, row, r, ln_s, sh, loss);
-        if(p.loss && i == 0 && threadIdx.x == 0) p.loss[row] = loss;
+        const int64_t row = p.dz ? item / p.pieces : item;
+        const int     i   = p.dz ? static_cast<int>(item - row * p.pieces) : 0;
+        const T*      z   = static_cast<const T*>(p.z) + row * p.ld;
+        if(threadIdx.x < kWaveSize)
+        {
+            entries_fetch(p, row, sh);
+            entries_prepare(p, z, sh);
+        }
+        const Moments r = join_pieces<kRowThreads>(p.part + row * p.pieces, p.pieces, p.scale * kLog2e, slots);
+        if(p.loss && i == 0 && threadIdx.x < kWaveSize)
+        {
+            const float loss = entries_loss(p, r, log_sum(r), sh);
+            if(threadIdx.x == 0) p.loss[row] = loss;
+        }
         if(p.dz)
         {
-            const int begin = i * p.piece, end = p.cols - begin < p.piece ? p.cols : begin + p.piece;
-            row_gradient<T, kRowThreads>(p, row, begin, end, r, ln_s, e, sh);
+            const int begin = i * p.piece;
+            span_gradient<T, kRowThreads>(p, row, RowSpan<T>(z, begin, p.cols - begin < p.piece ? p.cols : begin + p.piece), r, sh);
         }
         __syncthreads();
     }
@@ -692,7 +1000,7 @@ int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int vector_elements(int dt) { return dt == kF32 ? 4 : 8; }
 
 struct Split { int pieces, piece; };
-// Pieces of a row: enough to fill the device, of one vector a thread at least, and of `most` elements at most.
+// Pieces of a row: enough to fill the device, multiples of `least` elements, and of `most` elements at most.
 Split split_rows(int64_t rows, int64_t cols, int64_t least, int64_t most)
 {
     int64_t pieces = div_up(kFill, rows);
@@ -703,16 +1011,35 @@ Split split_rows(int64_t rows, int64_t cols, int64_t least, int64_t most)
     if(piece > most) piece = most;
     return Split{static_cast<int>(div_up(cols, piece)), static_cast<int>(piece)};
 }
+// A row a workgroup, or in pieces?  A compute unit takes in `unit` bytes of a row in a microsecond, however many threads ask for them, all of
+// them together `device`; pieces cost a second launch and what it reads, `launch` microseconds.
+struct RowRates { double unit, device, launch; };
+//   log probabilities, 20 alternatives, us, a row a workgroup -> in pieces: 1 x 131072 bfloat16 17.5 -> 11.9, 64 x 131072 18.3 -> 16.9,
+//   128 x 131072 18.9 -> 19.2, 1 x 32768 9.4 -> 11.1, 333 x 50021 fp32 22.3 -> 28.7
+constexpr RowRates kLogprobsRates = {27.0e3, 3.3e6, 3.5};
+//   loss alone: 1 x 131072 bfloat16 10.4 -> 8.3, 64 x 131072 12.1 -> 9.8, 1 x 32768 5.8 -> 8.3
+constexpr RowRates kLossRates = {45.0e3, 1.0e7, 3.0};
+//   loss and gradient: 1 x 131072 bfloat16 25.5 -> 11.4, 64 x 131072 27.5 -> 19.3, 200 x 131072 37.4 -> 41.8, 1 x 32768 11.3 -> 11.4
+constexpr RowRates kGradientRates = {14.0e3, 2.0e6, 5.0};
+bool in_pieces(const RowRates& t, int zdt, int64_t rows, int64_t cols)
+{
+    const double bytes = static_cast<double>(cols) * (zdt == kF32 ? 4 : 2);
+    return bytes / t.unit > t.launch + static_cast<double>(rows) * bytes / t.device;
+}
+// A top search keeps 6 bytes of LDS for every chunk of a thread: of 64 KB, beside its lists.
+constexpr int64_t kMaxChunks = 24;
+int64_t span_elements(int zdt) { return static_cast<int64_t>(kRowThreads) * vector_elements(zdt) * kUnroll; }
+int64_t piece_most(int zdt, int top) { return top > 0 ? span_elements(zdt) * kMaxChunks : kLogitsMaxCols; }
+Split whole_row(int64_t cols) { return Split{1, static_cast<int>(cols)}; }
 Split logprobs_split(int zdt, int64_t rows, int64_t cols, int top)
 {
-    const int64_t vector = static_cast<int64_t>(kRowThreads) * vector_elements(zdt);
-    return split_rows(rows, cols, vector, top > 0 ? vector * kUnroll * kMaxChunks : kLogitsMaxCols);
+    if(cols <= piece_most(zdt, top) && !in_pieces(kLogprobsRates, zdt, rows, cols)) return whole_row(cols);
+    return split_rows(rows, cols, span_elements(zdt), piece_most(zdt, top));
 }
 // what `rows` rows or fewer are cut into at most
 int64_t most_items(int zdt, int64_t rows, int64_t cols, int top)
 {
-    const int64_t vector = static_cast<int64_t>(kRowThreads) * vector_elements(zdt);
-    const int64_t fill = kFill + rows, cap = rows * (top > 0 ? div_up(cols, vector * kUnroll * kMaxChunks) : div_up(cols, kLogitsMaxCols));
+    const int64_t fill = kFill + rows, cap = rows * div_up(cols, piece_most(zdt, top));
     return fill > cap ? fill : cap;
 }
 dim3 groups(int64_t items) { return dim3(static_cast<unsigned>(items < kMostGroups ? items : kMostGroups)); }
@@ -720,7 +1047,7 @@ dim3 groups(int64_t items) { return dim3(static_cast<unsigned>(items < kMostGrou
 template <typename T> hipError_t logprobs_type(const LogitsArgs& a, hipStream_t st)
 {
     const dim3   grid = groups(a.rows * a.pieces), block(kRowThreads);
-    const size_t lds  = a.top > 0 ? top_lds_bytes((a.piece + chunk_span<T>() - 1) / chunk_span<T>()) : 0;
+    const size_t lds  = a.top > 0 ? top_lds_bytes(static_cast<int>(div_up(a.piece, chunk_span<T>(kRowThreads)))) : 0;
     if(a.top > 0)
     {
         if(a.entropy) logprobs_kernel<T, true, true><<<grid, block, lds, st>>>(a);
@@ -731,7 +1058,7 @@ template <typename T> hipError_t logprobs_type(const LogitsArgs& a, hipStream_t 
         if(a.entropy) logprobs_kernel<T, true, false><<<grid, block, 0, st>>>(a);
         else          logprobs_kernel<T, false, false><<<grid, block, 0, st>>>(a);
     }
-    hipError_t e = hipGetLastError();
+    const hipError_t e = hipGetLastError();
     if(e != hipSuccess || a.pieces == 1) return e;
     logprobs_join_kernel<T><<<groups(a.rows), block, 0, st>>>(a);
     return hipGetLastError();
@@ -744,12 +1071,25 @@ template <typename T> hipError_t logprobs_grad_type(const LogprobsGradArgs& a, h
     return hipGetLastError();
 }
 
+template <typename T, int WG, int NV, bool REST = false> hipError_t distill_held(const DistillArgs& a, hipStream_t st)
+{
+    distill_held_kernel<T, WG, NV, REST><<<groups(a.rows), dim3(WG), 0, st>>>(a);
+    return hipGetLastError();
+}
 template <typename T> hipError_t distill_type(const DistillArgs& a, hipStream_t st)
 {
-    if(a.pieces == 1)
+    if(a.pieces == 1 && !a.dz)
     {
-        distill_row_kernel<T, kRowThreads><<<groups(a.rows), dim3(kRowThreads), 0, st>>>(a);
+        distill_loss_kernel<T><<<groups(a.rows), dim3(kRowThreads), 0, st>>>(a);
         return hipGetLastError();
+    }
+    if(a.pieces == 1)
+    {   // (the fewest registers that hold a row: 4096 x 32768 bfloat16 on 512 threads of 8 vectors 132 us, 256 of 16 141; 8192 x 8000 on 256
+        // of 4 76)
+        const int64_t vectors = a.cols / RowType<T>::N;
+        if(vectors <= 256 * 4) return distill_held<T, 256, 4>(a, st);
+        if(vectors <= 512 * 8) return distill_held<T, 512, 8>(a, st);
+        return vectors <= 512 * 16 ? distill_held<T, 512, 16>(a, st) : distill_held<T, 512, 16, true>(a, st);
     }
     distill_pieces_kernel<T><<<groups(a.rows * a.pieces), dim3(kRowThreads), 0, st>>>(a);
     hipError_t e = hipGetLastError();
@@ -811,7 +1151,8 @@ hipError_t launch_distill_topk(const void* z, int zdt, int64_t rows, int64_t col
                                const void* index, bool wide, int k, const float* weight, float* loss, void* dz, int ddt, void* workspace,
                                hipStream_t st)
 {
-    const Split s = logprobs_split(zdt, rows, cols, 0);
+    const Split s = in_pieces(dz ? kGradientRates : kLossRates, zdt, rows, cols) ? split_rows(rows, cols, span_elements(zdt) / kUnroll, kLogitsMaxCols)
+                                                                                 : whole_row(cols);
     DistillArgs a{};
     a.z = z; a.rows = rows; a.ld = ld; a.cols = static_cast<int>(cols); a.scale = scale;
     a.pieces = s.pieces; a.piece = s.piece;
