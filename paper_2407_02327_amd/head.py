@@ -21,7 +21,9 @@ from . import qsync as Q
 from .operator import _scratch
 
 _FLOATS = (torch.float32, torch.float16, torch.bfloat16)
-_INTEGERS = (torch.int32, torch.int64)
+# The checks of the binding: an input's rows (-> its leading dimension), packed matrices and (0 columns) vectors of a kind of elements
+_check_rows, _check_packed = Q._native.check_rows, Q._native.check_packed
+_FLOAT32, _ANY_FLOAT, _INTEGER = 1, 2, 4
 
 
 def _float_type(dtype, what: str) -> None:
@@ -34,40 +36,12 @@ def _sizes(rows: int, cols: int) -> None:
         raise ValueError("rows must not be negative, cols must be positive")
 
 
-def _matrix(t: torch.Tensor, rows: int, cols: int, what: str) -> int:
-    """Checks an input [n <= rows, cols] whose rows are contiguous; returns its leading dimension."""
-    if t.dim() != 2 or t.shape[1] != cols or t.shape[0] > rows:
-        raise ValueError(f"{what}: at most {rows} rows of {cols} expected, not {tuple(t.shape)}")
-    if t.dtype not in _FLOATS:
-        raise ValueError(f"{what}: float32, float16 or bfloat16, not {t.dtype}")
-    n, ld = t.shape[0], t.stride(0)
-    if n <= 1:
-        ld = cols
-    if (cols > 1 and t.stride(1) != 1) or ld < cols:
-        raise ValueError(f"{what}: contiguous rows that do not overlap expected, strides {t.stride()}")
-    return ld
-
-
-def _vector(t: Optional[torch.Tensor], n: int, dtypes, what: str) -> None:
-    if t is not None and (t.dim() != 1 or t.shape[0] != n or t.dtype not in dtypes or not t.is_contiguous()):
-        raise ValueError(f"{what}: {n} contiguous elements of {' or '.join(str(d) for d in dtypes)} expected, not {tuple(t.shape)} of {t.dtype}")
-
-
-def _one_device(op, **tensors) -> None:
-    if op.device.type != "cuda":
-        raise ValueError(f"the operator's buffers are on {op.device}: its kernels run on a GPU")
-    for name, t in tensors.items():
-        if t is not None and t.device != op.device:
-            raise ValueError(f"{name} is on {t.device}, the operator's buffers on {op.device}")
-
-
-def _device(device) -> torch.device:
+def _gpu(device) -> int:
+    """The index of the GPU that buffers on `device` are on; -1: they are on none, and every call is refused."""
     d = torch.device(device)
-    return torch.device(d.type, torch.cuda.current_device()) if d.type == "cuda" and d.index is None else d
-
-
-def _first(t: Optional[torch.Tensor], n: int) -> Optional[torch.Tensor]:
-    return t if t is None or t.shape[0] == n else t[:n]
+    if d.type != "cuda":
+        return -1
+    return torch.cuda.current_device() if d.index is None else d.index
 
 
 class LayerNorm:
@@ -81,12 +55,12 @@ class LayerNorm:
         y_dtype, dx_dtype = y_dtype or x_dtype, dx_dtype or x_dtype
         for what, dt in (("x_dtype", x_dtype), ("y_dtype", y_dtype), ("dx_dtype", dx_dtype)):
             _float_type(dt, what)
-        self.rows, self.cols, self.eps, self.device = rows, cols, float(eps), _device(device)
+        self.rows, self.cols, self.eps, self.device = rows, cols, float(eps), _gpu(device)
         e = lambda *s, dt=torch.float32: torch.empty(*s, dtype=dt, device=device)
         self.y = e(rows, cols, dt=y_dtype)
         self.y_amax = torch.zeros(1, dtype=torch.float32, device=device) if collect_y_amax else None
         self.training = training
-        self._saved = None
+        self._saved = self.mean = self.rstd = None
         if training:
             self.mean, self.rstd = e(rows), e(rows)
             self.dx, self.dgamma, self.dbeta = e(rows, cols, dt=dx_dtype), e(cols), e(cols)
@@ -94,18 +68,16 @@ class LayerNorm:
 
     def forward(self, x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """x [n <= rows, cols], rows at any stride; gamma, beta: float32 or None (1 and 0).  `backward` reads x and gamma again."""
-        ld = _matrix(x, self.rows, self.cols, "x")
-        _vector(gamma, self.cols, (torch.float32,), "gamma")
-        _vector(beta, self.cols, (torch.float32,), "beta")
-        _one_device(self, x=x, gamma=gamma, beta=beta)
+        cols, device = self.cols, self.device
+        ld = _check_rows(x, self.rows, cols, device, "x")
+        _check_packed(gamma, cols, 0, _FLOAT32, device, "gamma")
+        _check_packed(beta, cols, 0, _FLOAT32, device, "beta")
         n = x.shape[0]
-        y = _first(self.y, n)
-        mean, rstd = (self.mean, self.rstd) if self.training else (None, None)
         if n:      # (a tensor without elements has no address)
-            Q.qsync_layernorm_fwd(x, n, self.cols, ld, gamma, beta, self.eps, y, mean, rstd, self.y_amax, stream)
+            Q.qsync_layernorm_fwd(x, n, cols, ld, gamma, beta, self.eps, self.y, self.mean, self.rstd, self.y_amax, stream)
         if self.training:
             self._saved = (x, gamma, ld)
-        return y
+        return self.y if n == self.rows else self.y[:n]
 
     def backward(self, dy: torch.Tensor, stream=None):
         """(dx, dgamma, dbeta) of the last `forward`; dy [n, cols] of the same number of rows."""
@@ -113,11 +85,10 @@ class LayerNorm:
             raise RuntimeError("backward without a forward of an operator with training=True")
         x, gamma, ldx = self._saved
         n = x.shape[0]
-        lddy = _matrix(dy, n, self.cols, "dy")
+        lddy = _check_rows(dy, n, self.cols, self.device, "dy")
         if dy.shape[0] != n:
             raise ValueError(f"dy has {dy.shape[0]} rows, the forward pass had {n}")
-        _one_device(self, dy=dy)
-        dx = _first(self.dx, n)
+        dx = self.dx if n == self.rows else self.dx[:n]
         if n == 0:
             self.dgamma.zero_()
             self.dbeta.zero_()
@@ -135,7 +106,7 @@ class TokenLogProbs:
         _sizes(rows, cols)
         if not 0 <= top_k <= min(64, cols):
             raise ValueError("top_k must lie between 0 and 64 and not exceed cols")
-        self.rows, self.cols, self.top_k, self.scale, self.device = rows, cols, top_k, float(scale), _device(device)
+        self.rows, self.cols, self.top_k, self.scale, self.device = rows, cols, top_k, float(scale), _gpu(device)
         e = lambda *s, dt=torch.float32: torch.empty(*s, dtype=dt, device=device)
         self.logp, self.stats = e(rows), e(rows, 2)
         self.entropy = e(rows) if entropy else None
@@ -149,15 +120,16 @@ class TokenLogProbs:
     def forward(self, logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, stream=None):
         """(logp, entropy, top_logp, top_index), each None where it is not wanted (logp: without tokens).  logits [n <= rows, cols], rows at
         any stride; tokens: n of int64 or int32, negative where a position has none.  `backward` reads logits and tokens again."""
-        ld = _matrix(logits, self.rows, self.cols, "logits")
+        ld = _check_rows(logits, self.rows, self.cols, self.device, "logits")
         n = logits.shape[0]
-        _vector(tokens, n, _INTEGERS, "tokens")
-        _one_device(self, logits=logits, tokens=tokens)
+        _check_packed(tokens, n, 0, _INTEGER, self.device, "tokens")
         logp = self.logp if tokens is not None else None
         if n:      # (a tensor without elements has no address)
             Q.qsync_token_logprobs(logits, n, self.cols, ld, self.scale, tokens, logp, self.entropy, self.stats, self.top_k, self.top_logp,
                                    self.top_index, self.ws, stream)
         self._saved = (logits, tokens, ld)
+        if n == self.rows:
+            return logp, self.entropy, self.top_logp, self.top_index
         return _first(logp, n), _first(self.entropy, n), _first(self.top_logp, n), _first(self.top_index, n)
 
     def backward(self, dlogp: Optional[torch.Tensor] = None, dentropy: Optional[torch.Tensor] = None, stream=None,
@@ -174,10 +146,9 @@ class TokenLogProbs:
             raise ValueError("dlogp needs a forward with tokens")
         if dentropy is not None and self.entropy is None:
             raise ValueError("dentropy needs an operator with entropy=True")
-        _vector(dlogp, n, (torch.float32,), "dlogp")
-        _vector(dentropy, n, (torch.float32,), "dentropy")
+        _check_packed(dlogp, n, 0, _FLOAT32, self.device, "dlogp")
+        _check_packed(dentropy, n, 0, _FLOAT32, self.device, "dentropy")
         out = _output(self, out, n)
-        _one_device(self, dlogp=dlogp, dentropy=dentropy, out=out)
         if n:
             Q.qsync_token_logprobs_bwd(logits, n, self.cols, ld, self.scale, tokens, self.stats, None if dentropy is None else self.entropy,
                                        dlogp, dentropy, out, stream)
@@ -193,7 +164,7 @@ class Distillation:
         _sizes(rows, cols)
         if not 1 <= k <= 256:
             raise ValueError("k must lie between 1 and 256")
-        self.rows, self.cols, self.k, self.scale, self.device = rows, cols, k, float(scale), _device(device)
+        self.rows, self.cols, self.k, self.scale, self.device = rows, cols, k, float(scale), _gpu(device)
         if dlogits_dtype is not None:
             _float_type(dlogits_dtype, "dlogits_dtype")
         self.loss = torch.empty(rows, dtype=torch.float32, device=device)
@@ -201,16 +172,15 @@ class Distillation:
         self.ws = _scratch(max(Q.qsync_distill_topk_workspace_bytes(t, rows, cols) for t in (Q.F32, Q.F16)), device)
 
     def _run(self, logits, teacher, index, weight, out, stream) -> torch.Tensor:
-        ld = _matrix(logits, self.rows, self.cols, "logits")
+        device = self.device
+        ld = _check_rows(logits, self.rows, self.cols, device, "logits")
         n = logits.shape[0]
-        for what, t, dtypes in (("teacher", teacher, _FLOATS), ("index", index, _INTEGERS)):
-            if t.dim() != 2 or tuple(t.shape) != (n, self.k) or t.dtype not in dtypes or not t.is_contiguous():
-                raise ValueError(f"{what}: contiguous [{n}, {self.k}] of {' or '.join(str(d) for d in dtypes)} expected, not {tuple(t.shape)} of {t.dtype}")
-        _vector(weight, n, (torch.float32,), "weight")
-        _one_device(self, logits=logits, teacher=teacher, index=index, weight=weight, out=out)
+        _check_packed(teacher, n, self.k, _ANY_FLOAT, device, "teacher")
+        _check_packed(index, n, self.k, _INTEGER, device, "index")
+        _check_packed(weight, n, 0, _FLOAT32, device, "weight")
         if n:      # (a tensor without elements has no address)
             Q.qsync_distill_topk(logits, n, self.cols, ld, self.scale, teacher, index, self.k, weight, self.loss, out, self.ws, stream)
-        return _first(self.loss, n)
+        return self.loss if n == self.rows else self.loss[:n]
 
     def forward(self, logits: torch.Tensor, teacher: torch.Tensor, index: torch.Tensor, stream=None) -> torch.Tensor:
         """The losses alone.  logits [n <= rows, cols], rows at any stride; teacher [n, k] logits or log probabilities, index [n, k] their
@@ -225,11 +195,14 @@ class Distillation:
         return self._run(logits, teacher, index, weight, out, stream), out
 
 
+def _first(t: Optional[torch.Tensor], n: int) -> Optional[torch.Tensor]:
+    return None if t is None else t[:n]
+
+
 def _output(op, out: Optional[torch.Tensor], n: int) -> torch.Tensor:
     if out is None:
         if op.dlogits is None:
             raise ValueError("an operator without dlogits_dtype needs `out`")
-        return _first(op.dlogits, n)
-    if out.dim() != 2 or tuple(out.shape) != (n, op.cols) or out.dtype not in _FLOATS or not out.is_contiguous():
-        raise ValueError(f"out: contiguous [{n}, {op.cols}] of float32, float16 or bfloat16 expected, not {tuple(out.shape)} of {out.dtype}")
+        return op.dlogits if n == op.rows else op.dlogits[:n]
+    _check_packed(out, n, op.cols, _ANY_FLOAT, op.device, "out")
     return out
