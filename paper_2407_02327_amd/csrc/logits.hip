@@ -15,6 +15,7 @@
 #include "row_ops.h"
 
 #include <cfloat>
+#include <type_traits>
 
 namespace qsync {
 
@@ -41,6 +42,7 @@ struct LogitsArgs
     int         cols;
     float       scale;
     int         pieces, piece;      // pieces of a row, elements of a piece
+    bool        streamed;
     const void* tokens;             // or nullptr
     int         wide;               // 64-bit tokens (indices)
     float *     logp, *entropy, *stats;
@@ -100,7 +102,7 @@ struct LaneBest
 // A row's elements [begin, end): whole 16-byte lines of memory, taken as vectors, and the fewer than two lines' elements in front of and
 // behind them, one each for the first threads ("edge").  A row of an odd number of elements is so read and written in whole lines: 2048 x
 // 65535 bfloat16 63.0 -> 54.8 us, a distillation step over 4096 x 65535 363 -> 256.
-template <typename T> struct RowSpan
+template <typename T, bool STREAMED> struct RowSpan
 {
     const T* row;
     int      begin, end, body, vectors;      // body: column of the first vector
@@ -119,13 +121,13 @@ template <typename T> struct RowSpan
         const int behind = body + vectors * RowType<T>::N + t - (body - begin);
         return behind < end ? behind : -1;
     }
-    template <int WG> __device__ int chunks() const { return (vectors + WG * kUnroll - 1) / (WG * kUnroll); }
+    template <int WG, int U = kUnroll> __device__ int chunks() const { return (vectors + WG * U - 1) / (WG * U); }
     // the number of vector u of chunk c of thread t, and a vector's column
-    template <int WG> static __device__ int vector(int c, int u, int t) { return (c * kUnroll + u) * WG + t; }
+    template <int WG, int U = kUnroll> static __device__ int vector(int c, int u, int t) { return (c * U + u) * WG + t; }
     // the vectors from number i on, without edges
-    __device__ RowSpan from(int i) const
+    template <bool S> __device__ RowSpan<T, S> from(int i) const
     {
-        RowSpan s;
+        RowSpan<T, S> s;
         s.row     = row;
         s.vectors = vectors > i ? vectors - i : 0;
         s.begin = s.body = column(i);
@@ -134,34 +136,35 @@ template <typename T> struct RowSpan
     }
     __device__ int column(int i) const { return body + i * RowType<T>::N; }
     // (a row's address in scalar registers and 32-bit offsets: a row of 2^30 fp32 elements ends below 2^32 bytes)
-    __device__ __forceinline__ row_v4u32 load(int i) const
+    __device__ __forceinline__ const T* at(int i) const
     {
-        return row_load(reinterpret_cast<const T*>(reinterpret_cast<const uint8_t*>(row) + static_cast<uint32_t>(column(i)) * static_cast<uint32_t>(sizeof(T))));
+        return reinterpret_cast<const T*>(reinterpret_cast<const uint8_t*>(row) + static_cast<uint32_t>(column(i)) * static_cast<uint32_t>(sizeof(T)));
     }
+    __device__ __forceinline__ row_v4u32 load(int i) const { return row_load<STREAMED>(at(i)); }
 };
 
 // One pass over a span.  FAR: the differences to the maximum are taken first, so that any finite logits do; otherwise z k2 less the rounded
 // product m k2 is one operation, for rows whose maximum lies within 1e30 (a lane's reference does not go below -1e30: what lies there is 0
 // beside such a maximum).  The lanes' sums are then relative to that product; join_lanes keeps to it.
-template <typename T, int WG, bool ENTROPY, bool TOP, bool FAR>
-__device__ __forceinline__ Moments row_pass(const RowSpan<T>& z, float k2, float* chunk_max, LaneBest& best)
+template <typename T, int WG, int U, bool ENTROPY, bool TOP, bool FAR, bool STREAMED>
+__device__ __forceinline__ Moments row_pass(const RowSpan<T, STREAMED>& z, float k2, float* chunk_max, LaneBest& best)
 {
     constexpr int N = RowType<T>::N;
-    const int     tid = threadIdx.x, chunks = z.template chunks<WG>();
-    row_v4u32     next[kUnroll];
+    const int     tid = threadIdx.x, chunks = z.template chunks<WG, U>();
+    row_v4u32     next[U];
     auto          fetch = [&](int c) {
-        if((c + 1) * kUnroll * WG <= z.vectors)
+        if((c + 1) * U * WG <= z.vectors)
         {
 #pragma unroll
-            for(int u = 0; u < kUnroll; ++u) next[u] = z.load(z.template vector<WG>(c, u, tid));
+            for(int u = 0; u < U; ++u) next[u] = z.load(z.template vector<WG, U>(c, u, tid));
             return;
         }
 #pragma unroll
-        for(int u = 0; u < kUnroll; ++u)
+        for(int u = 0; u < U; ++u)
         {
             constexpr uint32_t absent = RowType<T>::kMinusInf;
             next[u] = row_v4u32{absent, absent, absent, absent};
-            if(tid < z.vectors - z.template vector<WG>(c, u, 0)) next[u] = z.load(z.template vector<WG>(c, u, tid));
+            if(tid < z.vectors - z.template vector<WG, U>(c, u, 0)) next[u] = z.load(z.template vector<WG, U>(c, u, tid));
         }
     };
     const int edge = z.edge(tid);
@@ -175,13 +178,13 @@ __device__ __forceinline__ Moments row_pass(const RowSpan<T>& z, float k2, float
     }
     for(int c = 0; c < chunks; ++c)
     {
-        float v[kUnroll * N];
+        float v[U * N];
 #pragma unroll
-        for(int u = 0; u < kUnroll; ++u) row_decode<T>(next[u], v + u * N);
+        for(int u = 0; u < U; ++u) row_decode<T>(next[u], v + u * N);
         if(c + 1 < chunks) fetch(c + 1);
         float top = v[0];
 #pragma unroll
-        for(int i = 1; i < kUnroll * N; ++i) top = fmaxf(top, v[i]);
+        for(int i = 1; i < U * N; ++i) top = fmaxf(top, v[i]);
         if constexpr(TOP)
         {
             chunk_max[c * WG + tid] = top;
@@ -194,7 +197,7 @@ __device__ __forceinline__ Moments row_pass(const RowSpan<T>& z, float k2, float
         r.s *= f;
         r.m = m;
 #pragma unroll
-        for(int i = 0; i < kUnroll * N; ++i)
+        for(int i = 0; i < U * N; ++i)
         {
             const float d = FAR ? (v[i] - m) * k2 : fmaf(v[i], k2, -mk), e = exp2_fast(d);
             r.s += e;
@@ -205,17 +208,14 @@ __device__ __forceinline__ Moments row_pass(const RowSpan<T>& z, float k2, float
 }
 
 // The moments of a span, in every lane.
-template <typename T, int WG, bool ENTROPY, bool TOP>
-__device__ __forceinline__ Moments span_moments(const RowSpan<T>& z, float k2, float* chunk_max, LaneBest& best, float4* slots)
+template <typename T, int WG, int U, bool ENTROPY, bool TOP, bool STREAMED>
+__device__ __forceinline__ Moments span_moments(const RowSpan<T, STREAMED>& z, float k2, float* chunk_max, LaneBest& best, float4* slots)
 {
-    if(k2 < 1.0e7f)
-    {
-        const Moments r = join_lanes<WG, false>(row_pass<T, WG, ENTROPY, TOP, false>(z, k2, chunk_max, best), k2, slots);
-        if(fabsf(r.m) < -kFar) return r;
-        __syncthreads();      // (all lanes have read the slots)
-    }
-    best = LaneBest{};
-    return join_lanes<WG, true>(row_pass<T, WG, ENTROPY, TOP, true>(z, k2, chunk_max, best), k2, slots);
+    const Moments r = join_lanes<WG, false>(row_pass<T, WG, U, ENTROPY, TOP, false>(z, k2, chunk_max, best), k2, slots);
+    if(fabsf(r.m) < -kFar && k2 < 1.0e7f) return r;
+    __syncthreads();      // (all lanes have read the slots)
+    LaneBest none;
+    return join_lanes<WG, true>(row_pass<T, WG, 1, ENTROPY, false, true>(z, k2, nullptr, none), k2, slots);
 }
 
 // ---- top alternatives -------------------------------------------------------------------------------------------------------
@@ -324,8 +324,8 @@ __device__ __forceinline__ void join_lists(uint64_t& key, int lists, uint64_t (&
 // below it is not looked at again.  About k chunks (32 or 16 elements) remain of a row, and never more than the k best groups
 // have; they are read a second time, out of a cache, and what reaches the bound is sorted.  The work beside the pass hardly depends on
 // the order of the logits, and the order (value, then lower column) makes equal logits as good as different ones.
-template <typename T>
-__device__ __forceinline__ uint64_t row_top(const RowSpan<T>& z, int top, const LaneBest& best, const float* chunk_max, uint16_t* chosen, TopShared& sh)
+template <typename T, bool STREAMED>
+__device__ __forceinline__ uint64_t row_top(const RowSpan<T, STREAMED>& z, int top, const LaneBest& best, const float* chunk_max, uint16_t* chosen, TopShared& sh)
 {
     constexpr int N = RowType<T>::N, WG = kRowThreads, WAVES = WG / kWaveSize;
     const int     tid = threadIdx.x, lane = tid % kWaveSize, wave = tid / kWaveSize, chunks = z.template chunks<WG>();
@@ -484,7 +484,7 @@ __device__ __forceinline__ void write_logprobs(const LogitsArgs& p, int64_t row,
 }
 
 // Item: a piece of a row.  One piece a row: the results; several: their moments and lists.
-template <typename T, bool ENTROPY, bool TOP> __global__ __launch_bounds__(kRowThreads) void logprobs_kernel(const LogitsArgs p)
+template <typename T, bool ENTROPY, bool TOP, bool STREAMED> __global__ __launch_bounds__(kRowThreads) void logprobs_kernel(const LogitsArgs p)
 {
     constexpr int WG = kRowThreads;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
@@ -496,9 +496,9 @@ template <typename T, bool ENTROPY, bool TOP> __global__ __launch_bounds__(kRowT
     {
         const int64_t    row   = item / p.pieces;
         const int        begin = static_cast<int>(item - row * p.pieces) * p.piece;
-        const RowSpan<T> z(static_cast<const T*>(p.z) + row * p.ld, begin, p.cols - begin < p.piece ? p.cols : begin + p.piece);
+        const RowSpan<T, STREAMED> z(static_cast<const T*>(p.z) + row * p.ld, begin, p.cols - begin < p.piece ? p.cols : begin + p.piece);
         LaneBest         best;
-        const Moments    r   = span_moments<T, WG, ENTROPY, TOP>(z, k2, chunk_max, best, slots);
+        const Moments    r   = span_moments<T, WG, kUnroll, ENTROPY, TOP>(z, k2, chunk_max, best, slots);
         uint64_t         key = 0;
         if constexpr(TOP)
         {
@@ -573,6 +573,7 @@ struct LogprobsGradArgs
     int          cols;
     float        scale;
     int          pieces, piece;
+    bool         streamed;
     const void*  tokens;
     int          wide;
     const float *stats, *entropy, *dlogp, *dentropy;      // entropy and dentropy both or neither; dlogp or nullptr
@@ -581,7 +582,7 @@ struct LogprobsGradArgs
 };
 
 // Walks over a span, 32 bytes of a lane in flight: body(column, values of a vector), edge(column, value).
-template <typename T, int WG, typename F, typename G> __device__ __forceinline__ void walk(const RowSpan<T>& z, F&& body, G&& edge)
+template <typename T, int WG, bool STREAMED, typename F, typename G> __device__ __forceinline__ void walk(const RowSpan<T, STREAMED>& z, F&& body, G&& edge)
 {
     constexpr int U = 2, N = RowType<T>::N;
     int           i = threadIdx.x;
@@ -606,7 +607,7 @@ template <typename T, int WG, typename F, typename G> __device__ __forceinline__
     }
 }
 // The result of f for every element of a span, to a buffer of type dtype whose row begins at `at`.
-template <typename T, int WG, typename F> __device__ __forceinline__ void map_span(const RowSpan<T>& z, void* out, int dtype, int64_t at, F&& f)
+template <typename T, int WG, bool STREAMED, typename F> __device__ __forceinline__ void map_span(const RowSpan<T, STREAMED>& z, void* out, int dtype, int64_t at, F&& f)
 {
     constexpr int N = RowType<T>::N;
     walk<T, WG>(
@@ -615,19 +616,19 @@ template <typename T, int WG, typename F> __device__ __forceinline__ void map_sp
             float o[N];
 #pragma unroll
             for(int e = 0; e < N; ++e) o[e] = f(c + e, v[e]);
-            vector_store<T>(out, dtype, at + c, o);
+            vector_store<T, STREAMED>(out, dtype, at + c, o);
         },
         [&](int c, float v) { element_store(out, dtype, at + c, f(c, v)); });
 }
-template <typename T, int WG> __device__ __forceinline__ void zero_span(const RowSpan<T>& z, void* out, int dtype, int64_t at)
+template <typename T, int WG, bool STREAMED> __device__ __forceinline__ void zero_span(const RowSpan<T, STREAMED>& z, void* out, int dtype, int64_t at)
 {
     const float o[RowType<T>::N] = {};
-    for(int i = threadIdx.x; i < z.vectors; i += WG) vector_store<T>(out, dtype, at + z.column(i), o);
+    for(int i = threadIdx.x; i < z.vectors; i += WG) vector_store<T, STREAMED>(out, dtype, at + z.column(i), o);
     const int e = z.edge(threadIdx.x);
     if(e >= 0) element_store(out, dtype, at + e, 0.0f);
 }
 
-template <typename T, bool ENTROPY> __global__ __launch_bounds__(kRowThreads) void logprobs_grad_kernel(const LogprobsGradArgs p)
+template <typename T, bool ENTROPY, bool STREAMED> __global__ __launch_bounds__(kRowThreads) void logprobs_grad_kernel(const LogprobsGradArgs p)
 {
     const float   k2    = p.scale * kLog2e;
     const int64_t items = p.rows * p.pieces;
@@ -647,7 +648,7 @@ template <typename T, bool ENTROPY> __global__ __launch_bounds__(kRowThreads) vo
         }
         if(given >= p.cols) g = NAN;      // (no column of it: the row says so)
         const int64_t    at = row * p.cols;
-        const RowSpan<T> z(static_cast<const T*>(p.z) + row * p.ld, begin, end);
+        const RowSpan<T, STREAMED> z(static_cast<const T*>(p.z) + row * p.ld, begin, end);
         if(ln_s == -INFINITY || (g == 0.0f && h == 0.0f))
         {
             zero_span<T, kRowThreads>(z, p.dz, p.ddt, at);
@@ -672,6 +673,7 @@ struct DistillArgs
     int          cols;
     float        scale;
     int          pieces, piece;
+    bool         streamed;
     const void*  teacher;
     int          tdt;
     const void*  index;
@@ -779,8 +781,8 @@ __device__ __forceinline__ float row_factor(const DistillArgs& p, int64_t row, c
 __device__ __forceinline__ float log_sum(const Moments& r) { return r.s == 0.0f ? -INFINITY : logf(r.s); }
 
 // The gradient of a span from logits that are read again.
-template <typename T, int WG>
-__device__ __forceinline__ void span_gradient(const DistillArgs& p, int64_t row, const RowSpan<T>& z, const Moments& r, const EntriesShared& sh)
+template <typename T, int WG, bool STREAMED>
+__device__ __forceinline__ void span_gradient(const DistillArgs& p, int64_t row, const RowSpan<T, STREAMED>& z, const Moments& r, const EntriesShared& sh)
 {
     const int64_t at = row * p.cols;
     const float   g  = row_factor(p, row, r, sh);
@@ -802,7 +804,7 @@ __device__ __forceinline__ void span_gradient(const DistillArgs& p, int64_t row,
 //   twice 272 (512 threads) and 309 (256).
 // (Four wavefronts of a SIMD leave 128 registers.  The scheduling barriers keep the phases from being unrolled into more values than
 // that; the words are taken apart again in each phase, as fp32 values they would take twice the registers.)
-template <typename T, int WG, int NV, bool REST> __global__ __launch_bounds__(WG, 4) void distill_held_kernel(const DistillArgs p)
+template <typename T, int WG, int NV, bool REST, bool STREAMED> __global__ __launch_bounds__(WG, 4) void distill_held_kernel(const DistillArgs p)
 {
     constexpr int            N = RowType<T>::N, WAVES = WG / kWaveSize;
     __shared__ EntriesShared sh;
@@ -813,7 +815,7 @@ template <typename T, int WG, int NV, bool REST> __global__ __launch_bounds__(WG
     const float              k2 = p.scale * kLog2e;
     for(int64_t row = blockIdx.x; row < p.rows; row += gridDim.x)
     {
-        const RowSpan<T> z(static_cast<const T*>(p.z) + row * p.ld, 0, p.cols);
+        const RowSpan<T, STREAMED> z(static_cast<const T*>(p.z) + row * p.ld, 0, p.cols);
         if(first) entries_fetch(p, row, sh);
         row_v4u32 w[NV];
         int       t = tid;
@@ -828,13 +830,13 @@ template <typename T, int WG, int NV, bool REST> __global__ __launch_bounds__(WG
         const int   edge    = z.edge(tid);
         const float at_edge = edge >= 0 ? row_element(z.row + edge) : -INFINITY;
         if(first) entries_prepare(p, z.row, sh);
-        RowSpan<T> rest;
-        LaneBest   none;
-        Moments    r{-FLT_MAX, 0.0f, 0.0f};
+        RowSpan<T, false> rest;      // (read again)
+        LaneBest          none;
+        Moments           r{-FLT_MAX, 0.0f, 0.0f};
         if constexpr(REST)
         {
-            rest = z.from(WG * NV);
-            r    = row_pass<T, WG, false, false, false>(rest, k2, nullptr, none);
+            rest = z.template from<false>(WG * NV);
+            r    = row_pass<T, WG, 2, false, false, false>(rest, k2, nullptr, none);
         }
         const float rest_m = r.m;
         r.m = fmaxf(r.m, at_edge);
@@ -885,7 +887,7 @@ template <typename T, int WG, int NV, bool REST> __global__ __launch_bounds__(WG
             exact = r;
             exact.s *= exp2_fast(-fmaf(r.m, k2, -mk));
         }
-        else exact = r = span_moments<T, WG, false, false>(z, k2, nullptr, none, slots);
+        else exact = r = join_lanes<WG, true>(row_pass<T, WG, 1, false, false, true>(z, k2, nullptr, none), k2, slots);
         if(first)
         {
             const float loss = entries_loss(p, exact, log_sum(exact), sh);
@@ -906,12 +908,12 @@ template <typename T, int WG, int NV, bool REST> __global__ __launch_bounds__(WG
 #pragma unroll
                 for(int i = 0; i < N; ++i) v[i] = mass(v[i]);
                 if(t < z.vectors - u * WG)
-                    row_store(reinterpret_cast<T*>(reinterpret_cast<uint8_t*>(out) + static_cast<uint32_t>(z.column(u * WG + t)) * static_cast<uint32_t>(sizeof(T))),
-                              RowType<T>::pack(v));
+                    row_store<STREAMED>(reinterpret_cast<T*>(reinterpret_cast<uint8_t*>(out) + static_cast<uint32_t>(z.column(u * WG + t)) * static_cast<uint32_t>(sizeof(T))),
+                                        RowType<T>::pack(v));
                 __builtin_amdgcn_sched_barrier(0);
             }
             if(edge >= 0) out[edge] = static_cast<T>(mass(at_edge));
-            if constexpr(REST) map_span<T, WG>(rest, p.dz, p.ddt, row * p.cols, [&](int, float v) { return mass(v); });
+            if constexpr(REST) map_span<T, WG>(z.template from<STREAMED>(WG * NV), p.dz, p.ddt, row * p.cols, [&](int, float v) { return mass(v); });
             __syncthreads();      // (behind the probabilities)
             if(first) entries_subtract(p, row * p.cols, 0, p.cols, g, sh, mass);
         }
@@ -921,21 +923,21 @@ template <typename T, int WG, int NV, bool REST> __global__ __launch_bounds__(WG
 }
 
 // The loss alone, a row a workgroup.
-template <typename T> __global__ __launch_bounds__(kRowThreads) void distill_loss_kernel(const DistillArgs p)
+template <typename T, bool STREAMED> __global__ __launch_bounds__(kRowThreads) void distill_loss_kernel(const DistillArgs p)
 {
     __shared__ EntriesShared sh;
     __shared__ float4        slots[kRowThreads / kWaveSize];
     const float              k2 = p.scale * kLog2e;
     for(int64_t row = blockIdx.x; row < p.rows; row += gridDim.x)
     {
-        const RowSpan<T> z(static_cast<const T*>(p.z) + row * p.ld, 0, p.cols);
+        const RowSpan<T, STREAMED> z(static_cast<const T*>(p.z) + row * p.ld, 0, p.cols);
         if(threadIdx.x < kWaveSize)
         {
             entries_fetch(p, row, sh);
             entries_prepare(p, z.row, sh);
         }
         LaneBest      none;
-        const Moments r = span_moments<T, kRowThreads, false, false>(z, k2, nullptr, none, slots);
+        const Moments r = span_moments<T, kRowThreads, kUnroll, false, false>(z, k2, nullptr, none, slots);
         if(threadIdx.x < kWaveSize)
         {
             const float loss = entries_loss(p, r, log_sum(r), sh);
@@ -954,9 +956,9 @@ template <typename T> __global__ __launch_bounds__(kRowThreads) void distill_pie
     {
         const int64_t    row   = item / p.pieces;
         const int        begin = static_cast<int>(item - row * p.pieces) * p.piece;
-        const RowSpan<T> z(static_cast<const T*>(p.z) + row * p.ld, begin, p.cols - begin < p.piece ? p.cols : begin + p.piece);
+        const RowSpan<T, false> z(static_cast<const T*>(p.z) + row * p.ld, begin, p.cols - begin < p.piece ? p.cols : begin + p.piece);
         LaneBest         none;
-        const Moments    r = span_moments<T, kRowThreads, false, false>(z, p.scale * kLog2e, nullptr, none, slots);
+        const Moments    r = span_moments<T, kRowThreads, kUnroll, false, false>(z, p.scale * kLog2e, nullptr, none, slots);
         if(threadIdx.x == 0) p.part[item] = make_float4(r.m, r.s, r.w, 0.0f);
         __syncthreads();
     }
@@ -986,7 +988,7 @@ template <typename T> __global__ __launch_bounds__(kRowThreads) void distill_joi
         if(p.dz)
         {
             const int begin = i * p.piece;
-            span_gradient<T, kRowThreads>(p, row, RowSpan<T>(z, begin, p.cols - begin < p.piece ? p.cols : begin + p.piece), r, sh);
+            span_gradient<T, kRowThreads>(p, row, RowSpan<T, false>(z, begin, p.cols - begin < p.piece ? p.cols : begin + p.piece), r, sh);
         }
         __syncthreads();
     }
@@ -1042,22 +1044,29 @@ int64_t most_items(int zdt, int64_t rows, int64_t cols, int top)
     const int64_t fill = kFill + rows, cap = rows * div_up(cols, piece_most(zdt, top));
     return fill > cap ? fill : cap;
 }
+// Logits and gradients that no cache (256 MB in front of the memory) holds until their next reader are streamed.  us, ordinary -> streamed:
+// log probabilities of 2048 x 65536 bfloat16 (268 MB) 55.2 -> 49.1, their gradient 109.5 -> 102, distillation 4096 x 65536 233 -> 219;
+// the latter with the INT8 conversion of the gradient behind it 4096 x 32768 binary16 260 -> 249, but 2048 x 32768 128 -> 132.
+bool streamed(int dt, int64_t rows, int64_t cols) { return rows * cols * (dt == kF32 ? 4 : 2) > (int64_t(192) << 20); }
+// f(std::true_type or std::false_type)
+template <typename F> void choose(bool v, F&& f)
+{
+    if(v) f(std::true_type{});
+    else  f(std::false_type{});
+}
 dim3 groups(int64_t items) { return dim3(static_cast<unsigned>(items < kMostGroups ? items : kMostGroups)); }
 
 template <typename T> hipError_t logprobs_type(const LogitsArgs& a, hipStream_t st)
 {
     const dim3   grid = groups(a.rows * a.pieces), block(kRowThreads);
     const size_t lds  = a.top > 0 ? top_lds_bytes(static_cast<int>(div_up(a.piece, chunk_span<T>(kRowThreads)))) : 0;
-    if(a.top > 0)
-    {
-        if(a.entropy) logprobs_kernel<T, true, true><<<grid, block, lds, st>>>(a);
-        else          logprobs_kernel<T, false, true><<<grid, block, lds, st>>>(a);
-    }
-    else
-    {
-        if(a.entropy) logprobs_kernel<T, true, false><<<grid, block, 0, st>>>(a);
-        else          logprobs_kernel<T, false, false><<<grid, block, 0, st>>>(a);
-    }
+    choose(a.entropy != nullptr, [&](auto entropy) {
+        choose(a.top > 0, [&](auto top) {
+            choose(a.streamed, [&](auto through) {
+                logprobs_kernel<T, decltype(entropy)::value, decltype(top)::value, decltype(through)::value><<<grid, block, lds, st>>>(a);
+            });
+        });
+    });
     const hipError_t e = hipGetLastError();
     if(e != hipSuccess || a.pieces == 1) return e;
     logprobs_join_kernel<T><<<groups(a.rows), block, 0, st>>>(a);
@@ -1066,21 +1075,24 @@ template <typename T> hipError_t logprobs_type(const LogitsArgs& a, hipStream_t 
 
 template <typename T> hipError_t logprobs_grad_type(const LogprobsGradArgs& a, hipStream_t st)
 {
-    if(a.dentropy) logprobs_grad_kernel<T, true><<<groups(a.rows * a.pieces), dim3(kRowThreads), 0, st>>>(a);
-    else           logprobs_grad_kernel<T, false><<<groups(a.rows * a.pieces), dim3(kRowThreads), 0, st>>>(a);
+    choose(a.dentropy != nullptr, [&](auto entropy) {
+        choose(a.streamed, [&](auto through) {
+            logprobs_grad_kernel<T, decltype(entropy)::value, decltype(through)::value><<<groups(a.rows * a.pieces), dim3(kRowThreads), 0, st>>>(a);
+        });
+    });
     return hipGetLastError();
 }
 
 template <typename T, int WG, int NV, bool REST = false> hipError_t distill_held(const DistillArgs& a, hipStream_t st)
 {
-    distill_held_kernel<T, WG, NV, REST><<<groups(a.rows), dim3(WG), 0, st>>>(a);
+    choose(a.streamed, [&](auto through) { distill_held_kernel<T, WG, NV, REST, decltype(through)::value><<<groups(a.rows), dim3(WG), 0, st>>>(a); });
     return hipGetLastError();
 }
 template <typename T> hipError_t distill_type(const DistillArgs& a, hipStream_t st)
 {
     if(a.pieces == 1 && !a.dz)
     {
-        distill_loss_kernel<T><<<groups(a.rows), dim3(kRowThreads), 0, st>>>(a);
+        choose(a.streamed, [&](auto through) { distill_loss_kernel<T, decltype(through)::value><<<groups(a.rows), dim3(kRowThreads), 0, st>>>(a); });
         return hipGetLastError();
     }
     if(a.pieces == 1)
@@ -1124,7 +1136,7 @@ hipError_t launch_token_logprobs(const void* z, int zdt, int64_t rows, int64_t c
     const Split s = logprobs_split(zdt, rows, cols, top);
     LogitsArgs  a{};
     a.z = z; a.rows = rows; a.ld = ld; a.cols = static_cast<int>(cols); a.scale = scale;
-    a.pieces = s.pieces; a.piece = s.piece;
+    a.pieces = s.pieces; a.piece = s.piece; a.streamed = streamed(zdt, rows, cols);
     a.tokens = tokens; a.wide = wide; a.logp = logp; a.entropy = entropy; a.stats = stats;
     a.top = top; a.top_logp = top_logp; a.top_index = top_index;
     a.part = static_cast<float4*>(workspace);
@@ -1139,7 +1151,7 @@ hipError_t launch_token_logprobs_bwd(const void* z, int zdt, int64_t rows, int64
     const Split      s = split_rows(rows, cols, kRowThreads * 8, kRowThreads * 8 * 16);
     LogprobsGradArgs a{};
     a.z = z; a.rows = rows; a.ld = ld; a.cols = static_cast<int>(cols); a.scale = scale;
-    a.pieces = s.pieces; a.piece = s.piece;
+    a.pieces = s.pieces; a.piece = s.piece; a.streamed = streamed(zdt, rows, cols);
     a.tokens = tokens; a.wide = wide; a.stats = stats; a.entropy = entropy; a.dlogp = dlogp; a.dentropy = dentropy;
     a.dz = dz; a.ddt = ddt;
     return by_type(zdt, [&](auto tag) { return logprobs_grad_type<decltype(tag)>(a, st); });
@@ -1155,7 +1167,7 @@ hipError_t launch_distill_topk(const void* z, int zdt, int64_t rows, int64_t col
                                                                                  : whole_row(cols);
     DistillArgs a{};
     a.z = z; a.rows = rows; a.ld = ld; a.cols = static_cast<int>(cols); a.scale = scale;
-    a.pieces = s.pieces; a.piece = s.piece;
+    a.pieces = s.pieces; a.piece = s.piece; a.streamed = streamed(zdt, rows, cols);
     a.teacher = teacher; a.tdt = tdt; a.index = index; a.wide = wide; a.k = k; a.weight = weight; a.loss = loss;
     a.dz = dz; a.ddt = ddt;
     a.part = static_cast<float4*>(workspace);

@@ -67,31 +67,35 @@ template <> struct RowType<__bf16>
     }
 };
 
-template <typename T> __device__ __forceinline__ row_v4u32 row_load(const T* p)
+// (STREAMED: past the caches' room for what is read again.  A template's argument: of two branches that differ in it alone the compiler
+// makes one ordinary access.)
+template <bool STREAMED = false, typename T> __device__ __forceinline__ row_v4u32 row_load(const T* p)
 {
-    return *reinterpret_cast<const typename RowType<T>::vec_t*>(p);
+    if constexpr(STREAMED) return __builtin_nontemporal_load(reinterpret_cast<const typename RowType<T>::vec_t*>(p));
+    else                   return *reinterpret_cast<const typename RowType<T>::vec_t*>(p);
 }
-template <typename T> __device__ __forceinline__ void row_store(T* p, const row_v4u32& w)
+template <bool STREAMED = false, typename T> __device__ __forceinline__ void row_store(T* p, const row_v4u32& w)
 {
-    *reinterpret_cast<typename RowType<T>::vec_t*>(p) = w;
+    if constexpr(STREAMED) __builtin_nontemporal_store(w, reinterpret_cast<typename RowType<T>::vec_t*>(p));
+    else                   *reinterpret_cast<typename RowType<T>::vec_t*>(p) = w;
 }
 template <typename T> __device__ __forceinline__ float row_element(const T* p) { return static_cast<float>(*p); }
 
 // A vector of T as values, to a buffer of any type (the same for every lane); and one element.
-template <typename T> __device__ __forceinline__ void vector_store(void* base, int dtype, int64_t at, const float (&v)[RowType<T>::N])
+template <typename T, bool STREAMED> __device__ __forceinline__ void vector_store(void* base, int dtype, int64_t at, const float (&v)[RowType<T>::N])
 {
     if constexpr(RowType<T>::N == 8)
     {
-        if(dtype == kF16) row_store(static_cast<_Float16*>(base) + at, RowType<_Float16>::pack(v));
-        else if(dtype == kBF16) row_store(static_cast<__bf16*>(base) + at, RowType<__bf16>::pack(v));
+        if(dtype == kF16) row_store<STREAMED>(static_cast<_Float16*>(base) + at, RowType<_Float16>::pack(v));
+        else if(dtype == kBF16) row_store<STREAMED>(static_cast<__bf16*>(base) + at, RowType<__bf16>::pack(v));
         else
         {
             const float lo[4] = {v[0], v[1], v[2], v[3]}, hi[4] = {v[4], v[5], v[6], v[7]};
-            row_store(static_cast<float*>(base) + at, RowType<float>::pack(lo));
-            row_store(static_cast<float*>(base) + at + 4, RowType<float>::pack(hi));
+            row_store<STREAMED>(static_cast<float*>(base) + at, RowType<float>::pack(lo));
+            row_store<STREAMED>(static_cast<float*>(base) + at + 4, RowType<float>::pack(hi));
         }
     }
-    else if(dtype == kF32) row_store(static_cast<float*>(base) + at, RowType<float>::pack(v));
+    else if(dtype == kF32) row_store<STREAMED>(static_cast<float*>(base) + at, RowType<float>::pack(v));
     else
     {
         typedef unsigned half_vector __attribute__((ext_vector_type(2), aligned(2)));
