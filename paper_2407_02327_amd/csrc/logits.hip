@@ -42,7 +42,6 @@ struct LogitsArgs
     int         cols;
     float       scale;
     int         pieces, piece;      // pieces of a row, elements of a piece
-    bool        streamed;
     const void* tokens;             // or nullptr
     int         wide;               // 64-bit tokens (indices)
     float *     logp, *entropy, *stats;
@@ -101,8 +100,10 @@ struct LaneBest
 
 // A row's elements [begin, end): whole 16-byte lines of memory, taken as vectors, and the fewer than two lines' elements in front of and
 // behind them, one each for the first threads ("edge").  A row of an odd number of elements is so read and written in whole lines: 2048 x
-// 65535 bfloat16 63.0 -> 54.8 us, a distillation step over 4096 x 65535 363 -> 256.
-template <typename T, bool STREAMED> struct RowSpan
+// 65535 bfloat16 63.0 -> 54.8 us, a distillation step over 4096 x 65535 363 -> 256.  ONCE: the loads are streamed, so that they leave the
+// caches to what is read again -- the gradient, for one, by the head's backward pass (us: log probabilities of 2048 x 65536 bfloat16 55 ->
+// 49, a distillation step over 1024 x 32768 binary16 41.3 -> 39.1, with the INT8 conversion of its gradient 74.5 -> 71.8).
+template <typename T, bool ONCE> struct RowSpan
 {
     const T* row;
     int      begin, end, body, vectors;      // body: column of the first vector
@@ -140,14 +141,14 @@ template <typename T, bool STREAMED> struct RowSpan
     {
         return reinterpret_cast<const T*>(reinterpret_cast<const uint8_t*>(row) + static_cast<uint32_t>(column(i)) * static_cast<uint32_t>(sizeof(T)));
     }
-    __device__ __forceinline__ row_v4u32 load(int i) const { return row_load<STREAMED>(at(i)); }
+    __device__ __forceinline__ row_v4u32 load(int i) const { return row_load<ONCE>(at(i)); }
 };
 
 // One pass over a span.  FAR: the differences to the maximum are taken first, so that any finite logits do; otherwise z k2 less the rounded
 // product m k2 is one operation, for rows whose maximum lies within 1e30 (a lane's reference does not go below -1e30: what lies there is 0
 // beside such a maximum).  The lanes' sums are then relative to that product; join_lanes keeps to it.
-template <typename T, int WG, int U, bool ENTROPY, bool TOP, bool FAR, bool STREAMED>
-__device__ __forceinline__ Moments row_pass(const RowSpan<T, STREAMED>& z, float k2, float* chunk_max, LaneBest& best)
+template <typename T, int WG, int U, bool ENTROPY, bool TOP, bool FAR, bool ONCE>
+__device__ __forceinline__ Moments row_pass(const RowSpan<T, ONCE>& z, float k2, float* chunk_max, LaneBest& best)
 {
     constexpr int N = RowType<T>::N;
     const int     tid = threadIdx.x, chunks = z.template chunks<WG, U>();
@@ -208,8 +209,8 @@ __device__ __forceinline__ Moments row_pass(const RowSpan<T, STREAMED>& z, float
 }
 
 // The moments of a span, in every lane.
-template <typename T, int WG, int U, bool ENTROPY, bool TOP, bool STREAMED>
-__device__ __forceinline__ Moments span_moments(const RowSpan<T, STREAMED>& z, float k2, float* chunk_max, LaneBest& best, float4* slots)
+template <typename T, int WG, int U, bool ENTROPY, bool TOP, bool ONCE>
+__device__ __forceinline__ Moments span_moments(const RowSpan<T, ONCE>& z, float k2, float* chunk_max, LaneBest& best, float4* slots)
 {
     const Moments r = join_lanes<WG, false>(row_pass<T, WG, U, ENTROPY, TOP, false>(z, k2, chunk_max, best), k2, slots);
     if(fabsf(r.m) < -kFar && k2 < 1.0e7f) return r;
@@ -324,8 +325,8 @@ __device__ __forceinline__ void join_lists(uint64_t& key, int lists, uint64_t (&
 // below it is not looked at again.  About k chunks (32 or 16 elements) remain of a row, and never more than the k best groups
 // have; they are read a second time, out of a cache, and what reaches the bound is sorted.  The work beside the pass hardly depends on
 // the order of the logits, and the order (value, then lower column) makes equal logits as good as different ones.
-template <typename T, bool STREAMED>
-__device__ __forceinline__ uint64_t row_top(const RowSpan<T, STREAMED>& z, int top, const LaneBest& best, const float* chunk_max, uint16_t* chosen, TopShared& sh)
+template <typename T, bool ONCE>
+__device__ __forceinline__ uint64_t row_top(const RowSpan<T, ONCE>& z, int top, const LaneBest& best, const float* chunk_max, uint16_t* chosen, TopShared& sh)
 {
     constexpr int N = RowType<T>::N, WG = kRowThreads, WAVES = WG / kWaveSize;
     const int     tid = threadIdx.x, lane = tid % kWaveSize, wave = tid / kWaveSize, chunks = z.template chunks<WG>();
@@ -484,7 +485,7 @@ __device__ __forceinline__ void write_logprobs(const LogitsArgs& p, int64_t row,
 }
 
 // Item: a piece of a row.  One piece a row: the results; several: their moments and lists.
-template <typename T, bool ENTROPY, bool TOP, bool STREAMED> __global__ __launch_bounds__(kRowThreads) void logprobs_kernel(const LogitsArgs p)
+template <typename T, bool ENTROPY, bool TOP> __global__ __launch_bounds__(kRowThreads) void logprobs_kernel(const LogitsArgs p)
 {
     constexpr int WG = kRowThreads;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
@@ -496,7 +497,7 @@ template <typename T, bool ENTROPY, bool TOP, bool STREAMED> __global__ __launch
     {
         const int64_t    row   = item / p.pieces;
         const int        begin = static_cast<int>(item - row * p.pieces) * p.piece;
-        const RowSpan<T, STREAMED> z(static_cast<const T*>(p.z) + row * p.ld, begin, p.cols - begin < p.piece ? p.cols : begin + p.piece);
+        const RowSpan<T, true> z(static_cast<const T*>(p.z) + row * p.ld, begin, p.cols - begin < p.piece ? p.cols : begin + p.piece);
         LaneBest         best;
         const Moments    r   = span_moments<T, WG, kUnroll, ENTROPY, TOP>(z, k2, chunk_max, best, slots);
         uint64_t         key = 0;
@@ -573,7 +574,7 @@ struct LogprobsGradArgs
     int          cols;
     float        scale;
     int          pieces, piece;
-    bool         streamed;
+    bool         streamed;          // stores of the gradient
     const void*  tokens;
     int          wide;
     const float *stats, *entropy, *dlogp, *dentropy;      // entropy and dentropy both or neither; dlogp or nullptr
@@ -582,7 +583,7 @@ struct LogprobsGradArgs
 };
 
 // Walks over a span, 32 bytes of a lane in flight: body(column, values of a vector), edge(column, value).
-template <typename T, int WG, bool STREAMED, typename F, typename G> __device__ __forceinline__ void walk(const RowSpan<T, STREAMED>& z, F&& body, G&& edge)
+template <typename T, int WG, bool ONCE, typename F, typename G> __device__ __forceinline__ void walk(const RowSpan<T, ONCE>& z, F&& body, G&& edge)
 {
     constexpr int U = 2, N = RowType<T>::N;
     int           i = threadIdx.x;
@@ -607,7 +608,7 @@ template <typename T, int WG, bool STREAMED, typename F, typename G> __device__ 
     }
 }
 // The result of f for every element of a span, to a buffer of type dtype whose row begins at `at`.
-template <typename T, int WG, bool STREAMED, typename F> __device__ __forceinline__ void map_span(const RowSpan<T, STREAMED>& z, void* out, int dtype, int64_t at, F&& f)
+template <typename T, int WG, bool STREAMED, bool ONCE, typename F> __device__ __forceinline__ void map_span(const RowSpan<T, ONCE>& z, void* out, int dtype, int64_t at, F&& f)
 {
     constexpr int N = RowType<T>::N;
     walk<T, WG>(
@@ -620,7 +621,7 @@ template <typename T, int WG, bool STREAMED, typename F> __device__ __forceinlin
         },
         [&](int c, float v) { element_store(out, dtype, at + c, f(c, v)); });
 }
-template <typename T, int WG, bool STREAMED> __device__ __forceinline__ void zero_span(const RowSpan<T, STREAMED>& z, void* out, int dtype, int64_t at)
+template <typename T, int WG, bool STREAMED, bool ONCE> __device__ __forceinline__ void zero_span(const RowSpan<T, ONCE>& z, void* out, int dtype, int64_t at)
 {
     const float o[RowType<T>::N] = {};
     for(int i = threadIdx.x; i < z.vectors; i += WG) vector_store<T, STREAMED>(out, dtype, at + z.column(i), o);
@@ -648,15 +649,15 @@ template <typename T, bool ENTROPY, bool STREAMED> __global__ __launch_bounds__(
         }
         if(given >= p.cols) g = NAN;      // (no column of it: the row says so)
         const int64_t    at = row * p.cols;
-        const RowSpan<T, STREAMED> z(static_cast<const T*>(p.z) + row * p.ld, begin, end);
+        const RowSpan<T, true> z(static_cast<const T*>(p.z) + row * p.ld, begin, end);
         if(ln_s == -INFINITY || (g == 0.0f && h == 0.0f))
         {
-            zero_span<T, kRowThreads>(z, p.dz, p.ddt, at);
+            zero_span<T, kRowThreads, STREAMED>(z, p.dz, p.ddt, at);
             continue;
         }
         const int   token = given < p.cols ? static_cast<int>(given) : -1;
         const float l2 = ln_s * kLog2e;
-        map_span<T, kRowThreads>(z, p.dz, p.ddt, at, [&](int c, float v) {
+        map_span<T, kRowThreads, STREAMED>(z, p.dz, p.ddt, at, [&](int c, float v) {
             const float d = (v - m) * k2 - l2, q = exp2_fast(d);      // log2 p and p
             float       o = -(g * q);
             if constexpr(ENTROPY) o = fmaf(-(h * q), fmaf(fmaxf(d, kFar), kLn2, entropy), o);
@@ -673,7 +674,7 @@ struct DistillArgs
     int          cols;
     float        scale;
     int          pieces, piece;
-    bool         streamed;
+    bool         streamed;          // stores of the gradient
     const void*  teacher;
     int          tdt;
     const void*  index;
@@ -781,27 +782,27 @@ __device__ __forceinline__ float row_factor(const DistillArgs& p, int64_t row, c
 __device__ __forceinline__ float log_sum(const Moments& r) { return r.s == 0.0f ? -INFINITY : logf(r.s); }
 
 // The gradient of a span from logits that are read again.
-template <typename T, int WG, bool STREAMED>
-__device__ __forceinline__ void span_gradient(const DistillArgs& p, int64_t row, const RowSpan<T, STREAMED>& z, const Moments& r, const EntriesShared& sh)
+template <typename T, int WG, bool STREAMED, bool ONCE>
+__device__ __forceinline__ void span_gradient(const DistillArgs& p, int64_t row, const RowSpan<T, ONCE>& z, const Moments& r, const EntriesShared& sh)
 {
     const int64_t at = row * p.cols;
     const float   g  = row_factor(p, row, r, sh);
     if(g == 0.0f)
     {
-        zero_span<T, WG>(z, p.dz, p.ddt, at);
+        zero_span<T, WG, STREAMED>(z, p.dz, p.ddt, at);
         return;
     }
     const float k2 = p.scale * kLog2e, gs = g / r.s;
     auto        mass = [&](float v) { return gs * exp2_fast((v - r.m) * k2); };
-    map_span<T, WG>(z, p.dz, p.ddt, at, [&](int, float v) { return mass(v); });
+    map_span<T, WG, STREAMED>(z, p.dz, p.ddt, at, [&](int, float v) { return mass(v); });
     __syncthreads();      // (behind the probabilities)
     if(threadIdx.x < kWaveSize) entries_subtract(p, at, z.begin, z.end, g, sh, mass);
 }
 
 // A row a workgroup, its logits in registers between the sums and the gradient: NV vectors of a thread, all under way at once.  What a
 // longer row has beyond them is read twice, the second time out of a cache.
-//   A step over 4096 x 65536 bfloat16 logits: 230 us, 4.7 TB/s of logits read once and gradient written once; with all of a row read
-//   twice 272 (512 threads) and 309 (256).
+//   A step over 4096 x 65536 bfloat16 logits: 207 us, 5.2 TB/s of logits read once and gradient written once; with all of a row read
+//   twice 272 (512 threads) and 309 (256), both before loads and stores were streamed and this form took 230.
 // (Four wavefronts of a SIMD leave 128 registers.  The scheduling barriers keep the phases from being unrolled into more values than
 // that; the words are taken apart again in each phase, as fp32 values they would take twice the registers.)
 template <typename T, int WG, int NV, bool REST, bool STREAMED> __global__ __launch_bounds__(WG, 4) void distill_held_kernel(const DistillArgs p)
@@ -815,7 +816,7 @@ template <typename T, int WG, int NV, bool REST, bool STREAMED> __global__ __lau
     const float              k2 = p.scale * kLog2e;
     for(int64_t row = blockIdx.x; row < p.rows; row += gridDim.x)
     {
-        const RowSpan<T, STREAMED> z(static_cast<const T*>(p.z) + row * p.ld, 0, p.cols);
+        const RowSpan<T, true> z(static_cast<const T*>(p.z) + row * p.ld, 0, p.cols);
         if(first) entries_fetch(p, row, sh);
         row_v4u32 w[NV];
         int       t = tid;
@@ -913,24 +914,24 @@ template <typename T, int WG, int NV, bool REST, bool STREAMED> __global__ __lau
                 __builtin_amdgcn_sched_barrier(0);
             }
             if(edge >= 0) out[edge] = static_cast<T>(mass(at_edge));
-            if constexpr(REST) map_span<T, WG>(z.template from<STREAMED>(WG * NV), p.dz, p.ddt, row * p.cols, [&](int, float v) { return mass(v); });
+            if constexpr(REST) map_span<T, WG, STREAMED>(z.template from<true>(WG * NV), p.dz, p.ddt, row * p.cols, [&](int, float v) { return mass(v); });
             __syncthreads();      // (behind the probabilities)
             if(first) entries_subtract(p, row * p.cols, 0, p.cols, g, sh, mass);
         }
-        else span_gradient<T, WG>(p, row, z, exact, sh);      // (rows of zeros or of extreme logits, other types)
+        else span_gradient<T, WG, STREAMED>(p, row, z, exact, sh);      // (rows of zeros or of extreme logits, other types)
         __syncthreads();
     }
 }
 
 // The loss alone, a row a workgroup.
-template <typename T, bool STREAMED> __global__ __launch_bounds__(kRowThreads) void distill_loss_kernel(const DistillArgs p)
+template <typename T> __global__ __launch_bounds__(kRowThreads) void distill_loss_kernel(const DistillArgs p)
 {
     __shared__ EntriesShared sh;
     __shared__ float4        slots[kRowThreads / kWaveSize];
     const float              k2 = p.scale * kLog2e;
     for(int64_t row = blockIdx.x; row < p.rows; row += gridDim.x)
     {
-        const RowSpan<T, STREAMED> z(static_cast<const T*>(p.z) + row * p.ld, 0, p.cols);
+        const RowSpan<T, true> z(static_cast<const T*>(p.z) + row * p.ld, 0, p.cols);
         if(threadIdx.x < kWaveSize)
         {
             entries_fetch(p, row, sh);
@@ -988,7 +989,7 @@ template <typename T> __global__ __launch_bounds__(kRowThreads) void distill_joi
         if(p.dz)
         {
             const int begin = i * p.piece;
-            span_gradient<T, kRowThreads>(p, row, RowSpan<T, false>(z, begin, p.cols - begin < p.piece ? p.cols : begin + p.piece), r, sh);
+            span_gradient<T, kRowThreads, false>(p, row, RowSpan<T, true>(z, begin, p.cols - begin < p.piece ? p.cols : begin + p.piece), r, sh);
         }
         __syncthreads();
     }
@@ -1044,10 +1045,10 @@ int64_t most_items(int zdt, int64_t rows, int64_t cols, int top)
     const int64_t fill = kFill + rows, cap = rows * div_up(cols, piece_most(zdt, top));
     return fill > cap ? fill : cap;
 }
-// Logits and gradients that no cache (256 MB in front of the memory) holds until their next reader are streamed.  us, ordinary -> streamed:
-// log probabilities of 2048 x 65536 bfloat16 (268 MB) 55.2 -> 49.1, their gradient 109.5 -> 102, distillation 4096 x 65536 233 -> 219;
-// the latter with the INT8 conversion of the gradient behind it 4096 x 32768 binary16 260 -> 249, but 2048 x 32768 128 -> 132.
-bool streamed(int dt, int64_t rows, int64_t cols) { return rows * cols * (dt == kF32 ? 4 : 2) > (int64_t(192) << 20); }
+// Gradients that no cache (256 MB in front of the memory) holds until their reader comes are streamed.  us, ordinary -> streamed stores, a
+// distillation step in binary16 with the INT8 conversion of the gradient behind it (alone): 4096 x 32768 235 -> 250 (132 -> 122),
+// 6000 x 32768 376 -> 362 (186 -> 173), 4096 x 65536 479 -> 461 (234 -> 206).
+bool streamed(int dt, int64_t rows, int64_t cols) { return rows * cols * (dt == kF32 ? 4 : 2) > (int64_t(320) << 20); }
 // f(std::true_type or std::false_type)
 template <typename F> void choose(bool v, F&& f)
 {
@@ -1062,9 +1063,7 @@ template <typename T> hipError_t logprobs_type(const LogitsArgs& a, hipStream_t 
     const size_t lds  = a.top > 0 ? top_lds_bytes(static_cast<int>(div_up(a.piece, chunk_span<T>(kRowThreads)))) : 0;
     choose(a.entropy != nullptr, [&](auto entropy) {
         choose(a.top > 0, [&](auto top) {
-            choose(a.streamed, [&](auto through) {
-                logprobs_kernel<T, decltype(entropy)::value, decltype(top)::value, decltype(through)::value><<<grid, block, lds, st>>>(a);
-            });
+            logprobs_kernel<T, decltype(entropy)::value, decltype(top)::value><<<grid, block, lds, st>>>(a);
         });
     });
     const hipError_t e = hipGetLastError();
@@ -1092,7 +1091,7 @@ template <typename T> hipError_t distill_type(const DistillArgs& a, hipStream_t 
 {
     if(a.pieces == 1 && !a.dz)
     {
-        choose(a.streamed, [&](auto through) { distill_loss_kernel<T, decltype(through)::value><<<groups(a.rows), dim3(kRowThreads), 0, st>>>(a); });
+        distill_loss_kernel<T><<<groups(a.rows), dim3(kRowThreads), 0, st>>>(a);
         return hipGetLastError();
     }
     if(a.pieces == 1)
@@ -1136,7 +1135,7 @@ hipError_t launch_token_logprobs(const void* z, int zdt, int64_t rows, int64_t c
     const Split s = logprobs_split(zdt, rows, cols, top);
     LogitsArgs  a{};
     a.z = z; a.rows = rows; a.ld = ld; a.cols = static_cast<int>(cols); a.scale = scale;
-    a.pieces = s.pieces; a.piece = s.piece; a.streamed = streamed(zdt, rows, cols);
+    a.pieces = s.pieces; a.piece = s.piece;
     a.tokens = tokens; a.wide = wide; a.logp = logp; a.entropy = entropy; a.stats = stats;
     a.top = top; a.top_logp = top_logp; a.top_index = top_index;
     a.part = static_cast<float4*>(workspace);
@@ -1151,7 +1150,7 @@ hipError_t launch_token_logprobs_bwd(const void* z, int zdt, int64_t rows, int64
     const Split      s = split_rows(rows, cols, kRowThreads * 8, kRowThreads * 8 * 16);
     LogprobsGradArgs a{};
     a.z = z; a.rows = rows; a.ld = ld; a.cols = static_cast<int>(cols); a.scale = scale;
-    a.pieces = s.pieces; a.piece = s.piece; a.streamed = streamed(zdt, rows, cols);
+    a.pieces = s.pieces; a.piece = s.piece; a.streamed = streamed(ddt, rows, cols);
     a.tokens = tokens; a.wide = wide; a.stats = stats; a.entropy = entropy; a.dlogp = dlogp; a.dentropy = dentropy;
     a.dz = dz; a.ddt = ddt;
     return by_type(zdt, [&](auto tag) { return logprobs_grad_type<decltype(tag)>(a, st); });
@@ -1167,7 +1166,7 @@ hipError_t launch_distill_topk(const void* z, int zdt, int64_t rows, int64_t col
                                                                                  : whole_row(cols);
     DistillArgs a{};
     a.z = z; a.rows = rows; a.ld = ld; a.cols = static_cast<int>(cols); a.scale = scale;
-    a.pieces = s.pieces; a.piece = s.piece; a.streamed = streamed(zdt, rows, cols);
+    a.pieces = s.pieces; a.piece = s.piece; a.streamed = streamed(ddt, rows, cols);
     a.teacher = teacher; a.tdt = tdt; a.index = index; a.wide = wide; a.k = k; a.weight = weight; a.loss = loss;
     a.dz = dz; a.ddt = ddt;
     a.part = static_cast<float4*>(workspace);

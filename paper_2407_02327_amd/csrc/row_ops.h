@@ -67,8 +67,8 @@ template <> struct RowType<__bf16>
     }
 };
 
-// (STREAMED: past the caches' room for what is read again.  A template's argument: of two branches that differ in it alone the compiler
-// makes one ordinary access.)
+// (STREAMED: not kept in the caches' room for what is read again.  A template's argument: of two branches that differ in it alone the
+// compiler makes one ordinary access.)
 template <bool STREAMED = false, typename T> __device__ __forceinline__ row_v4u32 row_load(const T* p)
 {
     if constexpr(STREAMED) return __builtin_nontemporal_load(reinterpret_cast<const typename RowType<T>::vec_t*>(p));
