@@ -92,7 +92,9 @@ __device__ __forceinline__ void publish_largest(float run, unsigned int* word, f
     if(bits > __hip_atomic_load(word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(word, bits);
 }
 
-// TPR lanes a row, NU units of eight elements a lane; WG / TPR rows of a workgroup at a time.
+// TPR lanes a row, NU units of eight elements a lane; WG / TPR rows of a workgroup at a time.  Short rows take a wavefront, or a quarter of
+// one, whose lanes exchange their sums without LDS; longer ones the workgroup, with one barrier.  Bound by memory: 16384 x 4096 bfloat16
+// 50 us (5.3 TB/s of x and y), 16384 x 1024 binary16 15 (4.5); a single row of 4096 is 2.9 us of launch and two memory latencies.
 template <typename T, int TPR, int NU, int WG>
 __global__ __launch_bounds__(WG) void norm_forward_kernel(const NormArgs p)
 {
@@ -208,7 +210,8 @@ template <int WG, typename F, typename G> __device__ __forceinline__ void each_o
     if(edge >= 0) one(edge);
 }
 
-// Rows longer than the registers of a workgroup hold: read three times (the second and third time out of a cache).
+// Rows longer than the registers of a workgroup hold (16384 columns): read three times, the second and third time out of a cache.  200 x 20000
+// fp32 11 us.
 template <typename T> __global__ __launch_bounds__(1024) void norm_forward_long_kernel(const NormArgs p)
 {
     __shared__ float2 slots[3][16];
@@ -274,7 +277,9 @@ template <typename T> __global__ __launch_bounds__(1024) void norm_forward_long_
     if(p.amax_bits) publish_largest(run, p.amax_bits, reinterpret_cast<float*>(slots[2]));
 }
 
-// TD: dy, T: x.
+// TD: dy, T: x.  One pass: the row's two sums (one barrier for both), dx from registers, and the parameters' sums, which a lane keeps for its
+// columns over all rows of the workgroup -- 32 registers a unit, the reason for at most two.  16384 x 1024 binary16 19 us (5.3 TB/s of x, dy
+// and dx) and 3.7 for the fold of 256 partial rows; 16384 x 4096 bfloat16 84 with it (4.8 TB/s).
 template <typename TD, typename T, int TPR, int NU, int WG>
 __global__ __launch_bounds__(WG) void norm_backward_kernel(const NormArgs p)
 {
@@ -423,7 +428,7 @@ __global__ __launch_bounds__(WG) void norm_backward_kernel(const NormArgs p)
     }
 }
 
-// Long rows: dx of a row by a workgroup, x and dy read twice.
+// Long rows: dx of a row by a workgroup, x and dy read twice (and once more for the parameters): 4096 x 16384 bfloat16 165 us.
 template <typename TD, typename T> __global__ __launch_bounds__(1024) void norm_backward_long_kernel(const NormArgs p)
 {
     __shared__ float2 slots[2][16];
