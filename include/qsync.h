@@ -628,8 +628,8 @@ int qsync_layernorm_fwd(const void* x, int xdt, int64_t rows, int64_t cols, int6
  *            any other overlap is QSYNC_ERR_UNSUPPORTED.
  * dgamma_opt, dbeta_opt  out, cols floats each, or NULL; zeros when rows == 0.  Summed in fp32 in an order that depends on the
  *            sizes alone.  One of the three outputs is required.
- * workspace  at least qsync_layernorm_bwd_workspace_bytes(rows, cols) bytes, 16-byte aligned, no contents needed; NULL when
- *            neither dgamma nor dbeta is wanted.
+ * workspace  at least qsync_layernorm_bwd_workspace_bytes(rows, cols) bytes, 16-byte aligned, no contents needed (what is
+ *            enough for some number of rows is enough for fewer); NULL when neither dgamma nor dbeta is wanted.
  */
 int qsync_layernorm_bwd(const void* dy, int dydt, int64_t lddy, const void* x, int xdt, int64_t rows, int64_t cols, int64_t ldx,
                         const float* gamma_opt, const float* mean, const float* rstd, void* dx_opt, int dxdt,

@@ -596,12 +596,19 @@ BackwardShape backward_shape(int64_t cols)
     return cols <= 128 ? BackwardShape{16, 256} : cols <= 1024 ? BackwardShape{8, 256}
            : cols <= 2048 ? BackwardShape{1, 768} : cols <= 4096 ? BackwardShape{1, 512} : BackwardShape{1, 256};
 }
+int64_t backward_wanted(int64_t rows) { return rows / 20 < 256 ? 256 : rows / 20; }
 int64_t backward_groups(int64_t rows, int64_t cols)
 {
     if(cols > kNormMaxCols) return at_most(rows, kNormParamRows);
     const BackwardShape s = backward_shape(cols);
-    const int64_t       wanted = rows / 20 < 256 ? 256 : rows / 20;
-    return even_groups(div_up(rows, s.rows_at_once), at_most(wanted, s.most), rows);
+    return even_groups(div_up(rows, s.rows_at_once), at_most(backward_wanted(rows), s.most), rows);
+}
+// No number of rows up to this one has more workgroups (backward_groups itself falls where a turn more evens them out).
+int64_t most_backward_groups(int64_t rows, int64_t cols)
+{
+    if(cols > kNormMaxCols) return at_most(rows, kNormParamRows);
+    const BackwardShape s = backward_shape(cols);
+    return at_most(div_up(rows, s.rows_at_once), at_most(backward_wanted(rows), s.most));
 }
 template <typename TD, typename T, int TPR, int NU, int WG> hipError_t backward_rows(const NormArgs& a, int64_t groups, hipStream_t st)
 {
@@ -646,7 +653,7 @@ hipError_t launch_layernorm_fwd(const void* x, int xdt, int64_t rows, int64_t co
 
 size_t layernorm_bwd_workspace_bytes(int64_t rows, int64_t cols)
 {
-    return static_cast<size_t>(backward_groups(rows, cols)) * 2 * static_cast<size_t>(cols) * sizeof(float);
+    return static_cast<size_t>(most_backward_groups(rows, cols)) * 2 * static_cast<size_t>(cols) * sizeof(float);
 }
 
 hipError_t launch_layernorm_bwd(const void* dy, int dydt, int64_t lddy, const void* x, int xdt, int64_t rows, int64_t cols, int64_t ldx,

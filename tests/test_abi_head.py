@@ -175,3 +175,10 @@ def test_classes_refuse_sizes_and_devices():
             op.forward(x)
     with pytest.raises(RuntimeError):
         LayerNorm(4, 8, training=False, device="cpu").backward(x)
+
+
+@pytest.mark.parametrize("cols", [64, 128, 700, 1024, 1025, 2048, 2443, 4096, 4097, 8192, 8193, 20000])
+def test_layernorm_workspace_serves_fewer_rows(cols):
+    """A workspace for some number of rows is enough for fewer: an operator's batches may be shorter than it was made for."""
+    sizes = [Q.qsync_layernorm_bwd_workspace_bytes(rows, cols) for rows in range(1, 20000)]
+    assert all(a <= b for a, b in zip(sizes, sizes[1:]))

@@ -216,3 +216,14 @@ def test_gradient_against_differences():
     moved = (R.f64(hi) - R.f64(lo)) / (2 * step)
     noise = (R.layernorm_bound(R.f64(x), R.f64(gamma), R.f64(beta), 1e-5) * np.abs(R.f64(dy))).sum() / step
     assert abs((f(hi) - f(lo)) / (2 * step) - (dx * moved).sum()) <= noise + 2.0 ** -10 * np.abs(dx * moved).sum()
+
+
+@pytest.mark.parametrize("made_for, rows, cols", [(513, 512, 1030), (513, 512, 2443), (2049, 2048, 1001), (5200, 5120, 2051)])
+@pytest.mark.parametrize("x_dtype, dy_dtype", [(F32, F32), (BF16, BF16), (F16, F32)])
+def test_batches_shorter_than_the_operator(made_for, rows, cols, x_dtype, dy_dtype):
+    """Fewer rows that are divided among more workgroups than the rows which the operator was made for."""
+    say("layernorm fewer rows", made_for, rows, cols, x_dtype, dy_dtype)
+    gamma, beta = _params(cols, 3)
+    op = LayerNorm(made_for, cols, x_dtype=x_dtype, y_dtype=dy_dtype, dx_dtype=x_dtype, eps=EPS)
+    for n in (rows, made_for):
+        _check(_filled(n, cols, x_dtype, 1, 0.3), gamma, beta, _filled(n, cols, dy_dtype, 2), op, f"{n} of {made_for} x {cols}")
