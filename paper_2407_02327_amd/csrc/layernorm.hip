@@ -589,26 +589,33 @@ template <typename T> hipError_t forward_type(const NormArgs& a, hipStream_t st)
 // How a row of the backward pass is divided, and the most workgroups: what registers let run at once, less where their partial rows --
 // written, and read again by the fold -- would weigh.  us with 256, 512, 768 and 1024 of them: 16384 x 4096 bfloat16 90.7 83.7 90.0 98.9,
 // 16384 x 2048 binary16 62.7 52.1 48.5 48.7, 4096 x 8192 48.4 58.1 66.8 77.5; 16384 x 1024 with eight rows at a time and 256 24.8, four and
-// 512 26.2.
+// 512 26.2.  Where x and dy have 16 bits, a workgroup for every seven rows, and more of them where rows are not whole units of eight,
+// whose loads and stores straddle lines: 7199 x 2443 bfloat16 61 -> 49, 16384 x 2501 binary16 102 -> 84, 7199 x 4096 bfloat16 47 -> 43.  With
+// fp32 one for every twenty: seven make 4096 x 4095 50 of 45, and up to 768 of them 10000 x 3001 87 of 77.
 struct BackwardShape { int64_t rows_at_once, most; };
-BackwardShape backward_shape(int64_t cols)
+BackwardShape backward_shape(int64_t cols, bool narrow)
 {
     return cols <= 128 ? BackwardShape{16, 256} : cols <= 1024 ? BackwardShape{8, 256}
-           : cols <= 2048 ? BackwardShape{1, 768} : cols <= 4096 ? BackwardShape{1, 512} : BackwardShape{1, 256};
+           : cols <= 2048 ? BackwardShape{1, 768} : cols <= 4096 ? BackwardShape{1, narrow && cols % 8 ? 768 : 512} : BackwardShape{1, 256};
 }
-int64_t backward_wanted(int64_t rows) { return rows / 20 < 256 ? 256 : rows / 20; }
-int64_t backward_groups(int64_t rows, int64_t cols)
+int64_t backward_wanted(int64_t rows, bool narrow)
+{
+    const int64_t groups = rows / (narrow ? 7 : 20);
+    return groups < 256 ? 256 : groups;
+}
+int64_t backward_groups(int64_t rows, int64_t cols, bool narrow)
 {
     if(cols > kNormMaxCols) return at_most(rows, kNormParamRows);
-    const BackwardShape s = backward_shape(cols);
-    return even_groups(div_up(rows, s.rows_at_once), at_most(backward_wanted(rows), s.most), rows);
+    const BackwardShape s = backward_shape(cols, narrow);
+    return even_groups(div_up(rows, s.rows_at_once), at_most(backward_wanted(rows, narrow), s.most), rows);
 }
-// No number of rows up to this one has more workgroups (backward_groups itself falls where a turn more evens them out).
+// No number of rows up to this one, whatever the types, has more workgroups (16-bit ones have the most; backward_groups itself falls where a turn more evens them out).
 int64_t most_backward_groups(int64_t rows, int64_t cols)
 {
+    constexpr bool narrow = true;
     if(cols > kNormMaxCols) return at_most(rows, kNormParamRows);
-    const BackwardShape s = backward_shape(cols);
-    return at_most(div_up(rows, s.rows_at_once), at_most(backward_wanted(rows), s.most));
+    const BackwardShape s = backward_shape(cols, narrow);
+    return at_most(div_up(rows, s.rows_at_once), at_most(backward_wanted(rows, narrow), s.most));
 }
 template <typename TD, typename T, int TPR, int NU, int WG> hipError_t backward_rows(const NormArgs& a, int64_t groups, hipStream_t st)
 {
@@ -617,7 +624,7 @@ template <typename TD, typename T, int TPR, int NU, int WG> hipError_t backward_
 }
 template <typename TD, typename T> hipError_t backward_types(const NormArgs& a, hipStream_t st)
 {
-    const int64_t groups = backward_groups(a.rows, a.cols);
+    const int64_t groups = backward_groups(a.rows, a.cols, sizeof(TD) == 2 && sizeof(T) == 2);
     if(a.cols <= 128) return backward_rows<TD, T, 16, 1, 256>(a, groups, st);
     if(a.cols <= 512) return backward_rows<TD, T, 64, 1, 512>(a, groups, st);
     if(a.cols <= 1024) return backward_rows<TD, T, 64, 2, 512>(a, groups, st);
@@ -668,7 +675,7 @@ hipError_t launch_layernorm_bwd(const void* dy, int dydt, int64_t lddy, const vo
     const hipError_t e = dydt == kF32 ? backward_type<float>(a, xdt, st) : dydt == kF16 ? backward_type<_Float16>(a, xdt, st) : backward_type<__bf16>(a, xdt, st);
     if(e != hipSuccess || !a.partial) return e;
     norm_fold_kernel<<<dim3(static_cast<unsigned>((2 * cols + 15) / 16)), dim3(256), 0, st>>>(
-        a.partial, static_cast<int>(backward_groups(rows, cols)), cols, dgamma, dbeta);
+        a.partial, static_cast<int>(backward_groups(rows, cols, dydt != kF32 && xdt != kF32)), cols, dgamma, dbeta);
     return hipGetLastError();
 }
 
