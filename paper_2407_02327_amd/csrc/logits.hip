@@ -175,7 +175,9 @@ __device__ __forceinline__ Moments row_pass(const RowSpan<T, ONCE>& z, float k2,
     {
         const float v = row_element(z.row + edge);
         r.m = fmaxf(r.m, v);
-        r.s = exp2_fast(FAR ? (v - r.m) * k2 : fmaf(v, k2, -(r.m * k2)));
+        const float d = FAR ? (v - r.m) * k2 : fmaf(v, k2, -(r.m * k2));      // (not 0: what the product lost by its rounding)
+        r.s = exp2_fast(d);
+        if constexpr(ENTROPY) r.w = r.s * fmaxf(d, kFar);
     }
     for(int c = 0; c < chunks; ++c)
     {

@@ -411,3 +411,16 @@ def test_what_the_classes_refuse():
                 lambda: dist.forward_backward(z, teacher, index), lambda: dist.forward(z, teacher.t().contiguous().t(), index)):
         with pytest.raises(ValueError):
             bad()
+
+
+@pytest.mark.parametrize("value", [-1e9, 7e8])
+@pytest.mark.parametrize("first", range(8))
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_entropy_of_rows_of_one_value(dtype, first, value):
+    """... wherever the row starts: ln cols.  The elements in front of and behind whole lines of memory count like the others."""
+    for cols in (5, 27, 700, 70001):
+        z = torch.full((1, cols + 8), value, dtype=dtype, device="cuda")[:, first:first + cols]
+        _, entropy, _, _ = TokenLogProbs(1, cols).forward(z)
+        # ... by what logits_bound counts, and the quotient of the two sums, up to 64 here, by the roundings of a lane's and the lanes' additions in each
+        bound = (R.logits_bound(R.f64(z), 1.0)[0].max() + 64 * R.U * (cols // 256 + 40)) * 2 + R.rounded(np.log(cols), F32)
+        R.assert_within(entropy, np.array([np.log(cols)]), bound, f"entropy {cols}")
