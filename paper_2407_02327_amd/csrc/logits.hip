@@ -14,6 +14,7 @@
 #include "device_utils.h"
 #include "row_ops.h"
 
+#include <algorithm>
 #include <cfloat>
 #include <type_traits>
 
@@ -25,6 +26,9 @@ constexpr int   kRowThreads = 256;        // a row, or a piece of one
 constexpr int   kUnroll     = 4;          // vectors of a lane in flight: a chunk
 constexpr float kLn2 = 0.693147180559945309f, kLog2e = 1.44269504088896341f;
 constexpr float kFar = -1.0e30f;          // stands for differences to the maximum that overflow: e^x is 0 there, and 0 * x is 0
+// The fast form of a pass (row_pass) leaves the rounding of m k2 in its exponents, half a spacing of fp32 there: at most 64 below 2^31, and
+// 2^64 times a row's 2^30 terms is still finite.  (Masks of -1e9 at a scale of 1 lie within; at 2^32 a row of one such value would be 0 or infinite.)
+constexpr float kNearProduct = 2.0e9f;
 constexpr int   kTopMost = kTopAlternatives;      // a sorted list is a value per lane
 static_assert(kTopMost == kWaveSize, "an alternative per lane");
 
@@ -40,7 +44,7 @@ struct LogitsArgs
     const void* z;
     int64_t     rows, ld;
     int         cols;
-    float       scale;
+    float       scale, reach;       // reach: |z| below which the fast form of a pass holds (host-made: it takes no vector register)
     int         pieces, piece;      // pieces of a row, elements of a piece
     const void* tokens;             // or nullptr
     int         wide;               // 64-bit tokens (indices)
@@ -145,10 +149,11 @@ template <typename T, bool ONCE> struct RowSpan
 };
 
 // One pass over a span.  FAR: the differences to the maximum are taken first, so that any finite logits do; otherwise z k2 less the rounded
-// product m k2 is one operation, for rows whose maximum lies within 1e30 (a lane's reference does not go below -1e30: what lies there is 0
-// beside such a maximum).  The lanes' sums are then relative to that product; join_lanes keeps to it.
+// product m k2 is one operation, for rows whose maximum lies within `reach`.  A lane's reference does not go below -reach, whatever it has met:
+// masked logits far below it are terms of 0 beside such a maximum, and so is what a lane that meets nothing else adds up.  The lanes'
+// sums are relative to the product; join_lanes keeps to it.
 template <typename T, int WG, int U, bool ENTROPY, bool TOP, bool FAR, bool ONCE>
-__device__ __forceinline__ Moments row_pass(const RowSpan<T, ONCE>& z, float k2, float* chunk_max, LaneBest& best)
+__device__ __forceinline__ Moments row_pass(const RowSpan<T, ONCE>& z, float k2, float reach, float* chunk_max, LaneBest& best)
 {
     constexpr int N = RowType<T>::N;
     const int     tid = threadIdx.x, chunks = z.template chunks<WG, U>();
@@ -170,7 +175,7 @@ __device__ __forceinline__ Moments row_pass(const RowSpan<T, ONCE>& z, float k2,
     };
     const int edge = z.edge(tid);
     if(chunks > 0) fetch(0);
-    Moments r{FAR ? -FLT_MAX : kFar, 0.0f, 0.0f};
+    Moments r{FAR ? -FLT_MAX : -reach, 0.0f, 0.0f};
     if(edge >= 0)
     {
         const float v = row_element(z.row + edge);
@@ -212,13 +217,13 @@ __device__ __forceinline__ Moments row_pass(const RowSpan<T, ONCE>& z, float k2,
 
 // The moments of a span, in every lane.
 template <typename T, int WG, int U, bool ENTROPY, bool TOP, bool ONCE>
-__device__ __forceinline__ Moments span_moments(const RowSpan<T, ONCE>& z, float k2, float* chunk_max, LaneBest& best, float4* slots)
+__device__ __forceinline__ Moments span_moments(const RowSpan<T, ONCE>& z, float k2, float reach, float* chunk_max, LaneBest& best, float4* slots)
 {
-    const Moments r = join_lanes<WG, false>(row_pass<T, WG, U, ENTROPY, TOP, false>(z, k2, chunk_max, best), k2, slots);
-    if(fabsf(r.m) < -kFar && k2 < 1.0e7f) return r;
+    const Moments r = join_lanes<WG, false>(row_pass<T, WG, U, ENTROPY, TOP, false>(z, k2, reach, chunk_max, best), k2, slots);
+    if(fabsf(r.m) < reach) return r;
     __syncthreads();      // (all lanes have read the slots)
     LaneBest none;
-    return join_lanes<WG, true>(row_pass<T, WG, 1, ENTROPY, false, true>(z, k2, nullptr, none), k2, slots);
+    return join_lanes<WG, true>(row_pass<T, WG, 1, ENTROPY, false, true>(z, k2, reach, nullptr, none), k2, slots);
 }
 
 // ---- top alternatives -------------------------------------------------------------------------------------------------------
@@ -505,7 +510,7 @@ template <typename T, bool ENTROPY, bool TOP> __global__ __launch_bounds__(kRowT
         const int        begin = static_cast<int>(item - row * p.pieces) * p.piece;
         const RowSpan<T, true> z(static_cast<const T*>(p.z) + row * p.ld, begin, p.cols - begin < p.piece ? p.cols : begin + p.piece);
         LaneBest         best;
-        const Moments    r   = span_moments<T, WG, kUnroll, ENTROPY, TOP>(z, k2, chunk_max, best, slots);
+        const Moments    r   = span_moments<T, WG, kUnroll, ENTROPY, TOP>(z, k2, p.reach, chunk_max, best, slots);
         uint64_t         key = 0;
         if constexpr(TOP)
         {
@@ -679,7 +684,7 @@ struct DistillArgs
     const void*  z;
     int64_t      rows, ld;
     int          cols;
-    float        scale;
+    float        scale, reach;
     int          pieces, piece;
     bool         streamed;          // stores of the gradient
     const void*  teacher;
@@ -844,7 +849,7 @@ template <typename T, int WG, int NV, bool REST, bool STREAMED> __global__ __lau
         if constexpr(REST)
         {
             rest = z.template from<false>(WG * NV);
-            r    = row_pass<T, WG, 2, false, false, false>(rest, k2, nullptr, none);
+            r    = row_pass<T, WG, 2, false, false, false>(rest, k2, p.reach, nullptr, none);
         }
         const float rest_m = r.m;
         r.m = fmaxf(r.m, at_edge);
@@ -864,7 +869,7 @@ template <typename T, int WG, int NV, bool REST, bool STREAMED> __global__ __lau
         for(int i = 0; i < WAVES; ++i) r.m = fmaxf(r.m, largest[i]);
         // as in row_pass, one operation where the maximum allows it; the product's rounding is common to the sum and the probabilities,
         // and is taken out of the sum that the loss has
-        const bool  near = fabsf(r.m) < -kFar && k2 < 1.0e7f;
+        const bool  near = fabsf(r.m) < p.reach;
         const float mk   = r.m * k2;
         auto        again = [&]() {
 #pragma unroll
@@ -895,7 +900,7 @@ template <typename T, int WG, int NV, bool REST, bool STREAMED> __global__ __lau
             exact = r;
             exact.s *= exp2_fast(-fmaf(r.m, k2, -mk));
         }
-        else exact = r = join_lanes<WG, true>(row_pass<T, WG, 1, false, false, true>(z, k2, nullptr, none), k2, slots);
+        else exact = r = join_lanes<WG, true>(row_pass<T, WG, 1, false, false, true>(z, k2, p.reach, nullptr, none), k2, slots);
         if(first)
         {
             const float loss = entries_loss(p, exact, log_sum(exact), sh);
@@ -945,7 +950,7 @@ template <typename T> __global__ __launch_bounds__(kRowThreads) void distill_los
             entries_prepare(p, z.row, sh);
         }
         LaneBest      none;
-        const Moments r = span_moments<T, kRowThreads, kUnroll, false, false>(z, k2, nullptr, none, slots);
+        const Moments r = span_moments<T, kRowThreads, kUnroll, false, false>(z, k2, p.reach, nullptr, none, slots);
         if(threadIdx.x < kWaveSize)
         {
             const float loss = entries_loss(p, r, log_sum(r), sh);
@@ -967,7 +972,7 @@ template <typename T> __global__ __launch_bounds__(kRowThreads) void distill_pie
         const int        begin = static_cast<int>(item - row * p.pieces) * p.piece;
         const RowSpan<T, false> z(static_cast<const T*>(p.z) + row * p.ld, begin, p.cols - begin < p.piece ? p.cols : begin + p.piece);
         LaneBest         none;
-        const Moments    r = span_moments<T, kRowThreads, kUnroll, false, false>(z, p.scale * kLog2e, nullptr, none, slots);
+        const Moments    r = span_moments<T, kRowThreads, kUnroll, false, false>(z, p.scale * kLog2e, p.reach, nullptr, none, slots);
         if(threadIdx.x == 0) p.part[item] = make_float4(r.m, r.s, r.w, 0.0f);
         __syncthreads();
     }
@@ -1008,6 +1013,7 @@ constexpr int64_t kFill = 1024;           // workgroups that fill the device: fo
 constexpr int64_t kMostGroups = 1 << 22;  // of a launch; larger problems loop
 
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+float near_reach(float scale) { return std::min(-kFar, kNearProduct / (scale * kLog2e)); }
 int vector_elements(int dt) { return dt == kF32 ? 4 : 8; }
 
 struct Split { int pieces, piece; };
@@ -1142,7 +1148,7 @@ hipError_t launch_token_logprobs(const void* z, int zdt, int64_t rows, int64_t c
 {
     const Split s = logprobs_split(zdt, rows, cols, top);
     LogitsArgs  a{};
-    a.z = z; a.rows = rows; a.ld = ld; a.cols = static_cast<int>(cols); a.scale = scale;
+    a.z = z; a.rows = rows; a.ld = ld; a.cols = static_cast<int>(cols); a.scale = scale; a.reach = near_reach(scale);
     a.pieces = s.pieces; a.piece = s.piece;
     a.tokens = tokens; a.wide = wide; a.logp = logp; a.entropy = entropy; a.stats = stats;
     a.top = top; a.top_logp = top_logp; a.top_index = top_index;
@@ -1173,7 +1179,7 @@ hipError_t launch_distill_topk(const void* z, int zdt, int64_t rows, int64_t col
     const Split s = in_pieces(dz ? kGradientRates : kLossRates, zdt, rows, cols) ? split_rows(rows, cols, span_elements(zdt) / kUnroll, kLogitsMaxCols)
                                                                                  : whole_row(cols);
     DistillArgs a{};
-    a.z = z; a.rows = rows; a.ld = ld; a.cols = static_cast<int>(cols); a.scale = scale;
+    a.z = z; a.rows = rows; a.ld = ld; a.cols = static_cast<int>(cols); a.scale = scale; a.reach = near_reach(scale);
     a.pieces = s.pieces; a.piece = s.piece; a.streamed = streamed(ddt, rows, cols);
     a.teacher = teacher; a.tdt = tdt; a.index = index; a.wide = wide; a.k = k; a.weight = weight; a.loss = loss;
     a.dz = dz; a.ddt = ddt;

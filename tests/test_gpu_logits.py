@@ -424,3 +424,66 @@ def test_entropy_of_rows_of_one_value(dtype, first, value):
         # ... by what logits_bound counts, and the quotient of the two sums, up to 64 here, by the roundings of a lane's and the lanes' additions in each
         bound = (R.logits_bound(R.f64(z), 1.0)[0].max() + 64 * R.U * (cols // 256 + 40)) * 2 + R.rounded(np.log(cols), F32)
         R.assert_within(entropy, np.array([np.log(cols)]), bound, f"entropy {cols}")
+
+
+class _Repeated:
+    """An operator for `copies` times a batch's rows, called with them one after the other, `pad` elements between rows: so many rows are each
+    kept whole, where a few would be cut into pieces.  All copies' results have the same bits -- of a multiple of eight rows, which all start
+    at the same alignments in every copy --; the first's are returned."""
+
+    def __init__(self, op, copies, pad=0):
+        self.op, self.copies, self.pad = op, copies, pad
+
+    def _given(self, t):
+        if t is None or t.dim() == 1:
+            return None if t is None else t.repeat(self.copies)
+        return torch.nn.functional.pad(t.repeat(self.copies, 1), (0, self.pad))[:, :t.shape[1]] if self.pad and t.shape[1] == self.op.cols else t.repeat(self.copies, 1)
+
+    def _first(self, t):
+        if t is None:
+            return None
+        parts = t.view(self.copies, -1, *t.shape[1:])
+        assert torch.equal(parts, parts[:1].expand_as(parts))
+        return parts[0]
+
+    def _call(self, f, *a):
+        out = f(*[self._given(t) for t in a])
+        return self._first(out) if isinstance(out, torch.Tensor) else tuple(self._first(t) for t in out)
+
+    def forward(self, *a):
+        return self._call(self.op.forward, *a)
+
+    def backward(self, *a):
+        return self._call(self.op.backward, *a)
+
+    def forward_backward(self, *a):
+        return self._call(self.op.forward_backward, *a)
+
+
+# both sides of where a product with the scale leaves the reach of the fast form, far beyond it, and maxima as far up
+FAR = [(dtype, value, scale) for dtype in (F32, BF16) for value, scale in
+       ((-1e9, 1.0), (-1.38e9, 1.0), (-1.5e9, 1.0), (-1e10, 1.0), (-1e10, 2.5), (-1e15, 1.0), (-1e20, 0.7), (-1e29, 1.0), (1e9, 1.0), (1e10, 1.0), (1e20, 1.0))]
+FAR += [(F16, -60000.0, 1e5), (F16, 30000.0, 1e6), (F16, 30000.0, 1e4)]
+
+
+@pytest.mark.parametrize("copies, cols", [(1, 700), (1, 70001), (20, 70001)])
+@pytest.mark.parametrize("dtype, value, scale", FAR)
+def test_finite_values_far_from_zero(dtype, value, scale, copies, cols):
+    """Rows of one such value, of nothing else but an ordinary one, with a few ordinary ones, in their second half, and in one place: rows of a
+    workgroup, in pieces, and longer than a workgroup's registers."""
+    say("far", dtype, value, scale, copies, cols)
+    z = _masked(8, cols, dtype, value)
+    z[4, cols // 2] = value
+    tokens, k = _tokens(8, cols, 2), 7
+    op = _Repeated(TokenLogProbs(8 * copies, cols, top_k=6, scale=scale, dlogits_dtype=dtype), copies)
+    dist = _Repeated(Distillation(8 * copies, cols, k, scale=scale, dlogits_dtype=dtype), copies)
+    _check_logprobs(z, tokens, scale, 6, "far", op)
+    _check_distill(z, k, scale, "far", dist)
+    # what lies so far below a row's maximum that its probability is 0 is as good as absent
+    apart = torch.where(z.float() < z.float().amax(1, keepdim=True) - 1e4, -INF, z.float()).to(dtype)
+    g, h, (teacher, index) = _randn(8, 3), _randn(8, 4), _entries(8, cols, k, 5)
+
+    def results(a):
+        _, entropy, _, _ = op.forward(a, tokens)
+        return [entropy.clone(), op.backward(g, h).clone(), dist.forward_backward(a, teacher, index, g)[1].clone()]
+    assert all(torch.equal(a, b) for a, b in zip(results(z), results(apart)))
