@@ -89,9 +89,9 @@ class LayerNorm:
         if dy.shape[0] != n:
             raise ValueError(f"dy has {dy.shape[0]} rows, the forward pass had {n}")
         dx = self.dx if n == self.rows else self.dx[:n]
-        if n == 0:
-            self.dgamma.zero_()
-            self.dbeta.zero_()
+        if n == 0:      # zeros, on the call's stream; the empty tensors have no address, and any will do
+            one = self.dgamma
+            Q.qsync_layernorm_bwd(one, self.cols, one, 0, self.cols, self.cols, gamma, one, one, None, self.dgamma, self.dbeta, None, stream)
             return dx, self.dgamma, self.dbeta
         Q.qsync_layernorm_bwd(dy, lddy, x, n, self.cols, ldx, gamma, self.mean, self.rstd, dx, self.dgamma, self.dbeta, self.ws, stream)
         return dx, self.dgamma, self.dbeta

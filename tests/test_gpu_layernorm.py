@@ -227,3 +227,23 @@ def test_batches_shorter_than_the_operator(made_for, rows, cols, x_dtype, dy_dty
     op = LayerNorm(made_for, cols, x_dtype=x_dtype, y_dtype=dy_dtype, dx_dtype=x_dtype, eps=EPS)
     for n in (rows, made_for):
         _check(_filled(n, cols, x_dtype, 1, 0.3), gamma, beta, _filled(n, cols, dy_dtype, 2), op, f"{n} of {made_for} x {cols}")
+
+
+@pytest.mark.parametrize("rows", [0, 40])
+def test_empty_batch_on_a_stream(rows):
+    """The cleared gradients come in the order of the caller's stream, not of torch's current one."""
+    op = LayerNorm(rows, 300, x_dtype=F16, eps=EPS)
+    x, a = torch.empty(0, 300, dtype=F16, device="cuda"), torch.zeros(8192, 8192, dtype=F16, device="cuda")
+    b, side = torch.empty_like(a), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(20):                                # some milliseconds, behind which an earlier batch's gradients arrive
+            torch.mm(a, a, out=b)
+        op.dgamma.fill_(5.0)
+        op.dbeta.fill_(6.0)
+    op.forward(x, stream=side)
+    dx, dgamma, dbeta = op.backward(x, stream=side)
+    with torch.cuda.stream(side):
+        seen = dgamma.clone(), dbeta.clone()
+    torch.cuda.synchronize()
+    assert dx.shape == (0, 300) and not any(t.any() for t in (*seen, dgamma, dbeta))
