@@ -546,15 +546,24 @@ __global__ __launch_bounds__(256) void norm_fold_kernel(const float* partial, in
 {
     __shared__ float lds[256];
     const int        q = threadIdx.x / 16;
-    const int64_t    c = static_cast<int64_t>(blockIdx.x) * 16 + threadIdx.x % 16;
-    const float      t = fold_column<false>(partial, S, 2 * cols, c, q, lds);
-    if(q != 0 || c >= 2 * cols) return;
-    if(c < cols) { if(dgamma) dgamma[c] = t; }
-    else if(dbeta) dbeta[c - cols] = t;
+    for(int64_t first = static_cast<int64_t>(blockIdx.x) * 16; first < 2 * cols; first += static_cast<int64_t>(gridDim.x) * 16)
+    {
+        const int64_t c = first + threadIdx.x % 16;
+        const float   t = fold_column<false>(partial, S, 2 * cols, c, q, lds);
+        if(q == 0 && c < 2 * cols)
+        {
+            if(c < cols) { if(dgamma) dgamma[c] = t; }
+            else if(dbeta) dbeta[c - cols] = t;
+        }
+        __syncthreads();      // (the next columns' sums take the same LDS)
+    }
 }
 
 constexpr int64_t kNormMaxCols   = 8192;      // columns of a row that is kept in registers by the backward pass
 constexpr int64_t kNormParamRows = 64;        // partial rows of the parameters' gradients of rows that are longer
+
+// Workgroups of a launch: larger problems loop.  A launch of 2^32 threads is refused, and one of a few more runs as those few alone.
+constexpr int64_t kNormMostGroups = 1 << 22;
 
 int64_t at_most(int64_t v, int64_t most) { return v < most ? v : most; }
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -569,8 +578,8 @@ int64_t even_groups(int64_t turns, int64_t most, int64_t turns_each)
 // at 1, 2, 4 and 8 turns: 16384 x 1024 binary16 17.4 17.1 15.7 16.9, 16384 x 2048 (4, 8, 16) 31.3 33.4 35.7, 4096 x 8192 (4, 8) 31.2 29.7.
 template <typename T, int TPR, int NU, int WG> hipError_t forward_rows(const NormArgs& a, hipStream_t st)
 {
-    const int64_t turns = div_up(a.rows, WG / TPR);
-    norm_forward_kernel<T, TPR, NU, WG><<<dim3(static_cast<unsigned>(even_groups(turns, WG == 256 ? 1024 : 512, WG == 256 ? 4 : 8))), dim3(WG), 0, st>>>(a);
+    const int64_t turns = div_up(a.rows, WG / TPR), groups = even_groups(turns, WG == 256 ? 1024 : 512, WG == 256 ? 4 : 8);
+    norm_forward_kernel<T, TPR, NU, WG><<<dim3(static_cast<unsigned>(at_most(groups, kNormMostGroups))), dim3(WG), 0, st>>>(a);
     return hipGetLastError();
 }
 template <typename T> hipError_t forward_type(const NormArgs& a, hipStream_t st)
@@ -674,7 +683,7 @@ hipError_t launch_layernorm_bwd(const void* dy, int dydt, int64_t lddy, const vo
     a.partial = dgamma || dbeta ? static_cast<float*>(workspace) : nullptr;
     const hipError_t e = dydt == kF32 ? backward_type<float>(a, xdt, st) : dydt == kF16 ? backward_type<_Float16>(a, xdt, st) : backward_type<__bf16>(a, xdt, st);
     if(e != hipSuccess || !a.partial) return e;
-    norm_fold_kernel<<<dim3(static_cast<unsigned>((2 * cols + 15) / 16)), dim3(256), 0, st>>>(
+    norm_fold_kernel<<<dim3(static_cast<unsigned>(at_most((2 * cols + 15) / 16, kNormMostGroups))), dim3(256), 0, st>>>(
         a.partial, static_cast<int>(backward_groups(rows, cols, dydt != kF32 && xdt != kF32)), cols, dgamma, dbeta);
     return hipGetLastError();
 }

@@ -247,3 +247,29 @@ def test_empty_batch_on_a_stream(rows):
         seen = dgamma.clone(), dbeta.clone()
     torch.cuda.synchronize()
     assert dx.shape == (0, 300) and not any(t.any() for t in (*seen, dgamma, dbeta))
+
+
+def test_more_rows_than_a_launch_has_workgroups_for():
+    rows = 1 << 30
+    say("layernorm rows", rows)
+    x = torch.zeros(rows, 2, dtype=F16, device="cuda")
+    x[:, 1] = 1.0
+    x[-3:] = torch.tensor([[3.0, -1.0], [-2.0, 2.0], [5.0, 5.0]], dtype=F16, device="cuda")
+    gamma, beta = torch.tensor([0.5, 2.0], device="cuda"), torch.tensor([0.25, -1.0], device="cuda")
+    op = LayerNorm(rows, 2, x_dtype=F16, eps=EPS, training=False)
+    y = op.forward(x, gamma, beta)
+    want, _, _ = R.layernorm(R.f64(x[-4:]), R.f64(gamma), R.f64(beta), EPS)
+    R.assert_within(y[-4:], want, R.layernorm_bound(R.f64(x[-4:]), R.f64(gamma), R.f64(beta), EPS) + R.rounded(want, F16), "last rows")
+    assert bool((y[:-3] == y[0]).all()) and torch.equal(y[0], y[-4])
+
+
+def test_more_columns_than_a_launch_has_workgroups_for():
+    cols = (1 << 27) + 8
+    say("layernorm columns", cols)
+    x, dy = torch.zeros(1, cols, dtype=BF16, device="cuda"), torch.ones(1, cols, dtype=BF16, device="cuda")
+    dy[0, 0], dy[0, -1], dy[0, -9] = 3.0, -2.0, 4.0
+    dgamma, dbeta = torch.full((cols,), 7.0, device="cuda"), torch.full((cols,), 7.0, device="cuda")
+    mean, rstd = torch.full((1,), -0.5, device="cuda"), torch.full((1,), 2.0, device="cuda")      # xh is 1
+    ws = torch.empty(Q.qsync_layernorm_bwd_workspace_bytes(1, cols), dtype=torch.uint8, device="cuda")
+    Q.qsync_layernorm_bwd(dy, cols, x, 1, cols, cols, None, mean, rstd, None, dgamma, dbeta, ws)
+    assert torch.equal(dgamma, dy[0].float()) and torch.equal(dbeta, dy[0].float())
