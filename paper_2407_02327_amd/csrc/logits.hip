@@ -44,7 +44,7 @@ struct LogitsArgs
     const void* z;
     int64_t     rows, ld;
     int         cols;
-    float       scale, reach;       // reach: |z| below which the fast form of a pass holds (host-made: it takes no vector register)
+    float       scale, k2, reach;   // see set_scale
     int         pieces, piece;      // pieces of a row, elements of a piece
     const void* tokens;             // or nullptr
     int         wide;               // 64-bit tokens (indices)
@@ -502,7 +502,7 @@ template <typename T, bool ENTROPY, bool TOP> __global__ __launch_bounds__(kRowT
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     __shared__ float4 slots[WG / kWaveSize];
     float*            chunk_max = reinterpret_cast<float*>(lds);
-    const float       k2        = p.scale * kLog2e;
+    const float       k2        = p.k2;
     const int64_t     items     = p.rows * p.pieces;
     for(int64_t item = blockIdx.x; item < items; item += gridDim.x)
     {
@@ -553,7 +553,7 @@ template <typename T> __global__ __launch_bounds__(kRowThreads) void logprobs_jo
     const int           lane = threadIdx.x % kWaveSize, wave = threadIdx.x / kWaveSize;
     for(int64_t row = blockIdx.x; row < p.rows; row += gridDim.x)
     {
-        const Moments r    = join_pieces<kRowThreads>(p.part + row * p.pieces, p.pieces, p.scale * kLog2e, slots);
+        const Moments r    = join_pieces<kRowThreads>(p.part + row * p.pieces, p.pieces, p.k2, slots);
         uint64_t      list = 0;
         if(p.top > 0)
         {
@@ -584,7 +584,7 @@ struct LogprobsGradArgs
     const void*  z;
     int64_t      rows, ld;
     int          cols;
-    float        scale;
+    float        scale, k2;
     int          pieces, piece;
     bool         streamed;          // stores of the gradient
     const void*  tokens;
@@ -643,7 +643,7 @@ template <typename T, int WG, bool STREAMED, bool ONCE> __device__ __forceinline
 
 template <typename T, bool ENTROPY, bool STREAMED> __global__ __launch_bounds__(kRowThreads) void logprobs_grad_kernel(const LogprobsGradArgs p)
 {
-    const float   k2    = p.scale * kLog2e;
+    const float   k2    = p.k2;
     const int64_t items = p.rows * p.pieces;
     for(int64_t item = blockIdx.x; item < items; item += gridDim.x)
     {
@@ -684,7 +684,7 @@ struct DistillArgs
     const void*  z;
     int64_t      rows, ld;
     int          cols;
-    float        scale, reach;
+    float        scale, k2, reach;
     int          pieces, piece;
     bool         streamed;          // stores of the gradient
     const void*  teacher;
@@ -740,7 +740,7 @@ template <typename T> __device__ __forceinline__ void entries_prepare(const Dist
 #pragma unroll 1
     for(int i = threadIdx.x; i < p.k; i += kWaveSize)
     {
-        const float q = any ? exp2_fast((sh.log_q[i] - top) * (p.scale * kLog2e)) : 0.0f;
+        const float q = any ? exp2_fast((sh.log_q[i] - top) * p.k2) : 0.0f;
         sh.q[i] = q;
         total += q;
     }
@@ -804,7 +804,7 @@ __device__ __forceinline__ void span_gradient(const DistillArgs& p, int64_t row,
         zero_span<T, WG, STREAMED>(z, p.dz, p.ddt, at);
         return;
     }
-    const float k2 = p.scale * kLog2e, gs = g / r.s;
+    const float k2 = p.k2, gs = g / r.s;
     auto        mass = [&](float v) { return gs * exp2_fast((v - r.m) * k2); };
     map_span<T, WG, STREAMED>(z, p.dz, p.ddt, at, [&](int, float v) { return mass(v); });
     __syncthreads();      // (behind the probabilities)
@@ -825,7 +825,7 @@ template <typename T, int WG, int NV, bool REST, bool STREAMED> __global__ __lau
     __shared__ float4        slots[WAVES];
     const int                tid = threadIdx.x;
     const bool               first = tid < kWaveSize;
-    const float              k2 = p.scale * kLog2e;
+    const float              k2 = p.k2;
     for(int64_t row = blockIdx.x; row < p.rows; row += gridDim.x)
     {
         const RowSpan<T, true> z(static_cast<const T*>(p.z) + row * p.ld, 0, p.cols);
@@ -940,7 +940,7 @@ template <typename T> __global__ __launch_bounds__(kRowThreads) void distill_los
 {
     __shared__ EntriesShared sh;
     __shared__ float4        slots[kRowThreads / kWaveSize];
-    const float              k2 = p.scale * kLog2e;
+    const float              k2 = p.k2;
     for(int64_t row = blockIdx.x; row < p.rows; row += gridDim.x)
     {
         const RowSpan<T, true> z(static_cast<const T*>(p.z) + row * p.ld, 0, p.cols);
@@ -972,7 +972,7 @@ template <typename T> __global__ __launch_bounds__(kRowThreads) void distill_pie
         const int        begin = static_cast<int>(item - row * p.pieces) * p.piece;
         const RowSpan<T, false> z(static_cast<const T*>(p.z) + row * p.ld, begin, p.cols - begin < p.piece ? p.cols : begin + p.piece);
         LaneBest         none;
-        const Moments    r = span_moments<T, kRowThreads, kUnroll, false, false>(z, p.scale * kLog2e, p.reach, nullptr, none, slots);
+        const Moments    r = span_moments<T, kRowThreads, kUnroll, false, false>(z, p.k2, p.reach, nullptr, none, slots);
         if(threadIdx.x == 0) p.part[item] = make_float4(r.m, r.s, r.w, 0.0f);
         __syncthreads();
     }
@@ -993,7 +993,7 @@ template <typename T> __global__ __launch_bounds__(kRowThreads) void distill_joi
             entries_fetch(p, row, sh);
             entries_prepare(p, z, sh);
         }
-        const Moments r = join_pieces<kRowThreads>(p.part + row * p.pieces, p.pieces, p.scale * kLog2e, slots);
+        const Moments r = join_pieces<kRowThreads>(p.part + row * p.pieces, p.pieces, p.k2, slots);
         if(p.loss && i == 0 && threadIdx.x < kWaveSize)
         {
             const float loss = entries_loss(p, r, log_sum(r), sh);
@@ -1013,7 +1013,15 @@ constexpr int64_t kFill = 1024;           // workgroups that fill the device: fo
 constexpr int64_t kMostGroups = 1 << 22;  // of a launch; larger problems loop
 
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
-float near_reach(float scale) { return std::min(-kFar, kNearProduct / (scale * kLog2e)); }
+// k2: scale log2(e), the largest number where that has none (0 of a difference must stay 0).  reach: |z| below which the fast form of a pass
+// holds.  (Made here they take no vector registers.)
+float exponent_scale(float scale) { return std::min(scale * kLog2e, FLT_MAX); }
+template <typename A> void set_scale(A& a, float scale)
+{
+    a.scale = scale;
+    a.k2    = exponent_scale(scale);
+    a.reach = std::min(-kFar, kNearProduct / a.k2);
+}
 int vector_elements(int dt) { return dt == kF32 ? 4 : 8; }
 
 struct Split { int pieces, piece; };
@@ -1148,7 +1156,7 @@ hipError_t launch_token_logprobs(const void* z, int zdt, int64_t rows, int64_t c
 {
     const Split s = logprobs_split(zdt, rows, cols, top);
     LogitsArgs  a{};
-    a.z = z; a.rows = rows; a.ld = ld; a.cols = static_cast<int>(cols); a.scale = scale; a.reach = near_reach(scale);
+    a.z = z; a.rows = rows; a.ld = ld; a.cols = static_cast<int>(cols); set_scale(a, scale);
     a.pieces = s.pieces; a.piece = s.piece;
     a.tokens = tokens; a.wide = wide; a.logp = logp; a.entropy = entropy; a.stats = stats;
     a.top = top; a.top_logp = top_logp; a.top_index = top_index;
@@ -1163,7 +1171,7 @@ hipError_t launch_token_logprobs_bwd(const void* z, int zdt, int64_t rows, int64
 {
     const Split      s = split_rows(rows, cols, kRowThreads * 8, kRowThreads * 8 * 16);
     LogprobsGradArgs a{};
-    a.z = z; a.rows = rows; a.ld = ld; a.cols = static_cast<int>(cols); a.scale = scale;
+    a.z = z; a.rows = rows; a.ld = ld; a.cols = static_cast<int>(cols); a.scale = scale; a.k2 = exponent_scale(scale);
     a.pieces = s.pieces; a.piece = s.piece; a.streamed = streamed(ddt, rows, cols);
     a.tokens = tokens; a.wide = wide; a.stats = stats; a.entropy = entropy; a.dlogp = dlogp; a.dentropy = dentropy;
     a.dz = dz; a.ddt = ddt;
@@ -1179,7 +1187,7 @@ hipError_t launch_distill_topk(const void* z, int zdt, int64_t rows, int64_t col
     const Split s = in_pieces(dz ? kGradientRates : kLossRates, zdt, rows, cols) ? split_rows(rows, cols, span_elements(zdt) / kUnroll, kLogitsMaxCols)
                                                                                  : whole_row(cols);
     DistillArgs a{};
-    a.z = z; a.rows = rows; a.ld = ld; a.cols = static_cast<int>(cols); a.scale = scale; a.reach = near_reach(scale);
+    a.z = z; a.rows = rows; a.ld = ld; a.cols = static_cast<int>(cols); set_scale(a, scale);
     a.pieces = s.pieces; a.piece = s.piece; a.streamed = streamed(ddt, rows, cols);
     a.teacher = teacher; a.tdt = tdt; a.index = index; a.wide = wide; a.k = k; a.weight = weight; a.loss = loss;
     a.dz = dz; a.ddt = ddt;

@@ -487,3 +487,25 @@ def test_finite_values_far_from_zero(dtype, value, scale, copies, cols):
         _, entropy, _, _ = op.forward(a, tokens)
         return [entropy.clone(), op.backward(g, h).clone(), dist.forward_backward(a, teacher, index, g)[1].clone()]
     assert all(torch.equal(a, b) for a, b in zip(results(z), results(apart)))
+
+
+@pytest.mark.parametrize("copies, cols", [(1, 700), (1, 70001), (20, 70001)])
+def test_the_largest_and_smallest_scales(copies, cols):
+    """A scale whose product with log2(e) no fp32 number holds: all weight is on the largest logits.  The smallest one: the uniform distribution."""
+    say("scales", copies, cols)
+    z, tokens = _logits(8, cols, BF16, 1).clone(), _tokens(8, cols, 2)
+    z[0], z[1, 3] = 0.0, 50.0
+    tokens[:2] = 3
+    teacher, index = torch.zeros(8, 1, device="cuda"), torch.from_numpy(R.f64(z).argmax(1)).cuda()[:, None]      # (the first of equal ones)
+    ties = (z == z.amax(1, keepdim=True)).sum(1).double().cpu().numpy()
+    for scale, alive in ((3.2e38, ties), (1e-42, np.full(8, float(cols)))):
+        op = _Repeated(TokenLogProbs(8 * copies, cols, top_k=1, scale=scale), copies)
+        dist = _Repeated(Distillation(8 * copies, cols, 1, scale=scale), copies)
+        logp, entropy, top_logp, top_index = op.forward(z, tokens)
+        want = np.log(alive)
+        bound = R.U * (cols // 256 + 120) + R.rounded(want, F32)
+        R.assert_within(logp[:2], -want[:2], bound[:2], "logp")
+        R.assert_within(top_logp[:, 0], -want, bound, "top_logp")
+        R.assert_within(entropy, want, 2 * bound, "entropy")
+        assert torch.equal(top_index.long(), index)
+        R.assert_within(dist.forward(z, teacher, index), want, bound, "loss")
