@@ -676,8 +676,8 @@ size_t qsync_token_logprobs_workspace_bytes(int ldt, int64_t rows, int64_t cols,
  * dentropy_opt rows floats or NULL (0), with entropy_opt.  One of the two is required.
  * dlogits    out, packed [rows, cols] of ddt (the same three types), rounded once.  It may be the logits themselves when the types
  *            agree and ld == cols; any other overlap is QSYNC_ERR_UNSUPPORTED.
- * Masked logits (-inf) and rows of nothing else have a gradient of 0, and so have rows whose dlogp and dentropy are 0, whatever
- * their logits hold.
+ * A masked logit (-inf) has a gradient of 0, unless it is the row's token: there it is the formula's, scale dlogp[r].  Rows of
+ * nothing else have a gradient of 0, and so have rows whose dlogp and dentropy are 0, whatever their logits hold.
  */
 int qsync_token_logprobs_bwd(const void* logits, int ldt, int64_t rows, int64_t cols, int64_t ld, float scale,
                              const void* tokens_opt, int tdt, const float* stats, const float* entropy_opt,

@@ -509,3 +509,22 @@ def test_the_largest_and_smallest_scales(copies, cols):
         R.assert_within(entropy, want, 2 * bound, "entropy")
         assert torch.equal(top_index.long(), index)
         R.assert_within(dist.forward(z, teacher, index), want, bound, "loss")
+
+
+@pytest.mark.parametrize("copies", [1, 304])
+def test_gradient_of_a_token_on_a_masked_column(copies):
+    """Its log probability is -inf, whose gradient is the formula's: scale dlogp in its own column, and -scale dlogp p in the others, none
+    of them masked; a row of nothing but masks has none."""
+    z, tokens = _logits(3, 5000, F32, 1).clone(), torch.tensor([7, 4999, 3], device="cuda")
+    z[0, 5:10], z[1, 2500:], z[2] = -INF, -INF, -INF
+    op = _Repeated(TokenLogProbs(3 * copies, 5000, scale=0.5, dlogits_dtype=F32), copies)
+    assert torch.isneginf(op.forward(z, tokens)[0]).all()
+    g = torch.tensor([2.0, -3.0, 1.0], device="cuda")
+    dz = op.backward(g)
+    assert dz[0, 7] == 1.0 and dz[1, 4999] == -1.5 and not dz[2].any()
+    masked = torch.isneginf(z)
+    masked[[0, 1], tokens[:2]] = False
+    assert not dz[masked].any()
+    want = R.token_logprobs_grad(R.f64(z), tokens.cpu().numpy(), 0.5, R.f64(g), np.zeros(3))
+    rel, _ = R.logits_bound(R.f64(z), 0.5)
+    R.assert_within(dz, want, 4 * rel * np.abs(want) + 2.0 ** -120 + R.rounded(want, F32), "gradient")
