@@ -273,3 +273,12 @@ def test_more_columns_than_a_launch_has_workgroups_for():
     ws = torch.empty(Q.qsync_layernorm_bwd_workspace_bytes(1, cols), dtype=torch.uint8, device="cuda")
     Q.qsync_layernorm_bwd(dy, cols, x, 1, cols, cols, None, mean, rstd, None, dgamma, dbeta, ws)
     assert torch.equal(dgamma, dy[0].float()) and torch.equal(dbeta, dy[0].float())
+
+
+@pytest.mark.parametrize("rows, cols", [(1100, 4500), (1100, 5003), (1100, 8192), (1100, 16384), (1100, 17001)])
+@pytest.mark.parametrize("dtype", [F16, F32])
+def test_many_wide_rows(rows, cols, dtype):
+    """More rows than workgroups where a row takes a whole one: several turns of each, whose sums meet."""
+    say("layernorm wide", rows, cols, dtype)
+    gamma, beta = _params(cols, 3)
+    _check(_filled(rows, cols, dtype, 1, 0.3), gamma, beta, _filled(rows, cols, dtype, 2), LayerNorm(rows, cols, x_dtype=dtype, eps=EPS), f"{rows}x{cols}")

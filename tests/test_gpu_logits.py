@@ -528,3 +528,33 @@ def test_gradient_of_a_token_on_a_masked_column(copies):
     want = R.token_logprobs_grad(R.f64(z), tokens.cpu().numpy(), 0.5, R.f64(g), np.zeros(3))
     rel, _ = R.logits_bound(R.f64(z), 0.5)
     R.assert_within(dz, want, 4 * rel * np.abs(want) + 2.0 ** -120 + R.rounded(want, F32), "gradient")
+
+
+# (20 copies of eight rows: enough that a row of any of these lengths is kept whole)
+@pytest.mark.parametrize("pad", [0, 3])
+@pytest.mark.parametrize("cols, dtype", [(20000, F32), (50021, F32), (40003, F16), (40003, BF16), (70001, F16), (70001, BF16), (131072, BF16)])
+def test_long_rows_kept_whole(cols, dtype, pad):
+    """Distillation steps over rows that fill the registers of a workgroup, and over longer ones, whose rest is read again."""
+    say("whole", cols, dtype, pad)
+    for z in (_logits(8, cols, dtype, 1), _masked(8, cols, dtype, -INF), _masked(8, cols, dtype, torch.finfo(dtype).min)):
+        for grad_dtype in {dtype, F32}:
+            _check_distill(z, 7, 0.7, f"{cols} {grad_dtype}", _Repeated(Distillation(160, cols, 7, scale=0.7, dlogits_dtype=grad_dtype), 20, pad))
+
+
+@pytest.mark.parametrize("cols, dtype", [(50021, F32), (70001, BF16)])
+def test_long_rows_kept_whole_in_place(cols, dtype):
+    say("whole in place", cols, dtype)
+    z, (teacher, index) = _logits(150, cols, dtype, 1).contiguous(), _entries(150, cols, 8, 5)
+    g, op = _randn(150, 3), Distillation(150, cols, 8, dlogits_dtype=dtype)
+    loss, dz = (t.clone() for t in op.forward_backward(z, teacher, index, g))
+    again = op.forward_backward(z, teacher, index, g, out=z)
+    assert torch.equal(again[0], loss) and torch.equal(z, dz)
+
+
+@pytest.mark.parametrize("cols, top_k", [(98304, 9), (98305, 9), (200003, 64)])
+def test_many_long_rows_with_alternatives(cols, top_k):
+    """fp32 rows on both sides of what a search keeps of a row: one piece, and two or more of it, of more rows than the device has room for."""
+    say("many long rows", cols, top_k)
+    z = _logits(8, cols, F32, 1)
+    z[3, cols // 2 - 40:cols // 2 + 40] = 30.0            # (equal ones on both sides of a limit)
+    _check_logprobs(z, _tokens(8, cols, 2), 1.0, top_k, f"{cols}", _Repeated(TokenLogProbs(1104, cols, top_k=top_k, dlogits_dtype=F32), 138))
