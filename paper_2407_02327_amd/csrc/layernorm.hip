@@ -541,29 +541,23 @@ template <typename TD, typename T> __global__ __launch_bounds__(256) void norm_p
     }
 }
 
+// Workgroups of a launch: larger problems loop, or go on in the grid's next row.  A launch of 2^32 threads is refused, and one of a few more runs as those few alone.
+constexpr int64_t kNormMostGroups = 1 << 22;
+
 // dgamma and dbeta from S partial rows [S][2][cols]
 __global__ __launch_bounds__(256) void norm_fold_kernel(const float* partial, int S, int64_t cols, float* dgamma, float* dbeta)
 {
     __shared__ float lds[256];
     const int        q = threadIdx.x / 16;
-    for(int64_t first = static_cast<int64_t>(blockIdx.x) * 16; first < 2 * cols; first += static_cast<int64_t>(gridDim.x) * 16)
-    {
-        const int64_t c = first + threadIdx.x % 16;
-        const float   t = fold_column<false>(partial, S, 2 * cols, c, q, lds);
-        if(q == 0 && c < 2 * cols)
-        {
-            if(c < cols) { if(dgamma) dgamma[c] = t; }
-            else if(dbeta) dbeta[c - cols] = t;
-        }
-        __syncthreads();      // (the next columns' sums take the same LDS)
-    }
+    const int64_t    c = (static_cast<int64_t>(blockIdx.y) * kNormMostGroups + blockIdx.x) * 16 + threadIdx.x % 16;
+    const float      t = fold_column<false>(partial, S, 2 * cols, c, q, lds);
+    if(q != 0 || c >= 2 * cols) return;
+    if(c < cols) { if(dgamma) dgamma[c] = t; }
+    else if(dbeta) dbeta[c - cols] = t;
 }
 
 constexpr int64_t kNormMaxCols   = 8192;      // columns of a row that is kept in registers by the backward pass
 constexpr int64_t kNormParamRows = 64;        // partial rows of the parameters' gradients of rows that are longer
-
-// Workgroups of a launch: larger problems loop.  A launch of 2^32 threads is refused, and one of a few more runs as those few alone.
-constexpr int64_t kNormMostGroups = 1 << 22;
 
 int64_t at_most(int64_t v, int64_t most) { return v < most ? v : most; }
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -683,7 +677,8 @@ hipError_t launch_layernorm_bwd(const void* dy, int dydt, int64_t lddy, const vo
     a.partial = dgamma || dbeta ? static_cast<float*>(workspace) : nullptr;
     const hipError_t e = dydt == kF32 ? backward_type<float>(a, xdt, st) : dydt == kF16 ? backward_type<_Float16>(a, xdt, st) : backward_type<__bf16>(a, xdt, st);
     if(e != hipSuccess || !a.partial) return e;
-    norm_fold_kernel<<<dim3(static_cast<unsigned>(at_most((2 * cols + 15) / 16, kNormMostGroups))), dim3(256), 0, st>>>(
+    const int64_t groups = div_up(2 * cols, 16);
+    norm_fold_kernel<<<dim3(static_cast<unsigned>(at_most(groups, kNormMostGroups)), static_cast<unsigned>(div_up(groups, kNormMostGroups))), dim3(256), 0, st>>>(
         a.partial, static_cast<int>(backward_groups(rows, cols, dydt != kF32 && xdt != kF32)), cols, dgamma, dbeta);
     return hipGetLastError();
 }
