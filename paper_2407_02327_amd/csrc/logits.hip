@@ -44,12 +44,15 @@ struct LogitsArgs
     const void* z;
     int64_t     rows, ld;
     int         cols;
-    float       scale, k2, reach;   // see set_scale
+    float       scale;
     int         pieces, piece;      // pieces of a row, elements of a piece
     const void* tokens;             // or nullptr
     int         wide;               // 64-bit tokens (indices)
+    float       reach;              // see set_scale.  (It and k2 lie in gaps: eight bytes more put the grid's size, which stands behind
+                                    // these, into a third line of memory, 4 x 131072 bfloat16 with 20 alternatives 12.0 -> 12.4 us.)
     float *     logp, *entropy, *stats;
     int         top;
+    float       k2;
     float*      top_logp;
     int32_t*    top_index;
     float4*     part;               // [rows][pieces] moments
@@ -502,7 +505,8 @@ template <typename T, bool ENTROPY, bool TOP> __global__ __launch_bounds__(kRowT
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     __shared__ float4 slots[WG / kWaveSize];
     float*            chunk_max = reinterpret_cast<float*>(lds);
-    const float       k2        = p.k2;
+    float             k2        = p.k2;
+    asm volatile("" : "+v"(k2));      // (in a vector register: scalar ones are short here, and are spilled)
     const int64_t     items     = p.rows * p.pieces;
     for(int64_t item = blockIdx.x; item < items; item += gridDim.x)
     {
@@ -584,11 +588,12 @@ struct LogprobsGradArgs
     const void*  z;
     int64_t      rows, ld;
     int          cols;
-    float        scale, k2;
+    float        scale;
     int          pieces, piece;
     bool         streamed;          // stores of the gradient
     const void*  tokens;
     int          wide;
+    float        k2;                // see set_scale
     const float *stats, *entropy, *dlogp, *dentropy;      // entropy and dentropy both or neither; dlogp or nullptr
     void*        dz;
     int          ddt;
@@ -684,11 +689,13 @@ struct DistillArgs
     const void*  z;
     int64_t      rows, ld;
     int          cols;
-    float        scale, k2, reach;
+    float        scale;
     int          pieces, piece;
     bool         streamed;          // stores of the gradient
+    float        reach;             // see set_scale
     const void*  teacher;
     int          tdt;
+    float        k2;
     const void*  index;
     int          wide, k;
     const float* weight;      // or nullptr: 1
@@ -825,7 +832,10 @@ template <typename T, int WG, int NV, bool REST, bool STREAMED> __global__ __lau
     __shared__ float4        slots[WAVES];
     const int                tid = threadIdx.x;
     const bool               first = tid < kWaveSize;
-    const float              k2 = p.k2;
+    float                    k2 = p.k2;
+    // (In a vector register.  The six that binary16 saves otherwise let a third workgroup onto a unit: a step over 4096 x 32768 with one
+    // entry 100 -> 105 us, with 64 of them 133 -> 129.)
+    asm volatile("" : "+v"(k2));
     for(int64_t row = blockIdx.x; row < p.rows; row += gridDim.x)
     {
         const RowSpan<T, true> z(static_cast<const T*>(p.z) + row * p.ld, 0, p.cols);
@@ -1014,7 +1024,7 @@ constexpr int64_t kMostGroups = 1 << 22;  // of a launch; larger problems loop
 
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // k2: scale log2(e), the largest number where that has none (0 of a difference must stay 0).  reach: |z| below which the fast form of a pass
-// holds.  (Made here they take no vector registers.)
+// holds.  (Made on the host: beside its kernels' registers a division would cost two more.)
 float exponent_scale(float scale) { return std::min(scale * kLog2e, FLT_MAX); }
 template <typename A> void set_scale(A& a, float scale)
 {
