@@ -820,8 +820,9 @@ __device__ __forceinline__ void span_gradient(const DistillArgs& p, int64_t row,
 
 // A row a workgroup, its logits in registers between the sums and the gradient: NV vectors of a thread, all under way at once.  What a
 // longer row has beyond them is read twice, the second time out of a cache.
-//   A step over 4096 x 65536 bfloat16 logits: 207 us, 5.2 TB/s of logits read once and gradient written once; with all of a row read
-//   twice 272 (512 threads) and 309 (256), both before loads and stores were streamed and this form took 230.
+//   A step over 4096 x 65536 bfloat16 logits: 205 us, 5.2 TB/s of logits read once and gradient written once (under the profiler 217 to 223
+//   on average, 208 the shortest); with all of a row read twice 272 (512 threads) and 309 (256), both before loads and stores were streamed and
+//   this form took 230.
 // (Four wavefronts of a SIMD leave 128 registers.  The scheduling barriers keep the phases from being unrolled into more values than
 // that; the words are taken apart again in each phase, as fp32 values they would take twice the registers.)
 template <typename T, int WG, int NV, bool REST, bool STREAMED> __global__ __launch_bounds__(WG, 4) void distill_held_kernel(const DistillArgs p)
@@ -1049,8 +1050,9 @@ Split split_rows(int64_t rows, int64_t cols, int64_t least, int64_t most)
 // A row a workgroup, or in pieces?  A compute unit takes in `unit` bytes of a row in a microsecond, however many threads ask for them, all of
 // them together `device`; pieces cost a second launch and what it reads, `launch` microseconds.
 struct RowRates { double unit, device, launch; };
-//   log probabilities, 20 alternatives, us, a row a workgroup -> in pieces: 1 x 131072 bfloat16 17.5 -> 11.9, 64 x 131072 18.3 -> 16.9,
-//   128 x 131072 18.9 -> 19.2, 1 x 32768 9.4 -> 11.1, 333 x 50021 fp32 22.3 -> 28.7
+//   log probabilities, 20 alternatives (the rates serve for none and for 64 as well, where they were not measured), us, a row a workgroup ->
+//   in pieces: 1 x 131072 bfloat16 17.5 -> 11.9, 64 x 131072 18.3 -> 16.9, 128 x 131072 18.9 -> 19.2, 1 x 32768 9.4 -> 11.1,
+//   333 x 50021 fp32 22.3 -> 28.7
 constexpr RowRates kLogprobsRates = {27.0e3, 3.3e6, 3.5};
 //   loss alone: 1 x 131072 bfloat16 10.4 -> 8.3, 64 x 131072 12.1 -> 9.8, 1 x 32768 5.8 -> 8.3
 constexpr RowRates kLossRates = {45.0e3, 1.0e7, 3.0};
