@@ -40,8 +40,8 @@ extern "C" {
 /* Per-operator precision tag b_io (paper: problem (1); evaluation uses INT8, FP16, FP32). */
 typedef enum { QSYNC_INT8 = 8, QSYNC_FP16 = 16, QSYNC_FP32 = 32 } qsync_prec_t;
 
-/* Element type of a buffer.  QSYNC_BF16 and QSYNC_I64: layer norm and logits only (qsync_layernorm_*, qsync_token_logprobs*,
- * qsync_distill_topk); every other call answers QSYNC_ERR_BAD_ENUM to them. */
+/* Element type of a buffer.  QSYNC_BF16 and QSYNC_I64: layer norm, logits, token scales and experts only (qsync_layernorm_*,
+ * qsync_token_*, qsync_distill_topk, qsync_expert_*); every other call answers QSYNC_ERR_BAD_ENUM to them. */
 typedef enum { QSYNC_F32 = 0, QSYNC_F16 = 1, QSYNC_I8 = 2, QSYNC_I32 = 3, QSYNC_BF16 = 4, QSYNC_I64 = 5 } qsync_dtype_t;
 
 /* Granularity of a scale: one per tensor ("layer-wise"), one per row, or one per column
@@ -709,6 +709,122 @@ int qsync_distill_topk(const void* logits, int ldt, int64_t rows, int64_t cols, 
                        int teacher_dt, const void* index, int idt, int64_t k, const float* weight_opt, float* loss,
                        void* dlogits_opt, int ddt, void* workspace, size_t workspace_bytes, void* stream);
 size_t qsync_distill_topk_workspace_bytes(int ldt, int64_t rows, int64_t cols);
+
+/*
+ * ---- INT8 linear operators with a scale for each token, and experts ----------------------------------------------------------------
+ *
+ * One scale for a whole activation is set by its widest token; here every token (row) of the activation, and every channel of the
+ * weights, has its own.  Paper: Cost Mapper paragraph (channel-wise quantization and its dequantizer), here on both operands.
+ *
+ * Codes of a slice v (a row, or a column within a set of rows) with a = max |v|:
+ *   a < 2^-100: scale 1, codes 0.   a not finite: scale NaN, codes 0 (what takes part in its products is NaN, nothing else is).
+ *   otherwise scale = a / 127, inverse = 127 / a (one fp32 division each), code = clamp(round(v * inverse), -127, 127).
+ * round: to nearest even, or stochastic as in qsync_quantize, where the element (row, col) has the draw col % 8 of the Philox block
+ * offset + row * ceil(cols / 8) + col / 8; a call consumes rows * ceil(cols / 8) counters.
+ *
+ * Rows of codes are padded with zeros to qsync_token_code_cols(cols) = cols rounded up to a multiple of 128.
+ * Sets of rows: with offsets_opt (device, sets + 1 int32, ascending from 0), set e has the rows offsets[e] .. offsets[e+1]-1 and rows from
+ * offsets[sets] on belong to none: they are not read, and what is theirs in an output stays as it was.  NULL: equal shares of the rows
+ * (rows % sets == 0, QSYNC_ERR_BAD_SHAPE otherwise).  Offsets that do not ascend or reach beyond the rows give undefined results in the
+ * outputs and no access outside of the buffers.
+ * Codes along the rows (of the columns, transposed) hold, set after set, a packed matrix [cols][rows of the set rounded up to 128]; the
+ * buffer has qsync_token_code_rows(rows, sets, offsets != NULL) * cols bytes.
+ * Limits: rows <= 2^23, cols <= 2^20, sets 1..512 (QSYNC_ERR_UNSUPPORTED beyond).  x is of QSYNC_F32, QSYNC_F16 or QSYNC_BF16 at any
+ * element's alignment; codes, and the workspace, are 16-byte aligned.  Outputs do not overlap inputs.
+ */
+int64_t qsync_token_code_cols(int64_t cols);
+int64_t qsync_token_code_rows(int64_t rows, int64_t sets, int with_offsets);
+
+/*
+ * qsync_token_quantize - codes with a scale for each row.
+ * x           [x_rows, ld] of xdt, ld >= cols.  Without source_opt x_rows == rows (QSYNC_ERR_BAD_SHAPE otherwise).
+ * source_opt  rows int32 or NULL: row r is x's row source[r] / group (qsync_expert_sort), group >= 1.  A place outside of x: as a row
+ *             that is not finite; nothing is read there.
+ * count_opt   device int32 or NULL: rows from it on are none (offsets + sets of a sort).
+ * rnd         QSYNC_ROUND_NEAREST or QSYNC_ROUND_STOCHASTIC (QSYNC_ERR_UNSUPPORTED otherwise).
+ * scale       out, rows floats.    q  out, [rows, qsync_token_code_cols(cols)] int8.
+ */
+int qsync_token_quantize(const void* x, int xdt, int64_t x_rows, int64_t cols, int64_t ld, const int32_t* source_opt, int64_t group,
+                         int64_t rows, const int32_t* count_opt, int rnd, uint64_t philox_seed, uint64_t philox_offset, float* scale,
+                         void* q, void* stream);
+
+/*
+ * qsync_token_quantize_both - codes with a scale for each row, and codes with a scale for each column of each set, from two reads of x
+ * (stochastic: from the same draws).  The first are an operand of the forward pass or the data gradient, the second of the weight
+ * gradient; of weights ([sets * N, K], offsets_opt NULL) the second are the operand of the data gradient.
+ * row_scale rows floats, q as above; col_scale [sets, cols] floats, qT as described above; a column of an empty set has scale 1.
+ * colsum_opt  out, [sets, cols] floats or NULL: the sums of the columns (a bias gradient), in fp32 in an order that depends on the sizes
+ *             and offsets alone.
+ * workspace   at least qsync_token_quantize_both_workspace_bytes(rows, cols, sets, offsets_opt != NULL) bytes, no contents needed.
+ */
+int qsync_token_quantize_both(const void* x, int xdt, int64_t x_rows, int64_t cols, int64_t ld, const int32_t* source_opt, int64_t group,
+                              int64_t rows, int64_t sets, const int32_t* offsets_opt, int rnd, uint64_t philox_seed,
+                              uint64_t philox_offset, float* row_scale, void* q, float* col_scale, void* qT, float* colsum_opt,
+                              void* workspace, size_t workspace_bytes, void* stream);
+size_t qsync_token_quantize_both_workspace_bytes(int64_t rows, int64_t cols, int64_t sets, int with_offsets);
+
+/*
+ * qsync_token_linear_fwd - Y = X W^T + b on codes, with the scales of both in the epilogue:
+ *   acc[m,n] = sum_k xq[m,k] wq[e,n,k]  (int32, wraps mod 2^32)        Y[m,n] = float(acc) * (sx[m] * sw[e,n]) + bias[e,n]
+ * e is the set that row m belongs to.  The data gradient is this call on the codes of dY and the transposed codes of the weights.
+ * xq [rows, code_cols(K)], sx rows floats; wq [sets, N, code_cols(K)], sw [sets, N] floats; bias_opt [sets, N] floats or NULL.
+ * offsets_opt NULL: one set (QSYNC_ERR_UNSUPPORTED otherwise).
+ * y   out, packed [rows, N] of ydt (QSYNC_F32, QSYNC_F16 or QSYNC_BF16), rounded once.
+ * workspace   at least qsync_token_linear_workspace_bytes(rows, N, K, sets) bytes (may be NULL if that is 0), no contents needed.
+ */
+int qsync_token_linear_fwd(int64_t rows, int64_t N, int64_t K, int64_t sets, const int32_t* offsets_opt, const void* xq, const float* sx,
+                           const void* wq, const float* sw, const float* bias_opt, void* y, int ydt, void* workspace,
+                           size_t workspace_bytes, void* stream);
+size_t qsync_token_linear_workspace_bytes(int64_t rows, int64_t N, int64_t K, int64_t sets);
+
+/*
+ * qsync_token_linear_wgrad - dW[e,n,k] = (sum over the rows m of set e of dyqT[n,m] xqT[k,m]) * (sdy[e,n] * sx[e,k]), on codes along the rows
+ * (qsync_token_quantize_both) of dY [rows, N] and X [rows, K].  dw out, [sets, N, K] of dwdt; zeros for a set without rows.
+ * offsets_opt NULL: one set.  workspace: qsync_token_wgrad_workspace_bytes(rows, N, K, sets).
+ */
+int qsync_token_linear_wgrad(int64_t rows, int64_t N, int64_t K, int64_t sets, const int32_t* offsets_opt, const void* dyqT,
+                             const float* sdy, const void* xqT, const float* sx, void* dw, int dwdt, void* workspace,
+                             size_t workspace_bytes, void* stream);
+size_t qsync_token_wgrad_workspace_bytes(int64_t rows, int64_t N, int64_t K, int64_t sets);
+
+/*
+ * qsync_expert_sort - the rows of a batch sorted by expert.  ids packed [tokens, group] of idt (QSYNC_I32 or QSYNC_I64): the experts that
+ * a router gave each token.  Entries outside of 0 .. experts-1 have none.  Stable: by expert, then in the order of ids.
+ * offsets     out, experts + 1 int32: the first row of each expert, and the number of rows.
+ * source      out, tokens * group int32: the place in ids of every row; behind the last row left as it was.
+ * slot        out, [tokens, group] int32: the row of every entry, -1 where there is none.
+ * experts 1..512 and tokens * group <= 2^23 (QSYNC_ERR_UNSUPPORTED beyond).
+ * workspace   at least qsync_expert_sort_workspace_bytes(tokens * group, experts) bytes, no contents needed.
+ */
+int qsync_expert_sort(const void* ids, int idt, int64_t tokens, int64_t group, int64_t experts, int32_t* offsets, int32_t* source,
+                      int32_t* slot, void* workspace, size_t workspace_bytes, void* stream);
+size_t qsync_expert_sort_workspace_bytes(int64_t entries, int64_t experts);
+
+/*
+ * qsync_expert_gather - the tokens' rows in the experts' order: y[r] = x[source[r] / group] for r < count[0].
+ * x [x_rows, ld] of dt; y out, packed [rows, cols] of the same type; rows from count on stay as they were; a source outside of x gives NaN.
+ */
+int qsync_expert_gather(const void* x, int dt, int64_t x_rows, int64_t cols, int64_t ld, const int32_t* source, int64_t group,
+                        int64_t rows, const int32_t* count, void* y, void* stream);
+
+/*
+ * qsync_expert_combine - the experts' rows back to the tokens: y[t] = sum_j weight[t,j] z[slot[t,j]], in fp32 in the order of j, rounded once.
+ * z [rows, ldz] of zdt; slot [tokens, group] (entries outside of 0 .. rows-1 take no part, whatever their weight); weight_opt [tokens, group]
+ * floats or NULL (1: the gradient of qsync_expert_gather); y out, packed [tokens, cols] of ydt.
+ */
+int qsync_expert_combine(const void* z, int zdt, int64_t rows, int64_t cols, int64_t ldz, const int32_t* slot, int64_t tokens,
+                         int64_t group, const float* weight_opt, void* y, int ydt, void* stream);
+
+/*
+ * qsync_expert_combine_bwd - gradients of qsync_expert_combine:
+ *   dz[slot[t,j]] = weight[t,j] dy[t]        dweight[t,j] = sum_c dy[t,c] z[slot[t,j],c]   (0 where the entry has no row)
+ * dy [tokens, lddy] of dydt; dz_opt out, packed [rows, cols] of dzdt, rows of no entry left as they were; dweight_opt out, [tokens, group]
+ * floats, summed in an order that depends on the sizes alone; one of the two is required; z_opt may be NULL without dweight.  Entries
+ * that name the same row leave one of their gradients in it.
+ */
+int qsync_expert_combine_bwd(const void* dy, int dydt, int64_t tokens, int64_t cols, int64_t lddy, const void* z_opt, int zdt, int64_t rows,
+                             int64_t ldz, const int32_t* slot, int64_t group, const float* weight_opt, void* dz_opt, int dzdt,
+                             float* dweight_opt, void* stream);
 
 /* hipError_t (as int) of the last failing HIP call made by this thread, 0 if none. */
 int qsync_last_hip_error(void);

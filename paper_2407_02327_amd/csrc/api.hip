@@ -1130,4 +1130,206 @@ int qsync_distill_topk(const void* logits, int ldt, int64_t rows, int64_t cols, 
                                           weight_opt, loss, dlogits_opt, ddt, workspace, static_cast<hipStream_t>(stream)));
 }
 
+// ---- token scales, experts -----------------------------------------------------------------------
+namespace {
+
+bool on_16(std::initializer_list<const void*> ps)
+{
+    for(const void* p : ps)
+        if(!aligned16(p)) return false;
+    return true;
+}
+bool ints_aligned(std::initializer_list<const void*> ps)
+{
+    for(const void* p : ps)
+        if(!elements_aligned(p, QSYNC_I32)) return false;
+    return true;
+}
+bool apart(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return !a || !b || x + static_cast<uintptr_t>(a_bytes) <= y || y + static_cast<uintptr_t>(b_bytes) <= x;
+}
+int64_t span_bytes(int64_t rows, int64_t cols, int64_t ld, int dt) { return rows > 0 ? ((rows - 1) * ld + cols) * dtype_bytes(dt) : 0; }
+int workspace_status(const void* workspace, size_t bytes, size_t needed)
+{
+    if(needed == 0) return QSYNC_OK;
+    if(!workspace || bytes < needed) return QSYNC_ERR_WORKSPACE;
+    return aligned16(workspace) ? QSYNC_OK : QSYNC_ERR_ALIGN;
+}
+// what the two quantizers share; a status, or 1: nothing to do
+int token_matrix(const void* x, int xdt, int64_t x_rows, int64_t cols, int64_t ld, const int32_t* source, int64_t group, int64_t rows, int rnd)
+{
+    if(!x) return QSYNC_ERR_NULL;
+    if(!is_row_dtype(xdt) || !is_round(rnd)) return QSYNC_ERR_BAD_ENUM;
+    if(!count_ok(rows, cols) || x_rows < 0 || ld < cols || !count_ok(x_rows, ld) || group < 1 || (!source && x_rows != rows)) return QSYNC_ERR_BAD_SHAPE;
+    if(rnd == QSYNC_ROUND_FLOOR || rows > kTokenMaxRows || x_rows > kTokenMaxRows || cols > kTokenMaxCols || group > kTokenMaxRows) return QSYNC_ERR_UNSUPPORTED;
+    if(rows == 0 || cols == 0) return 1;
+    return elements_aligned(x, xdt) && elements_aligned(source, QSYNC_I32) ? QSYNC_OK : QSYNC_ERR_ALIGN;
+}
+int token_sets(int64_t rows, int64_t sets, const int32_t* offsets)
+{
+    if(sets < 0) return QSYNC_ERR_BAD_SHAPE;
+    if(sets < 1 || sets > kMaxSets) return QSYNC_ERR_UNSUPPORTED;
+    return offsets || rows % sets == 0 ? QSYNC_OK : QSYNC_ERR_BAD_SHAPE;
+}
+int token_product(int64_t rows, int64_t N, int64_t K, int64_t sets, const int32_t* offsets, const void* a, const float* sa, const void* b, const float* sb, const float* bias,
+                  const void* c, int cdt)
+{
+    if(!a || !sa || !b || !sb || !c) return QSYNC_ERR_NULL;
+    if(!is_row_dtype(cdt)) return QSYNC_ERR_BAD_ENUM;
+    if(rows < 0 || N < 0 || K < 0) return QSYNC_ERR_BAD_SHAPE;
+    if(rows > kTokenMaxRows || N > kTokenMaxCols || K > kTokenMaxCols || sets < 1 || sets > kMaxSets || (!offsets && sets != 1)) return QSYNC_ERR_UNSUPPORTED;
+    return on_16({a, b}) && floats_aligned({sa, sb, bias}) && elements_aligned(c, cdt) && elements_aligned(offsets, QSYNC_I32) ? QSYNC_OK : QSYNC_ERR_ALIGN;
+}
+
+}  // namespace
+
+int64_t qsync_token_code_cols(int64_t cols) { return cols < 0 || cols > kTokenMaxCols ? 0 : (cols + 127) / 128 * 128; }
+int64_t qsync_token_code_rows(int64_t rows, int64_t sets, int with_offsets)
+{
+    if(rows < 0 || rows > kTokenMaxRows || sets < 1 || sets > kMaxSets || (!with_offsets && rows % sets != 0)) return 0;
+    return with_offsets ? (rows + 127) / 128 * 128 + 128 * sets : (rows / sets + 127) / 128 * 128 * sets;
+}
+
+int qsync_token_quantize(const void* x, int xdt, int64_t x_rows, int64_t cols, int64_t ld, const int32_t* source_opt, int64_t group, int64_t rows,
+                         const int32_t* count_opt, int rnd, uint64_t philox_seed, uint64_t philox_offset, float* scale, void* q, void* stream)
+{
+    if(!scale || !q) return QSYNC_ERR_NULL;
+    const int rc = token_matrix(x, xdt, x_rows, cols, ld, source_opt, group, rows, rnd);
+    if(rc != QSYNC_OK) return rc < 0 ? rc : QSYNC_OK;
+    if(!aligned16(q) || !floats_aligned({scale}) || !ints_aligned({count_opt})) return QSYNC_ERR_ALIGN;
+    const int64_t xb = span_bytes(x_rows, cols, ld, xdt);
+    if(!apart(q, rows * qsync_token_code_cols(cols), x, xb) || !apart(scale, rows * 4, x, xb)) return QSYNC_ERR_UNSUPPORTED;
+    return hip_status(launch_token_quantize(TokenMatrix{x, xdt, x_rows, cols, ld, rows, source_opt, static_cast<int>(group)}, count_opt, rnd, philox_seed,
+                                            philox_offset, scale, static_cast<int8_t*>(q), static_cast<hipStream_t>(stream)));
+}
+
+size_t qsync_token_quantize_both_workspace_bytes(int64_t rows, int64_t cols, int64_t sets, int with_offsets)
+{
+    if(rows < 1 || cols < 1 || rows > kTokenMaxRows || cols > kTokenMaxCols || sets < 1 || sets > kMaxSets) return 0;
+    return round256(token_both_workspace_bytes(rows, cols, sets, with_offsets != 0));
+}
+
+int qsync_token_quantize_both(const void* x, int xdt, int64_t x_rows, int64_t cols, int64_t ld, const int32_t* source_opt, int64_t group, int64_t rows,
+                              int64_t sets, const int32_t* offsets_opt, int rnd, uint64_t philox_seed, uint64_t philox_offset, float* row_scale, void* q,
+                              float* col_scale, void* qT, float* colsum_opt, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if(!row_scale || !q || !col_scale || !qT) return QSYNC_ERR_NULL;
+    int rc = token_matrix(x, xdt, x_rows, cols, ld, source_opt, group, rows, rnd);
+    if(rc < 0) return rc;
+    const int sc = token_sets(rows, sets, offsets_opt);
+    if(sc != QSYNC_OK) return sc;
+    if(rc == 1)
+    {   // no rows: no scale is set by any; the sums are zeros
+        return colsum_opt && cols > 0 ? hip_status(launch_zero_f32(colsum_opt, sets * cols, static_cast<hipStream_t>(stream))) : QSYNC_OK;
+    }
+    if(!on_16({q, qT}) || !floats_aligned({row_scale, col_scale, colsum_opt}) || !ints_aligned({offsets_opt})) return QSYNC_ERR_ALIGN;
+    rc = workspace_status(workspace, workspace_bytes, qsync_token_quantize_both_workspace_bytes(rows, cols, sets, offsets_opt != nullptr));
+    if(rc != QSYNC_OK) return rc;
+    const int64_t xb = span_bytes(x_rows, cols, ld, xdt);
+    if(!apart(q, rows * qsync_token_code_cols(cols), x, xb) || !apart(qT, qsync_token_code_rows(rows, sets, offsets_opt != nullptr) * cols, x, xb)) return QSYNC_ERR_UNSUPPORTED;
+    return hip_status(launch_token_quantize_both(TokenMatrix{x, xdt, x_rows, cols, ld, rows, source_opt, static_cast<int>(group)}, sets, offsets_opt, rnd, philox_seed,
+                                                 philox_offset, row_scale, static_cast<int8_t*>(q), col_scale, static_cast<int8_t*>(qT), colsum_opt, workspace,
+                                                 static_cast<hipStream_t>(stream)));
+}
+
+size_t qsync_token_linear_workspace_bytes(int64_t, int64_t, int64_t, int64_t) { return 0; }
+
+int qsync_token_linear_fwd(int64_t rows, int64_t N, int64_t K, int64_t sets, const int32_t* offsets_opt, const void* xq, const float* sx, const void* wq,
+                           const float* sw, const float* bias_opt, void* y, int ydt, void* workspace, size_t workspace_bytes, void* stream)
+{
+    int rc = token_product(rows, N, K, sets, offsets_opt, xq, sx, wq, sw, bias_opt, y, ydt);
+    if(rc != QSYNC_OK) return rc;
+    if(rows == 0 || N == 0) return QSYNC_OK;
+    rc = workspace_status(workspace, workspace_bytes, qsync_token_linear_workspace_bytes(rows, N, K, sets));
+    if(rc != QSYNC_OK) return rc;
+    if(!apart(y, rows * N * dtype_bytes(ydt), xq, rows * qsync_token_code_cols(K))) return QSYNC_ERR_UNSUPPORTED;
+    return hip_status(launch_token_product(TokenProduct{static_cast<const int8_t*>(xq), static_cast<const int8_t*>(wq), sx, sw, bias_opt, y, ydt, rows, rows, N, K, sets,
+                                                        offsets_opt}, false, static_cast<hipStream_t>(stream)));
+}
+
+size_t qsync_token_wgrad_workspace_bytes(int64_t, int64_t, int64_t, int64_t) { return 0; }
+
+int qsync_token_linear_wgrad(int64_t rows, int64_t N, int64_t K, int64_t sets, const int32_t* offsets_opt, const void* dyqT, const float* sdy, const void* xqT,
+                             const float* sx, void* dw, int dwdt, void* workspace, size_t workspace_bytes, void* stream)
+{
+    int rc = token_product(rows, N, K, sets, offsets_opt, dyqT, sdy, xqT, sx, nullptr, dw, dwdt);
+    if(rc != QSYNC_OK) return rc;
+    if(!count_ok(sets * N, K)) return QSYNC_ERR_BAD_SHAPE;
+    if(N == 0 || K == 0) return QSYNC_OK;
+    rc = workspace_status(workspace, workspace_bytes, qsync_token_wgrad_workspace_bytes(rows, N, K, sets));
+    if(rc != QSYNC_OK) return rc;
+    return hip_status(launch_token_product(TokenProduct{static_cast<const int8_t*>(dyqT), static_cast<const int8_t*>(xqT), sdy, sx, nullptr, dw, dwdt, rows, N, K, rows, sets,
+                                                        offsets_opt}, true, static_cast<hipStream_t>(stream)));
+}
+
+size_t qsync_expert_sort_workspace_bytes(int64_t entries, int64_t experts)
+{
+    if(entries < 1 || entries > kTokenMaxRows || experts < 1 || experts > kMaxSets) return 0;
+    return round256(expert_sort_workspace_bytes(entries, static_cast<int>(experts)));
+}
+
+int qsync_expert_sort(const void* ids, int idt, int64_t tokens, int64_t group, int64_t experts, int32_t* offsets, int32_t* source, int32_t* slot, void* workspace,
+                      size_t workspace_bytes, void* stream)
+{
+    if(!ids || !offsets || !source || !slot) return QSYNC_ERR_NULL;
+    if(!is_index_dtype(idt)) return QSYNC_ERR_BAD_ENUM;
+    if(tokens < 0 || group < 1 || !count_ok(tokens, group) || experts < 0) return QSYNC_ERR_BAD_SHAPE;
+    if(tokens * group > kTokenMaxRows || experts < 1 || experts > kMaxSets) return QSYNC_ERR_UNSUPPORTED;
+    if(!elements_aligned(ids, idt) || !ints_aligned({offsets, source, slot})) return QSYNC_ERR_ALIGN;
+    const int rc = workspace_status(workspace, workspace_bytes, qsync_expert_sort_workspace_bytes(tokens * group, experts));
+    if(rc != QSYNC_OK) return rc;
+    return hip_status(launch_expert_sort(ids, idt == QSYNC_I64, tokens * group, static_cast<int>(experts), offsets, source, slot, workspace, static_cast<hipStream_t>(stream)));
+}
+
+int qsync_expert_gather(const void* x, int dt, int64_t x_rows, int64_t cols, int64_t ld, const int32_t* source, int64_t group, int64_t rows, const int32_t* count,
+                        void* y, void* stream)
+{
+    if(!x || !source || !count || !y) return QSYNC_ERR_NULL;
+    if(!is_row_dtype(dt)) return QSYNC_ERR_BAD_ENUM;
+    if(!count_ok(rows, cols) || x_rows < 0 || ld < cols || !count_ok(x_rows, ld) || group < 1) return QSYNC_ERR_BAD_SHAPE;
+    if(rows > kTokenMaxRows || x_rows > kTokenMaxRows || cols > kTokenMaxCols || group > kTokenMaxRows) return QSYNC_ERR_UNSUPPORTED;
+    if(rows == 0 || cols == 0) return QSYNC_OK;
+    if(!elements_aligned(x, dt) || !elements_aligned(y, dt) || !ints_aligned({source, count})) return QSYNC_ERR_ALIGN;
+    if(!apart(y, rows * cols * dtype_bytes(dt), x, span_bytes(x_rows, cols, ld, dt))) return QSYNC_ERR_UNSUPPORTED;
+    return hip_status(launch_expert_gather(x, dt, x_rows, cols, ld, source, static_cast<int>(group), rows, count, y, static_cast<hipStream_t>(stream)));
+}
+
+int qsync_expert_combine(const void* z, int zdt, int64_t rows, int64_t cols, int64_t ldz, const int32_t* slot, int64_t tokens, int64_t group,
+                         const float* weight_opt, void* y, int ydt, void* stream)
+{
+    if(!z || !slot || !y) return QSYNC_ERR_NULL;
+    if(!is_row_dtype(zdt) || !is_row_dtype(ydt)) return QSYNC_ERR_BAD_ENUM;
+    if(!count_ok(rows, cols) || ldz < cols || !count_ok(rows, ldz) || group < 1 || !count_ok(tokens, cols) || !count_ok(tokens, group)) return QSYNC_ERR_BAD_SHAPE;
+    if(rows > kTokenMaxRows || tokens * group > kTokenMaxRows || cols > kTokenMaxCols) return QSYNC_ERR_UNSUPPORTED;
+    if(tokens == 0 || cols == 0) return QSYNC_OK;
+    if(!elements_aligned(z, zdt) || !elements_aligned(y, ydt) || !ints_aligned({slot}) || !floats_aligned({weight_opt})) return QSYNC_ERR_ALIGN;
+    if(!apart(y, tokens * cols * dtype_bytes(ydt), z, span_bytes(rows, cols, ldz, zdt))) return QSYNC_ERR_UNSUPPORTED;
+    return hip_status(launch_expert_combine(z, zdt, rows, cols, ldz, slot, tokens, static_cast<int>(group), weight_opt, y, ydt, static_cast<hipStream_t>(stream)));
+}
+
+int qsync_expert_combine_bwd(const void* dy, int dydt, int64_t tokens, int64_t cols, int64_t lddy, const void* z_opt, int zdt, int64_t rows, int64_t ldz,
+                             const int32_t* slot, int64_t group, const float* weight_opt, void* dz_opt, int dzdt, float* dweight_opt, void* stream)
+{
+    if(!dy || !slot || (!dz_opt && !dweight_opt) || (dweight_opt && !z_opt)) return QSYNC_ERR_NULL;
+    if(!is_row_dtype(dydt) || (dweight_opt && !is_row_dtype(zdt)) || (dz_opt && !is_row_dtype(dzdt))) return QSYNC_ERR_BAD_ENUM;
+    if(!count_ok(rows, cols) || (dweight_opt && (ldz < cols || !count_ok(rows, ldz))) || group < 1 || lddy < cols || !count_ok(tokens, lddy) || !count_ok(tokens, group))
+        return QSYNC_ERR_BAD_SHAPE;
+    if(rows > kTokenMaxRows || tokens * group > kTokenMaxRows || cols > kTokenMaxCols) return QSYNC_ERR_UNSUPPORTED;
+    if(tokens == 0) return QSYNC_OK;
+    if(!elements_aligned(dy, dydt) || (dweight_opt && !elements_aligned(z_opt, zdt)) || (dz_opt && !elements_aligned(dz_opt, dzdt)) || !ints_aligned({slot})
+       || !floats_aligned({weight_opt, dweight_opt}))
+        return QSYNC_ERR_ALIGN;
+    if(dz_opt)
+    {
+        const int64_t bytes = rows * cols * dtype_bytes(dzdt);
+        if(!apart(dz_opt, bytes, dy, span_bytes(tokens, cols, lddy, dydt))
+           || (dweight_opt && !apart(dz_opt, bytes, z_opt, span_bytes(rows, cols, ldz, zdt))))
+            return QSYNC_ERR_UNSUPPORTED;
+    }
+    return hip_status(launch_expert_combine_bwd(dy, dydt, tokens, cols, lddy, dweight_opt ? z_opt : nullptr, zdt, rows, ldz, slot, static_cast<int>(group), weight_opt,
+                                                dz_opt, dzdt, dweight_opt, static_cast<hipStream_t>(stream)));
+}
+
 }  // extern "C"

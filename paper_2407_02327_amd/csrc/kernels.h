@@ -143,6 +143,40 @@ hipError_t launch_distill_topk(const void* z, int zdt, int64_t rows, int64_t col
                                const void* index, bool wide, int k, const float* weight, float* loss, void* dz, int ddt, void* workspace,
                                hipStream_t st);
 
+// ---- operators with a scale for each token (token_quant.hip, token_gemm.hip), routing to experts (experts.hip) ----
+constexpr int64_t kTokenMaxRows = int64_t(1) << 23, kTokenMaxCols = int64_t(1) << 20;
+constexpr int64_t kMaxSets = 512;      // experts
+struct TokenMatrix      // rows of x (kF32, kF16, kBF16), or what `source` takes from it: row r is x's row source[r] / group
+{
+    const void*    x;
+    int            dtype;
+    int64_t        x_rows, cols, ld, rows;
+    const int32_t* source;
+    int            group;
+};
+hipError_t launch_token_quantize(const TokenMatrix& m, const int32_t* count, int rnd, uint64_t seed, uint64_t offset, float* scale, int8_t* q, hipStream_t st);
+size_t token_both_workspace_bytes(int64_t rows, int64_t cols, int64_t sets, bool offsets);
+hipError_t launch_token_quantize_both(const TokenMatrix& m, int64_t sets, const int32_t* offsets, int rnd, uint64_t seed, uint64_t offset, float* row_scale, int8_t* q,
+                                      float* col_scale, int8_t* qT, float* colsum, void* workspace, hipStream_t st);
+// Forward pass, data gradient: A [rows, code_pad(K)], B [sets][N][code_pad(K)], C [rows, N].  Weight gradient: A and B hold codes along
+// `rows` as token_quantize_both leaves them, of M and N columns; C [sets][M][N].  sa: of A's rows ([sets][M]), sb [sets][N].
+struct TokenProduct
+{
+    const int8_t * A, *B;
+    const float *  sa, *sb, *bias;
+    void*          C;
+    int            c_dtype;
+    int64_t        rows, M, N, K, sets;
+    const int32_t* offsets;
+};
+hipError_t launch_token_product(const TokenProduct& p, bool wgrad, hipStream_t st);
+hipError_t launch_expert_sort(const void* ids, bool wide, int64_t n, int experts, int32_t* offsets, int32_t* source, int32_t* slot, void* workspace, hipStream_t st);
+size_t expert_sort_workspace_bytes(int64_t n, int experts);
+hipError_t launch_expert_gather(const void* x, int dtype, int64_t x_rows, int64_t cols, int64_t ld, const int32_t* source, int group, int64_t rows, const int32_t* count, void* y, hipStream_t st);
+hipError_t launch_expert_combine(const void* z, int zdt, int64_t rows, int64_t cols, int64_t ld, const int32_t* slot, int64_t tokens, int group, const float* weight, void* y, int ydt, hipStream_t st);
+hipError_t launch_expert_combine_bwd(const void* dy, int dydt, int64_t tokens, int64_t cols, int64_t lddy, const void* z, int zdt, int64_t rows, int64_t ldz, const int32_t* slot, int group,
+                                     const float* weight, void* dz, int dzdt, float* dweight, hipStream_t st);
+
 // ---- GEMM  C[M,N] = epilogue( sum_k A[M,k] B[N,k] ) ------------------------------------
 // epilogue(acc) = float(acc) * (s0 * s1 * col_scale[n]) + col_bias[n]; absent factors are 1 / 0.
 struct GemmProblem {

@@ -1,0 +1,348 @@
+// INT8 codes with a scale for each row (token) of a matrix, for each column of each set of its rows, or both.
+//
+// Rows only (serving; the forward pass without a backward): a row stays in the registers of 64 or 256 threads between its maximum and
+// its codes, so x is read once.  Both (training): the codes along the columns contract over the rows, in the weight gradient; a first pass leaves
+// the maxima of rows and columns, a second reads x again and writes both sets of codes, the second one transposed through LDS.
+#include "device_utils.h"
+#include "row_ops.h"
+#include "token_ops.h"
+
+namespace qsync {
+
+namespace {
+
+struct TokenSource      // where the matrix's rows come from
+{
+    const void*    x;
+    int64_t        x_rows, cols, ld, rows;
+    const int32_t* source;      // row r is x's row source[r] / group; nullptr: row r
+    int            group;
+};
+// x's row of row r, or -1: there is none
+__device__ __forceinline__ int64_t source_row(const TokenSource& s, int64_t r)
+{
+    if(!s.source) return r;
+    const int32_t i = s.source[r];
+    return i >= 0 && i / s.group < s.x_rows ? i / s.group : -1;
+}
+
+template <typename T> __device__ __forceinline__ void load8(const T* row, int64_t c, int64_t cols, Row8<T>& v)
+{
+    if(c + 8 <= cols) v.load(row + c);
+    else
+    {
+        float e[8];
+#pragma unroll
+        for(int i = 0; i < 8; ++i) e[i] = c + i < cols ? row_element(row + c + i) : 0.0f;
+        v.encode(e);
+    }
+}
+// (bits of the largest magnitude: of the values as they are, NaN among them)
+template <typename T> __device__ __forceinline__ uint32_t max8(const Row8<T>& v, uint32_t m)
+{
+    float e[8];
+    v.decode(e);
+#pragma unroll
+    for(int i = 0; i < 8; ++i) m = max(m, abs_bits(e[i]));
+    return m;
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t m)
+{
+#pragma unroll
+    for(int off = 32; off >= 1; off >>= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), off)));
+    return m;
+}
+
+template <typename T, int RND, int THREADS, int V>
+__global__ __launch_bounds__(256) void token_rows_kernel(TokenSource s, const int32_t* count, uint64_t seed, uint64_t offset, float* scale, int8_t* q)
+{
+    constexpr int kRows = 256 / THREADS;
+    __shared__ uint32_t part[4];
+    const int     t = threadIdx.x % THREADS;
+    const int64_t r = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / THREADS;
+    const int64_t rows = count ? min(s.rows, static_cast<int64_t>(*count)) : s.rows;
+    if(r >= rows) return;      // (a whole workgroup, or whole wavefronts that meet no barrier)
+    const int64_t from = source_row(s, r), groups = code_pad(s.cols) / 8, per_row = (s.cols + 7) / 8;
+    const T*      row = static_cast<const T*>(s.x) + (from < 0 ? 0 : from) * s.ld;
+    const int64_t cols = from < 0 ? 0 : s.cols;
+    Row8<T>       v[V];
+    uint32_t      m = from < 0 ? 0x7FC00000u : 0u;
+#pragma unroll
+    for(int i = 0; i < V; ++i)
+    {
+        load8(row, (i * THREADS + t) * 8, cols, v[i]);
+        m = max8(v[i], m);
+    }
+    for(int64_t g = V * THREADS + t; g < groups; g += THREADS)
+    {
+        Row8<T> w;
+        load8(row, g * 8, cols, w);
+        m = max8(w, m);
+    }
+    m = wave_max(m);
+    if constexpr(THREADS > 64)
+    {
+        if(threadIdx.x % 64 == 0) part[threadIdx.x / 64] = m;
+        __syncthreads();
+        m = max(max(part[0], part[1]), max(part[2], part[3]));
+    }
+    const CodeScale cs = code_scale(m);
+    if(t == 0) scale[r] = cs.scale;
+    int8_t* out = q + r * groups * 8;
+    auto    put = [&](const Row8<T>& w, int64_t g) {
+        float e[8];
+        w.decode(e);
+        if(cs.inv == 0.0f)
+#pragma unroll
+            for(int j = 0; j < 8; ++j) e[j] = 0.0f;
+        uint4 blk = make_uint4(0, 0, 0, 0);
+        if constexpr(RND == kStochastic) blk = philox_group(seed, offset, static_cast<uint64_t>(r * per_row + g));
+        uint32_t c[2];
+        quantize_group<float, RND>(e, cs.inv, 127, blk, c);
+        *reinterpret_cast<uint2*>(out + g * 8) = make_uint2(c[0], c[1]);
+    };
+#pragma unroll
+    for(int i = 0; i < V; ++i)
+        if(i * THREADS + t < groups) put(v[i], i * THREADS + t);
+    for(int64_t g = V * THREADS + t; g < groups; g += THREADS)
+    {
+        Row8<T> w;
+        load8(row, g * 8, cols, w);
+        put(w, g);
+    }
+}
+
+template <typename T, int RND>
+hipError_t launch_rows(const TokenSource& s, const int32_t* count, uint64_t seed, uint64_t offset, float* scale, int8_t* q, hipStream_t st)
+{
+    const int64_t groups = code_pad(s.cols) / 8;
+    const dim3    few(static_cast<unsigned>((s.rows + 3) / 4)), one(static_cast<unsigned>(s.rows));
+    if(groups <= 64) token_rows_kernel<T, RND, 64, 1><<<few, 256, 0, st>>>(s, count, seed, offset, scale, q);
+    else if(groups <= 128) token_rows_kernel<T, RND, 64, 2><<<few, 256, 0, st>>>(s, count, seed, offset, scale, q);
+    else if(groups <= 256) token_rows_kernel<T, RND, 256, 1><<<one, 256, 0, st>>>(s, count, seed, offset, scale, q);
+    else if(groups <= 512) token_rows_kernel<T, RND, 256, 2><<<one, 256, 0, st>>>(s, count, seed, offset, scale, q);
+    else token_rows_kernel<T, RND, 256, 4><<<one, 256, 0, st>>>(s, count, seed, offset, scale, q);
+    return hipGetLastError();
+}
+
+// ---- rows and columns ------------------------------------------------------------------------------------------------------------
+// The rows' axis is walked in chunks of 128 positions (see set_start): a chunk lies in one set.
+struct Chunk { int64_t set, first, row0, start; int len; };      // (first: the set's first position / len: rows of the chunk, <= 0: none)
+__device__ __forceinline__ Chunk chunk_rows(const int32_t* offsets, int64_t rows, int64_t sets, int64_t chunk)
+{
+    const int64_t p = chunk * kCodePad;
+    int64_t       lo = 0, hi = sets - 1;      // the last set that starts at or before p
+    while(lo < hi)
+    {
+        const int64_t mid = (lo + hi + 1) / 2;
+        if(set_start(offsets, set_rows(offsets, rows, sets, mid), mid) <= p) lo = mid;
+        else hi = mid - 1;
+    }
+    const SetRows s = set_rows(offsets, rows, sets, lo);
+    const int64_t start = set_start(offsets, s, lo), left = s.len - (p - start);
+    return {lo, start, s.first + (p - start), p - start, static_cast<int>(p < start || left < 0 ? 0 : left > kCodePad ? kCodePad : left)};
+}
+
+constexpr int kStatCols = 512;      // columns of a workgroup of the first pass: eight a lane
+// rowpart [column tiles][rows], colpart [chunks][2 or 1][cols]: maxima, sums
+template <typename T, bool SUM>
+__global__ __launch_bounds__(256) void token_stats_kernel(TokenSource s, const int32_t* offsets, int64_t sets, uint32_t* rowpart, uint32_t* colmax, float* colsum)
+{
+    __shared__ uint32_t lmax[4][kStatCols];
+    __shared__ float    lsum[SUM ? 4 : 1][SUM ? kStatCols : 1];
+    const int     lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const Chunk   c    = chunk_rows(offsets, s.rows, sets, blockIdx.x);
+    if(c.len <= 0) return;
+    const int64_t col = static_cast<int64_t>(blockIdx.y) * kStatCols + lane * 8;
+    uint32_t      m[8];
+    float         sum[8];
+#pragma unroll
+    for(int i = 0; i < 8; ++i) { m[i] = 0u; sum[i] = 0.0f; }
+    for(int i = wave * 32; i < min(c.len, wave * 32 + 32); ++i)
+    {
+        const int64_t r = c.row0 + i, from = source_row(s, r);
+        Row8<T>       v;
+        float         e[8];
+        load8(static_cast<const T*>(s.x) + (from < 0 ? 0 : from) * s.ld, col, from < 0 ? 0 : s.cols, v);
+        v.decode(e);
+        uint32_t rm = from < 0 ? 0x7FC00000u : 0u;
+#pragma unroll
+        for(int j = 0; j < 8; ++j)
+        {
+            const uint32_t a = from < 0 ? 0x7FC00000u : abs_bits(e[j]);
+            m[j] = max(m[j], a);
+            rm   = max(rm, a);
+            if constexpr(SUM) sum[j] += from < 0 ? __uint_as_float(0x7FC00000u) : e[j];
+        }
+        rm = wave_max(rm);
+        if(lane == 0) rowpart[blockIdx.y * s.rows + r] = rm;
+    }
+#pragma unroll
+    for(int j = 0; j < 8; ++j)
+    {
+        lmax[wave][lane * 8 + j] = m[j];
+        if constexpr(SUM) lsum[wave][lane * 8 + j] = sum[j];
+    }
+    __syncthreads();
+    for(int i = threadIdx.x; i < kStatCols; i += 256)
+    {
+        const int64_t at = static_cast<int64_t>(blockIdx.y) * kStatCols + i;
+        if(at >= s.cols) continue;
+        colmax[blockIdx.x * s.cols + at] = max(max(lmax[0][i], lmax[1][i]), max(lmax[2][i], lmax[3][i]));
+        if constexpr(SUM) colsum[blockIdx.x * s.cols + at] = (lsum[0][i] + lsum[1][i]) + (lsum[2][i] + lsum[3][i]);
+    }
+}
+
+// Scales and inverse scales of the rows (workgroups behind `col_blocks`) and of the sets' columns; a set's chunks in order.
+__global__ __launch_bounds__(256) void token_scales_kernel(const int32_t* offsets, int64_t rows, int64_t cols, int64_t sets, int64_t col_blocks, int col_tiles, const uint32_t* rowpart,
+                                                           const uint32_t* colmax, const float* colsum, float* row_scale, float* row_inv, float* col_scale, float* col_inv, float* sum_out)
+{
+    if(blockIdx.x >= col_blocks)
+    {
+        const int64_t r = (static_cast<int64_t>(blockIdx.x) - col_blocks) * 256 + threadIdx.x;
+        if(r >= rows || (offsets && r >= offsets[sets])) return;
+        uint32_t m = 0u;
+        for(int t = 0; t < col_tiles; ++t) m = max(m, rowpart[t * rows + r]);
+        const CodeScale cs = code_scale(m);
+        row_scale[r] = cs.scale;
+        row_inv[r]   = cs.inv;
+        return;
+    }
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    if(i >= sets * cols) return;
+    const int64_t e = i / cols, c = i % cols;
+    const SetRows s = set_rows(offsets, rows, sets, e);
+    const int64_t first = set_start(offsets, s, e) / kCodePad, n = code_pad(s.len) / kCodePad;
+    uint32_t      m = 0u;
+    float         sum = 0.0f;
+    for(int64_t k = first; k < first + n; ++k)
+    {
+        m = max(m, colmax[k * cols + c]);
+        if(colsum) sum += colsum[k * cols + c];
+    }
+    const CodeScale cs = code_scale(m);
+    col_scale[i] = cs.scale;
+    col_inv[i]   = cs.inv;
+    if(sum_out) sum_out[i] = sum;
+}
+
+// 128 positions x 64 columns a workgroup: a thread has four rows of eight columns, whose codes along the columns leave as words of four rows.
+template <typename T, int RND>
+__global__ __launch_bounds__(256) void token_codes_kernel(TokenSource s, const int32_t* offsets, int64_t sets, uint64_t seed, uint64_t offset, const float* row_inv,
+                                                          const float* col_inv, int8_t* q, int8_t* qT)
+{
+    __shared__ uint32_t lds[64 * 33];
+    const Chunk   c = chunk_rows(offsets, s.rows, sets, blockIdx.x);
+    if(c.len <= 0) return;
+    const int     cg = threadIdx.x % 8, rq = threadIdx.x / 8;
+    const int64_t col0 = static_cast<int64_t>(blockIdx.y) * 64, col = col0 + cg * 8, per_row = (s.cols + 7) / 8, qcols = code_pad(s.cols);
+    float         ci[8];
+#pragma unroll
+    for(int j = 0; j < 8; ++j) ci[j] = col + j < s.cols ? col_inv[c.set * s.cols + col + j] : 0.0f;
+    uint32_t w[8];
+#pragma unroll
+    for(int j = 0; j < 8; ++j) w[j] = 0u;
+#pragma unroll
+    for(int i = 0; i < 4; ++i)
+    {
+        if(rq * 4 + i >= c.len) break;
+        const int64_t r = c.row0 + rq * 4 + i, from = source_row(s, r);
+        Row8<T>       v;
+        float         e[8];
+        load8(static_cast<const T*>(s.x) + (from < 0 ? 0 : from) * s.ld, col, from < 0 ? 0 : s.cols, v);
+        v.decode(e);
+        uint4 blk = make_uint4(0, 0, 0, 0);
+        if constexpr(RND == kStochastic) blk = philox_group(seed, offset, static_cast<uint64_t>(r * per_row + col / 8));
+        uint32_t    b[2];
+        const float ri = row_inv[r];
+        float       er[8];
+#pragma unroll
+        for(int j = 0; j < 8; ++j)
+        {
+            er[j] = ri == 0.0f ? 0.0f : e[j];
+            e[j]  = ci[j] == 0.0f ? 0.0f : e[j];
+        }
+        quantize_group<float, RND>(er, ri, 127, blk, b);
+        *reinterpret_cast<uint2*>(q + r * qcols + col) = make_uint2(b[0], b[1]);
+#pragma unroll
+        for(int j = 0; j < 8; ++j)
+            w[j] |= (static_cast<uint32_t>(quantize_code<RND>(e[j], ci[j], 127, philox_draw16(blk, j))) & 0xFFu) << (8 * i);
+    }
+#pragma unroll
+    for(int j = 0; j < 8; ++j) lds[(cg * 8 + j) * 33 + rq] = w[j];
+    __syncthreads();
+    const SetRows set = set_rows(offsets, s.rows, sets, c.set);
+    const int64_t ldt = code_pad(set.len);
+    int8_t*       out = qT + c.first * s.cols + c.start;
+#pragma unroll
+    for(int k = 0; k < 2; ++k)
+    {
+        const int  i = threadIdx.x + k * 256, cc = i / 8, seg = i % 8;
+        const uint32_t* at = lds + cc * 33 + seg * 4;
+        if(col0 + cc < s.cols) *reinterpret_cast<uint4*>(out + (col0 + cc) * ldt + seg * 16) = make_uint4(at[0], at[1], at[2], at[3]);
+    }
+}
+
+struct BothWorkspace { size_t rowpart, row_inv, col_inv, colmax, colsum, total; };
+BothWorkspace both_workspace(int64_t rows, int64_t cols, int64_t sets, bool offsets)
+{
+    auto         up = [](size_t n) { return (n + 255) / 256 * 256; };
+    const size_t chunks = static_cast<size_t>(code_positions(rows, sets, offsets) / kCodePad), tiles = static_cast<size_t>((cols + kStatCols - 1) / kStatCols);
+    BothWorkspace w;
+    w.rowpart = 0;
+    w.row_inv = w.rowpart + up(tiles * rows * 4);
+    w.col_inv = w.row_inv + up(static_cast<size_t>(rows) * 4);
+    w.colmax  = w.col_inv + up(static_cast<size_t>(sets) * cols * 4);
+    w.colsum  = w.colmax + up(chunks * cols * 4);
+    w.total   = w.colsum + up(chunks * cols * 4);
+    return w;
+}
+
+template <typename T, int RND>
+hipError_t launch_both(const TokenSource& s, int64_t sets, const int32_t* offsets, uint64_t seed, uint64_t offset, float* row_scale, int8_t* q, float* col_scale, int8_t* qT,
+                       float* colsum, void* workspace, hipStream_t st)
+{
+    const BothWorkspace w = both_workspace(s.rows, s.cols, sets, offsets != nullptr);
+    uint8_t* const      base = static_cast<uint8_t*>(workspace);
+    uint32_t*           rowpart = reinterpret_cast<uint32_t*>(base + w.rowpart);
+    uint32_t*           cm = reinterpret_cast<uint32_t*>(base + w.colmax);
+    float *             ri = reinterpret_cast<float*>(base + w.row_inv), *ci = reinterpret_cast<float*>(base + w.col_inv), *sm = reinterpret_cast<float*>(base + w.colsum);
+    const unsigned      chunks = static_cast<unsigned>(code_positions(s.rows, sets, offsets != nullptr) / kCodePad);
+    const unsigned      tiles = static_cast<unsigned>((s.cols + kStatCols - 1) / kStatCols);
+    if(colsum) token_stats_kernel<T, true><<<dim3(chunks, tiles), 256, 0, st>>>(s, offsets, sets, rowpart, cm, sm);
+    else       token_stats_kernel<T, false><<<dim3(chunks, tiles), 256, 0, st>>>(s, offsets, sets, rowpart, cm, sm);
+    const int64_t col_blocks = (sets * s.cols + 255) / 256;
+    token_scales_kernel<<<static_cast<unsigned>(col_blocks + (s.rows + 255) / 256), 256, 0, st>>>(offsets, s.rows, s.cols, sets, col_blocks, static_cast<int>(tiles), rowpart, cm,
+                                                                                                colsum ? sm : nullptr, row_scale, ri, col_scale, ci, colsum);
+    token_codes_kernel<T, RND><<<dim3(chunks, static_cast<unsigned>(code_pad(s.cols) / 64)), 256, 0, st>>>(s, offsets, sets, seed, offset, ri, ci, q, qT);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t token_both_workspace_bytes(int64_t rows, int64_t cols, int64_t sets, bool offsets) { return both_workspace(rows, cols, sets, offsets).total; }
+
+hipError_t launch_token_quantize(const TokenMatrix& m, const int32_t* count, int rnd, uint64_t seed, uint64_t offset, float* scale, int8_t* q, hipStream_t st)
+{
+    const TokenSource s{m.x, m.x_rows, m.cols, m.ld, m.rows, m.source, m.group};
+    auto typed = [&](auto tag) {
+        typedef decltype(tag) T;
+        if(rnd == kStochastic) return launch_rows<T, kStochastic>(s, count, seed, offset, scale, q, st);
+        return launch_rows<T, kNearest>(s, count, seed, offset, scale, q, st);
+    };
+    return m.dtype == kF16 ? typed(_Float16{}) : m.dtype == kBF16 ? typed(__bf16{}) : typed(float{});
+}
+
+hipError_t launch_token_quantize_both(const TokenMatrix& m, int64_t sets, const int32_t* offsets, int rnd, uint64_t seed, uint64_t offset, float* row_scale, int8_t* q,
+                                      float* col_scale, int8_t* qT, float* colsum, void* workspace, hipStream_t st)
+{
+    const TokenSource s{m.x, m.x_rows, m.cols, m.ld, m.rows, m.source, m.group};
+    auto typed = [&](auto tag) {
+        typedef decltype(tag) T;
+        if(rnd == kStochastic) return launch_both<T, kStochastic>(s, sets, offsets, seed, offset, row_scale, q, col_scale, qT, colsum, workspace, st);
+        return launch_both<T, kNearest>(s, sets, offsets, seed, offset, row_scale, q, col_scale, qT, colsum, workspace, st);
+    };
+    return m.dtype == kF16 ? typed(_Float16{}) : m.dtype == kBF16 ? typed(__bf16{}) : typed(float{});
+}
+
+}  // namespace qsync

@@ -85,6 +85,21 @@ SIGNATURES = {
     "qsync_token_logprobs_bwd": (_i, [_vp, _i, _i64, _i64, _i64, _f, _vp, _i, _vp, _vp, _vp, _vp, _vp, _i, _vp]),
     "qsync_distill_topk": (_i, [_vp, _i, _i64, _i64, _i64, _f, _vp, _i, _vp, _i, _i64, _vp, _vp, _vp, _i, _vp, _sz, _vp]),
     "qsync_distill_topk_workspace_bytes": (_sz, [_i, _i64, _i64]),
+    "qsync_token_code_cols": (_i64, [_i64]),
+    "qsync_token_code_rows": (_i64, [_i64, _i64, _i]),
+    "qsync_token_quantize": (_i, [_vp, _i, _i64, _i64, _i64, _vp, _i64, _i64, _vp, _i, _u64, _u64, _vp, _vp, _vp]),
+    "qsync_token_quantize_both": (_i, [_vp, _i, _i64, _i64, _i64, _vp, _i64, _i64, _i64, _vp, _i, _u64, _u64, _vp, _vp, _vp, _vp, _vp, _vp, _sz,
+                                       _vp]),
+    "qsync_token_quantize_both_workspace_bytes": (_sz, [_i64, _i64, _i64, _i]),
+    "qsync_token_linear_fwd": (_i, [_i64, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _vp, _sz, _vp]),
+    "qsync_token_linear_workspace_bytes": (_sz, [_i64, _i64, _i64, _i64]),
+    "qsync_token_linear_wgrad": (_i, [_i64, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _i, _vp, _sz, _vp]),
+    "qsync_token_wgrad_workspace_bytes": (_sz, [_i64, _i64, _i64, _i64]),
+    "qsync_expert_sort": (_i, [_vp, _i, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "qsync_expert_sort_workspace_bytes": (_sz, [_i64, _i64]),
+    "qsync_expert_gather": (_i, [_vp, _i, _i64, _i64, _i64, _vp, _i64, _i64, _vp, _vp, _vp]),
+    "qsync_expert_combine": (_i, [_vp, _i, _i64, _i64, _i64, _vp, _i64, _i64, _vp, _vp, _i, _vp]),
+    "qsync_expert_combine_bwd": (_i, [_vp, _i, _i64, _i64, _i64, _vp, _i, _i64, _i64, _vp, _i64, _vp, _vp, _i, _vp, _vp]),
     "qsync_last_hip_error": (_i, []),
     "qsync_strerror": (ctypes.c_char_p, [_i]),
     "qsync_version": (_i, []),
@@ -352,6 +367,65 @@ def qsync_distill_topk_workspace_bytes(logits_dtype_code: int, rows: int, cols: 
 def qsync_distill_topk(logits, rows, cols, ld, scale, teacher, index, k, weight_opt, loss, dlogits_opt, workspace, stream=None) -> None:
     _native.qsync_distill_topk(logits, logits, rows, cols, ld, scale, teacher, teacher, index, index, k, weight_opt, loss, dlogits_opt,
                                _or_f32(dlogits_opt), workspace, workspace, stream)
+
+
+def qsync_token_code_cols(cols: int) -> int:
+    return lib.qsync_token_code_cols(cols)
+
+
+def qsync_token_code_rows(rows: int, sets: int, with_offsets: bool) -> int:
+    return lib.qsync_token_code_rows(rows, sets, int(with_offsets))
+
+
+def qsync_token_quantize(x, x_rows, cols, ld, source_opt, group, rows, count_opt, rnd, seed, offset, scale, q, stream=None) -> None:
+    _native.qsync_token_quantize(x, x, x_rows, cols, ld, source_opt, group, rows, count_opt, rnd, seed, offset, scale, q, stream)
+
+
+def qsync_token_quantize_both_workspace_bytes(rows: int, cols: int, sets: int, with_offsets: bool) -> int:
+    return lib.qsync_token_quantize_both_workspace_bytes(rows, cols, sets, int(with_offsets))
+
+
+def qsync_token_quantize_both(x, x_rows, cols, ld, source_opt, group, rows, sets, offsets_opt, rnd, seed, offset, row_scale, q, col_scale, qT,
+                              colsum_opt, workspace, stream=None) -> None:
+    _native.qsync_token_quantize_both(x, x, x_rows, cols, ld, source_opt, group, rows, sets, offsets_opt, rnd, seed, offset, row_scale, q,
+                                      col_scale, qT, colsum_opt, workspace, workspace, stream)
+
+
+def qsync_token_linear_workspace_bytes(rows: int, N: int, K: int, sets: int) -> int:
+    return lib.qsync_token_linear_workspace_bytes(rows, N, K, sets)
+
+
+def qsync_token_linear_fwd(rows, N, K, sets, offsets_opt, xq, sx, wq, sw, bias_opt, y, workspace, stream=None) -> None:
+    _native.qsync_token_linear_fwd(rows, N, K, sets, offsets_opt, xq, sx, wq, sw, bias_opt, y, y, workspace, workspace, stream)
+
+
+def qsync_token_wgrad_workspace_bytes(rows: int, N: int, K: int, sets: int) -> int:
+    return lib.qsync_token_wgrad_workspace_bytes(rows, N, K, sets)
+
+
+def qsync_token_linear_wgrad(rows, N, K, sets, offsets_opt, dyqT, sdy, xqT, sx, dw, workspace, stream=None) -> None:
+    _native.qsync_token_linear_wgrad(rows, N, K, sets, offsets_opt, dyqT, sdy, xqT, sx, dw, dw, workspace, workspace, stream)
+
+
+def qsync_expert_sort_workspace_bytes(entries: int, experts: int) -> int:
+    return lib.qsync_expert_sort_workspace_bytes(entries, experts)
+
+
+def qsync_expert_sort(ids, tokens, group, experts, offsets, source, slot, workspace, stream=None) -> None:
+    _native.qsync_expert_sort(ids, ids, tokens, group, experts, offsets, source, slot, workspace, workspace, stream)
+
+
+def qsync_expert_gather(x, x_rows, cols, ld, source, group, rows, count, y, stream=None) -> None:
+    _native.qsync_expert_gather(x, x, x_rows, cols, ld, source, group, rows, count, y, stream)
+
+
+def qsync_expert_combine(z, rows, cols, ldz, slot, tokens, group, weight_opt, y, stream=None) -> None:
+    _native.qsync_expert_combine(z, z, rows, cols, ldz, slot, tokens, group, weight_opt, y, y, stream)
+
+
+def qsync_expert_combine_bwd(dy, tokens, cols, lddy, z_opt, rows, ldz, slot, group, weight_opt, dz_opt, dweight_opt, stream=None) -> None:
+    _native.qsync_expert_combine_bwd(dy, dy, tokens, cols, lddy, z_opt, _or_f32(z_opt), rows, ldz, slot, group, weight_opt, dz_opt,
+                                     _or_f32(dz_opt), dweight_opt, stream)
 
 
 class TensorStatsC(ctypes.Structure):
