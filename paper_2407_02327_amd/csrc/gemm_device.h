@@ -99,7 +99,11 @@ struct GemmKernelArgs
     int8_t*        codes;
     const float*   code_inv;
     int            code_qmax;
+    // scales of the rows (store_tile's TOKEN form); c_is_f16 is 2 there for bfloat16
+    const float*   row_scale;
 };
+// LDS behind the stages: column scales and biases [2][BN], maximum slots; the rows' scales [BM] of the TOKEN form behind them
+template <int BN> constexpr int kColumnBytes = 2 * BN * 4 + 64;
 
 // A 64-bit value that is the same in every lane, as a pair of scalar registers.
 __device__ __forceinline__ int64_t uniform64(int64_t v)
@@ -328,7 +332,8 @@ __device__ __forceinline__ void lds_write_b32(uint32_t addr, uint32_t v) { asm v
 // C^T fragments: lane -> output row m = lane%R of the fragment (R = 16 or 32 rows); register v -> output column n = 8*(v/4) +
 // 4*(lane/R) + v%4, i.e. four consecutive columns per register quad (one quad for 16 rows).  `lds`: STG_BYTES per wavefront that nobody reads any more behind the
 // first barrier here; `colp`: column scales and biases [2][BN], maximum slots behind them.
-template <typename TR, int BM, int BN, int WGM, int WGN, int STG_BYTES, bool SPLIT>
+// TOKEN: every row has a scale, y = acc * (row * column scale) + bias, in fp32, binary16 or bfloat16.
+template <typename TR, int BM, int BN, int WGM, int WGN, int STG_BYTES, bool SPLIT, bool TOKEN = false>
 __device__ __forceinline__ void store_tile(const GemmKernelArgs& p, typename TR::accv_t (&acc)[BM / WGM / TR::kRows][BN / WGN / TR::kRows], uint8_t* lds,
                                            float* colp, int64_t m0, int64_t n0, int split, float alpha, float code_inv, uint32_t amax_seen)
 {
@@ -345,6 +350,7 @@ __device__ __forceinline__ void store_tile(const GemmKernelArgs& p, typename TR:
     // longer) row segments.  RAW writes the accumulators themselves (split-K partials); otherwise
     // they are dequantized in registers first.
     uint8_t*      stg       = lds + wave * STG_BYTES;
+    [[maybe_unused]] const float* rowp = reinterpret_cast<const float*>(reinterpret_cast<uint8_t*>(colp) + kColumnBytes<BN>) + wm * WTM + frag_row;
     uint32_t out_run = 0u;     // running maximum of |C| of this lane (packed like the output type)
     // one atomic maximum per workgroup at most: lanes -> wavefront (shuffles) -> workgroup (LDS slots behind the
     // column parameters).  Atomics on one word retire about 10 ns apart, so a workgroup skips its own when the
@@ -425,8 +431,21 @@ __device__ __forceinline__ void store_tile(const GemmKernelArgs& p, typename TR:
                         {
                             const float a0 = static_cast<float>(a[vq * 4]), a1 = static_cast<float>(a[vq * 4 + 1]);
                             const float a2 = static_cast<float>(a[vq * 4 + 2]), a3 = static_cast<float>(a[vq * 4 + 3]);
-                            const float4 f = fs[vq], b = bs[vq];
-                            if constexpr(OS == 2)
+                            float4       f = fs[vq];
+                            const float4 b = bs[vq];
+                            if constexpr(TOKEN)
+                            {
+                                const float rs = p.row_scale ? rowp[(pass * FPP + ii) * R] : 1.0f;
+                                f = make_float4(rs * f.x, rs * f.y, rs * f.z, rs * f.w);
+                            }
+                            if constexpr(std::is_same<out_t, __bf16>::value)
+                            {
+                                typedef __bf16 bf2_t __attribute__((ext_vector_type(2)));
+                                const bf2_t lo = {static_cast<__bf16>(fmaf(a0, f.x, b.x)), static_cast<__bf16>(fmaf(a1, f.y, b.y))};
+                                const bf2_t hi = {static_cast<__bf16>(fmaf(a2, f.z, b.z)), static_cast<__bf16>(fmaf(a3, f.w, b.w))};
+                                *reinterpret_cast<uint2*>(dst) = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
+                            }
+                            else if constexpr(OS == 2)
                                 *reinterpret_cast<uint2*>(dst) = make_uint2(fma_out_half2(a0, f.x, b.x, a1, f.y, b.y),
                                                                             fma_out_half2(a2, f.z, b.z, a3, f.w, b.w));
                             else
@@ -528,6 +547,13 @@ __device__ __forceinline__ void store_tile(const GemmKernelArgs& p, typename TR:
     }
     if constexpr(std::is_same<acc_t, int32_t>::value)
         if(p.acc_dump) staged_store(acc_t{}, std::true_type{}, reinterpret_cast<uint8_t*>(p.acc_dump));
+    if constexpr(TOKEN)
+    {
+        if(p.c_is_f16 == 1) staged_store(__half{}, std::false_type{}, static_cast<uint8_t*>(p.C));
+        else if(p.c_is_f16 == 2) staged_store(__bf16{}, std::false_type{}, static_cast<uint8_t*>(p.C));
+        else staged_store(float{}, std::false_type{}, static_cast<uint8_t*>(p.C));
+        return;
+    }
     if(p.c_is_f16)
     {
         staged_store(__half{}, std::false_type{}, static_cast<uint8_t*>(p.C));
