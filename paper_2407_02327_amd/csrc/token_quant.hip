@@ -7,6 +7,8 @@
 #include "row_ops.h"
 #include "token_ops.h"
 
+#include <type_traits>
+
 namespace qsync {
 
 namespace {
@@ -143,57 +145,89 @@ __device__ __forceinline__ Chunk chunk_rows(const int32_t* offsets, int64_t rows
     return {lo, start, s.first + (p - start), p - start, static_cast<int>(p < start || left < 0 ? 0 : left > kCodePad ? kCodePad : left)};
 }
 
-constexpr int kStatCols = 512;      // columns of a workgroup of the first pass: eight a lane
-// rowpart [column tiles][rows], colpart [chunks][2 or 1][cols]: maxima, sums
+// First pass: maxima of 128 columns (eight a lane) over a chunk and of the chunk's rows over those columns.  Sixteen lanes stand side by side, so
+// a workgroup has sixteen rows at a time and, with all eight of a lane's loads requested before the first is used, 32 to 64 KB in flight.
+// With 512 columns, a row a wavefront and one load in flight a chunk took 30 us whatever its size.
+// rowpart [column tiles][rows], colpart [chunks][cols]: maxima, sums
+constexpr int kStatCols = 128;
+__device__ __forceinline__ uint32_t max_of_16(uint32_t v)
+{
+    auto step = [&](auto ctrl) { v = max(v, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), decltype(ctrl)::value, 0xF, 0xF, false))); };
+    step(std::integral_constant<int, kRotate + 8>{});
+    step(std::integral_constant<int, kRotate + 4>{});
+    step(std::integral_constant<int, kRotate + 2>{});
+    step(std::integral_constant<int, kRotate + 1>{});
+    return v;
+}
 template <typename T, bool SUM>
 __global__ __launch_bounds__(256) void token_stats_kernel(TokenSource s, const int32_t* offsets, int64_t sets, uint32_t* rowpart, uint32_t* colmax, float* colsum)
 {
     __shared__ uint32_t lmax[4][kStatCols];
     __shared__ float    lsum[SUM ? 4 : 1][SUM ? kStatCols : 1];
-    const int     lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int     lane = threadIdx.x % 64, wave = threadIdx.x / 64, side = threadIdx.x % 16, down = threadIdx.x / 16;
     const Chunk   c    = chunk_rows(offsets, s.rows, sets, blockIdx.x);
     if(c.len <= 0) return;
-    const int64_t col = static_cast<int64_t>(blockIdx.y) * kStatCols + lane * 8;
-    uint32_t      m[8];
-    float         sum[8];
+    const int64_t col = static_cast<int64_t>(blockIdx.y) * kStatCols + side * 8;
+    constexpr int N = kCodePad / 16;
+    Row8<T>       v[N];
+    bool          there[N];
 #pragma unroll
-    for(int i = 0; i < 8; ++i) { m[i] = 0u; sum[i] = 0.0f; }
-    for(int i = wave * 32; i < min(c.len, wave * 32 + 32); ++i)
+    for(int i = 0; i < N; ++i)
     {
-        const int64_t r = c.row0 + i, from = source_row(s, r);
-        Row8<T>       v;
-        float         e[8];
-        load8(static_cast<const T*>(s.x) + (from < 0 ? 0 : from) * s.ld, col, from < 0 ? 0 : s.cols, v);
-        v.decode(e);
-        uint32_t rm = from < 0 ? 0x7FC00000u : 0u;
+        const int64_t from = down + i * 16 < c.len ? source_row(s, c.row0 + down + i * 16) : 0;
+        there[i] = from >= 0;
+        load8(static_cast<const T*>(s.x) + (from < 0 ? 0 : from) * s.ld, col, from < 0 || down + i * 16 >= c.len ? 0 : s.cols, v[i]);
+    }
+    uint32_t m[8];
+    float    sum[8];
+#pragma unroll
+    for(int j = 0; j < 8; ++j) { m[j] = 0u; sum[j] = 0.0f; }
+#pragma unroll
+    for(int i = 0; i < N; ++i)
+    {
+        float e[8];
+        v[i].decode(e);
+        uint32_t rm = 0u;
+        if(!there[i])
+#pragma unroll
+            for(int j = 0; j < 8; ++j) e[j] = __uint_as_float(0x7FC00000u);
 #pragma unroll
         for(int j = 0; j < 8; ++j)
         {
-            const uint32_t a = from < 0 ? 0x7FC00000u : abs_bits(e[j]);
+            const uint32_t a = abs_bits(e[j]);
             m[j] = max(m[j], a);
             rm   = max(rm, a);
-            if constexpr(SUM) sum[j] += from < 0 ? __uint_as_float(0x7FC00000u) : e[j];
+            if constexpr(SUM) sum[j] += e[j];
         }
-        rm = wave_max(rm);
-        if(lane == 0) rowpart[blockIdx.y * s.rows + r] = rm;
+        rm = max_of_16(rm);
+        if(side == 0 && down + i * 16 < c.len) rowpart[blockIdx.y * s.rows + c.row0 + down + i * 16] = rm;
     }
 #pragma unroll
     for(int j = 0; j < 8; ++j)
     {
-        lmax[wave][lane * 8 + j] = m[j];
-        if constexpr(SUM) lsum[wave][lane * 8 + j] = sum[j];
+#pragma unroll
+        for(int off = 16; off < 64; off <<= 1)
+        {
+            m[j] = max(m[j], static_cast<uint32_t>(__shfl_xor(static_cast<int>(m[j]), off)));
+            if constexpr(SUM) sum[j] += __shfl_xor(sum[j], off);
+        }
+        if(lane < 16)
+        {
+            lmax[wave][lane * 8 + j] = m[j];
+            if constexpr(SUM) lsum[wave][lane * 8 + j] = sum[j];
+        }
     }
     __syncthreads();
-    for(int i = threadIdx.x; i < kStatCols; i += 256)
-    {
-        const int64_t at = static_cast<int64_t>(blockIdx.y) * kStatCols + i;
-        if(at >= s.cols) continue;
-        colmax[blockIdx.x * s.cols + at] = max(max(lmax[0][i], lmax[1][i]), max(lmax[2][i], lmax[3][i]));
-        if constexpr(SUM) colsum[blockIdx.x * s.cols + at] = (lsum[0][i] + lsum[1][i]) + (lsum[2][i] + lsum[3][i]);
-    }
+    const int     i  = threadIdx.x;
+    const int64_t at = static_cast<int64_t>(blockIdx.y) * kStatCols + i;
+    if(i >= kStatCols || at >= s.cols) return;
+    colmax[blockIdx.x * s.cols + at] = max(max(lmax[0][i], lmax[1][i]), max(lmax[2][i], lmax[3][i]));
+    if constexpr(SUM) colsum[blockIdx.x * s.cols + at] = (lsum[0][i] + lsum[1][i]) + (lsum[2][i] + lsum[3][i]);
 }
 
-// Scales and inverse scales of the rows (workgroups behind `col_blocks`) and of the sets' columns; a set's chunks in order.
+// Scales and inverse scales of the rows (workgroups behind `col_blocks`) and of the sets' columns: sixteen threads fold a column's chunks,
+// every sixteenth each, then their results in order (one thread a column took 35 us for 128 chunks).
+template <bool SUM>
 __global__ __launch_bounds__(256) void token_scales_kernel(const int32_t* offsets, int64_t rows, int64_t cols, int64_t sets, int64_t col_blocks, int col_tiles, const uint32_t* rowpart,
                                                            const uint32_t* colmax, const float* colsum, float* row_scale, float* row_inv, float* col_scale, float* col_inv, float* sum_out)
 {
@@ -202,28 +236,59 @@ __global__ __launch_bounds__(256) void token_scales_kernel(const int32_t* offset
         const int64_t r = (static_cast<int64_t>(blockIdx.x) - col_blocks) * 256 + threadIdx.x;
         if(r >= rows || (offsets && r >= offsets[sets])) return;
         uint32_t m = 0u;
-        for(int t = 0; t < col_tiles; ++t) m = max(m, rowpart[t * rows + r]);
+        for(int t0 = 0; t0 < col_tiles; t0 += 8)
+        {
+            uint32_t o[8];
+#pragma unroll
+            for(int u = 0; u < 8; ++u) o[u] = rowpart[(t0 + u < col_tiles ? t0 + u : 0) * rows + r];
+#pragma unroll
+            for(int u = 0; u < 8; ++u) m = max(m, o[u]);
+        }
         const CodeScale cs = code_scale(m);
         row_scale[r] = cs.scale;
         row_inv[r]   = cs.inv;
         return;
     }
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    if(i >= sets * cols) return;
-    const int64_t e = i / cols, c = i % cols;
+    __shared__ uint32_t lmax[16][16];
+    __shared__ float    lsum[16][16];
+    const int     side = threadIdx.x % 16, part = threadIdx.x / 16;
+    const int64_t tiles = (cols + 15) / 16, e = blockIdx.x / tiles, c = blockIdx.x % tiles * 16 + side, cc = c < cols ? c : cols - 1;
     const SetRows s = set_rows(offsets, rows, sets, e);
-    const int64_t first = set_start(offsets, s, e) / kCodePad, n = code_pad(s.len) / kCodePad;
+    const int64_t first = set_start(offsets, s, e) / kCodePad, end = first + code_pad(s.len) / kCodePad;
     uint32_t      m = 0u;
     float         sum = 0.0f;
-    for(int64_t k = first; k < first + n; ++k)
+    for(int64_t k0 = first + part; k0 < end; k0 += 64)
     {
-        m = max(m, colmax[k * cols + c]);
-        if(colsum) sum += colsum[k * cols + c];
+        uint32_t o[4];
+        float    f[4];
+#pragma unroll
+        for(int u = 0; u < 4; ++u)
+        {
+            const int64_t k = k0 + u * 16 < end ? k0 + u * 16 : k0;
+            o[u] = colmax[k * cols + cc];
+            if constexpr(SUM) f[u] = colsum[k * cols + cc];
+        }
+#pragma unroll
+        for(int u = 0; u < 4; ++u)
+        {
+            m = max(m, o[u]);
+            if constexpr(SUM) sum += k0 + u * 16 < end ? f[u] : 0.0f;
+        }
+    }
+    lmax[part][side] = m;
+    if constexpr(SUM) lsum[part][side] = sum;
+    __syncthreads();
+    if(part != 0 || c >= cols) return;
+#pragma unroll
+    for(int i = 1; i < 16; ++i)
+    {
+        m = max(m, lmax[i][side]);
+        if constexpr(SUM) sum += lsum[i][side];
     }
     const CodeScale cs = code_scale(m);
-    col_scale[i] = cs.scale;
-    col_inv[i]   = cs.inv;
-    if(sum_out) sum_out[i] = sum;
+    col_scale[e * cols + c] = cs.scale;
+    col_inv[e * cols + c]   = cs.inv;
+    if constexpr(SUM) sum_out[e * cols + c] = sum;
 }
 
 // 128 positions x 64 columns a workgroup: a thread has four rows of eight columns, whose codes along the columns leave as words of four rows.
@@ -311,9 +376,10 @@ hipError_t launch_both(const TokenSource& s, int64_t sets, const int32_t* offset
     const unsigned      tiles = static_cast<unsigned>((s.cols + kStatCols - 1) / kStatCols);
     if(colsum) token_stats_kernel<T, true><<<dim3(chunks, tiles), 256, 0, st>>>(s, offsets, sets, rowpart, cm, sm);
     else       token_stats_kernel<T, false><<<dim3(chunks, tiles), 256, 0, st>>>(s, offsets, sets, rowpart, cm, sm);
-    const int64_t col_blocks = (sets * s.cols + 255) / 256;
-    token_scales_kernel<<<static_cast<unsigned>(col_blocks + (s.rows + 255) / 256), 256, 0, st>>>(offsets, s.rows, s.cols, sets, col_blocks, static_cast<int>(tiles), rowpart, cm,
-                                                                                                colsum ? sm : nullptr, row_scale, ri, col_scale, ci, colsum);
+    const int64_t  col_blocks = sets * ((s.cols + 15) / 16);
+    const unsigned blocks = static_cast<unsigned>(col_blocks + (s.rows + 255) / 256);
+    if(colsum) token_scales_kernel<true><<<blocks, 256, 0, st>>>(offsets, s.rows, s.cols, sets, col_blocks, static_cast<int>(tiles), rowpart, cm, sm, row_scale, ri, col_scale, ci, colsum);
+    else       token_scales_kernel<false><<<blocks, 256, 0, st>>>(offsets, s.rows, s.cols, sets, col_blocks, static_cast<int>(tiles), rowpart, cm, nullptr, row_scale, ri, col_scale, ci, nullptr);
     token_codes_kernel<T, RND><<<dim3(chunks, static_cast<unsigned>(code_pad(s.cols) / 64)), 256, 0, st>>>(s, offsets, sets, seed, offset, ri, ci, q, qT);
     return hipGetLastError();
 }
