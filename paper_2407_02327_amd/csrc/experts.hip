@@ -3,6 +3,8 @@
 #include "row_ops.h"
 #include "token_ops.h"
 
+#include <type_traits>
+
 namespace qsync {
 
 namespace {
@@ -95,59 +97,183 @@ __global__ __launch_bounds__(64 * kSortWaves) void expert_sort_kernel(const I* i
 }
 
 // ---- rows ------------------------------------------------------------------------------------------------------------------------
-// rows[r] = x[source[r] / group], a workgroup a row; a place outside of x: NaN
-template <typename T>
-__global__ __launch_bounds__(256) void expert_gather_kernel(const T* x, int64_t x_rows, int64_t cols, int64_t ld, const int32_t* source, int group, int64_t rows, const int32_t* count, T* y)
+// Eight columns a thread; a workgroup's 256 threads are 256 / side rows (or tokens) of `side` threads, as many as a row has vectors up to 256, and
+// longer rows take several workgroups: whatever the shape, a thread does little, and a launch has as many threads as there is data.
+struct RowGrid { int side_log2, blocks_x; };
+RowGrid row_grid(int64_t cols, int least)
 {
-    const int64_t r = blockIdx.x;
-    if(r >= *count) return;
-    const int32_t i = source[r];
-    const bool    ok = i >= 0 && i / group < x_rows;
-    const T*      from = x + (ok ? i / group : 0) * ld;
-    for(int64_t c = threadIdx.x; c < cols; c += 256) y[r * cols + c] = ok ? from[c] : static_cast<T>(__uint_as_float(0x7FC00000u));
+    const int64_t vectors = (cols + 7) / 8;
+    int           log2 = least;
+    while(log2 < 8 && (int64_t(1) << log2) < vectors) ++log2;
+    return {log2, static_cast<int>((vectors + (1 << log2) - 1) >> log2)};
+}
+template <typename T> __device__ __forceinline__ void load_tail(const T* row, int64_t c, int64_t cols, Row8<T>& v)
+{
+    if(c + 8 <= cols) v.load(row + c);
+    else
+    {
+        float e[8];
+#pragma unroll
+        for(int i = 0; i < 8; ++i) e[i] = c + i < cols ? row_element(row + c + i) : 0.0f;
+        v.encode(e);
+    }
+}
+__device__ __forceinline__ void store_tail(void* base, int dtype, int64_t at, int64_t c, int64_t cols, float (&v)[8])
+{
+    if(c + 8 <= cols) row8_store<false>(base, dtype, at + c, v);
+    else
+#pragma unroll
+        for(int i = 0; i < 8; ++i)
+            if(c + i < cols) element_store(base, dtype, at + c + i, v[i]);
 }
 
+// rows[r] = x[source[r] / group]; a place outside of x: NaN
 template <typename T>
-__global__ __launch_bounds__(256) void expert_combine_kernel(const T* z, int64_t rows, int64_t cols, int64_t ld, const int32_t* slot, int group, const float* weight, void* y, int ydt)
+__global__ __launch_bounds__(256) void expert_gather_kernel(const T* x, int64_t x_rows, int64_t cols, int64_t ld, const int32_t* source, int group, const int32_t* count, int64_t rows, T* y,
+                                                            int side_log2)
 {
-    const int64_t t = blockIdx.x;
-    for(int64_t c = threadIdx.x; c < cols; c += 256)
+    const int     side = threadIdx.x & ((1 << side_log2) - 1);
+    const int64_t r = static_cast<int64_t>(blockIdx.y) * gridDim.z * (256 >> side_log2) + blockIdx.z * (256 >> side_log2) + (threadIdx.x >> side_log2);
+    const int64_t c = ((static_cast<int64_t>(blockIdx.x) << side_log2) + side) * 8;
+    if(r >= rows || c >= cols) return;
+    const int32_t n = *count, i = source[r];      // (behind the count: whatever lies there, unused)
+    if(r >= n) return;
+    const bool ok = i >= 0 && i / group < x_rows;
+    Row8<T>    v;
+    load_tail(x + (ok ? i / group : 0) * ld, c, cols, v);
+    if(!ok)
     {
-        float sum = 0.0f;
-        for(int j = 0; j < group; ++j)
-        {
-            const int32_t r = slot[t * group + j];
-            if(r < 0 || r >= rows) continue;
-            sum = fmaf(weight ? weight[t * group + j] : 1.0f, row_element(z + r * ld + c), sum);
-        }
-        element_store(y, ydt, t * cols + c, sum);
+        float e[8];
+#pragma unroll
+        for(int j = 0; j < 8; ++j) e[j] = __uint_as_float(0x7FC00000u);
+        v.encode(e);
+    }
+    T* out = y + r * cols;
+    if(c + 8 <= cols) v.store(out + c);
+    else
+    {
+        float e[8];
+        v.decode(e);
+#pragma unroll
+        for(int j = 0; j < 8; ++j)
+            if(c + j < cols) out[c + j] = static_cast<T>(e[j]);
     }
 }
 
-template <typename T, typename U>
-__global__ __launch_bounds__(256) void expert_combine_bwd_kernel(const T* dy, int64_t cols, int64_t lddy, const U* z, int64_t rows, int64_t ldz, const int32_t* slot, int group, const float* weight,
-                                                                 void* dz, int dzdt, float* dweight)
+// (Four rows requested at a time.)
+template <typename T>
+__global__ __launch_bounds__(256) void expert_combine_kernel(const T* z, int64_t rows, int64_t cols, int64_t ld, const int32_t* slot, int64_t tokens, int group, const float* weight, void* y, int ydt,
+                                                             int side_log2)
 {
-    __shared__ float lds[16];
-    const int64_t t = blockIdx.x;
-    for(int j = 0; j < group; ++j)
+    const int     side = threadIdx.x & ((1 << side_log2) - 1);
+    const int64_t t = static_cast<int64_t>(blockIdx.y) * gridDim.z * (256 >> side_log2) + blockIdx.z * (256 >> side_log2) + (threadIdx.x >> side_log2);
+    const int64_t c = ((static_cast<int64_t>(blockIdx.x) << side_log2) + side) * 8;
+    if(t >= tokens || c >= cols) return;
+    float sum[8];
+#pragma unroll
+    for(int j = 0; j < 8; ++j) sum[j] = 0.0f;
+    for(int j0 = 0; j0 < group; j0 += 4)
     {
-        const int32_t r = slot[t * group + j];
-        const bool    ok = r >= 0 && r < rows;
-        float         dot = 0.0f;
-        const float   w = weight ? weight[t * group + j] : 1.0f;
-        if(ok)
-            for(int64_t c = threadIdx.x; c < cols; c += 256)
-            {
-                const float g = row_element(dy + t * lddy + c);
-                if(dweight) dot = fmaf(g, row_element(z + r * ldz + c), dot);
-                if(dz) element_store(dz, dzdt, r * cols + c, w * g);
-            }
-        if(dweight)
+        Row8<T> v[4];
+        float   w[4];
+        bool    ok[4];
+#pragma unroll
+        for(int u = 0; u < 4; ++u)
         {
-            dot = block_reduce_sum(dot, lds);
-            if(threadIdx.x == 0) dweight[t * group + j] = dot;
-            __syncthreads();
+            const int64_t at = t * group + (j0 + u < group ? j0 + u : j0);
+            const int32_t r = slot[at];
+            ok[u] = j0 + u < group && r >= 0 && r < rows;
+            w[u]  = weight ? weight[at] : 1.0f;
+            load_tail(z + (ok[u] ? r : 0) * ld, c, ok[u] ? cols : 0, v[u]);
+        }
+#pragma unroll
+        for(int u = 0; u < 4; ++u)
+            if(ok[u])
+            {
+                float e[8];
+                v[u].decode(e);
+#pragma unroll
+                for(int j = 0; j < 8; ++j) sum[j] = fmaf(w[u], e[j], sum[j]);
+            }
+    }
+    store_tail(y, ydt, t * cols, c, cols, sum);
+}
+
+// A token's gradient is read once for all its rows: `side` threads (64 at least, so that whole wavefronts share a token) walk its columns with
+// four rows' vectors in flight, and leave the rows' gradients and their part of the products dy z, which meet by wavefronts and in LDS.
+template <typename T, typename U, bool DOT, bool DZ>
+__global__ __launch_bounds__(256) void expert_combine_bwd_kernel(const T* dy, int64_t tokens, int64_t cols, int64_t lddy, const U* z, int64_t rows, int64_t ldz, const int32_t* slot, int group,
+                                                                 const float* weight, void* dz, int dzdt, float* dweight, int side_log2)
+{
+    __shared__ float part[4][4];
+    const int     threads = 1 << side_log2, side = threadIdx.x & (threads - 1), wave = threadIdx.x / 64;
+    const int64_t t = (static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x) * (256 >> side_log2) + (threadIdx.x >> side_log2);
+    const bool    here = t < tokens;
+    const int64_t tt = here ? t : 0;
+    for(int j0 = 0; j0 < group; j0 += 4)
+    {
+        int64_t r[4];
+        float   w[4], dot[4];
+#pragma unroll
+        for(int u = 0; u < 4; ++u)
+        {
+            const int64_t at = tt * group + (j0 + u < group ? j0 + u : j0);
+            const int32_t i = slot[at];
+            r[u]   = here && j0 + u < group && i >= 0 && i < rows ? i : -1;
+            w[u]   = weight ? weight[at] : 1.0f;
+            dot[u] = 0.0f;
+        }
+        for(int64_t c = side * 8; c < cols; c += threads * 8)
+        {
+            Row8<T> g;
+            Row8<U> v[4];
+            load_tail(dy + tt * lddy, c, cols, g);
+            if constexpr(DOT)
+#pragma unroll
+                for(int u = 0; u < 4; ++u) load_tail(z + (r[u] < 0 ? 0 : r[u]) * ldz, c, r[u] < 0 ? 0 : cols, v[u]);
+            float d[8];
+            g.decode(d);
+#pragma unroll
+            for(int u = 0; u < 4; ++u)
+                if(r[u] >= 0)
+                {
+                    float e[8];
+                    if constexpr(DOT)
+                    {
+                        v[u].decode(e);
+#pragma unroll
+                        for(int j = 0; j < 8; ++j) dot[u] = c + j < cols ? fmaf(d[j], e[j], dot[u]) : dot[u];
+                    }
+                    if constexpr(DZ)
+                    {
+#pragma unroll
+                        for(int j = 0; j < 8; ++j) e[j] = w[u] * d[j];
+                        store_tail(dz, dzdt, r[u] * cols, c, cols, e);
+                    }
+                }
+        }
+        if constexpr(DOT)
+        {
+#pragma unroll
+            for(int u = 0; u < 4; ++u) dot[u] = wave64_sum(dot[u]);
+            if(side_log2 > 6)
+            {
+                if(threadIdx.x % 64 == 0)
+#pragma unroll
+                    for(int u = 0; u < 4; ++u) part[wave][u] = dot[u];
+                __syncthreads();
+#pragma unroll
+                for(int u = 0; u < 4; ++u)
+                {
+                    dot[u] = part[wave & ~(threads / 64 - 1)][u];
+                    for(int i = 1; i < threads / 64; ++i) dot[u] += part[(wave & ~(threads / 64 - 1)) + i][u];
+                }
+                __syncthreads();
+            }
+            if(side == 0 && here)
+#pragma unroll
+                for(int u = 0; u < 4; ++u)
+                    if(j0 + u < group) dweight[t * group + j0 + u] = r[u] >= 0 ? dot[u] : 0.0f;
         }
     }
 }
@@ -166,11 +292,19 @@ hipError_t launch_expert_sort(const void* ids, bool wide, int64_t n, int experts
     return hipGetLastError();
 }
 
+// rows (of 256 >> side_log2 a workgroup) over the grid's y and z: neither may count more than 65535
+dim3 rows_over_grid(const RowGrid& g, int64_t rows)
+{
+    const int64_t blocks = (rows + (256 >> g.side_log2) - 1) / (256 >> g.side_log2), z = blocks < 128 ? 1 : 128;
+    return dim3(static_cast<unsigned>(g.blocks_x), static_cast<unsigned>((blocks + z - 1) / z), static_cast<unsigned>(z));
+}
+
 hipError_t launch_expert_gather(const void* x, int dtype, int64_t x_rows, int64_t cols, int64_t ld, const int32_t* source, int group, int64_t rows, const int32_t* count, void* y, hipStream_t st)
 {
+    const RowGrid g = row_grid(cols, 3);
     auto typed = [&](auto tag) {
         typedef decltype(tag) T;
-        expert_gather_kernel<T><<<static_cast<unsigned>(rows), 256, 0, st>>>(static_cast<const T*>(x), x_rows, cols, ld, source, group, rows, count, static_cast<T*>(y));
+        expert_gather_kernel<T><<<rows_over_grid(g, rows), 256, 0, st>>>(static_cast<const T*>(x), x_rows, cols, ld, source, group, count, rows, static_cast<T*>(y), g.side_log2);
     };
     dtype == kF16 ? typed(_Float16{}) : dtype == kBF16 ? typed(__bf16{}) : typed(float{});
     return hipGetLastError();
@@ -178,9 +312,10 @@ hipError_t launch_expert_gather(const void* x, int dtype, int64_t x_rows, int64_
 
 hipError_t launch_expert_combine(const void* z, int zdt, int64_t rows, int64_t cols, int64_t ld, const int32_t* slot, int64_t tokens, int group, const float* weight, void* y, int ydt, hipStream_t st)
 {
+    const RowGrid g = row_grid(cols, 3);
     auto typed = [&](auto tag) {
         typedef decltype(tag) T;
-        expert_combine_kernel<T><<<static_cast<unsigned>(tokens), 256, 0, st>>>(static_cast<const T*>(z), rows, cols, ld, slot, group, weight, y, ydt);
+        expert_combine_kernel<T><<<rows_over_grid(g, tokens), 256, 0, st>>>(static_cast<const T*>(z), rows, cols, ld, slot, tokens, group, weight, y, ydt, g.side_log2);
     };
     zdt == kF16 ? typed(_Float16{}) : zdt == kBF16 ? typed(__bf16{}) : typed(float{});
     return hipGetLastError();
@@ -189,10 +324,21 @@ hipError_t launch_expert_combine(const void* z, int zdt, int64_t rows, int64_t c
 hipError_t launch_expert_combine_bwd(const void* dy, int dydt, int64_t tokens, int64_t cols, int64_t lddy, const void* z, int zdt, int64_t rows, int64_t ldz, const int32_t* slot, int group,
                                      const float* weight, void* dz, int dzdt, float* dweight, hipStream_t st)
 {
+    const int     side_log2 = row_grid(cols, 6).side_log2;
+    const int64_t blocks = (tokens + (256 >> side_log2) - 1) / (256 >> side_log2), x = blocks < 65536 ? blocks : 65536;
+    const dim3    grid(static_cast<unsigned>(x), static_cast<unsigned>((blocks + x - 1) / x));
     auto typed = [&](auto tag, auto ztag) {
         typedef decltype(tag) T;
         typedef decltype(ztag) U;
-        expert_combine_bwd_kernel<T, U><<<static_cast<unsigned>(tokens), 256, 0, st>>>(static_cast<const T*>(dy), cols, lddy, static_cast<const U*>(z), rows, ldz, slot, group, weight, dz, dzdt, dweight);
+        auto go = [&](auto dot, auto out) {
+            expert_combine_bwd_kernel<T, U, decltype(dot)::value, decltype(out)::value><<<grid, 256, 0, st>>>(static_cast<const T*>(dy), tokens, cols, lddy, static_cast<const U*>(z), rows, ldz, slot,
+                                                                                                            group, weight, dz, dzdt, dweight, side_log2);
+        };
+        constexpr std::true_type  yes{};
+        constexpr std::false_type no{};
+        if(dweight && dz) go(yes, yes);
+        else if(dweight) go(yes, no);
+        else go(no, yes);
     };
     auto with_z = [&](auto tag) { zdt == kF16 ? typed(tag, _Float16{}) : zdt == kBF16 ? typed(tag, __bf16{}) : typed(tag, float{}); };
     dydt == kF16 ? with_z(_Float16{}) : dydt == kBF16 ? with_z(__bf16{}) : with_z(float{});

@@ -130,19 +130,30 @@ hipError_t launch_rows(const TokenSource& s, const int32_t* count, uint64_t seed
 // ---- rows and columns ------------------------------------------------------------------------------------------------------------
 // The rows' axis is walked in chunks of 128 positions (see set_start): a chunk lies in one set.
 struct Chunk { int64_t set, first, row0, start; int len; };      // (first: the set's first position / len: rows of the chunk, <= 0: none)
+// (The set is the last one that starts at or before the chunk: each wavefront's lanes look at one each, 64 at a time.  A search by halves, a
+// memory latency a step, took 6 of the 12 us of a launch over 37 sets.)
 __device__ __forceinline__ Chunk chunk_rows(const int32_t* offsets, int64_t rows, int64_t sets, int64_t chunk)
 {
     const int64_t p = chunk * kCodePad;
-    int64_t       lo = 0, hi = sets - 1;      // the last set that starts at or before p
-    while(lo < hi)
-    {
-        const int64_t mid = (lo + hi + 1) / 2;
-        if(set_start(offsets, set_rows(offsets, rows, sets, mid), mid) <= p) lo = mid;
-        else hi = mid - 1;
-    }
-    const SetRows s = set_rows(offsets, rows, sets, lo);
-    const int64_t start = set_start(offsets, s, lo), left = s.len - (p - start);
-    return {lo, start, s.first + (p - start), p - start, static_cast<int>(p < start || left < 0 ? 0 : left > kCodePad ? kCodePad : left)};
+    int64_t       set = 0;
+    if(!offsets) set = min(p / code_pad(rows / sets), sets - 1);
+    else
+        for(int64_t e0 = 0; e0 < sets; e0 += 64)
+        {
+            const int64_t e = e0 + threadIdx.x % 64;
+            bool          from = false;
+            if(e < sets)
+            {
+                int64_t a = offsets[e];
+                a    = a < 0 ? 0 : a > rows ? rows : a;
+                from = code_pad(a) + kCodePad * e <= p;
+            }
+            set += __popcll(__ballot(from));
+        }
+    if(offsets) set = max(static_cast<int64_t>(0), set - 1);
+    const SetRows s = set_rows(offsets, rows, sets, set);
+    const int64_t start = set_start(offsets, s, set), left = s.len - (p - start);
+    return {set, start, s.first + (p - start), p - start, static_cast<int>(p < start || left < 0 ? 0 : left > kCodePad ? kCodePad : left)};
 }
 
 // First pass: maxima of 128 columns (eight a lane) over a chunk and of the chunk's rows over those columns.  Sixteen lanes stand side by side, so
