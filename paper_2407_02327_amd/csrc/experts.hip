@@ -10,10 +10,11 @@ namespace qsync {
 namespace {
 
 // ---- sort ------------------------------------------------------------------------------------------------------------------------
-// Stable by expert: an entry's place is the number of entries of lower experts, plus those of its own in front of it.  One workgroup: each
-// wavefront counts its stretch of the entries, the counts are added up over experts and wavefronts, and each wavefront walks its stretch
-// again.  Entries of the same expert among 64 find each other by comparing the ids bit by bit.
-constexpr int kSortWaves = 16;
+// Stable by expert: an entry's place is the number of entries of lower experts, plus those of its own in front of it.  A workgroup has a section
+// of the entries, a wavefront a stretch of that.  Up to 2048 entries are one section and one launch; more are counted by a first launch
+// (hist [sections][experts]), and each workgroup of the second adds up what lies in front of its own.  Entries of the same expert among a
+// wavefront's 64 find each other by comparing the ids bit by bit.  One workgroup for everything took 81 us for 65536 entries.
+constexpr int kSortWaves = 16, kSortThreads = 64 * kSortWaves, kSortSections = 256;
 template <typename I> __device__ __forceinline__ int expert_of(const I* ids, int64_t i, int experts)
 {
     const I v = ids[i];
@@ -29,69 +30,109 @@ __device__ __forceinline__ uint64_t same_expert(int e, bool valid, int bits)
     }
     return m;
 }
+template <typename I> __global__ __launch_bounds__(kSortThreads) void expert_count_kernel(const I* ids, int64_t n, int64_t section, int experts, int32_t* hist)
+{
+    extern __shared__ int32_t counts[];      // [experts]
+    for(int i = threadIdx.x; i < experts; i += kSortThreads) counts[i] = 0;
+    __syncthreads();
+    const int64_t begin = blockIdx.x * section, end = min(n, begin + section);
+    for(int64_t i = begin + threadIdx.x; i < end; i += kSortThreads)
+    {
+        const int e = expert_of(ids, i, experts);
+        if(e >= 0) atomicAdd(counts + e, 1);
+    }
+    __syncthreads();
+    for(int i = threadIdx.x; i < experts; i += kSortThreads) hist[static_cast<int64_t>(blockIdx.x) * experts + i] = counts[i];
+}
+
+// `bits`: of experts - 1; hist nullptr: one section
 template <typename I>
-__global__ __launch_bounds__(64 * kSortWaves) void expert_sort_kernel(const I* ids, int64_t n, int experts, int bits, int32_t* offsets, int32_t* source, int32_t* slot)
+__global__ __launch_bounds__(kSortThreads) void expert_place_kernel(const I* ids, int64_t n, int64_t section, int experts, int bits, const int32_t* hist, int32_t* offsets, int32_t* source, int32_t* slot)
 {
     extern __shared__ int32_t counts[];      // [wavefronts][experts], then running places
-    __shared__ int32_t carry[kSortWaves], total;
+    __shared__ int32_t before[kSortThreads], whole[kSortThreads], carry[kSortWaves];
     const int     lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int64_t per = ((n + kSortWaves - 1) / kSortWaves + 63) / 64 * 64, begin = min(n, wave * per), end = min(n, begin + per);
-    for(int i = threadIdx.x; i < kSortWaves * experts; i += 64 * kSortWaves) counts[i] = 0;
+    const int64_t first = blockIdx.x * section, last = min(n, first + section);
+    const int64_t per = (section / kSortWaves + 63) / 64 * 64, begin = min(last, first + wave * per), end = min(last, begin + per);
+    for(int i = threadIdx.x; i < kSortWaves * experts; i += kSortThreads) counts[i] = 0;
     __syncthreads();
     int32_t* mine = counts + wave * experts;
-    for(int64_t i = begin + lane; i - lane < end; i += 64)
+    for(int64_t i = begin + lane; i < end; i += 64)
     {
-        const int e = i < end ? expert_of(ids, i, experts) : -1;
+        const int e = expert_of(ids, i, experts);
         if(e >= 0) atomicAdd(mine + e, 1);
     }
-    __syncthreads();
-    if(threadIdx.x == 0) total = 0;
-    __syncthreads();
-    for(int e0 = 0; e0 < experts; e0 += 64 * kSortWaves)
-    {   // places of the experts, 1024 at a time; of an expert, those of its wavefronts
-        const int e = e0 + threadIdx.x;
-        int32_t   sum = 0;
-        if(e < experts)
-            for(int w = 0; w < kSortWaves; ++w) sum += counts[w * experts + e];
-        int32_t scan = sum;
-        for(int off = 1; off < 64; off <<= 1)
+    // Of each expert: its entries, and those in sections before this one.  1024 >> bits threads share an expert.
+    const int e = threadIdx.x & ((1 << bits) - 1), part = threadIdx.x >> bits, parts = kSortThreads >> bits;
+    int32_t   all = 0, ahead = 0;
+    if(hist && e < experts)
+        for(int b0 = part; b0 < static_cast<int>(gridDim.x); b0 += 4 * parts)
         {
-            const int32_t o = __shfl_up(scan, off);
-            if(lane >= off) scan += o;
-        }
-        if(lane == 63) carry[wave] = scan;
-        __syncthreads();
-        int32_t at = total + scan - sum;
-        for(int w = 0; w < wave; ++w) at += carry[w];
-        if(e < experts)
-        {
-            offsets[e] = at;
-            for(int w = 0; w < kSortWaves; ++w)
+            int32_t o[4];
+#pragma unroll
+            for(int u = 0; u < 4; ++u) o[u] = b0 + u * parts < static_cast<int>(gridDim.x) ? hist[static_cast<int64_t>(b0 + u * parts) * experts + e] : 0;
+#pragma unroll
+            for(int u = 0; u < 4; ++u)
             {
-                const int32_t c = counts[w * experts + e];
-                counts[w * experts + e] = at;
-                at += c;
+                all += o[u];
+                ahead += b0 + u * parts < static_cast<int>(blockIdx.x) ? o[u] : 0;
             }
         }
-        __syncthreads();
-        if(threadIdx.x == 64 * kSortWaves - 1) total = at;      // (experts past the last have no entries: at is the running total)
-        __syncthreads();
+    whole[threadIdx.x]  = all;
+    before[threadIdx.x] = ahead;
+    __syncthreads();
+    if(part == 0 && e < experts)      // (the first 1 << bits threads)
+    {
+        if(hist)
+            for(int i = 1; i < parts; ++i)
+            {
+                all += whole[(i << bits) + e];
+                ahead += before[(i << bits) + e];
+            }
+        else
+            for(int w = 0; w < kSortWaves; ++w) all += counts[w * experts + e];
     }
-    if(threadIdx.x == 0) offsets[experts] = total;
+    else all = 0;
+    int32_t scan = all;      // (of the experts up to this one)
+#pragma unroll
+    for(int off = 1; off < 64; off <<= 1)
+    {
+        const int32_t o = __shfl_up(scan, off);
+        if(lane >= off) scan += o;
+    }
+    if(lane == 63) carry[wave] = scan;
+    __syncthreads();
+    for(int w = 0; w < wave; ++w) scan += carry[w];
+    if(part == 0 && e < experts)
+    {
+        if(blockIdx.x == 0)
+        {
+            offsets[e] = scan - all;
+            if(e == experts - 1) offsets[experts] = scan;
+        }
+        int32_t at = scan - all + ahead;
+        for(int w = 0; w < kSortWaves; ++w)
+        {
+            const int32_t c = counts[w * experts + e];
+            counts[w * experts + e] = at;
+            at += c;
+        }
+    }
+    __syncthreads();
     for(int64_t i = begin + lane; i - lane < end; i += 64)
     {
-        const int      e = i < end ? expert_of(ids, i, experts) : -1;
-        const uint64_t same = same_expert(e, e >= 0, bits);
-        const int      ahead = __popcll(same & ((1ull << lane) - 1));
+        const int      x = i < end ? expert_of(ids, i, experts) : -1;
+        const uint64_t same = same_expert(x, x >= 0, bits);
+        const int      rank = __popcll(same & ((1ull << lane) - 1));
         int32_t        place = -1;
-        if(e >= 0)
+        if(x >= 0)
         {
-            place = mine[e] + ahead;
+            place = mine[x] + rank;
             source[place] = static_cast<int32_t>(i);
         }
         if(i < end) slot[i] = place;
         __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-        if(e >= 0 && ahead == 0) mine[e] += static_cast<int32_t>(__popcll(same));
+        if(x >= 0 && rank == 0) mine[x] += static_cast<int32_t>(__popcll(same));
         __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
     }
 }
@@ -280,15 +321,32 @@ __global__ __launch_bounds__(256) void expert_combine_bwd_kernel(const T* dy, in
 
 }  // namespace
 
-size_t expert_sort_workspace_bytes(int64_t, int) { return 0; }
+static int64_t sort_section(int64_t n)
+{
+    if(n <= 2 * kSortThreads) return 2 * kSortThreads;
+    return ((n + kSortSections - 1) / kSortSections + kSortThreads - 1) / kSortThreads * kSortThreads;
+}
+size_t expert_sort_workspace_bytes(int64_t n, int experts)
+{
+    // (what is enough for some number of entries is enough for fewer, though a longer section may be cut into fewer of them)
+    const int64_t sections = (n + kSortThreads - 1) / kSortThreads;
+    return n > sort_section(n) ? static_cast<size_t>(sections < kSortSections ? sections : kSortSections) * experts * 4 : 0;
+}
 
-hipError_t launch_expert_sort(const void* ids, bool wide, int64_t n, int experts, int32_t* offsets, int32_t* source, int32_t* slot, void*, hipStream_t st)
+hipError_t launch_expert_sort(const void* ids, bool wide, int64_t n, int experts, int32_t* offsets, int32_t* source, int32_t* slot, void* workspace, hipStream_t st)
 {
     int bits = 0;
     while((1 << bits) < experts) ++bits;
-    const size_t lds = static_cast<size_t>(kSortWaves) * experts * 4;
-    if(wide) expert_sort_kernel<<<1, 64 * kSortWaves, lds, st>>>(static_cast<const int64_t*>(ids), n, experts, bits, offsets, source, slot);
-    else     expert_sort_kernel<<<1, 64 * kSortWaves, lds, st>>>(static_cast<const int32_t*>(ids), n, experts, bits, offsets, source, slot);
+    const int64_t  section = sort_section(n);
+    const unsigned sections = static_cast<unsigned>(n > section ? (n + section - 1) / section : 1);
+    const size_t   lds = static_cast<size_t>(experts) * 4;
+    int32_t*       hist = sections > 1 ? static_cast<int32_t*>(workspace) : nullptr;
+    auto typed = [&](auto tag) {
+        typedef decltype(tag) I;
+        if(hist) expert_count_kernel<I><<<sections, kSortThreads, lds, st>>>(static_cast<const I*>(ids), n, section, experts, hist);
+        expert_place_kernel<I><<<sections, kSortThreads, kSortWaves * lds, st>>>(static_cast<const I*>(ids), n, section, experts, bits, hist, offsets, source, slot);
+    };
+    wide ? typed(int64_t{}) : typed(int32_t{});
     return hipGetLastError();
 }
 

@@ -141,6 +141,17 @@ def test_sort():
         assert SORT.but(ws_bytes=need - 1) == Q.ERR_WORKSPACE and SORT.but(ws=NULL) == Q.ERR_WORKSPACE
 
 
+def test_workspaces_for_more_are_enough_for_fewer():
+    sizes = [1, 2, 100, 1000, 2048, 2049, 5000, 100_000, 262_144, 262_145, 300_000, 524_289, 4_000_000, 1 << 23]
+    for fewer, more in zip(sizes, sizes[1:]):
+        assert Q.qsync_expert_sort_workspace_bytes(fewer, 64) <= Q.qsync_expert_sort_workspace_bytes(more, 64)
+        for cols, sets, given in ((100, 1, False), (1000, 7, True)):
+            assert Q.qsync_token_quantize_both_workspace_bytes(fewer, cols, sets, given) <= Q.qsync_token_quantize_both_workspace_bytes(more, cols, sets, given)
+        for N, K, sets in ((64, 64, 1), (1000, 5000, 1), (4096, 130, 1), (300, 1000, 9)):
+            assert Q.qsync_token_linear_workspace_bytes(fewer, N, K, sets) <= Q.qsync_token_linear_workspace_bytes(more, N, K, sets)
+            assert Q.qsync_token_wgrad_workspace_bytes(fewer, N, K, sets) <= Q.qsync_token_wgrad_workspace_bytes(more, N, K, sets)
+
+
 def test_combine_backward():
     assert BWD.but(dz=NULL, dweight=NULL) == Q.ERR_NULL
     assert BWD.but(dweight=NULL, z=NULL) in OK_OR_NO_GPU and BWD.but(dz=NULL) in OK_OR_NO_GPU

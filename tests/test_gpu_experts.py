@@ -24,7 +24,7 @@ def ids_of(tokens, k, experts, seed, dtype=torch.int64, outside=0.0):
     return ids.to(dtype).cuda()
 
 
-@pytest.mark.parametrize("tokens, k", [(1, 1), (1, 8), (63, 1), (64, 1), (65, 1), (13, 5), (512, 2), (1025, 1), (700, 8), (8192, 8), (50000, 3)])
+@pytest.mark.parametrize("tokens, k", [(1, 1), (1, 8), (63, 1), (64, 1), (65, 1), (13, 5), (512, 2), (1025, 1), (700, 8), (8192, 8), (50000, 3), (2048, 1), (683, 3), (270000, 1)])
 @pytest.mark.parametrize("experts", [1, 2, 7, 64, 512])
 @pytest.mark.parametrize("dtype, outside", [(torch.int64, 0.0), (torch.int32, 0.2)])
 def test_sort(tokens, k, experts, dtype, outside):
