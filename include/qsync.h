@@ -778,6 +778,15 @@ int qsync_token_linear_fwd(int64_t rows, int64_t N, int64_t K, int64_t sets, con
 size_t qsync_token_linear_workspace_bytes(int64_t rows, int64_t N, int64_t K, int64_t sets);
 
 /*
+ * qsync_token_linear - qsync_token_quantize (to nearest) of x [x_rows, ld] into sx and xq, then qsync_token_linear_fwd with them: the serving
+ * form, with identical outputs y.  A handful of rows takes one launch, which leaves sx and xq as they were.  offsets_opt also gives
+ * the rows' count.  Arguments and errors as in the two calls.
+ */
+int qsync_token_linear(const void* x, int xdt, int64_t x_rows, int64_t K, int64_t ld, const int32_t* source_opt, int64_t group, int64_t rows,
+                       int64_t N, int64_t sets, const int32_t* offsets_opt, const void* wq, const float* sw, const float* bias_opt, void* y,
+                       int ydt, float* sx, void* xq, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * qsync_token_linear_wgrad - dW[e,n,k] = (sum over the rows m of set e of dyqT[n,m] xqT[k,m]) * (sdy[e,n] * sx[e,k]), on codes along the rows
  * (qsync_token_quantize_both) of dY [rows, N] and X [rows, K].  dw out, [sets, N, K] of dwdt; zeros for a set without rows.
  * offsets_opt NULL: one set.  workspace: qsync_token_wgrad_workspace_bytes(rows, N, K, sets).

@@ -15,7 +15,7 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libqsync.so")
 BINDING_PATH = os.path.join(PKG_DIR, "_native.so")      # CPython module over the library's C ABI and torch's tensors
 SOURCES = ["api.hip", "elementwise.hip", "gemm_mfma.hip", "conv3x3.hip", "conv_wgrad.hip", "gemm_rows.hip", "gemm_f32.hip", "layernorm.hip", "logits.hip", "token_quant.hip",
-           "token_gemm.hip", "experts.hip", "probe.hip", "indicator.hip"]
+           "token_gemm.hip", "token_few.hip", "experts.hip", "probe.hip", "indicator.hip"]
 
 # -ffp-contract=off: the quantizer's multiply and subtract must stay separately rounded.
 # packed fp32 VALU ops are disabled for the device pass (hipcc's host pass warns that it
@@ -32,7 +32,8 @@ HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-cont
 # gemm_f32_kernel has no such reads, but a lambda that is left as a call puts all it captures there (128 tile 8 -> 150 us).
 NO_SPILL = {"gemm_mfma.hip": ("gemm_nt_kernel", "gemm_nt_pair_kernel", "gemm_nt_persistent_kernel"),
             "conv3x3.hip": ("conv3x3_kernel",), "gemm_rows.hip": ("gemm_rows_kernel",),
-            "gemm_f32.hip": ("gemm_f32_kernel",), "token_gemm.hip": ("token_gemm_kernel",)}
+            "gemm_f32.hip": ("gemm_f32_kernel",), "token_gemm.hip": ("token_gemm_kernel",),
+            "token_few.hip": ("token_few_kernel",)}
 
 
 def _check_no_spill(src: str, remarks: str) -> None:

@@ -1249,6 +1249,30 @@ int qsync_token_linear_fwd(int64_t rows, int64_t N, int64_t K, int64_t sets, con
                                                         offsets_opt}, false, static_cast<hipStream_t>(stream)));
 }
 
+int qsync_token_linear(const void* x, int xdt, int64_t x_rows, int64_t K, int64_t ld, const int32_t* source_opt, int64_t group, int64_t rows, int64_t N, int64_t sets,
+                       const int32_t* offsets_opt, const void* wq, const float* sw, const float* bias_opt, void* y, int ydt, float* sx, void* xq, void* workspace,
+                       size_t workspace_bytes, void* stream)
+{
+    if(!sx || !xq) return QSYNC_ERR_NULL;
+    int rc = token_matrix(x, xdt, x_rows, K, ld, source_opt, group, rows, QSYNC_ROUND_NEAREST);
+    if(rc < 0) return rc;
+    rc = token_product(rows, N, K, sets, offsets_opt, xq, sx, wq, sw, bias_opt, y, ydt);
+    if(rc != QSYNC_OK) return rc;
+    if(rows == 0 || N == 0) return QSYNC_OK;
+    rc = workspace_status(workspace, workspace_bytes, qsync_token_linear_workspace_bytes(rows, N, K, sets));
+    if(rc != QSYNC_OK) return rc;
+    const int64_t xb = span_bytes(x_rows, K, ld, xdt), yb = rows * N * dtype_bytes(ydt), qb = rows * qsync_token_code_cols(K);
+    if(!apart(xq, qb, x, xb) || !apart(sx, rows * 4, x, xb) || !apart(y, yb, x, xb) || !apart(y, yb, xq, qb)) return QSYNC_ERR_UNSUPPORTED;
+    const TokenMatrix  m{x, xdt, x_rows, K, ld, rows, source_opt, static_cast<int>(group)};
+    const TokenProduct p{static_cast<const int8_t*>(xq), static_cast<const int8_t*>(wq), sx, sw, bias_opt, y, ydt, rows, rows, N, K, sets, offsets_opt};
+    const hipStream_t  st = static_cast<hipStream_t>(stream);
+    bool               taken;
+    hipError_t         e = launch_token_few(m, p, &taken, st);
+    if(taken || e != hipSuccess) return hip_status(e);
+    if(K > 0) e = launch_token_quantize(m, offsets_opt ? offsets_opt + sets : nullptr, kNearest, 0, 0, sx, static_cast<int8_t*>(xq), st);
+    return hip_status(e != hipSuccess ? e : launch_token_product(p, false, st));
+}
+
 size_t qsync_token_wgrad_workspace_bytes(int64_t, int64_t, int64_t, int64_t) { return 0; }
 
 int qsync_token_linear_wgrad(int64_t rows, int64_t N, int64_t K, int64_t sets, const int32_t* offsets_opt, const void* dyqT, const float* sdy, const void* xqT,

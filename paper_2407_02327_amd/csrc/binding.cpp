@@ -11,6 +11,7 @@
 #include <pthread.h>
 
 #include <c10/hip/HIPStream.h>
+#include <hip/hip_runtime_api.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -236,6 +237,17 @@ const char* text(PyObject* o)
     return s;
 }
 
+// check_device(device): the current GPU, where kernels run, is the operator's (-1: its buffers are on none, which the checks of tensors refuse)
+PyObject* check_device(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    return guarded(n, 1, [&]() -> PyObject* {
+        const int64_t device = static_cast<int64_t>(integer(args[0]));
+        int           current = -1;
+        if(device < 0 || (hipGetDevice(&current) == hipSuccess && current == device)) Py_RETURN_NONE;
+        PyErr_Format(PyExc_ValueError, "the operator's buffers are on GPU %lld, the current device is GPU %d", static_cast<long long>(device), current);
+        return nullptr;
+    });
+}
 // check_rows(t, rows, cols, device, name) -> leading dimension: [n <= rows, cols] of floats, contiguous rows that do not overlap
 PyObject* check_rows(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
@@ -281,6 +293,7 @@ PyObject* check_packed(PyObject*, PyObject* const* args, Py_ssize_t n)
 #define ENTRY_WIDE(name) ENTRY_OF(name, true)
 PyMethodDef methods[] = {
     {"set_error", set_error, METH_O, nullptr},
+    {"check_device", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&check_device)), METH_FASTCALL, nullptr},
     {"check_rows", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&check_rows)), METH_FASTCALL, nullptr},
     {"check_packed", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&check_packed)), METH_FASTCALL, nullptr},
     ENTRY(qsync_absmax_scale), ENTRY(qsync_absmax_scale_static), ENTRY(qsync_quantize), ENTRY(qsync_absmax_quantize),
@@ -290,7 +303,7 @@ PyMethodDef methods[] = {
     ENTRY(qsync_conv3x3_wgrad), ENTRY(qsync_conv3x3_prepare_weights), ENTRY(qsync_conv3x3_wflip), ENTRY(qsync_im2col3x3_i8),
     ENTRY(qsync_prepare_weights), ENTRY(qsync_dequantize), ENTRY_WIDE(qsync_layernorm_fwd), ENTRY_WIDE(qsync_layernorm_bwd),
     ENTRY_WIDE(qsync_token_logprobs), ENTRY_WIDE(qsync_token_logprobs_bwd), ENTRY_WIDE(qsync_distill_topk),
-    ENTRY_WIDE(qsync_token_quantize), ENTRY_WIDE(qsync_token_quantize_both), ENTRY_WIDE(qsync_token_linear_fwd), ENTRY_WIDE(qsync_token_linear_wgrad),
+    ENTRY_WIDE(qsync_token_quantize), ENTRY_WIDE(qsync_token_quantize_both), ENTRY_WIDE(qsync_token_linear), ENTRY_WIDE(qsync_token_linear_fwd), ENTRY_WIDE(qsync_token_linear_wgrad),
     ENTRY_WIDE(qsync_expert_sort), ENTRY_WIDE(qsync_expert_gather), ENTRY_WIDE(qsync_expert_combine), ENTRY_WIDE(qsync_expert_combine_bwd), {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -6,6 +6,7 @@
 // each through stages of its own with two or three turns in flight and no barrier, into the 16x16 matrix instructions; the
 // eight sums meet in LDS once at the end.
 #include "gemm_device.h"
+#include "token_ops.h"
 
 namespace qsync {
 
@@ -20,7 +21,8 @@ constexpr int64_t kRowsGroups = 256;                                        // o
 // each unit: the workgroups that read one piece of the longer operand then share an L2.  4096x128 by 3072, int8: 11.5 -> 7.5 us.
 template <int NF> __host__ __device__ constexpr bool rows_first(int64_t M, int64_t N) { return M > N * (4 / NF); }
 constexpr int rows_stages(int loads) { return loads > 4 ? 3 : 4; }             // turns in LDS: 144 KB of them at most
-template <typename TR, int MF, int NF>
+// TOKEN: scales of the rows and of the columns, outputs of fp32, binary16 or bfloat16 (c_is_f16 2).
+template <typename TR, int MF, int NF, bool TOKEN = false>
 __global__ __launch_bounds__(64 * kRowsWaves) void gemm_rows_kernel(const GemmKernelArgs p)
 {
     typedef typename TR::accv_t vec;
@@ -88,7 +90,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void gemm_rows_kernel(const GemmKe
 
     const int64_t m = m0 + wave % MF * 16 + row, n = n0 + wave / MF * 16 + quad * 4;
     if(m >= p.M || n >= p.N) return;
-    const float alpha = *(p.s0 ? p.s0 : &g_one) * *(p.s1 ? p.s1 : &g_one);
+    const float alpha = TOKEN ? (p.row_scale ? p.row_scale[m] : 1.0f) : *(p.s0 ? p.s0 : &g_one) * *(p.s1 ? p.s1 : &g_one);
     float       fs[4], bs[4];
 #pragma unroll
     for(int e = 0; e < 4; ++e)
@@ -104,6 +106,12 @@ __global__ __launch_bounds__(64 * kRowsWaves) void gemm_rows_kernel(const GemmKe
     float v[4];
 #pragma unroll
     for(int e = 0; e < 4; ++e) v[e] = static_cast<float>(sum[e]);
+    if constexpr(TOKEN)
+        if(p.c_is_f16 == 2)
+        {
+            for(int e = 0; e < 4 && n + e < p.N; ++e) reinterpret_cast<__bf16*>(dst)[e] = static_cast<__bf16>(fmaf(v[e], fs[e], bs[e]));
+            return;
+        }
     if(p.c_is_f16)
     {
         const uint2 h = make_uint2(fma_out_half2(v[0], fs[0], bs[0], v[1], fs[1], bs[1]), fma_out_half2(v[2], fs[2], bs[2], v[3], fs[3], bs[3]));
@@ -122,7 +130,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void gemm_rows_kernel(const GemmKe
     }
 }
 
-template <typename TR, int MF, int NF> hipError_t launch_fragments(const GemmKernelArgs& a, hipStream_t st)
+template <typename TR, int MF, int NF, bool TOKEN = false> hipError_t launch_fragments(const GemmKernelArgs& a, hipStream_t st)
 {
     static_assert(MF * NF <= kRowsWaves, "a wavefront per fragment in the epilogue");
     constexpr int kLds = kRowsWaves * rows_stages(MF + NF) * (MF + NF) * 1024;
@@ -131,25 +139,25 @@ template <typename TR, int MF, int NF> hipError_t launch_fragments(const GemmKer
     const bool    known = hipGetDevice(&dev) == hipSuccess && dev >= 0 && dev < 16;
     if(!known || !attr_set[dev])
     {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_rows_kernel<TR, MF, NF>), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_rows_kernel<TR, MF, NF, TOKEN>), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
         if(e != hipSuccess) return e;
         if(known) attr_set[dev] = true;
     }
     const int64_t m = (a.M + 63) / 64, n = (a.N + 16 * NF - 1) / (16 * NF), few = rows_first<NF>(a.M, a.N) ? n : m;
     int64_t       many = rows_first<NF>(a.M, a.N) ? m : n;
     if((many + 7) / 8 * 8 * few <= kRowsGroups) many = (many + 7) / 8 * 8;
-    gemm_rows_kernel<TR, MF, NF><<<dim3(static_cast<unsigned>(many), static_cast<unsigned>(few)), dim3(64 * kRowsWaves), kLds, st>>>(a);
+    gemm_rows_kernel<TR, MF, NF, TOKEN><<<dim3(static_cast<unsigned>(many), static_cast<unsigned>(few)), dim3(64 * kRowsWaves), kLds, st>>>(a);
     return hipGetLastError();
 }
-template <typename TR> hipError_t launch_rows(const GemmKernelArgs& a, int columns, hipStream_t st)
+template <typename TR, bool TOKEN = false> hipError_t launch_rows(const GemmKernelArgs& a, int columns, hipStream_t st)
 {
-    if(columns == 2) return launch_fragments<TR, 4, 2>(a, st);
+    if(columns == 2) return launch_fragments<TR, 4, 2, TOKEN>(a, st);
     switch(a.M > 64 ? 4 : (a.M + 15) / 16)
     {
-    case 1: return launch_fragments<TR, 1, 1>(a, st);
-    case 2: return launch_fragments<TR, 2, 1>(a, st);
-    case 3: return launch_fragments<TR, 3, 1>(a, st);
-    default: return launch_fragments<TR, 4, 1>(a, st);
+    case 1: return launch_fragments<TR, 1, 1, TOKEN>(a, st);
+    case 2: return launch_fragments<TR, 2, 1, TOKEN>(a, st);
+    case 3: return launch_fragments<TR, 3, 1, TOKEN>(a, st);
+    default: return launch_fragments<TR, 4, 1, TOKEN>(a, st);
     }
 }
 // Fragments of columns a workgroup, 0: other tiles are faster.  A second workgroup on a unit waits for the first (its stages fill
@@ -172,6 +180,22 @@ int rows_columns(const GemmProblem& p)
 }
 
 }  // namespace
+
+hipError_t launch_token_rows(const TokenProduct& p, bool* taken, hipStream_t st)
+{
+    GemmProblem shape{};
+    shape.prec = 8; shape.M = p.rows; shape.N = p.N; shape.K = code_pad(p.K);
+    const int columns = p.offsets || p.sets != 1 || p.K == 0 ? 0 : rows_columns(shape);
+    *taken = columns != 0;
+    if(!*taken) return hipSuccess;
+    GemmKernelArgs a{};
+    a.A = reinterpret_cast<const uint8_t*>(p.A);
+    a.B = reinterpret_cast<const uint8_t*>(p.B);
+    a.M = p.rows; a.N = p.N; a.Kb = shape.K;
+    a.C = p.C; a.c_is_f16 = p.c_dtype == kF16 ? 1 : p.c_dtype == kBF16 ? 2 : 0;
+    a.row_scale = p.sa; a.col_scale = p.sb; a.col_bias = p.bias;
+    return launch_rows<I8Traits, true>(a, columns, st);
+}
 
 bool gemm_rows_takes(const GemmProblem& p)
 {

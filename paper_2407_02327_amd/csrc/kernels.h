@@ -170,6 +170,10 @@ struct TokenProduct
     const int32_t* offsets;
 };
 hipError_t launch_token_product(const TokenProduct& p, bool wgrad, hipStream_t st);
+// Few rows or a small product of one set (gemm_rows.hip); *taken is false, and nothing launched, for any other.
+hipError_t launch_token_rows(const TokenProduct& p, bool* taken, hipStream_t st);
+// A handful of rows quantized and multiplied in one launch (token_few.hip); p.A and p.sa are not used.  *taken likewise.
+hipError_t launch_token_few(const TokenMatrix& m, const TokenProduct& p, bool* taken, hipStream_t st);
 hipError_t launch_expert_sort(const void* ids, bool wide, int64_t n, int experts, int32_t* offsets, int32_t* source, int32_t* slot, void* workspace, hipStream_t st);
 size_t expert_sort_workspace_bytes(int64_t n, int experts);
 hipError_t launch_expert_gather(const void* x, int dtype, int64_t x_rows, int64_t cols, int64_t ld, const int32_t* source, int group, int64_t rows, const int32_t* count, void* y, hipStream_t st);

@@ -148,6 +148,12 @@ template <bool WGRAD> hipError_t launch_product(const TokenProduct& p, hipStream
 
 }  // namespace
 
-hipError_t launch_token_product(const TokenProduct& p, bool wgrad, hipStream_t st) { return wgrad ? launch_product<true>(p, st) : launch_product<false>(p, st); }
+hipError_t launch_token_product(const TokenProduct& p, bool wgrad, hipStream_t st)
+{
+    if(wgrad) return launch_product<true>(p, st);
+    bool             taken;
+    const hipError_t e = launch_token_rows(p, &taken, st);
+    return taken || e != hipSuccess ? e : launch_product<false>(p, st);
+}
 
 }  // namespace qsync

@@ -28,10 +28,7 @@ from .head import _ANY_FLOAT, _FLOAT32, _INTEGER, _check_packed, _check_rows, _f
 from .operator import _scratch
 
 
-def _on_device(device: int) -> None:
-    """A kernel runs on the current device, and its buffers have to be there."""
-    if device >= 0 and torch.cuda.current_device() != device:
-        raise ValueError(f"the operator's buffers are on GPU {device}, the current device is GPU {torch.cuda.current_device()}")
+_on_device = Q._native.check_device      # a kernel runs on the current device, and its buffers have to be there
 
 
 class ExpertRoute:
@@ -56,99 +53,96 @@ class ExpertRoute:
             self.rows_out, self.y = e(tokens * k, cols, dt=dtype), e(tokens, cols, dt=dtype)
             if training:
                 self.dz, self.dweight, self.dx = e(tokens * k, cols, dt=dtype), e(tokens, k, dt=torch.float32), e(tokens, cols, dt=dtype)
-        self.n = None                                          # tokens of the last sort
+        self.n, self._rows_of_sort = None, -1                  # tokens and rows of the last sort
         self.sorts = 0
         self._saved = None
 
     @property
     def rows(self) -> int:
         """Rows of the last `sort`: its tokens times k.  Those from `offsets[experts]` on belong to no expert."""
-        self._sorted()
-        return self.n * self.k
-
-    def _sorted(self) -> None:
         if self.n is None:
             raise RuntimeError("a route without a sort")
-
-    def _columns(self) -> None:
-        _on_device(self.device)
-        self._sorted()
-        if self.cols is None:
-            raise ValueError("a route without cols only sorts")
+        return self._rows_of_sort
 
     def sort(self, ids: torch.Tensor, stream=None) -> torch.Tensor:
         """offsets [experts + 1] (int32): expert e has the rows offsets[e] .. offsets[e+1]-1, in the order of its entries in ids.  ids [n <= tokens, k] of
         int64 or int32; an entry outside of 0 .. experts-1 has no expert.  Also left: `source`, the entry of every row, and `slot`, the row
         of every entry or -1."""
         _on_device(self.device)
-        if not isinstance(ids, torch.Tensor) or ids.dim() != 2 or ids.shape[0] > self.tokens:
-            raise ValueError(f"ids: [at most {self.tokens}, {self.k}] expected")
-        n = ids.shape[0]
+        n = len(ids)
+        if n > self.tokens:
+            raise ValueError(f"ids: at most {self.tokens} tokens expected")
         _check_packed(ids, n, self.k, _INTEGER, self.device, "ids")
-        # (a tensor without elements has no address, and any will do)
-        Q.qsync_expert_sort(ids if n else self.offsets, n, self.k, self.experts, self.offsets, self.source if n else self.offsets,
-                            self.slot if n else self.offsets, self.ws, stream)
-        self.n, self._saved = n, None
+        if n:
+            Q.qsync_expert_sort(ids, n, self.k, self.experts, self.offsets, self.source, self.slot, self.ws, stream)
+        else:      # (a tensor without elements has no address, and any will do)
+            Q.qsync_expert_sort(self.offsets, 0, self.k, self.experts, self.offsets, self.offsets, self.offsets, self.ws, stream)
+        self.n, self._rows_of_sort, self._saved = n, n * self.k, None
         self.sorts += 1
         return self.offsets
 
     def gather(self, x: torch.Tensor, stream=None) -> torch.Tensor:
         """The tokens' rows in the experts' order, [rows, cols]; x [n, cols] of the route's dtype, rows at any stride.  Rows that belong to no
         expert are left as they were."""
-        self._columns()
-        ld = self._tokens(x, "x")
-        if x.dtype != self.rows_out.dtype:
-            raise ValueError(f"x: {self.rows_out.dtype} expected, not {x.dtype}")
-        if self.n:
-            Q.qsync_expert_gather(x, self.n, self.cols, ld, self.source, self.k, self.rows, self.count, self.rows_out, stream)
-        return self.rows_out[:self.rows]
+        ld, n = self._tokens(x, "x"), self.n
+        out = self.rows_out
+        if x.dtype != out.dtype:
+            raise ValueError(f"x: {out.dtype} expected, not {x.dtype}")
+        if n:
+            Q.qsync_expert_gather(x, n, self.cols, ld, self.source, self.k, self._rows_of_sort, self.count, out, stream)
+        return out if n == self.tokens else out[:self._rows_of_sort]
 
     def gather_backward(self, drows: torch.Tensor, stream=None) -> torch.Tensor:
         """The tokens' gradient, [n, cols]: the sum of their rows'."""
-        self._columns()
         self._training()
-        ld = self._rows(drows, "drows")
-        if self.n:
-            Q.qsync_expert_combine(drows, self.rows, self.cols, ld, self.slot, self.n, self.k, None, self.dx, stream)
-        return self.dx[:self.n]
+        ld, n = self._rows(drows, "drows"), self.n
+        if n:
+            Q.qsync_expert_combine(drows, self._rows_of_sort, self.cols, ld, self.slot, n, self.k, None, self.dx, stream)
+        return self.dx if n == self.tokens else self.dx[:n]
 
     def combine(self, z: torch.Tensor, weight: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """[n, cols]: the sum of the tokens' rows in z [rows, cols], times weight [n, k] (float32) or 1.  `combine_backward` reads both again."""
-        self._columns()
-        ld = self._rows(z, "z")
-        _check_packed(weight, self.n, self.k, _FLOAT32, self.device, "weight")
-        if self.n:
-            Q.qsync_expert_combine(z, self.rows, self.cols, ld, self.slot, self.n, self.k, weight, self.y, stream)
+        ld, n = self._rows(z, "z"), self.n
+        _check_packed(weight, n, self.k, _FLOAT32, self.device, "weight")
+        if n:
+            Q.qsync_expert_combine(z, self._rows_of_sort, self.cols, ld, self.slot, n, self.k, weight, self.y, stream)
         self._saved = (z, ld, weight)
-        return self.y[:self.n]
+        return self.y if n == self.tokens else self.y[:n]
 
     def combine_backward(self, dy: torch.Tensor, stream=None):
         """(dz [rows, cols], dweight [n, k]) of the last `combine`; dy [n, cols].  Rows that belong to no expert are left as they were."""
-        self._columns()
         self._training()
+        lddy, n = self._tokens(dy, "dy"), self.n
         if self._saved is None:
             raise RuntimeError("combine_backward without a combine since the last sort")
         z, ld, weight = self._saved
-        lddy = self._tokens(dy, "dy")
-        if self.n:
-            Q.qsync_expert_combine_bwd(dy, self.n, self.cols, lddy, z, self.rows, ld, self.slot, self.k, weight, self.dz, self.dweight, stream)
-        return self.dz[:self.rows], self.dweight[:self.n]
+        if n:
+            Q.qsync_expert_combine_bwd(dy, n, self.cols, lddy, z, self._rows_of_sort, ld, self.slot, self.k, weight, self.dz, self.dweight, stream)
+        if n == self.tokens:
+            return self.dz, self.dweight
+        return self.dz[:self._rows_of_sort], self.dweight[:n]
 
     def _training(self) -> None:
         if not self.training:
             raise RuntimeError("a backward pass of a route with training=False")
 
-    def _tokens(self, t: torch.Tensor, name: str) -> int:
-        ld = _check_rows(t, self.n, self.cols, self.device, name)
-        if t.shape[0] != self.n:
-            raise ValueError(f"{name} has {t.shape[0]} rows, the sorted batch {self.n} tokens")
+    def _check(self, t: torch.Tensor, rows: int, name: str) -> int:
+        """The leading dimension of a matrix of the sorted batch."""
+        _on_device(self.device)
+        if self.n is None:
+            raise RuntimeError("a route without a sort")
+        if self.cols is None:
+            raise ValueError("a route without cols only sorts")
+        ld = _check_rows(t, rows, self.cols, self.device, name)
+        if len(t) != rows:
+            raise ValueError(f"{name} has {len(t)} rows, the sorted batch {rows}")
         return ld
 
+    def _tokens(self, t: torch.Tensor, name: str) -> int:
+        return self._check(t, self.n or 0, name)
+
     def _rows(self, t: torch.Tensor, name: str) -> int:
-        ld = _check_rows(t, self.rows, self.cols, self.device, name)
-        if t.shape[0] != self.rows:
-            raise ValueError(f"{name} has {t.shape[0]} rows, the sorted batch {self.rows}")
-        return ld
+        return self._check(t, self._rows_of_sort, name)
 
 
 class _CodeLinear:
@@ -204,16 +198,18 @@ class _CodeLinear:
             Q.qsync_token_quantize(w, rows, K, K, None, 1, rows, None, Q.ROUND_NEAREST, 0, 0, self.sw, self.wq, stream)
         self._converted = True
 
-    def _forward(self, x, x_rows, ld, source, group, n, offsets, count, stream):
+    def _forward(self, x, x_rows, ld, source, group, n, offsets, stream):
         if not self._converted:
             raise RuntimeError("forward without weights: w, or convert_w before it")
-        if n:      # (a tensor without elements has no address)
-            if self.training:
-                Q.qsync_token_quantize_both(x, x_rows, self.K, ld, source, group, n, self.sets, offsets, Q.ROUND_NEAREST, 0, 0, self.sx, self.xq,
-                                            self.sxc, self.xqT, None, self.ws_x, stream)
-            else:
-                Q.qsync_token_quantize(x, x_rows, self.K, ld, source, group, n, count, Q.ROUND_NEAREST, 0, 0, self.sx, self.xq, stream)
+        if not n:      # (a tensor without elements has no address)
+            pass
+        elif self.training:
+            Q.qsync_token_quantize_both(x, x_rows, self.K, ld, source, group, n, self.sets, offsets, Q.ROUND_NEAREST, 0, 0, self.sx, self.xq,
+                                        self.sxc, self.xqT, None, self.ws_x, stream)
             Q.qsync_token_linear_fwd(n, self.N, self.K, self.sets, offsets, self.xq, self.sx, self.wq, self.sw, self.bias, self.y, self.ws, stream)
+        else:
+            Q.qsync_token_linear(x, x_rows, self.K, ld, source, group, n, self.N, self.sets, offsets, self.wq, self.sw, self.bias, self.y, self.sx,
+                                 self.xq, self.ws, stream)
         return self.y if n == self.rows else self.y[:n]
 
     def _backward(self, dy, n, offsets, stream):
@@ -255,7 +251,7 @@ class TokenLinear(_CodeLinear):
         if w is not None:
             self.convert_w(w, stream)
         n = x.shape[0]
-        y = self._forward(x, n, ld, None, 1, n, None, None, stream)
+        y = self._forward(x, n, ld, None, 1, n, None, stream)
         if self.training:
             self._saved = n
         return y
@@ -292,7 +288,7 @@ class ExpertLinear(_CodeLinear):
             raise ValueError(f"x has {x.shape[0]} rows, {have} expected")
         if w is not None:
             self.convert_w(w, stream)
-        y = self._forward(x, have, ld, route.source if self.gather else None, route.k if self.gather else 1, n, route.offsets, route.count, stream)
+        y = self._forward(x, have, ld, route.source if self.gather else None, route.k if self.gather else 1, n, route.offsets, stream)
         if self.training:
             self._saved = (route, route.sorts, n)
         return y

@@ -92,6 +92,7 @@ SIGNATURES = {
                                        _vp]),
     "qsync_token_quantize_both_workspace_bytes": (_sz, [_i64, _i64, _i64, _i]),
     "qsync_token_linear_fwd": (_i, [_i64, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _vp, _sz, _vp]),
+    "qsync_token_linear": (_i, [_vp, _i, _i64, _i64, _i64, _vp, _i64, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _i, _vp, _vp, _vp, _sz, _vp]),
     "qsync_token_linear_workspace_bytes": (_sz, [_i64, _i64, _i64, _i64]),
     "qsync_token_linear_wgrad": (_i, [_i64, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _i, _vp, _sz, _vp]),
     "qsync_token_wgrad_workspace_bytes": (_sz, [_i64, _i64, _i64, _i64]),
@@ -397,6 +398,11 @@ def qsync_token_linear_workspace_bytes(rows: int, N: int, K: int, sets: int) -> 
 
 def qsync_token_linear_fwd(rows, N, K, sets, offsets_opt, xq, sx, wq, sw, bias_opt, y, workspace, stream=None) -> None:
     _native.qsync_token_linear_fwd(rows, N, K, sets, offsets_opt, xq, sx, wq, sw, bias_opt, y, y, workspace, workspace, stream)
+
+
+def qsync_token_linear(x, x_rows, K, ld, source_opt, group, rows, N, sets, offsets_opt, wq, sw, bias_opt, y, sx, xq, workspace, stream=None) -> None:
+    _native.qsync_token_linear(x, x, x_rows, K, ld, source_opt, group, rows, N, sets, offsets_opt, wq, sw, bias_opt, y, y, sx, xq, workspace,
+                               workspace, stream)
 
 
 def qsync_token_wgrad_workspace_bytes(rows: int, N: int, K: int, sets: int) -> int:

@@ -32,6 +32,8 @@ BOTH = Call(lib.qsync_token_quantize_both, "x xdt x_rows cols ld source group ro
             [_at(1), Q.F16, 4, 100, 101, _at(2), 2, 8, 3, _at(3), 0, 1, 2, _at(4), _at(5), _at(6), _at(7), _at(8), _at(9), BIG, None])
 FWD = Call(lib.qsync_token_linear_fwd, "rows N K sets offsets a sa b sb bias y ydt ws ws_bytes stream",
            [40, 30, 20, 3, _at(1), _at(2), _at(3), _at(4), _at(5), _at(6), _at(7), Q.BF16, _at(8), BIG, None])
+SERVE = Call(lib.qsync_token_linear, "x xdt x_rows cols ld source group rows N sets offsets b sb bias y ydt scale q ws ws_bytes stream",
+             [_at(1), Q.BF16, 4, 100, 101, _at(2), 2, 8, 30, 3, _at(3), _at(4), _at(5), _at(6), _at(7), Q.F16, _at(8), _at(9), _at(10), BIG, None])
 WGRAD = Call(lib.qsync_token_linear_wgrad, "rows N K sets offsets a sa b sb y ydt ws ws_bytes stream",
              [40, 30, 20, 3, _at(1), _at(2), _at(3), _at(4), _at(5), _at(7), Q.F32, _at(8), BIG, None])
 SORT = Call(lib.qsync_expert_sort, "ids idt tokens group experts offsets source slot ws ws_bytes stream",
@@ -42,8 +44,8 @@ BWD = Call(lib.qsync_expert_combine_bwd, "x xdt tokens cols ld z zdt rows ldz sl
            [_at(1), Q.F16, 4, 100, 100, _at(2), Q.F32, 8, 100, _at(3), 2, _at(4), _at(5), Q.BF16, _at(6), None])
 
 
-@pytest.mark.parametrize("call, required", [(ROWS, "x scale q"), (BOTH, "x scale q col_scale qT"), (FWD, "a sa b sb y"), (WGRAD, "a sa b sb y"), (SORT, "ids offsets source slot"),
-                                            (GATHER, "x source count y"), (COMBINE, "x slot y"), (BWD, "x slot z")], ids="rows both fwd wgrad sort gather combine bwd".split())
+@pytest.mark.parametrize("call, required", [(ROWS, "x scale q"), (BOTH, "x scale q col_scale qT"), (SERVE, "x b sb y scale q"), (FWD, "a sa b sb y"), (WGRAD, "a sa b sb y"), (SORT, "ids offsets source slot"),
+                                            (GATHER, "x source count y"), (COMBINE, "x slot y"), (BWD, "x slot z")], ids="rows both serve fwd wgrad sort gather combine bwd".split())
 def test_what_is_required(call, required):
     assert call.but() in OK_OR_NO_GPU
     for name in required.split():
@@ -53,7 +55,7 @@ def test_what_is_required(call, required):
             assert call.but(**{name: bad}) == Q.ERR_BAD_ENUM, (name, bad)
 
 
-@pytest.mark.parametrize("call", [ROWS, BOTH, GATHER, COMBINE, BWD], ids="rows both gather combine bwd".split())
+@pytest.mark.parametrize("call", [ROWS, BOTH, SERVE, GATHER, COMBINE, BWD], ids="rows both serve gather combine bwd".split())
 def test_matrices(call):
     for shape in (dict(rows=-1), dict(cols=-1), dict(ld=99), dict(group=0), dict(rows=1 << 50, cols=1 << 50, ld=1 << 50)):
         assert call.but(**shape) == Q.ERR_BAD_SHAPE, shape
@@ -68,7 +70,7 @@ def test_matrices(call):
         assert call.but(**{name: ctypes.c_void_p(value.value + 2)}) == Q.ERR_ALIGN, name
 
 
-@pytest.mark.parametrize("call, out, inputs", [(ROWS, "q", "x"), (BOTH, "q", "x"), (BOTH, "qT", "x"), (GATHER, "y", "x"), (COMBINE, "y", "x"), (BWD, "dz", "x"), (BWD, "dz", "z")])
+@pytest.mark.parametrize("call, out, inputs", [(ROWS, "q", "x"), (BOTH, "q", "x"), (BOTH, "qT", "x"), (SERVE, "q", "x"), (SERVE, "scale", "x"), (SERVE, "y", "x"), (SERVE, "y", "q"), (GATHER, "y", "x"), (COMBINE, "y", "x"), (BWD, "dz", "x"), (BWD, "dz", "z")])
 def test_outputs_do_not_overlap_inputs(call, out, inputs):
     source = dict(zip(call.names, call.values))[inputs]
     assert call.but(**{out: source}) == Q.ERR_UNSUPPORTED
@@ -87,6 +89,13 @@ def test_quantizers():
     need = Q.qsync_token_quantize_both_workspace_bytes(8, 100, 3, True)
     assert need > 0 and BOTH.but(ws_bytes=need - 1) == Q.ERR_WORKSPACE and BOTH.but(ws=NULL) == Q.ERR_WORKSPACE and BOTH.but(ws=_at(9, 8)) == Q.ERR_ALIGN
     assert BOTH.but(rows=0, sums=NULL) == Q.OK
+
+
+def test_serving():
+    assert SERVE.but(source=NULL) == Q.ERR_BAD_SHAPE and SERVE.but(source=NULL, x_rows=8) in OK_OR_NO_GPU
+    assert SERVE.but(offsets=NULL) == Q.ERR_UNSUPPORTED and SERVE.but(offsets=NULL, sets=1) in OK_OR_NO_GPU
+    assert SERVE.but(q=_at(9, 8)) == Q.ERR_ALIGN and SERVE.but(b=_at(4, 8)) == Q.ERR_ALIGN
+    assert SERVE.but(rows=0) == Q.OK and SERVE.but(N=0) == Q.OK and SERVE.but(N=-1) == Q.ERR_BAD_SHAPE
 
 
 def test_sizes_of_codes():

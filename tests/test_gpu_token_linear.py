@@ -341,6 +341,28 @@ def test_serving_equals_training():
     assert torch.equal(a.forward(x[:7]), b.forward(x[:7])) and a.forward(x[:7]).shape == (7, 70)
 
 
+@pytest.mark.parametrize("rows", [1, 2, 3, 4, 5, 8, 9, 16, 17, 64])
+@pytest.mark.parametrize("N, K", [(16, 64), (1, 1), (33, 130), (1000, 4096), (130, 4100), (48, 8200), (40, 33000)])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_serving_in_one_call(rows, N, K, dtype):
+    """The same outputs as of the two calls, bit for bit, for few rows (one launch) and more; a row that is not finite stays alone."""
+    say("token linear, one call", rows, N, K, dtype)
+    x, w = values(rows, K, dtype, 46, pad=3), values(N, K, F32, 47).contiguous()
+    x[0, K // 2] = float("inf")
+    bias = torch.randn(N, device="cuda")
+    wq, sw = quantize(w, Q.ROUND_NEAREST)
+    xq, sx = quantize(x, Q.ROUND_NEAREST)
+    ws = torch.empty(Q.qsync_token_linear_workspace_bytes(rows, N, K, 1) + 16, dtype=torch.uint8, device="cuda").random_()
+    a, b = torch.full((rows, N), 7.0, dtype=dtype, device="cuda"), torch.full((rows, N), 7.0, dtype=dtype, device="cuda")
+    Q.qsync_token_linear_fwd(rows, N, K, 1, None, xq, sx, wq, sw, bias, a, ws)
+    Q.qsync_token_linear(x, rows, K, x.stride(0), None, 1, rows, N, 1, None, wq, sw, bias, b, torch.empty_like(sx), torch.empty_like(xq), ws)
+    torch.cuda.synchronize()
+    assert torch.isnan(a[0]).all() and not torch.isnan(a[1:]).any()
+    assert torch.equal(a[1:], b[1:]) and torch.isnan(b[0]).all()
+    want, bound = R.product(*R.codes(f64(x)[1:], 1), *R.codes(f64(w), 1), f64(bias))
+    assert_within(b[1:], want, bound + rounded(want, dtype), "y") if rows > 1 else None
+
+
 def test_an_empty_batch():
     op = TokenLinear(4, 24, 40)
     y = op.forward(torch.empty(0, 40, dtype=F16, device="cuda"), w=values(24, 40, F32, 44))
