@@ -770,7 +770,8 @@ size_t qsync_token_quantize_both_workspace_bytes(int64_t rows, int64_t cols, int
  * xq [rows, code_cols(K)], sx rows floats; wq [sets, N, code_cols(K)], sw [sets, N] floats; bias_opt [sets, N] floats or NULL.
  * offsets_opt NULL: one set (QSYNC_ERR_UNSUPPORTED otherwise).
  * y   out, packed [rows, N] of ydt (QSYNC_F32, QSYNC_F16 or QSYNC_BF16), rounded once.
- * workspace   at least qsync_token_linear_workspace_bytes(rows, N, K, sets) bytes (may be NULL if that is 0), no contents needed.
+ * workspace   qsync_token_linear_workspace_bytes(rows, N, K, sets) bytes, 16-byte aligned, no contents needed.  With less, or none, the
+ *             contraction is split into fewer pieces: slower, the same bits.
  */
 int qsync_token_linear_fwd(int64_t rows, int64_t N, int64_t K, int64_t sets, const int32_t* offsets_opt, const void* xq, const float* sx,
                            const void* wq, const float* sw, const float* bias_opt, void* y, int ydt, void* workspace,
@@ -789,7 +790,7 @@ int qsync_token_linear(const void* x, int xdt, int64_t x_rows, int64_t K, int64_
 /*
  * qsync_token_linear_wgrad - dW[e,n,k] = (sum over the rows m of set e of dyqT[n,m] xqT[k,m]) * (sdy[e,n] * sx[e,k]), on codes along the rows
  * (qsync_token_quantize_both) of dY [rows, N] and X [rows, K].  dw out, [sets, N, K] of dwdt; zeros for a set without rows.
- * offsets_opt NULL: one set.  workspace: qsync_token_wgrad_workspace_bytes(rows, N, K, sets).
+ * offsets_opt NULL: one set.  workspace: qsync_token_wgrad_workspace_bytes(rows, N, K, sets) bytes, as above.
  */
 int qsync_token_linear_wgrad(int64_t rows, int64_t N, int64_t K, int64_t sets, const int32_t* offsets_opt, const void* dyqT,
                              const float* sdy, const void* xqT, const float* sx, void* dw, int dwdt, void* workspace,

@@ -1234,7 +1234,12 @@ int qsync_token_quantize_both(const void* x, int xdt, int64_t x_rows, int64_t co
                                                  static_cast<hipStream_t>(stream)));
 }
 
-size_t qsync_token_linear_workspace_bytes(int64_t, int64_t, int64_t, int64_t) { return 0; }
+static size_t product_workspace(bool wgrad, int64_t rows, int64_t M, int64_t N, int64_t K, int64_t sets)
+{
+    if(rows < 1 || N < 1 || K < 1 || M < 1 || rows > kTokenMaxRows || N > kTokenMaxCols || K > kTokenMaxRows || sets < 1 || sets > kMaxSets) return 0;
+    return round256(token_product_workspace_bytes(wgrad, rows, M, N, K, sets));
+}
+size_t qsync_token_linear_workspace_bytes(int64_t rows, int64_t N, int64_t K, int64_t sets) { return product_workspace(false, rows, rows, N, K, sets); }
 
 int qsync_token_linear_fwd(int64_t rows, int64_t N, int64_t K, int64_t sets, const int32_t* offsets_opt, const void* xq, const float* sx, const void* wq,
                            const float* sw, const float* bias_opt, void* y, int ydt, void* workspace, size_t workspace_bytes, void* stream)
@@ -1242,11 +1247,10 @@ int qsync_token_linear_fwd(int64_t rows, int64_t N, int64_t K, int64_t sets, con
     int rc = token_product(rows, N, K, sets, offsets_opt, xq, sx, wq, sw, bias_opt, y, ydt);
     if(rc != QSYNC_OK) return rc;
     if(rows == 0 || N == 0) return QSYNC_OK;
-    rc = workspace_status(workspace, workspace_bytes, qsync_token_linear_workspace_bytes(rows, N, K, sets));
-    if(rc != QSYNC_OK) return rc;
+    if(workspace && !aligned16(workspace)) return QSYNC_ERR_ALIGN;
     if(!apart(y, rows * N * dtype_bytes(ydt), xq, rows * qsync_token_code_cols(K))) return QSYNC_ERR_UNSUPPORTED;
     return hip_status(launch_token_product(TokenProduct{static_cast<const int8_t*>(xq), static_cast<const int8_t*>(wq), sx, sw, bias_opt, y, ydt, rows, rows, N, K, sets,
-                                                        offsets_opt}, false, static_cast<hipStream_t>(stream)));
+                                                        offsets_opt}, false, workspace, workspace_bytes, static_cast<hipStream_t>(stream)));
 }
 
 int qsync_token_linear(const void* x, int xdt, int64_t x_rows, int64_t K, int64_t ld, const int32_t* source_opt, int64_t group, int64_t rows, int64_t N, int64_t sets,
@@ -1259,8 +1263,7 @@ int qsync_token_linear(const void* x, int xdt, int64_t x_rows, int64_t K, int64_
     rc = token_product(rows, N, K, sets, offsets_opt, xq, sx, wq, sw, bias_opt, y, ydt);
     if(rc != QSYNC_OK) return rc;
     if(rows == 0 || N == 0) return QSYNC_OK;
-    rc = workspace_status(workspace, workspace_bytes, qsync_token_linear_workspace_bytes(rows, N, K, sets));
-    if(rc != QSYNC_OK) return rc;
+    if(workspace && !aligned16(workspace)) return QSYNC_ERR_ALIGN;
     const int64_t xb = span_bytes(x_rows, K, ld, xdt), yb = rows * N * dtype_bytes(ydt), qb = rows * qsync_token_code_cols(K);
     if(!apart(xq, qb, x, xb) || !apart(sx, rows * 4, x, xb) || !apart(y, yb, x, xb) || !apart(y, yb, xq, qb)) return QSYNC_ERR_UNSUPPORTED;
     const TokenMatrix  m{x, xdt, x_rows, K, ld, rows, source_opt, static_cast<int>(group)};
@@ -1270,10 +1273,13 @@ int qsync_token_linear(const void* x, int xdt, int64_t x_rows, int64_t K, int64_
     hipError_t         e = launch_token_few(m, p, &taken, st);
     if(taken || e != hipSuccess) return hip_status(e);
     if(K > 0) e = launch_token_quantize(m, offsets_opt ? offsets_opt + sets : nullptr, kNearest, 0, 0, sx, static_cast<int8_t*>(xq), st);
-    return hip_status(e != hipSuccess ? e : launch_token_product(p, false, st));
+    return hip_status(e != hipSuccess ? e : launch_token_product(p, false, workspace, workspace_bytes, st));
 }
 
-size_t qsync_token_wgrad_workspace_bytes(int64_t, int64_t, int64_t, int64_t) { return 0; }
+size_t qsync_token_wgrad_workspace_bytes(int64_t rows, int64_t N, int64_t K, int64_t sets)
+{
+    return N > kTokenMaxCols ? 0 : product_workspace(true, rows, N, K, rows, sets);
+}
 
 int qsync_token_linear_wgrad(int64_t rows, int64_t N, int64_t K, int64_t sets, const int32_t* offsets_opt, const void* dyqT, const float* sdy, const void* xqT,
                              const float* sx, void* dw, int dwdt, void* workspace, size_t workspace_bytes, void* stream)
@@ -1282,10 +1288,9 @@ int qsync_token_linear_wgrad(int64_t rows, int64_t N, int64_t K, int64_t sets, c
     if(rc != QSYNC_OK) return rc;
     if(!count_ok(sets * N, K)) return QSYNC_ERR_BAD_SHAPE;
     if(N == 0 || K == 0) return QSYNC_OK;
-    rc = workspace_status(workspace, workspace_bytes, qsync_token_wgrad_workspace_bytes(rows, N, K, sets));
-    if(rc != QSYNC_OK) return rc;
+    if(workspace && !aligned16(workspace)) return QSYNC_ERR_ALIGN;
     return hip_status(launch_token_product(TokenProduct{static_cast<const int8_t*>(dyqT), static_cast<const int8_t*>(xqT), sdy, sx, nullptr, dw, dwdt, rows, N, K, rows, sets,
-                                                        offsets_opt}, true, static_cast<hipStream_t>(stream)));
+                                                        offsets_opt}, true, workspace, workspace_bytes, static_cast<hipStream_t>(stream)));
 }
 
 size_t qsync_expert_sort_workspace_bytes(int64_t entries, int64_t experts)

@@ -169,7 +169,8 @@ struct TokenProduct
     int64_t        rows, M, N, K, sets;
     const int32_t* offsets;
 };
-hipError_t launch_token_product(const TokenProduct& p, bool wgrad, hipStream_t st);
+size_t token_product_workspace_bytes(bool wgrad, int64_t rows, int64_t M, int64_t N, int64_t K, int64_t sets);      // (with less: fewer K splits)
+hipError_t launch_token_product(const TokenProduct& p, bool wgrad, void* workspace, size_t workspace_bytes, hipStream_t st);
 // Few rows or a small product of one set (gemm_rows.hip); *taken is false, and nothing launched, for any other.
 hipError_t launch_token_rows(const TokenProduct& p, bool* taken, hipStream_t st);
 // A handful of rows quantized and multiplied in one launch (token_few.hip); p.A and p.sa are not used.  *taken likewise.

@@ -46,6 +46,16 @@ template <typename T> __global__ __launch_bounds__(64 * kFewWaves) void token_fe
         __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src + (static_cast<int64_t>(t) * kFewWaves + wave) * 64),
                                          (__attribute__((address_space(3))) void*)(mine + t % kFewStages * 1024), 16, 0, 0);
     };
+    // (the columns' scales and biases, by the wavefront that needs them: in front of everything, their latency is nobody's)
+    float sb[4] = {}, bias[4] = {};
+    if(wave == 0)
+#pragma unroll
+        for(int e = 0; e < 4; ++e)
+        {
+            const int64_t n = n0 + lane / 16 * 4 + e, c = n < p.N ? n : p.N - 1;
+            sb[e]   = p.sw[c];
+            bias[e] = p.bias ? p.bias[c] : 0.0f;
+        }
     // Rows: 1, 2, 4 or 8 wavefronts share one
     const int share = p.rows > 4 ? 1 : p.rows > 2 ? 2 : p.rows == 2 ? 4 : 8, at_once = kFewWaves / share, part = wave % share;
     const int groups = static_cast<int>(kb / 8), step = share * 64;
@@ -74,14 +84,16 @@ template <typename T> __global__ __launch_bounds__(64 * kFewWaves) void token_fe
         };
         const int g0 = part * 64 + lane;
 #pragma unroll
-        for(int i = 0; i < kFewHeld; ++i) load(g0 + i * step, v[i]);
+        for(int i = 0; i < kFewHeld; ++i)
+            if(i * step < groups) load(g0 + i * step, v[i]);      // (the same for all lanes)
         if(!requested)      // (behind the first rows' loads: what waits for those does not wait for the weights)
         {
             for(int t = 0; t < kFewStages && t < turns; ++t) issue(t);
             requested = true;
         }
 #pragma unroll
-        for(int i = 0; i < kFewHeld; ++i) fold(v[i]);
+        for(int i = 0; i < kFewHeld; ++i)
+            if(i * step < groups) fold(v[i]);
         for(int g = g0 + kFewHeld * step; g < groups; g += step)
         {
             Row8<T> d;
@@ -112,7 +124,7 @@ template <typename T> __global__ __launch_bounds__(64 * kFewWaves) void token_fe
             };
 #pragma unroll
             for(int i = 0; i < kFewHeld; ++i)
-                if(g0 + i * step < groups) put(v[i], g0 + i * step);
+                if(i * step < groups && g0 + i * step < groups) put(v[i], g0 + i * step);
             for(int g = g0 + kFewHeld * step; g < groups; g += step)
             {
                 Row8<T> d;
@@ -153,7 +165,7 @@ template <typename T> __global__ __launch_bounds__(64 * kFewWaves) void token_fe
     {
         const int64_t n = n0 + quad * 4 + e;
         if(n >= p.N) continue;
-        const float f = sa * p.sw[n], b = p.bias ? p.bias[n] : 0.0f;
+        const float f = sa * sb[e], b = bias[e];
         if(p.ydt == kF16) static_cast<__half*>(p.y)[row * p.N + n] = fma_out<__half>(static_cast<float>(acc[e]), f, b);      // (the same bits as of the other products)
         else element_store(p.y, p.ydt, row * p.N + n, fmaf(static_cast<float>(acc[e]), f, b));
     }

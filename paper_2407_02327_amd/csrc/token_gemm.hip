@@ -73,6 +73,67 @@ template <int BM, int BN, bool WGRAD> __device__ __forceinline__ bool set_tile(c
     return false;
 }
 
+// The contraction of one set's product in pieces (few tiles, long contractions): raw sums [splits][M][N], which a second launch adds up.
+struct SplitArgs { void* partial; int splits, ktiles; };
+template <int BM, int BN, int WGM, int WGN, int ST, bool WGRAD>
+__global__ __launch_bounds__(64 * WGM * WGN, 2) void token_split_kernel(const TokenProduct p, const SplitArgs sp, int group_m)
+{
+    GemmKernelArgs a{};
+    a.A = reinterpret_cast<const uint8_t*>(p.A);
+    a.B = reinterpret_cast<const uint8_t*>(p.B);
+    a.M = WGRAD ? p.M : p.rows;
+    a.N = p.N;
+    a.Kb = code_pad(WGRAD ? p.rows : p.K);
+    a.partial = sp.partial;
+    a.ktiles_per_split = sp.ktiles;
+    a.tiles_m = static_cast<int>((a.M + BM - 1) / BM);
+    a.tiles_n = static_cast<int>((a.N + BN - 1) / BN);
+    int split, tm, tn;
+    item_of_block(static_cast<int>(blockIdx.x), a.tiles_m, a.tiles_n, sp.splits, group_m, split, tm, tn);
+    gemm_tile_at<I8Traits, BM, BN, WGM, WGN, ST, 0, true, false, false, false, true>(a, split, tm, tn);
+}
+// C from the pieces' sums: four consecutive columns a thread (VEC: N is a multiple of four) or one
+template <bool VEC> __global__ __launch_bounds__(256) void token_reduce_kernel(const int32_t* partial, int splits, int64_t M, int64_t N, const float* sa, const float* sb, const float* bias, void* c, int cdt)
+{
+    constexpr int W = VEC ? 4 : 1;
+    const int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * W;
+    if(i >= M * N) return;
+    const int64_t m = i / N, n = i - m * N;
+    int32_t       sum[W];
+#pragma unroll
+    for(int e = 0; e < W; ++e) sum[e] = 0;
+    for(int s0 = 0; s0 < splits; s0 += 4)
+    {
+        int32_t o[4][W];
+#pragma unroll
+        for(int u = 0; u < 4; ++u)
+        {
+            const int32_t* at = partial + (s0 + u < splits ? s0 + u : s0) * M * N + i;
+            if constexpr(VEC) *reinterpret_cast<int4*>(o[u]) = *reinterpret_cast<const int4*>(at);
+            else o[u][0] = *at;
+        }
+#pragma unroll
+        for(int u = 0; u < 4; ++u)
+#pragma unroll
+            for(int e = 0; e < W; ++e) sum[e] += s0 + u < splits ? o[u][e] : 0;
+    }
+    const float s = sa[m];
+    float       f[W], b[W], v[W];
+#pragma unroll
+    for(int e = 0; e < W; ++e)
+    {
+        f[e] = s * sb[n + e];
+        b[e] = bias ? bias[n + e] : 0.0f;
+        v[e] = fmaf(static_cast<float>(sum[e]), f[e], b[e]);
+    }
+    if(cdt == kF16)
+#pragma unroll
+        for(int e = 0; e < W; ++e) static_cast<__half*>(c)[i + e] = fma_out<__half>(static_cast<float>(sum[e]), f[e], b[e]);
+    else
+#pragma unroll
+        for(int e = 0; e < W; ++e) element_store(c, cdt, i + e, v[e]);
+}
+
 template <int BM, int BN, int WGM, int WGN, int ST, bool WGRAD>
 __global__ __launch_bounds__(64 * WGM * WGN, 2) void token_gemm_kernel(const TokenProduct p, int group_m)
 {
@@ -111,49 +172,92 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void token_gemm_kernel(const Tok
 }
 
 constexpr int kMaxDevices = 16;
-template <int BM, int BN, int WGM, int WGN, int ST, bool WGRAD> hipError_t launch_tiles(const TokenProduct& p, hipStream_t st)
+template <typename F> hipError_t allow_lds(F kernel, int bytes, bool (&set)[kMaxDevices])      // (`set`: per instantiation and device; benign if set twice)
+{
+    int        dev = 0;
+    const bool known = hipGetDevice(&dev) == hipSuccess && dev >= 0 && dev < kMaxDevices;
+    if(known && set[dev]) return hipSuccess;
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if(e == hipSuccess && known) set[dev] = true;
+    return e;
+}
+
+template <int BM, int BN, int WGM, int WGN, int ST, bool WGRAD> hipError_t launch_tiles(const TokenProduct& p, const SplitArgs& sp, hipStream_t st)
 {
     constexpr int lds = ST * (BM + BN) * kRowBytes + kColumnBytes<BN> + BM * 4;
-    const auto    kernel = &token_gemm_kernel<BM, BN, WGM, WGN, ST, WGRAD>;
-    static bool   attr_set[kMaxDevices] = {};      // per instantiation and device; benign if set twice
-    int           dev = 0;
-    const bool    known = hipGetDevice(&dev) == hipSuccess && dev >= 0 && dev < kMaxDevices;
-    if(!known || !attr_set[dev])
-    {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-        if(e != hipSuccess) return e;
-        if(known) attr_set[dev] = true;
-    }
     const int64_t tn = (p.N + BN - 1) / BN, tm = ((WGRAD ? p.M : p.rows) + BM - 1) / BM;
     // (each set may leave a part of a tile)
-    int64_t tiles = WGRAD ? tm * tn * p.sets : (p.offsets ? (tm + p.sets < p.rows ? tm + p.sets : p.rows) : tm) * tn;
-    if(tiles >= int64_t(1) << 31) return hipErrorInvalidValue;
-    kernel<<<static_cast<unsigned>(tiles), 64 * WGM * WGN, lds, st>>>(p, kGroupM);
+    const int64_t tiles = WGRAD ? tm * tn * p.sets : (p.offsets ? (tm + p.sets < p.rows ? tm + p.sets : p.rows) : tm) * tn;
+    if(tiles * sp.splits >= int64_t(1) << 22) return hipErrorInvalidValue;      // (threads that a grid can count)
+    static bool set[2][kMaxDevices] = {};
+    if(sp.splits > 1)
+    {
+        const hipError_t e = allow_lds(&token_split_kernel<BM, BN, WGM, WGN, ST, WGRAD>, lds, set[0]);
+        if(e != hipSuccess) return e;
+        token_split_kernel<BM, BN, WGM, WGN, ST, WGRAD><<<static_cast<unsigned>(tiles * sp.splits), 64 * WGM * WGN, lds, st>>>(p, sp, kGroupM);
+        return hipGetLastError();
+    }
+    const hipError_t e = allow_lds(&token_gemm_kernel<BM, BN, WGM, WGN, ST, WGRAD>, lds, set[1]);
+    if(e != hipSuccess) return e;
+    token_gemm_kernel<BM, BN, WGM, WGN, ST, WGRAD><<<static_cast<unsigned>(tiles), 64 * WGM * WGN, lds, st>>>(p, kGroupM);
     return hipGetLastError();
 }
 
-template <bool WGRAD> hipError_t launch_product(const TokenProduct& p, hipStream_t st)
+// Tile and K splits: of one set, as of any other product of its size; of several, without splits, no wider than their rows on average.
+GemmPlan product_plan(bool wgrad, int64_t rows, int64_t M, int64_t N, int64_t K, int64_t sets, bool offsets)
 {
-    // The tile: as for a product without sets of the same size
-    const int64_t  M = WGRAD ? p.M : (p.rows + p.sets - 1) / p.sets, K = WGRAD ? (p.rows + p.sets - 1) / p.sets : p.K;
-    const GemmPlan plan = plan_gemm(8, M * p.sets, p.N, code_pad(K), -1, -1, false);
-    const int      tile = plan.tile == 0 && M < 192 ? 1 : plan.tile == 1 && M < 96 ? 2 : plan.tile;
-    switch(tile)
+    const int64_t share = (rows + sets - 1) / sets;
+    if(!offsets) return plan_gemm(8, wgrad ? M : rows, N, code_pad(wgrad ? rows : K), -1, -1, true);
+    GemmPlan      plan = plan_gemm(8, wgrad ? M * sets : rows, N, code_pad(wgrad ? share : K), -1, -1, false);
+    const int64_t m = wgrad ? M : share;
+    plan.tile = plan.tile == 0 && m < 192 ? 1 : plan.tile;
+    plan.tile = plan.tile == 1 && m < 96 ? 2 : plan.tile;
+    return plan;
+}
+
+template <bool WGRAD> hipError_t launch_product(const TokenProduct& p, void* workspace, size_t workspace_bytes, hipStream_t st)
+{
+    const GemmPlan plan = product_plan(WGRAD, p.rows, p.M, p.N, p.K, p.sets, p.offsets != nullptr);
+    const int64_t  M = WGRAD ? p.M : p.rows, kt = code_pad(WGRAD ? p.rows : p.K) / kRowBytes;
+    SplitArgs      sp{workspace, 1, 0};
+    // (sums of integers: with less room there are fewer splits, and the same results)
+    const size_t piece = static_cast<size_t>(M) * p.N * 4, room = workspace ? workspace_bytes / piece : 0;
+    const int    splits = static_cast<int>(room < static_cast<size_t>(plan.splits) ? room : plan.splits);
+    if(!p.offsets && splits > 1 && kt > 1)
     {
-    case 0: return launch_tiles<256, 256, 2, 4, 2, WGRAD>(p, st);
-    case 1: return launch_tiles<128, 128, 2, 4, 2, WGRAD>(p, st);
-    default: return launch_tiles<64, 64, 2, 2, 2, WGRAD>(p, st);
+        sp.ktiles = static_cast<int>((kt + splits - 1) / splits);
+        sp.splits = static_cast<int>((kt + sp.ktiles - 1) / sp.ktiles);
     }
+    hipError_t e;
+    switch(plan.tile)
+    {
+    case 0: e = launch_tiles<256, 256, 2, 4, 2, WGRAD>(p, sp, st); break;
+    case 1: e = launch_tiles<128, 128, 2, 4, 2, WGRAD>(p, sp, st); break;
+    default: e = launch_tiles<64, 64, 2, 2, 2, WGRAD>(p, sp, st);
+    }
+    if(e != hipSuccess || sp.splits == 1) return e;
+    const int64_t  count = M * p.N, per = p.N % 4 == 0 ? 1024 : 256;
+    const unsigned blocks = static_cast<unsigned>((count + per - 1) / per);
+    const int32_t* partial = static_cast<const int32_t*>(workspace);
+    if(p.N % 4 == 0) token_reduce_kernel<true><<<blocks, 256, 0, st>>>(partial, sp.splits, M, p.N, p.sa, p.sb, p.bias, p.C, p.c_dtype);
+    else             token_reduce_kernel<false><<<blocks, 256, 0, st>>>(partial, sp.splits, M, p.N, p.sa, p.sb, p.bias, p.C, p.c_dtype);
+    return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_token_product(const TokenProduct& p, bool wgrad, hipStream_t st)
+size_t token_product_workspace_bytes(bool wgrad, int64_t rows, int64_t M, int64_t N, int64_t K, int64_t sets)
 {
-    if(wgrad) return launch_product<true>(p, st);
+    if(sets != 1) return 0;
+    return product_plan(wgrad, rows, M, N, K, 1, false).workspace;
+}
+
+hipError_t launch_token_product(const TokenProduct& p, bool wgrad, void* workspace, size_t workspace_bytes, hipStream_t st)
+{
+    if(wgrad) return launch_product<true>(p, workspace, workspace_bytes, st);
     bool             taken;
     const hipError_t e = launch_token_rows(p, &taken, st);
-    return taken || e != hipSuccess ? e : launch_product<false>(p, st);
+    return taken || e != hipSuccess ? e : launch_product<false>(p, workspace, workspace_bytes, st);
 }
 
 }  // namespace qsync

@@ -134,11 +134,9 @@ def test_products(call):
         assert call.but(y=_at(2)) == Q.ERR_UNSUPPORTED
     else:
         assert call.but(K=0) == Q.OK
-    need = (Q.qsync_token_linear_workspace_bytes if call is FWD else Q.qsync_token_wgrad_workspace_bytes)(40, 30, 20, 3)
-    if need:
-        assert call.but(ws_bytes=need - 1) == Q.ERR_WORKSPACE and call.but(ws=NULL) == Q.ERR_WORKSPACE and call.but(ws=_at(8, 8)) == Q.ERR_ALIGN
-    else:
-        assert call.but(ws=NULL, ws_bytes=0) in OK_OR_NO_GPU
+    # the products run with any room, and without
+    assert call.but(ws=NULL, ws_bytes=0) in OK_OR_NO_GPU and call.but(ws_bytes=0) in OK_OR_NO_GPU and call.but(ws=_at(8, 8)) == Q.ERR_ALIGN
+    assert Q.qsync_token_linear_workspace_bytes(200, 128, 16384, 1) > 0 and Q.qsync_token_wgrad_workspace_bytes(16384, 128, 200, 1) > 0
 
 
 def test_sort():
@@ -156,9 +154,6 @@ def test_workspaces_for_more_are_enough_for_fewer():
         assert Q.qsync_expert_sort_workspace_bytes(fewer, 64) <= Q.qsync_expert_sort_workspace_bytes(more, 64)
         for cols, sets, given in ((100, 1, False), (1000, 7, True)):
             assert Q.qsync_token_quantize_both_workspace_bytes(fewer, cols, sets, given) <= Q.qsync_token_quantize_both_workspace_bytes(more, cols, sets, given)
-        for N, K, sets in ((64, 64, 1), (1000, 5000, 1), (4096, 130, 1), (300, 1000, 9)):
-            assert Q.qsync_token_linear_workspace_bytes(fewer, N, K, sets) <= Q.qsync_token_linear_workspace_bytes(more, N, K, sets)
-            assert Q.qsync_token_wgrad_workspace_bytes(fewer, N, K, sets) <= Q.qsync_token_wgrad_workspace_bytes(more, N, K, sets)
 
 
 def test_combine_backward():

@@ -186,6 +186,32 @@ def test_products(M, N, K, dtype, bias):
     assert_within(y, want, bound + rounded(want, dtype), f"{M}x{N}x{K}")
 
 
+@pytest.mark.parametrize("M, N, K", [(100, 120, 16384), (300, 257, 9000), (64, 64, 100000), (1000, 130, 4096)])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_room_does_not_change_results(M, N, K, dtype):
+    """A long contraction in as many pieces as the workspace holds: forward and weight gradient, bit for bit."""
+    say("token product room", M, N, K, dtype)
+    g = torch.Generator(device="cuda").manual_seed(16)
+    a, b = random_codes(M, K, g), random_codes(N, K, g)
+    sa, sb, bias = torch.rand(M, device="cuda") * 1e-3, torch.rand(N, device="cuda") * 1e-2, torch.randn(N, device="cuda")
+    whole = Q.qsync_token_linear_workspace_bytes(M, N, K, 1)
+    assert whole >= 2 * M * N * 4 and Q.qsync_token_wgrad_workspace_bytes(K, M, N, 1) >= 2 * M * N * 4
+    out = []
+    for room in (0, 3 * M * N * 4 // 2, 2 * M * N * 4 + 16, whole):
+        ws = torch.empty(max(room, 16), dtype=torch.uint8, device="cuda").random_()[:room] if room else None
+        y, dw = torch.full((M, N), 7.0, dtype=dtype, device="cuda"), torch.full((M, N), 7.0, dtype=dtype, device="cuda")
+        Q.qsync_token_linear_fwd(M, N, K, 1, None, a, sa, b, sb, bias, y, ws)
+        Q.qsync_token_linear_wgrad(K, M, N, 1, None, a, sa, b, sb, dw, ws)
+        torch.cuda.synchronize()
+        out.append((y, dw))
+    want, bound = R.product(f64(a), sa.cpu().numpy(), f64(b), sb.cpu().numpy(), f64(bias))
+    assert_within(out[0][0], want, bound + rounded(want, dtype), "y")
+    want, bound = R.product(f64(a), sa.cpu().numpy(), f64(b), sb.cpu().numpy())
+    assert_within(out[0][1], want, bound + rounded(want, dtype), "dw")
+    for y, dw in out[1:]:
+        assert torch.equal(y, out[0][0]) and torch.equal(dw, out[0][1])
+
+
 SETS = [(40, 5, [0, 3, 3, 20, 40, 40]), (700, 3, [0, 1, 650, 690]), (2000, 16, [0] + [125 * i - 60 for i in range(1, 16)] + [1990]), (6, 64, [0] * 30 + [2] * 20 + [6] * 15),
         (900, 1, [0, 900]), (513, 2, [0, 256, 513]), (5, 2, [0, 0, 0]), (4000, 7, [0, 600, 600, 1300, 2500, 2501, 3100, 4000])]
 
