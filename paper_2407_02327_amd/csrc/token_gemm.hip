@@ -14,7 +14,7 @@ namespace qsync {
 namespace {
 
 // The set and tile of a workgroup; false: none.  Like item_of_block, an XCD takes a contiguous share of the tiles, a set's in groups of rows.
-struct SetTile { int64_t set; int tm, tn; };
+struct SetTile { int64_t set; int tm, tn, quarter; };
 __device__ __forceinline__ int64_t item_of_xcd(int64_t lin, int64_t total)
 {
     const int64_t per = total / kNumXcd, rem = total % kNumXcd, xcd = lin % kNumXcd, loc = lin / kNumXcd;
@@ -28,27 +28,44 @@ __device__ __forceinline__ void tile_of(int64_t item, int tiles_m, int tiles_n, 
     t.tm = __builtin_amdgcn_readfirstlane(first + in % gsz);
     t.tn = __builtin_amdgcn_readfirstlane(in / gsz);
 }
-template <int BM, int BN, bool WGRAD> __device__ __forceinline__ bool set_tile(const TokenProduct& p, int group_m, SetTile& t)
+// Forward form.  `all` tiles of which the first `whole` stand for themselves; a last, incomplete round of the units (kRest tiles at most) goes
+// in quarters, four times as many workgroups, where the kernel has them: 8 experts' 16384 rows by 1024 outputs, 4096 deep, are 272 tiles,
+// 16 more than units.
+constexpr int kRest = 64;
+template <int BM, int BN, bool QUARTERS> __device__ __forceinline__ bool set_tile(const TokenProduct& p, int group_m, SetTile& t)
 {
-    const int tiles_n = static_cast<int>((p.N + BN - 1) / BN);
-    if(WGRAD || !p.offsets)
+    const int tiles_n = static_cast<int>((p.N + BN - 1) / BN), lane = threadIdx.x % kWaveSize;
+    // lanes stand for sets, 64 at a time
+    auto rows_of = [&](int64_t e) { return e < p.sets ? static_cast<int>((set_rows(p.offsets, p.rows, p.sets, e).len + BM - 1) / BM) : 0; };
+    int  tiles_m = 0;
+    if(!p.offsets) tiles_m = static_cast<int>((p.rows + BM - 1) / BM);
+    else
     {
-        const int     tiles_m = static_cast<int>(((WGRAD ? p.M : p.rows) + BM - 1) / BM);
-        const int64_t tiles = static_cast<int64_t>(tiles_m) * tiles_n, item = item_of_xcd(blockIdx.x, tiles * p.sets);
+        for(int64_t e = lane; e < p.sets; e += kWaveSize) tiles_m += rows_of(e);
+#pragma unroll
+        for(int off = kWaveSize / 2; off > 0; off >>= 1) tiles_m += __shfl_xor(tiles_m, off);
+    }
+    const int64_t all = static_cast<int64_t>(tiles_m) * tiles_n, rest = QUARTERS && all > kNumCu && all % kNumCu <= kRest ? all % kNumCu : 0, whole = all - rest;
+    int64_t       item;
+    t.quarter = -1;
+    if(static_cast<int64_t>(blockIdx.x) < (whole + kNumXcd - 1) / kNumXcd * kNumXcd)
+    {
+        item = item_of_xcd(blockIdx.x, whole);
         if(item < 0) return false;
-        t.set = uniform64(item / tiles);
-        tile_of(item - t.set * tiles, tiles_m, tiles_n, group_m, t);
+    }
+    else
+    {
+        const int64_t q = static_cast<int64_t>(blockIdx.x) - (whole + kNumXcd - 1) / kNumXcd * kNumXcd;
+        if(q >= 4 * rest) return false;
+        item      = whole + q / 4;
+        t.quarter = static_cast<int>(q % 4);
+    }
+    if(!p.offsets)
+    {
+        t.set = 0;
+        tile_of(item, tiles_m, tiles_n, group_m, t);
         return true;
     }
-    // lanes stand for sets, 64 at a time
-    const int lane = threadIdx.x % kWaveSize;
-    auto      rows_of = [&](int64_t e) { return e < p.sets ? static_cast<int>((set_rows(p.offsets, p.rows, p.sets, e).len + BM - 1) / BM) : 0; };
-    int       all = 0;
-    for(int64_t e = lane; e < p.sets; e += kWaveSize) all += rows_of(e);
-#pragma unroll
-    for(int off = kWaveSize / 2; off > 0; off >>= 1) all += __shfl_xor(all, off);
-    int64_t item = item_of_xcd(blockIdx.x, static_cast<int64_t>(all) * tiles_n);
-    if(item < 0) return false;
     for(int64_t e0 = 0; e0 < p.sets; e0 += kWaveSize)
     {
         const int n = rows_of(e0 + lane);
@@ -71,6 +88,41 @@ template <int BM, int BN, bool WGRAD> __device__ __forceinline__ bool set_tile(c
         item -= static_cast<int64_t>(__shfl(upto, kWaveSize - 1)) * tiles_n;
     }
     return false;
+}
+// Weight gradient: every set has the same tiles, but as long a contraction as it has rows.  Each XCD takes an eighth of every set's tiles (sets
+// one after the other by XCD left half of the chip waiting for the two that had the most rows), the sets with the most rows first where
+// there are at most 64 of them.
+template <int BM, int BN> __device__ __forceinline__ bool set_tile_wgrad(const TokenProduct& p, int group_m, SetTile& t)
+{
+    const int tiles_m = static_cast<int>((p.M + BM - 1) / BM), tiles_n = static_cast<int>((p.N + BN - 1) / BN), tiles = tiles_m * tiles_n;
+    const int xcd = blockIdx.x % kNumXcd, loc = blockIdx.x / kNumXcd, per = tiles / kNumXcd, rem = tiles % kNumXcd;
+    // eight sets in a row give an XCD `tiles` tiles: of the q-th, per and one more where (xcd + q) % 8 < rem
+    int q = loc / tiles * kNumXcd, in = loc % tiles, n = 0, first = 0;
+    for(;; ++q)
+    {
+        const int turn = (xcd + q) % kNumXcd;
+        n     = per + (turn < rem ? 1 : 0);
+        first = turn * per + (turn < rem ? turn : rem);
+        if(in < n) break;
+        in -= n;
+    }
+    if(q >= p.sets) return false;
+    t.set     = q;
+    t.quarter = -1;
+    if(p.offsets && p.sets <= kWaveSize)
+    {   // the q-th by length; lanes stand for sets
+        const int lane = threadIdx.x % kWaveSize;
+        const int len = lane < p.sets ? static_cast<int>(set_rows(p.offsets, p.rows, p.sets, lane).len) : -1;
+        int       rank = 0;
+        for(int e = 0; e < p.sets; ++e)
+        {
+            const int other = __builtin_amdgcn_readlane(len, e);
+            rank += other > len || (other == len && e < lane) ? 1 : 0;
+        }
+        t.set = __builtin_ctzll(__ballot(rank == q && lane < p.sets));
+    }
+    tile_of(first + in, tiles_m, tiles_n, group_m, t);
+    return true;
 }
 
 // The contraction of one set's product in pieces (few tiles, long contractions): raw sums [splits][M][N], which a second launch adds up.
@@ -137,8 +189,13 @@ template <bool VEC> __global__ __launch_bounds__(256) void token_reduce_kernel(c
 template <int BM, int BN, int WGM, int WGN, int ST, bool WGRAD>
 __global__ __launch_bounds__(64 * WGM * WGN, 2) void token_gemm_kernel(const TokenProduct p, int group_m)
 {
-    SetTile t;
-    if(!set_tile<BM, BN, WGRAD>(p, group_m, t)) return;
+    constexpr bool QUARTERS = !WGRAD && BM == 256;
+    SetTile        t;
+    if constexpr(WGRAD)
+    {
+        if(!set_tile_wgrad<BM, BN>(p, group_m, t)) return;
+    }
+    else if(!set_tile<BM, BN, QUARTERS>(p, group_m, t)) return;
     SetRows s = set_rows(p.offsets, p.rows, p.sets, t.set);
     s = {uniform64(s.first), uniform64(s.len)};
     GemmKernelArgs a{};
@@ -168,6 +225,13 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void token_gemm_kernel(const Tok
         a.col_scale = a.Kb ? p.sb + t.set * p.N : nullptr;
         a.col_bias  = p.bias ? p.bias + t.set * p.N : nullptr;
     }
+    if constexpr(QUARTERS)
+        if(t.quarter >= 0)
+        {
+            const int tm = 2 * t.tm + t.quarter / 2, tn = 2 * t.tn + t.quarter % 2;
+            if(tm * (BM / 2) < a.M && tn * (BN / 2) < a.N) gemm_tile_at<I8Traits, BM / 2, BN / 2, WGM, WGN, ST, 0, false, false, false, false, true>(a, 0, tm, tn);
+            return;
+        }
     gemm_tile_at<I8Traits, BM, BN, WGM, WGN, ST, 0, false, false, false, false, true>(a, 0, t.tm, t.tn);
 }
 
@@ -199,7 +263,9 @@ template <int BM, int BN, int WGM, int WGN, int ST, bool WGRAD> hipError_t launc
     }
     const hipError_t e = allow_lds(&token_gemm_kernel<BM, BN, WGM, WGN, ST, WGRAD>, lds, set[1]);
     if(e != hipSuccess) return e;
-    token_gemm_kernel<BM, BN, WGM, WGN, ST, WGRAD><<<static_cast<unsigned>(tiles), 64 * WGM * WGN, lds, st>>>(p, kGroupM);
+    // (a set's tiles over eight XCDs; the first tiles rounded up to the XCDs, and quarters of the last)
+    const int64_t blocks = WGRAD ? (tiles + kNumXcd - 1) / kNumXcd * kNumXcd + (p.sets % kNumXcd ? tm * tn * kNumXcd : 0) : tiles + kNumXcd + (BM == 256 ? 3 * kRest : 0);
+    token_gemm_kernel<BM, BN, WGM, WGN, ST, WGRAD><<<static_cast<unsigned>(blocks), 64 * WGM * WGN, lds, st>>>(p, kGroupM);
     return hipGetLastError();
 }
 
