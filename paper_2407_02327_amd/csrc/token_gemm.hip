@@ -14,7 +14,7 @@ namespace qsync {
 namespace {
 
 // The set and tile of a workgroup; false: none.  Like item_of_block, an XCD takes a contiguous share of the tiles, a set's in groups of rows.
-struct SetTile { int64_t set; int tm, tn, quarter; };
+struct SetTile { int64_t set; SetRows rows; int tm, tn, quarter; };
 __device__ __forceinline__ int64_t item_of_xcd(int64_t lin, int64_t total)
 {
     const int64_t per = total / kNumXcd, rem = total % kNumXcd, xcd = lin % kNumXcd, loc = lin / kNumXcd;
@@ -32,20 +32,36 @@ __device__ __forceinline__ void tile_of(int64_t item, int tiles_m, int tiles_n, 
 // in quarters, four times as many workgroups, where the kernel has them: 8 experts' 16384 rows by 1024 outputs, 4096 deep, are 272 tiles,
 // 16 more than units.
 constexpr int kRest = 64;
+// (What stands in front of a workgroup's first load is paid once a tile.  The offsets are read once, a set a lane, and the set's rows come from that lane.)
+__device__ __forceinline__ SetRows rows_of_lane(const SetRows& mine, int lane)
+{
+    return {static_cast<int64_t>(__builtin_amdgcn_readlane(static_cast<int>(mine.first), lane)), static_cast<int64_t>(__builtin_amdgcn_readlane(static_cast<int>(mine.len), lane))};
+}
 template <int BM, int BN, bool QUARTERS> __device__ __forceinline__ bool set_tile(const TokenProduct& p, int group_m, SetTile& t)
 {
     const int tiles_n = static_cast<int>((p.N + BN - 1) / BN), lane = threadIdx.x % kWaveSize;
-    // lanes stand for sets, 64 at a time
-    auto rows_of = [&](int64_t e) { return e < p.sets ? static_cast<int>((set_rows(p.offsets, p.rows, p.sets, e).len + BM - 1) / BM) : 0; };
-    int  tiles_m = 0;
+    // lanes stand for sets, 64 at a time; `mine`, `tiles`, `upto`: of the 64 looked at last, tiles of the set and of those up to it
+    SetRows mine{0, 0};
+    int     tiles = 0, upto = 0;
+    auto    look = [&](int64_t e0) {
+        mine  = e0 + lane < p.sets ? set_rows(p.offsets, p.rows, p.sets, e0 + lane) : SetRows{0, 0};
+        tiles = static_cast<int>((mine.len + BM - 1) / BM);
+        upto  = tiles;
+#pragma unroll
+        for(int off = 1; off < kWaveSize; off <<= 1)
+        {
+            const int o = __shfl_up(upto, off);
+            if(lane >= off) upto += o;
+        }
+        return __builtin_amdgcn_readlane(upto, kWaveSize - 1);
+    };
+    int tiles_m = 0;
     if(!p.offsets) tiles_m = static_cast<int>((p.rows + BM - 1) / BM);
     else
-    {
-        for(int64_t e = lane; e < p.sets; e += kWaveSize) tiles_m += rows_of(e);
-#pragma unroll
-        for(int off = kWaveSize / 2; off > 0; off >>= 1) tiles_m += __shfl_xor(tiles_m, off);
-    }
-    const int64_t all = static_cast<int64_t>(tiles_m) * tiles_n, rest = QUARTERS && all > kNumCu && all % kNumCu <= kRest ? all % kNumCu : 0, whole = all - rest;
+        for(int64_t e0 = 0; e0 < p.sets; e0 += kWaveSize) tiles_m += look(e0);
+    const int64_t all = static_cast<int64_t>(tiles_m) * tiles_n;
+    // (with three rounds and more the units do not end together, and a short last one is hidden)
+    const int64_t rest = QUARTERS && all > kNumCu && all < 3 * kNumCu && all % kNumCu <= kRest ? all % kNumCu : 0, whole = all - rest;
     int64_t       item;
     t.quarter = -1;
     if(static_cast<int64_t>(blockIdx.x) < (whole + kNumXcd - 1) / kNumXcd * kNumXcd)
@@ -60,67 +76,70 @@ template <int BM, int BN, bool QUARTERS> __device__ __forceinline__ bool set_til
         item      = whole + q / 4;
         t.quarter = static_cast<int>(q % 4);
     }
+    t.set  = 0;
+    t.rows = SetRows{0, p.rows};
     if(!p.offsets)
     {
-        t.set = 0;
         tile_of(item, tiles_m, tiles_n, group_m, t);
         return true;
     }
     for(int64_t e0 = 0; e0 < p.sets; e0 += kWaveSize)
     {
-        const int n = rows_of(e0 + lane);
-        int       upto = n;
-#pragma unroll
-        for(int off = 1; off < kWaveSize; off <<= 1)
-        {
-            const int o = __shfl_up(upto, off);
-            if(lane >= off) upto += o;
-        }
+        const int      sum = p.sets > kWaveSize ? look(e0) : tiles_m;
         const uint64_t behind = __ballot(static_cast<int64_t>(upto) * tiles_n > item);
         if(behind)
         {
-            const int first = __builtin_ctzll(behind), mine = __shfl(n, first);
-            item -= static_cast<int64_t>(__shfl(upto, first) - mine) * tiles_n;
-            t.set = uniform64(e0 + first);
-            tile_of(item, mine, tiles_n, group_m, t);
+            const int at = __builtin_ctzll(behind), n = __builtin_amdgcn_readlane(tiles, at);
+            t.set  = e0 + at;
+            t.rows = rows_of_lane(mine, at);
+            tile_of(item - static_cast<int64_t>(__builtin_amdgcn_readlane(upto, at) - n) * tiles_n, n, tiles_n, group_m, t);
             return true;
         }
-        item -= static_cast<int64_t>(__shfl(upto, kWaveSize - 1)) * tiles_n;
+        item -= static_cast<int64_t>(sum) * tiles_n;
     }
     return false;
 }
-// Weight gradient: every set has the same tiles, but as long a contraction as it has rows.  Each XCD takes an eighth of every set's tiles (sets
-// one after the other by XCD left half of the chip waiting for the two that had the most rows), the sets with the most rows first where
-// there are at most 64 of them.
+// Weight gradient: every set has the same tiles, but as long a contraction as it has rows.  An XCD takes a contiguous share of all tiles, or, with
+// few sets, an eighth of every set's, the longest sets first (16 sets of different size one after the other by XCD: half of the chip waits for the
+// two longest, 16384 rows, 4096 x 1024 in 142 us, by eighths 124).
+constexpr int kFewSets = 23;
 template <int BM, int BN> __device__ __forceinline__ bool set_tile_wgrad(const TokenProduct& p, int group_m, SetTile& t)
 {
     const int tiles_m = static_cast<int>((p.M + BM - 1) / BM), tiles_n = static_cast<int>((p.N + BN - 1) / BN), tiles = tiles_m * tiles_n;
+    t.quarter = -1;
+    if(!p.offsets || p.sets > kFewSets)
+    {
+        const int64_t item = item_of_xcd(blockIdx.x, static_cast<int64_t>(tiles) * p.sets);
+        if(item < 0) return false;
+        t.set  = uniform64(item / tiles);
+        t.rows = set_rows(p.offsets, p.rows, p.sets, t.set);
+        tile_of(item - t.set * tiles, tiles_m, tiles_n, group_m, t);
+        return true;
+    }
+    // Eight sets in a row give an XCD `tiles` tiles: of the q-th, per and one more where (xcd + q) % 8 < rem
     const int xcd = blockIdx.x % kNumXcd, loc = blockIdx.x / kNumXcd, per = tiles / kNumXcd, rem = tiles % kNumXcd;
-    // eight sets in a row give an XCD `tiles` tiles: of the q-th, per and one more where (xcd + q) % 8 < rem
-    int q = loc / tiles * kNumXcd, in = loc % tiles, n = 0, first = 0;
+    int       q = loc / tiles * kNumXcd, in = loc % tiles, first = 0;
     for(;; ++q)
     {
-        const int turn = (xcd + q) % kNumXcd;
-        n     = per + (turn < rem ? 1 : 0);
+        const int turn = (xcd + q) % kNumXcd, n = per + (turn < rem ? 1 : 0);
         first = turn * per + (turn < rem ? turn : rem);
         if(in < n) break;
         in -= n;
     }
     if(q >= p.sets) return false;
-    t.set     = q;
-    t.quarter = -1;
-    if(p.offsets && p.sets <= kWaveSize)
-    {   // the q-th by length; lanes stand for sets
-        const int lane = threadIdx.x % kWaveSize;
-        const int len = lane < p.sets ? static_cast<int>(set_rows(p.offsets, p.rows, p.sets, lane).len) : -1;
-        int       rank = 0;
-        for(int e = 0; e < p.sets; ++e)
-        {
-            const int other = __builtin_amdgcn_readlane(len, e);
-            rank += other > len || (other == len && e < lane) ? 1 : 0;
-        }
-        t.set = __builtin_ctzll(__ballot(rank == q && lane < p.sets));
+    // the q-th by length; lanes stand for sets
+    const int     lane = threadIdx.x % kWaveSize;
+    const SetRows mine = lane < p.sets ? set_rows(p.offsets, p.rows, p.sets, lane) : SetRows{0, -1};
+    const int     len = static_cast<int>(mine.len);
+    int           rank = 0;
+    for(int e = 0; e < p.sets; ++e)
+    {
+        const int other = __builtin_amdgcn_readlane(len, e);
+        rank += other > len || (other == len && e < lane) ? 1 : 0;
     }
+    const int at = __builtin_ctzll(__ballot(rank == q && lane < p.sets));
+    t.set  = at;
+    t.rows = rows_of_lane(mine, at);
     tile_of(first + in, tiles_m, tiles_n, group_m, t);
     return true;
 }
@@ -196,8 +215,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void token_gemm_kernel(const Tok
         if(!set_tile_wgrad<BM, BN>(p, group_m, t)) return;
     }
     else if(!set_tile<BM, BN, QUARTERS>(p, group_m, t)) return;
-    SetRows s = set_rows(p.offsets, p.rows, p.sets, t.set);
-    s = {uniform64(s.first), uniform64(s.len)};
+    const SetRows s{uniform64(t.rows.first), uniform64(t.rows.len)};
     GemmKernelArgs a{};
     const int64_t  os = p.c_dtype == kF32 ? 4 : 2;
     a.N        = p.N;
@@ -265,7 +283,7 @@ template <int BM, int BN, int WGM, int WGN, int ST, bool WGRAD> hipError_t launc
     if(e != hipSuccess) return e;
     // (a set's tiles over eight XCDs; the first tiles rounded up to the XCDs, and quarters of the last)
     const int64_t blocks = WGRAD ? (tiles + kNumXcd - 1) / kNumXcd * kNumXcd + (p.sets % kNumXcd ? tm * tn * kNumXcd : 0) : tiles + kNumXcd + (BM == 256 ? 3 * kRest : 0);
-    token_gemm_kernel<BM, BN, WGM, WGN, ST, WGRAD><<<static_cast<unsigned>(blocks), 64 * WGM * WGN, lds, st>>>(p, kGroupM);
+    token_gemm_kernel<BM, BN, WGM, WGN, ST, WGRAD><<<static_cast<unsigned>(blocks), 64 * WGM * WGN, lds, st>>>(p, WGRAD && p.offsets && p.sets <= kFewSets ? 4 : kGroupM);
     return hipGetLastError();
 }
 
