@@ -291,7 +291,16 @@ template <int BM, int BN, int WGM, int WGN, int ST, bool WGRAD> hipError_t launc
 GemmPlan product_plan(bool wgrad, int64_t rows, int64_t M, int64_t N, int64_t K, int64_t sets, bool offsets)
 {
     const int64_t share = (rows + sets - 1) / sets;
-    if(!offsets) return plan_gemm(8, wgrad ? M : rows, N, code_pad(wgrad ? rows : K), -1, -1, true);
+    if(!offsets)
+    {
+        const int64_t m = wgrad ? M : rows, k = code_pad(wgrad ? rows : K);
+        GemmPlan      plan = plan_gemm(8, m, N, k, -1, -1, true);
+        // Operands beyond what the caches in front of the memory hold for them: the 256 tile, which reads half as much, in K splits instead of the
+        // 128 tile without (us, operands from memory: 1024x4096 of 16384 112 -> 83, 2048x2048 of 16384 95 -> 81, 1400x1400 of 16384 73 -> 54;
+        // below, 1024x4096 of 8192 47 -> 59, 1024x1024 of 16384 34 -> 40)
+        if(plan.tile == 1 && plan.splits == 1 && (m + N) * k >= (int64_t(44) << 20)) plan = plan_gemm(8, m, N, k, 0, 0, true);
+        return plan;
+    }
     GemmPlan      plan = plan_gemm(8, wgrad ? M * sets : rows, N, code_pad(wgrad ? share : K), -1, -1, false);
     const int64_t m = wgrad ? M : share;
     plan.tile = plan.tile == 0 && m < 192 ? 1 : plan.tile;

@@ -171,14 +171,15 @@ __device__ __forceinline__ uint32_t max_of_16(uint32_t v)
     return v;
 }
 template <typename T, bool SUM>
-__global__ __launch_bounds__(256) void token_stats_kernel(TokenSource s, const int32_t* offsets, int64_t sets, uint32_t* rowpart, uint32_t* colmax, float* colsum)
+__global__ __launch_bounds__(256) void token_stats_kernel(TokenSource s, const int32_t* offsets, int64_t sets, uint32_t tiles, uint32_t* rowpart, uint32_t* colmax, float* colsum)
 {
     __shared__ uint32_t lmax[4][kStatCols];
     __shared__ float    lsum[SUM ? 4 : 1][SUM ? kStatCols : 1];
     const int     lane = threadIdx.x % 64, wave = threadIdx.x / 64, side = threadIdx.x % 16, down = threadIdx.x / 16;
-    const Chunk   c    = chunk_rows(offsets, s.rows, sets, blockIdx.x);
+    const uint32_t tile = blockIdx.x % tiles, chunk = blockIdx.x / tiles;
+    const Chunk    c = chunk_rows(offsets, s.rows, sets, chunk);
     if(c.len <= 0) return;
-    const int64_t col = static_cast<int64_t>(blockIdx.y) * kStatCols + side * 8;
+    const int64_t col = static_cast<int64_t>(tile) * kStatCols + side * 8;
     constexpr int N = kCodePad / 16;
     Row8<T>       v[N];
     bool          there[N];
@@ -211,7 +212,7 @@ __global__ __launch_bounds__(256) void token_stats_kernel(TokenSource s, const i
             if constexpr(SUM) sum[j] += e[j];
         }
         rm = max_of_16(rm);
-        if(side == 0 && down + i * 16 < c.len) rowpart[blockIdx.y * s.rows + c.row0 + down + i * 16] = rm;
+        if(side == 0 && down + i * 16 < c.len) rowpart[tile * s.rows + c.row0 + down + i * 16] = rm;
     }
 #pragma unroll
     for(int j = 0; j < 8; ++j)
@@ -230,10 +231,10 @@ __global__ __launch_bounds__(256) void token_stats_kernel(TokenSource s, const i
     }
     __syncthreads();
     const int     i  = threadIdx.x;
-    const int64_t at = static_cast<int64_t>(blockIdx.y) * kStatCols + i;
+    const int64_t at = static_cast<int64_t>(tile) * kStatCols + i;
     if(i >= kStatCols || at >= s.cols) return;
-    colmax[blockIdx.x * s.cols + at] = max(max(lmax[0][i], lmax[1][i]), max(lmax[2][i], lmax[3][i]));
-    if constexpr(SUM) colsum[blockIdx.x * s.cols + at] = (lsum[0][i] + lsum[1][i]) + (lsum[2][i] + lsum[3][i]);
+    colmax[chunk * s.cols + at] = max(max(lmax[0][i], lmax[1][i]), max(lmax[2][i], lmax[3][i]));
+    if constexpr(SUM) colsum[chunk * s.cols + at] = (lsum[0][i] + lsum[1][i]) + (lsum[2][i] + lsum[3][i]);
 }
 
 // Scales and inverse scales of the rows (workgroups behind `col_blocks`) and of the sets' columns: sixteen threads fold a column's chunks,
@@ -302,16 +303,18 @@ __global__ __launch_bounds__(256) void token_scales_kernel(const int32_t* offset
     if constexpr(SUM) sum_out[e * cols + c] = sum;
 }
 
+// (Both passes walk the matrix row after row, the second one from its end: what the first one read last still lies in front of the memory.)
 // 128 positions x 64 columns a workgroup: a thread has four rows of eight columns, whose codes along the columns leave as words of four rows.
 template <typename T, int RND>
-__global__ __launch_bounds__(256) void token_codes_kernel(TokenSource s, const int32_t* offsets, int64_t sets, uint64_t seed, uint64_t offset, const float* row_inv,
-                                                          const float* col_inv, int8_t* q, int8_t* qT)
+__global__ __launch_bounds__(256) void token_codes_kernel(TokenSource s, const int32_t* offsets, int64_t sets, uint32_t tiles, uint64_t seed, uint64_t offset,
+                                                          const float* row_inv, const float* col_inv, int8_t* q, int8_t* qT)
 {
     __shared__ uint32_t lds[64 * 33];
-    const Chunk   c = chunk_rows(offsets, s.rows, sets, blockIdx.x);
+    const uint32_t back = gridDim.x - 1 - blockIdx.x, tile = back % tiles;
+    const Chunk    c = chunk_rows(offsets, s.rows, sets, back / tiles);
     if(c.len <= 0) return;
     const int     cg = threadIdx.x % 8, rq = threadIdx.x / 8;
-    const int64_t col0 = static_cast<int64_t>(blockIdx.y) * 64, col = col0 + cg * 8, per_row = (s.cols + 7) / 8, qcols = code_pad(s.cols);
+    const int64_t col0 = static_cast<int64_t>(tile) * 64, col = col0 + cg * 8, per_row = (s.cols + 7) / 8, qcols = code_pad(s.cols);
     float         ci[8];
 #pragma unroll
     for(int j = 0; j < 8; ++j) ci[j] = col + j < s.cols ? col_inv[c.set * s.cols + col + j] : 0.0f;
@@ -385,13 +388,14 @@ hipError_t launch_both(const TokenSource& s, int64_t sets, const int32_t* offset
     float *             ri = reinterpret_cast<float*>(base + w.row_inv), *ci = reinterpret_cast<float*>(base + w.col_inv), *sm = reinterpret_cast<float*>(base + w.colsum);
     const unsigned      chunks = static_cast<unsigned>(code_positions(s.rows, sets, offsets != nullptr) / kCodePad);
     const unsigned      tiles = static_cast<unsigned>((s.cols + kStatCols - 1) / kStatCols);
-    if(colsum) token_stats_kernel<T, true><<<dim3(chunks, tiles), 256, 0, st>>>(s, offsets, sets, rowpart, cm, sm);
-    else       token_stats_kernel<T, false><<<dim3(chunks, tiles), 256, 0, st>>>(s, offsets, sets, rowpart, cm, sm);
+    if(colsum) token_stats_kernel<T, true><<<chunks * tiles, 256, 0, st>>>(s, offsets, sets, tiles, rowpart, cm, sm);
+    else       token_stats_kernel<T, false><<<chunks * tiles, 256, 0, st>>>(s, offsets, sets, tiles, rowpart, cm, sm);
     const int64_t  col_blocks = sets * ((s.cols + 15) / 16);
     const unsigned blocks = static_cast<unsigned>(col_blocks + (s.rows + 255) / 256);
     if(colsum) token_scales_kernel<true><<<blocks, 256, 0, st>>>(offsets, s.rows, s.cols, sets, col_blocks, static_cast<int>(tiles), rowpart, cm, sm, row_scale, ri, col_scale, ci, colsum);
     else       token_scales_kernel<false><<<blocks, 256, 0, st>>>(offsets, s.rows, s.cols, sets, col_blocks, static_cast<int>(tiles), rowpart, cm, nullptr, row_scale, ri, col_scale, ci, nullptr);
-    token_codes_kernel<T, RND><<<dim3(chunks, static_cast<unsigned>(code_pad(s.cols) / 64)), 256, 0, st>>>(s, offsets, sets, seed, offset, ri, ci, q, qT);
+    const unsigned wide = static_cast<unsigned>(code_pad(s.cols) / 64);
+    token_codes_kernel<T, RND><<<chunks * wide, 256, 0, st>>>(s, offsets, sets, wide, seed, offset, ri, ci, q, qT);
     return hipGetLastError();
 }
 
