@@ -764,6 +764,15 @@ int qsync_token_quantize_both(const void* x, int xdt, int64_t x_rows, int64_t co
 size_t qsync_token_quantize_both_workspace_bytes(int64_t rows, int64_t cols, int64_t sets, int with_offsets);
 
 /*
+ * qsync_token_convert - qsync_token_quantize_both (to nearest, without sums) of the activation x -> sx, xq, sxc, xqT and of the weights
+ * w [sets, N, K] (packed, wdt) -> sw, wq, swc, wqT, each pass of the two in one launch: what a training step's forward pass starts with.  Results,
+ * arguments and errors as of the two calls, whose workspaces may not overlap.
+ */
+int qsync_token_convert(const void* x, int xdt, int64_t x_rows, int64_t K, int64_t ld, const int32_t* source_opt, int64_t group, int64_t rows,
+                        int64_t sets, const int32_t* offsets_opt, float* sx, void* xq, float* sxc, void* xqT, const void* w, int wdt, int64_t N,
+                        float* sw, void* wq, float* swc, void* wqT, void* ws_x, size_t ws_x_bytes, void* ws_w, size_t ws_w_bytes, void* stream);
+
+/*
  * qsync_token_linear_fwd - Y = X W^T + b on codes, with the scales of both in the epilogue:
  *   acc[m,n] = sum_k xq[m,k] wq[e,n,k]  (int32, wraps mod 2^32)        Y[m,n] = float(acc) * (sx[m] * sw[e,n]) + bias[e,n]
  * e is the set that row m belongs to.  The data gradient is this call on the codes of dY and the transposed codes of the weights.
@@ -796,6 +805,16 @@ int qsync_token_linear_wgrad(int64_t rows, int64_t N, int64_t K, int64_t sets, c
                              const float* sdy, const void* xqT, const float* sx, void* dw, int dwdt, void* workspace,
                              size_t workspace_bytes, void* stream);
 size_t qsync_token_wgrad_workspace_bytes(int64_t rows, int64_t N, int64_t K, int64_t sets);
+
+/*
+ * qsync_token_linear_bwd - both gradients of a linear operator: qsync_token_linear_fwd of (dyq, sdy) and the transposed codes of the weights
+ * (wqT [sets][K][code_cols(N)], swc [sets, K]) into dx [rows, K], and qsync_token_linear_wgrad of (dyqT, sdyc [sets, N]) and (xqT, sxc [sets, K])
+ * into dw [sets, N, K], with the same bits, in one launch where both are small.  workspace: as of the two calls, one after the other.
+ */
+int qsync_token_linear_bwd(int64_t rows, int64_t N, int64_t K, int64_t sets, const int32_t* offsets_opt, const void* dyq, const float* sdy,
+                           const void* wqT, const float* swc, const void* dyqT, const float* sdyc, const void* xqT, const float* sxc, void* dx,
+                           int dxdt, void* dw, int dwdt, void* workspace, size_t workspace_bytes, void* stream);
+size_t qsync_token_linear_bwd_workspace_bytes(int64_t rows, int64_t N, int64_t K, int64_t sets);
 
 /*
  * qsync_expert_sort - the rows of a batch sorted by expert.  ids packed [tokens, group] of idt (QSYNC_I32 or QSYNC_I64): the experts that

@@ -1229,9 +1229,48 @@ int qsync_token_quantize_both(const void* x, int xdt, int64_t x_rows, int64_t co
     if(rc != QSYNC_OK) return rc;
     const int64_t xb = span_bytes(x_rows, cols, ld, xdt);
     if(!apart(q, rows * qsync_token_code_cols(cols), x, xb) || !apart(qT, qsync_token_code_rows(rows, sets, offsets_opt != nullptr) * cols, x, xb)) return QSYNC_ERR_UNSUPPORTED;
-    return hip_status(launch_token_quantize_both(TokenMatrix{x, xdt, x_rows, cols, ld, rows, source_opt, static_cast<int>(group)}, sets, offsets_opt, rnd, philox_seed,
-                                                 philox_offset, row_scale, static_cast<int8_t*>(q), col_scale, static_cast<int8_t*>(qT), colsum_opt, workspace,
-                                                 static_cast<hipStream_t>(stream)));
+    return hip_status(launch_token_quantize_both(TokenMatrix{x, xdt, x_rows, cols, ld, rows, source_opt, static_cast<int>(group)},
+                                                 TokenBoth{sets, offsets_opt, row_scale, static_cast<int8_t*>(q), col_scale, static_cast<int8_t*>(qT), colsum_opt, workspace}, rnd,
+                                                 philox_seed, philox_offset, static_cast<hipStream_t>(stream)));
+}
+
+int qsync_token_convert(const void* x, int xdt, int64_t x_rows, int64_t K, int64_t ld, const int32_t* source_opt, int64_t group, int64_t rows, int64_t sets,
+                        const int32_t* offsets_opt, float* sx, void* xq, float* sxc, void* xqT, const void* w, int wdt, int64_t N, float* sw, void* wq, float* swc, void* wqT,
+                        void* ws_x, size_t ws_x_bytes, void* ws_w, size_t ws_w_bytes, void* stream)
+{
+    if(!sx || !xq || !sxc || !xqT || !sw || !wq || !swc || !wqT) return QSYNC_ERR_NULL;
+    if(sets < 0 || N < 0) return QSYNC_ERR_BAD_SHAPE;
+    if(sets < 1 || sets > kMaxSets || N > kTokenMaxCols || sets * N > kTokenMaxRows) return QSYNC_ERR_UNSUPPORTED;
+    const int64_t wrows = sets * N;
+    const int     rx = token_matrix(x, xdt, x_rows, K, ld, source_opt, group, rows, QSYNC_ROUND_NEAREST);
+    if(rx < 0) return rx;
+    const int rw = token_matrix(w, wdt, wrows, K, K, nullptr, 1, wrows, QSYNC_ROUND_NEAREST);
+    if(rw < 0) return rw;
+    const int sc = token_sets(rows, sets, offsets_opt);
+    if(sc != QSYNC_OK) return sc;
+    // an operand without elements: the other by itself
+    if(rx == 1)
+        return rw == 1 ? QSYNC_OK
+                       : qsync_token_quantize_both(w, wdt, wrows, K, K, nullptr, 1, wrows, sets, nullptr, QSYNC_ROUND_NEAREST, 0, 0, sw, wq, swc, wqT, nullptr, ws_w, ws_w_bytes, stream);
+    if(rw == 1)
+        return qsync_token_quantize_both(x, xdt, x_rows, K, ld, source_opt, group, rows, sets, offsets_opt, QSYNC_ROUND_NEAREST, 0, 0, sx, xq, sxc, xqT, nullptr, ws_x, ws_x_bytes, stream);
+    if(!on_16({xq, xqT, wq, wqT}) || !floats_aligned({sx, sxc, sw, swc}) || !ints_aligned({offsets_opt})) return QSYNC_ERR_ALIGN;
+    int rc = workspace_status(ws_x, ws_x_bytes, qsync_token_quantize_both_workspace_bytes(rows, K, sets, offsets_opt != nullptr));
+    if(rc == QSYNC_OK) rc = workspace_status(ws_w, ws_w_bytes, qsync_token_quantize_both_workspace_bytes(wrows, K, sets, 0));
+    if(rc != QSYNC_OK) return rc;
+    const int64_t xb = span_bytes(x_rows, K, ld, xdt), wb = wrows * K * dtype_bytes(wdt), qb = rows * qsync_token_code_cols(K), qtb = qsync_token_code_rows(rows, sets, offsets_opt != nullptr) * K;
+    const int64_t vb = wrows * qsync_token_code_cols(K), vtb = qsync_token_code_rows(wrows, sets, 0) * K;
+    for(const void* in : {x, w})
+    {
+        const int64_t n = x == w ? (xb > wb ? xb : wb) : in == x ? xb : wb;
+        if(!apart(xq, qb, in, n) || !apart(xqT, qtb, in, n) || !apart(wq, vb, in, n) || !apart(wqT, vtb, in, n)) return QSYNC_ERR_UNSUPPORTED;
+    }
+    // (both parts of a pass run at once, in either's buffers)
+    if(!apart(ws_x, static_cast<int64_t>(ws_x_bytes), ws_w, static_cast<int64_t>(ws_w_bytes))) return QSYNC_ERR_UNSUPPORTED;
+    return hip_status(launch_token_quantize_pair(TokenMatrix{x, xdt, x_rows, K, ld, rows, source_opt, static_cast<int>(group)},
+                                                 TokenBoth{sets, offsets_opt, sx, static_cast<int8_t*>(xq), sxc, static_cast<int8_t*>(xqT), nullptr, ws_x},
+                                                 TokenMatrix{w, wdt, wrows, K, K, wrows, nullptr, 1},
+                                                 TokenBoth{sets, nullptr, sw, static_cast<int8_t*>(wq), swc, static_cast<int8_t*>(wqT), nullptr, ws_w}, static_cast<hipStream_t>(stream)));
 }
 
 static size_t product_workspace(bool wgrad, int64_t rows, int64_t M, int64_t N, int64_t K, int64_t sets)
@@ -1291,6 +1330,43 @@ int qsync_token_linear_wgrad(int64_t rows, int64_t N, int64_t K, int64_t sets, c
     if(workspace && !aligned16(workspace)) return QSYNC_ERR_ALIGN;
     return hip_status(launch_token_product(TokenProduct{static_cast<const int8_t*>(dyqT), static_cast<const int8_t*>(xqT), sdy, sx, nullptr, dw, dwdt, rows, N, K, rows, sets,
                                                         offsets_opt}, true, workspace, workspace_bytes, static_cast<hipStream_t>(stream)));
+}
+
+size_t qsync_token_linear_bwd_workspace_bytes(int64_t rows, int64_t N, int64_t K, int64_t sets)
+{
+    const size_t x = qsync_token_linear_workspace_bytes(rows, K, N, sets), w = qsync_token_wgrad_workspace_bytes(rows, N, K, sets);
+    return x > w ? x : w;
+}
+
+int qsync_token_linear_bwd(int64_t rows, int64_t N, int64_t K, int64_t sets, const int32_t* offsets_opt, const void* dyq, const float* sdy, const void* wqT,
+                           const float* swc, const void* dyqT, const float* sdyc, const void* xqT, const float* sxc, void* dx, int dxdt, void* dw, int dwdt,
+                           void* workspace, size_t workspace_bytes, void* stream)
+{
+    int rc = token_product(rows, K, N, sets, offsets_opt, dyq, sdy, wqT, swc, nullptr, dx, dxdt);
+    if(rc == QSYNC_OK) rc = token_product(rows, N, K, sets, offsets_opt, dyqT, sdyc, xqT, sxc, nullptr, dw, dwdt);
+    if(rc != QSYNC_OK) return rc;
+    if(!count_ok(sets * N, K)) return QSYNC_ERR_BAD_SHAPE;
+    if(workspace && !aligned16(workspace)) return QSYNC_ERR_ALIGN;
+    const int64_t xb = rows * K * dtype_bytes(dxdt), wb = sets * N * K * dtype_bytes(dwdt), positions = qsync_token_code_rows(rows, sets, offsets_opt != nullptr);
+    // (the two run at once: neither may write what the other reads)
+    for(const void* out : {dx, dw})
+    {
+        const int64_t n = dx == dw ? (xb > wb ? xb : wb) : out == dx ? xb : wb;
+        if(!apart(out, n, dyq, rows * qsync_token_code_cols(N)) || !apart(out, n, wqT, qsync_token_code_rows(sets * N, sets, 0) * K) || !apart(out, n, dyqT, positions * N)
+           || !apart(out, n, xqT, positions * K))
+            return QSYNC_ERR_UNSUPPORTED;
+    }
+    if(!apart(dx, xb, dw, wb)) return QSYNC_ERR_UNSUPPORTED;
+    const TokenProduct x{static_cast<const int8_t*>(dyq), static_cast<const int8_t*>(wqT), sdy, swc, nullptr, dx, dxdt, rows, rows, K, N, sets, offsets_opt};
+    const TokenProduct w{static_cast<const int8_t*>(dyqT), static_cast<const int8_t*>(xqT), sdyc, sxc, nullptr, dw, dwdt, rows, N, K, rows, sets, offsets_opt};
+    const hipStream_t  st = static_cast<hipStream_t>(stream);
+    if(rows == 0 || N == 0 || K == 0)
+    {
+        if(N == 0 || K == 0)      // an empty contraction of the data gradient: zeros
+            return rows > 0 && K > 0 ? hip_status(launch_token_product(x, false, workspace, workspace_bytes, st)) : QSYNC_OK;
+        return hip_status(launch_token_product(w, true, workspace, workspace_bytes, st));
+    }
+    return hip_status(launch_token_gradients(x, w, workspace, workspace_bytes, st));
 }
 
 size_t qsync_expert_sort_workspace_bytes(int64_t entries, int64_t experts)

@@ -303,7 +303,7 @@ PyMethodDef methods[] = {
     ENTRY(qsync_conv3x3_wgrad), ENTRY(qsync_conv3x3_prepare_weights), ENTRY(qsync_conv3x3_wflip), ENTRY(qsync_im2col3x3_i8),
     ENTRY(qsync_prepare_weights), ENTRY(qsync_dequantize), ENTRY_WIDE(qsync_layernorm_fwd), ENTRY_WIDE(qsync_layernorm_bwd),
     ENTRY_WIDE(qsync_token_logprobs), ENTRY_WIDE(qsync_token_logprobs_bwd), ENTRY_WIDE(qsync_distill_topk),
-    ENTRY_WIDE(qsync_token_quantize), ENTRY_WIDE(qsync_token_quantize_both), ENTRY_WIDE(qsync_token_linear), ENTRY_WIDE(qsync_token_linear_fwd), ENTRY_WIDE(qsync_token_linear_wgrad),
+    ENTRY_WIDE(qsync_token_quantize), ENTRY_WIDE(qsync_token_quantize_both), ENTRY_WIDE(qsync_token_convert), ENTRY_WIDE(qsync_token_linear), ENTRY_WIDE(qsync_token_linear_fwd), ENTRY_WIDE(qsync_token_linear_wgrad), ENTRY_WIDE(qsync_token_linear_bwd),
     ENTRY_WIDE(qsync_expert_sort), ENTRY_WIDE(qsync_expert_gather), ENTRY_WIDE(qsync_expert_combine), ENTRY_WIDE(qsync_expert_combine_bwd), {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -181,17 +181,23 @@ int rows_columns(const GemmProblem& p)
 
 }  // namespace
 
-hipError_t launch_token_rows(const TokenProduct& p, bool* taken, hipStream_t st)
+static int token_rows_columns(const TokenProduct& p)
 {
     GemmProblem shape{};
     shape.prec = 8; shape.M = p.rows; shape.N = p.N; shape.K = code_pad(p.K);
-    const int columns = p.offsets || p.sets != 1 || p.K == 0 ? 0 : rows_columns(shape);
+    return p.offsets || p.sets != 1 || p.K == 0 ? 0 : rows_columns(shape);
+}
+bool token_rows_takes(const TokenProduct& p) { return token_rows_columns(p) != 0; }
+
+hipError_t launch_token_rows(const TokenProduct& p, bool* taken, hipStream_t st)
+{
+    const int columns = token_rows_columns(p);
     *taken = columns != 0;
     if(!*taken) return hipSuccess;
     GemmKernelArgs a{};
     a.A = reinterpret_cast<const uint8_t*>(p.A);
     a.B = reinterpret_cast<const uint8_t*>(p.B);
-    a.M = p.rows; a.N = p.N; a.Kb = shape.K;
+    a.M = p.rows; a.N = p.N; a.Kb = code_pad(p.K);
     a.C = p.C; a.c_is_f16 = p.c_dtype == kF16 ? 1 : p.c_dtype == kBF16 ? 2 : 0;
     a.row_scale = p.sa; a.col_scale = p.sb; a.col_bias = p.bias;
     return launch_rows<I8Traits, true>(a, columns, st);

@@ -156,8 +156,19 @@ struct TokenMatrix      // rows of x (kF32, kF16, kBF16), or what `source` takes
 };
 hipError_t launch_token_quantize(const TokenMatrix& m, const int32_t* count, int rnd, uint64_t seed, uint64_t offset, float* scale, int8_t* q, hipStream_t st);
 size_t token_both_workspace_bytes(int64_t rows, int64_t cols, int64_t sets, bool offsets);
-hipError_t launch_token_quantize_both(const TokenMatrix& m, int64_t sets, const int32_t* offsets, int rnd, uint64_t seed, uint64_t offset, float* row_scale, int8_t* q,
-                                      float* col_scale, int8_t* qT, float* colsum, void* workspace, hipStream_t st);
+struct TokenBoth      // the sets of a matrix's rows, and what its codes along rows and columns go to; colsum nullptr: no sums
+{
+    int64_t        sets;
+    const int32_t* offsets;
+    float*         row_scale;
+    int8_t*        q;
+    float*         col_scale;
+    int8_t*        qT;
+    float*         colsum;
+    void*          workspace;      // token_both_workspace_bytes
+};
+hipError_t launch_token_quantize_both(const TokenMatrix& m, const TokenBoth& o, int rnd, uint64_t seed, uint64_t offset, hipStream_t st);
+hipError_t launch_token_quantize_pair(const TokenMatrix& m, const TokenBoth& o, const TokenMatrix& m2, const TokenBoth& o2, hipStream_t st);      // to nearest, no sums
 // Forward pass, data gradient: A [rows, code_pad(K)], B [sets][N][code_pad(K)], C [rows, N].  Weight gradient: A and B hold codes along
 // `rows` as token_quantize_both leaves them, of M and N columns; C [sets][M][N].  sa: of A's rows ([sets][M]), sb [sets][N].
 struct TokenProduct
@@ -171,8 +182,11 @@ struct TokenProduct
 };
 size_t token_product_workspace_bytes(bool wgrad, int64_t rows, int64_t M, int64_t N, int64_t K, int64_t sets);      // (with less: fewer K splits)
 hipError_t launch_token_product(const TokenProduct& p, bool wgrad, void* workspace, size_t workspace_bytes, hipStream_t st);
+// The data gradient x (forward form) and the weight gradient w of one operator, in one launch where both are small.
+hipError_t launch_token_gradients(const TokenProduct& x, const TokenProduct& w, void* workspace, size_t workspace_bytes, hipStream_t st);
 // Few rows or a small product of one set (gemm_rows.hip); *taken is false, and nothing launched, for any other.
 hipError_t launch_token_rows(const TokenProduct& p, bool* taken, hipStream_t st);
+bool token_rows_takes(const TokenProduct& p);
 // A handful of rows quantized and multiplied in one launch (token_few.hip); p.A and p.sa are not used.  *taken likewise.
 hipError_t launch_token_few(const TokenMatrix& m, const TokenProduct& p, bool* taken, hipStream_t st);
 hipError_t launch_expert_sort(const void* ids, bool wide, int64_t n, int experts, int32_t* offsets, int32_t* source, int32_t* slot, void* workspace, hipStream_t st);

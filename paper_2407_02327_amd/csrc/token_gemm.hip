@@ -37,7 +37,7 @@ __device__ __forceinline__ SetRows rows_of_lane(const SetRows& mine, int lane)
 {
     return {static_cast<int64_t>(__builtin_amdgcn_readlane(static_cast<int>(mine.first), lane)), static_cast<int64_t>(__builtin_amdgcn_readlane(static_cast<int>(mine.len), lane))};
 }
-template <int BM, int BN, bool QUARTERS> __device__ __forceinline__ bool set_tile(const TokenProduct& p, int group_m, SetTile& t)
+template <int BM, int BN, bool QUARTERS> __device__ __forceinline__ bool set_tile(const TokenProduct& p, uint32_t block, int group_m, SetTile& t)
 {
     const int tiles_n = static_cast<int>((p.N + BN - 1) / BN), lane = threadIdx.x % kWaveSize;
     // lanes stand for sets, 64 at a time; `mine`, `tiles`, `upto`: of the 64 looked at last, tiles of the set and of those up to it
@@ -64,14 +64,14 @@ template <int BM, int BN, bool QUARTERS> __device__ __forceinline__ bool set_til
     const int64_t rest = QUARTERS && all > kNumCu && all < 3 * kNumCu && all % kNumCu <= kRest ? all % kNumCu : 0, whole = all - rest;
     int64_t       item;
     t.quarter = -1;
-    if(static_cast<int64_t>(blockIdx.x) < (whole + kNumXcd - 1) / kNumXcd * kNumXcd)
+    if(static_cast<int64_t>(block) < (whole + kNumXcd - 1) / kNumXcd * kNumXcd)
     {
-        item = item_of_xcd(blockIdx.x, whole);
+        item = item_of_xcd(block, whole);
         if(item < 0) return false;
     }
     else
     {
-        const int64_t q = static_cast<int64_t>(blockIdx.x) - (whole + kNumXcd - 1) / kNumXcd * kNumXcd;
+        const int64_t q = static_cast<int64_t>(block) - (whole + kNumXcd - 1) / kNumXcd * kNumXcd;
         if(q >= 4 * rest) return false;
         item      = whole + q / 4;
         t.quarter = static_cast<int>(q % 4);
@@ -103,13 +103,13 @@ template <int BM, int BN, bool QUARTERS> __device__ __forceinline__ bool set_til
 // few sets, an eighth of every set's, the longest sets first (16 sets of different size one after the other by XCD: half of the chip waits for the
 // two longest, 16384 rows, 4096 x 1024 in 142 us, by eighths 124).
 constexpr int kFewSets = 23;
-template <int BM, int BN> __device__ __forceinline__ bool set_tile_wgrad(const TokenProduct& p, int group_m, SetTile& t)
+template <int BM, int BN> __device__ __forceinline__ bool set_tile_wgrad(const TokenProduct& p, uint32_t block, int group_m, SetTile& t)
 {
     const int tiles_m = static_cast<int>((p.M + BM - 1) / BM), tiles_n = static_cast<int>((p.N + BN - 1) / BN), tiles = tiles_m * tiles_n;
     t.quarter = -1;
     if(!p.offsets || p.sets > kFewSets)
     {
-        const int64_t item = item_of_xcd(blockIdx.x, static_cast<int64_t>(tiles) * p.sets);
+        const int64_t item = item_of_xcd(block, static_cast<int64_t>(tiles) * p.sets);
         if(item < 0) return false;
         t.set  = uniform64(item / tiles);
         t.rows = set_rows(p.offsets, p.rows, p.sets, t.set);
@@ -117,7 +117,7 @@ template <int BM, int BN> __device__ __forceinline__ bool set_tile_wgrad(const T
         return true;
     }
     // Eight sets in a row give an XCD `tiles` tiles: of the q-th, per and one more where (xcd + q) % 8 < rem
-    const int xcd = blockIdx.x % kNumXcd, loc = blockIdx.x / kNumXcd, per = tiles / kNumXcd, rem = tiles % kNumXcd;
+    const int xcd = block % kNumXcd, loc = block / kNumXcd, per = tiles / kNumXcd, rem = tiles % kNumXcd;
     int       q = loc / tiles * kNumXcd, in = loc % tiles, first = 0;
     for(;; ++q)
     {
@@ -206,15 +206,15 @@ template <bool VEC> __global__ __launch_bounds__(256) void token_reduce_kernel(c
 }
 
 template <int BM, int BN, int WGM, int WGN, int ST, bool WGRAD>
-__global__ __launch_bounds__(64 * WGM * WGN, 2) void token_gemm_kernel(const TokenProduct p, int group_m)
+__device__ __forceinline__ void product_body(const TokenProduct& p, uint32_t block, int group_m)
 {
     constexpr bool QUARTERS = !WGRAD && BM == 256;
     SetTile        t;
     if constexpr(WGRAD)
     {
-        if(!set_tile_wgrad<BM, BN>(p, group_m, t)) return;
+        if(!set_tile_wgrad<BM, BN>(p, block, group_m, t)) return;
     }
-    else if(!set_tile<BM, BN, QUARTERS>(p, group_m, t)) return;
+    else if(!set_tile<BM, BN, QUARTERS>(p, block, group_m, t)) return;
     const SetRows s{uniform64(t.rows.first), uniform64(t.rows.len)};
     GemmKernelArgs a{};
     const int64_t  os = p.c_dtype == kF32 ? 4 : 2;
@@ -253,6 +253,19 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void token_gemm_kernel(const Tok
     gemm_tile_at<I8Traits, BM, BN, WGM, WGN, ST, 0, false, false, false, false, true>(a, 0, t.tm, t.tn);
 }
 
+template <int BM, int BN, int WGM, int WGN, int ST, bool WGRAD>
+__global__ __launch_bounds__(64 * WGM * WGN, 2) void token_gemm_kernel(const TokenProduct p, int group_m)
+{
+    product_body<BM, BN, WGM, WGN, ST, WGRAD>(p, blockIdx.x, group_m);
+}
+// Data and weight gradient side by side: each of them alone leaves units idle, and pays its own launch, first loads and drain.
+template <int BM, int BN, int WGM, int WGN, int ST>
+__global__ __launch_bounds__(64 * WGM * WGN, 2) void token_pair_kernel(const TokenProduct x, const TokenProduct w, uint32_t first, int group_x, int group_w)
+{
+    if(blockIdx.x < first) product_body<BM, BN, WGM, WGN, ST, false>(x, blockIdx.x, group_x);
+    else                   product_body<BM, BN, WGM, WGN, ST, true>(w, blockIdx.x - first, group_w);
+}
+
 constexpr int kMaxDevices = 16;
 template <typename F> hipError_t allow_lds(F kernel, int bytes, bool (&set)[kMaxDevices])      // (`set`: per instantiation and device; benign if set twice)
 {
@@ -264,12 +277,24 @@ template <typename F> hipError_t allow_lds(F kernel, int bytes, bool (&set)[kMax
     return e;
 }
 
+// The tiles that there may be at most: each set may leave a part of one.  And the workgroups for them: the first tiles rounded up to the XCDs, a
+// set's tiles shared out to eight of them, the last ones in quarters.
+template <bool WGRAD> int64_t most_tiles(const TokenProduct& p, int BM, int BN)
+{
+    const int64_t tn = (p.N + BN - 1) / BN, tm = ((WGRAD ? p.M : p.rows) + BM - 1) / BM;
+    return WGRAD ? tm * tn * p.sets : (p.offsets ? (tm + p.sets < p.rows ? tm + p.sets : p.rows) : tm) * tn;
+}
+template <bool WGRAD> int64_t blocks_of(const TokenProduct& p, int BM, int BN)
+{
+    const int64_t tiles = most_tiles<WGRAD>(p, BM, BN);
+    return WGRAD ? (tiles + kNumXcd - 1) / kNumXcd * kNumXcd + (p.sets % kNumXcd ? tiles / p.sets * kNumXcd : 0) : tiles + kNumXcd + (BM == 256 ? 3 * kRest : 0);
+}
+int wgrad_group(const TokenProduct& p) { return p.offsets && p.sets <= kFewSets ? 4 : kGroupM; }
+
 template <int BM, int BN, int WGM, int WGN, int ST, bool WGRAD> hipError_t launch_tiles(const TokenProduct& p, const SplitArgs& sp, hipStream_t st)
 {
     constexpr int lds = ST * (BM + BN) * kRowBytes + kColumnBytes<BN> + BM * 4;
-    const int64_t tn = (p.N + BN - 1) / BN, tm = ((WGRAD ? p.M : p.rows) + BM - 1) / BM;
-    // (each set may leave a part of a tile)
-    const int64_t tiles = WGRAD ? tm * tn * p.sets : (p.offsets ? (tm + p.sets < p.rows ? tm + p.sets : p.rows) : tm) * tn;
+    const int64_t tiles = most_tiles<WGRAD>(p, BM, BN);
     if(tiles * sp.splits >= int64_t(1) << 22) return hipErrorInvalidValue;      // (threads that a grid can count)
     static bool set[2][kMaxDevices] = {};
     if(sp.splits > 1)
@@ -281,9 +306,8 @@ template <int BM, int BN, int WGM, int WGN, int ST, bool WGRAD> hipError_t launc
     }
     const hipError_t e = allow_lds(&token_gemm_kernel<BM, BN, WGM, WGN, ST, WGRAD>, lds, set[1]);
     if(e != hipSuccess) return e;
-    // (a set's tiles over eight XCDs; the first tiles rounded up to the XCDs, and quarters of the last)
-    const int64_t blocks = WGRAD ? (tiles + kNumXcd - 1) / kNumXcd * kNumXcd + (p.sets % kNumXcd ? tm * tn * kNumXcd : 0) : tiles + kNumXcd + (BM == 256 ? 3 * kRest : 0);
-    token_gemm_kernel<BM, BN, WGM, WGN, ST, WGRAD><<<static_cast<unsigned>(blocks), 64 * WGM * WGN, lds, st>>>(p, WGRAD && p.offsets && p.sets <= kFewSets ? 4 : kGroupM);
+    const int64_t blocks = blocks_of<WGRAD>(p, BM, BN);
+    token_gemm_kernel<BM, BN, WGM, WGN, ST, WGRAD><<<static_cast<unsigned>(blocks), 64 * WGM * WGN, lds, st>>>(p, WGRAD ? wgrad_group(p) : kGroupM);
     return hipGetLastError();
 }
 
@@ -308,6 +332,7 @@ GemmPlan product_plan(bool wgrad, int64_t rows, int64_t M, int64_t N, int64_t K,
     return plan;
 }
 
+constexpr int64_t kPairBlocks = 4 * kNumCu * 2;
 template <bool WGRAD> hipError_t launch_product(const TokenProduct& p, void* workspace, size_t workspace_bytes, hipStream_t st)
 {
     const GemmPlan plan = product_plan(WGRAD, p.rows, p.M, p.N, p.K, p.sets, p.offsets != nullptr);
@@ -351,6 +376,23 @@ hipError_t launch_token_product(const TokenProduct& p, bool wgrad, void* workspa
     bool             taken;
     const hipError_t e = launch_token_rows(p, &taken, st);
     return taken || e != hipSuccess ? e : launch_product<false>(p, workspace, workspace_bytes, st);
+}
+
+hipError_t launch_token_gradients(const TokenProduct& x, const TokenProduct& w, void* workspace, size_t workspace_bytes, hipStream_t st)
+{
+    const GemmPlan px = product_plan(false, x.rows, x.M, x.N, x.K, x.sets, x.offsets != nullptr), pw = product_plan(true, w.rows, w.M, w.N, w.K, w.sets, w.offsets != nullptr);
+    const int64_t  first = (blocks_of<false>(x, 64, 64) + kNumXcd - 1) / kNumXcd * kNumXcd, all = first + blocks_of<true>(w, 64, 64);
+    if(px.tile >= 1 && px.splits == 1 && pw.tile >= 1 && pw.splits == 1 && all <= kPairBlocks && !token_rows_takes(x))
+    {
+        constexpr int lds = 2 * (64 + 64) * kRowBytes + kColumnBytes<64> + 64 * 4;
+        static bool   set[kMaxDevices] = {};
+        const hipError_t e = allow_lds(&token_pair_kernel<64, 64, 2, 2, 2>, lds, set);
+        if(e != hipSuccess) return e;
+        token_pair_kernel<64, 64, 2, 2, 2><<<static_cast<unsigned>(all), 64 * 4, lds, st>>>(x, w, static_cast<uint32_t>(first), kGroupM, wgrad_group(w));
+        return hipGetLastError();
+    }
+    const hipError_t e = launch_token_product(x, false, workspace, workspace_bytes, st);
+    return e != hipSuccess ? e : launch_token_product(w, true, workspace, workspace_bytes, st);
 }
 
 }  // namespace qsync

@@ -48,6 +48,38 @@ template <typename T> __device__ __forceinline__ uint32_t max8(const Row8<T>& v,
     for(int i = 0; i < 8; ++i) m = max(m, abs_bits(e[i]));
     return m;
 }
+// Codes in as few vector operations as they take (with the general quantizer's,
+// about twice as many, the vector unit is as busy as the memory).  A slice's own inverse keeps its products within 127 and a rounding:
+//   nearest: adding 1.5 2^23 leaves the integer, to nearest even, in the low byte of the sum;
+//   stochastic: t = floor(x inv 2^16), clamped, + 65535 - u has the code in byte 2 (2^16 in one factor with the inverse: it moves the exponent only).
+// The factor of a slice that is not finite is 0, and the product by the rule that zero times anything is zero.
+template <int RND> __device__ __forceinline__ float code_factor(float inv) { return RND == kStochastic ? inv * 65536.0f : inv; }
+template <int RND, int J> __device__ __forceinline__ uint32_t code_word(float x, float factor, const uint32_t (&not_u)[4])
+{
+    float v;
+    asm("v_mul_legacy_f32 %0, %1, %2" : "=v"(v) : "v"(x), "v"(factor));
+    if constexpr(RND == kStochastic) return add_half<J % 2>(clamped_fixed_point(v, 127), not_u[J / 2]);
+    else                             return __float_as_uint(v + 12582912.0f);
+}
+template <int RND> __device__ __forceinline__ uint32_t pack_codes(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    if constexpr(RND == kStochastic) return __builtin_amdgcn_perm(b, a, 0x0C0C0602u) | __builtin_amdgcn_perm(d, c, 0x06020C0Cu);
+    else                             return __builtin_amdgcn_perm(b, a, 0x0C0C0400u) | __builtin_amdgcn_perm(d, c, 0x04000C0Cu);
+}
+template <int RND> __device__ __forceinline__ uint2 codes8(const float (&e)[8], float f, const uint32_t (&u)[4])
+{
+    return make_uint2(pack_codes<RND>(code_word<RND, 0>(e[0], f, u), code_word<RND, 1>(e[1], f, u), code_word<RND, 2>(e[2], f, u), code_word<RND, 3>(e[3], f, u)),
+                      pack_codes<RND>(code_word<RND, 4>(e[4], f, u), code_word<RND, 5>(e[5], f, u), code_word<RND, 6>(e[6], f, u), code_word<RND, 7>(e[7], f, u)));
+}
+// the complements of the draws of a block of eight elements
+template <int RND> __device__ __forceinline__ void draws8(uint64_t seed, uint64_t offset, int64_t group, uint32_t (&not_u)[4])
+{
+    if constexpr(RND == kStochastic)
+    {
+        const uint4 b = philox_group(seed, offset, static_cast<uint64_t>(group));
+        not_u[0] = ~b.x; not_u[1] = ~b.y; not_u[2] = ~b.z; not_u[3] = ~b.w;
+    }
+}
 __device__ __forceinline__ uint32_t wave_max(uint32_t m)
 {
 #pragma unroll
@@ -91,17 +123,13 @@ __global__ __launch_bounds__(256) void token_rows_kernel(TokenSource s, const in
     const CodeScale cs = code_scale(m);
     if(t == 0) scale[r] = cs.scale;
     int8_t* out = q + r * groups * 8;
-    auto    put = [&](const Row8<T>& w, int64_t g) {
-        float e[8];
+    const float f = code_factor<RND>(cs.inv);
+    auto        put = [&](const Row8<T>& w, int64_t g) {
+        float    e[8];
+        uint32_t u[4];
         w.decode(e);
-        if(cs.inv == 0.0f)
-#pragma unroll
-            for(int j = 0; j < 8; ++j) e[j] = 0.0f;
-        uint4 blk = make_uint4(0, 0, 0, 0);
-        if constexpr(RND == kStochastic) blk = philox_group(seed, offset, static_cast<uint64_t>(r * per_row + g));
-        uint32_t c[2];
-        quantize_group<float, RND>(e, cs.inv, 127, blk, c);
-        *reinterpret_cast<uint2*>(out + g * 8) = make_uint2(c[0], c[1]);
+        draws8<RND>(seed, offset, r * per_row + g, u);
+        *reinterpret_cast<uint2*>(out + g * 8) = codes8<RND>(e, f, u);
     };
 #pragma unroll
     for(int i = 0; i < V; ++i)
@@ -170,13 +198,33 @@ __device__ __forceinline__ uint32_t max_of_16(uint32_t v)
     step(std::integral_constant<int, kRotate + 1>{});
     return v;
 }
-template <typename T, bool SUM>
-__global__ __launch_bounds__(256) void token_stats_kernel(TokenSource s, const int32_t* offsets, int64_t sets, uint32_t tiles, uint32_t* rowpart, uint32_t* colmax, float* colsum)
+struct BothArgs      // one matrix's part in the three passes
 {
-    __shared__ uint32_t lmax[4][kStatCols];
-    __shared__ float    lsum[SUM ? 4 : 1][SUM ? kStatCols : 1];
+    TokenSource    s;
+    const int32_t* offsets;
+    int64_t        sets;
+    uint32_t       chunks, stat_tiles, code_tiles, scale_blocks, col_blocks;      // (scale_blocks: of rows and columns, those of the columns first)
+    uint32_t *     rowpart, *colmax;
+    float *        colsum, *row_scale, *row_inv, *col_scale, *col_inv, *sum_out;
+    int8_t *       q, *qT;
+};
+template <bool SUM> struct StatsLds
+{
+    uint32_t lmax[4][kStatCols];
+    float    lsum[SUM ? 4 : 1][SUM ? kStatCols : 1];
+};
+template <typename T, bool SUM> __device__ __forceinline__ void stats_body(const BothArgs& p, uint32_t block, StatsLds<SUM>& lds)
+{
+    const TokenSource& s = p.s;
+    const int32_t*     offsets = p.offsets;
+    const int64_t      sets = p.sets;
+    const uint32_t     tiles = p.stat_tiles;
+    uint32_t *const    rowpart = p.rowpart, *const colmax = p.colmax;
+    float* const       colsum = p.colsum;
+    auto&              lmax = lds.lmax;
+    [[maybe_unused]] auto& lsum = lds.lsum;
     const int     lane = threadIdx.x % 64, wave = threadIdx.x / 64, side = threadIdx.x % 16, down = threadIdx.x / 16;
-    const uint32_t tile = blockIdx.x % tiles, chunk = blockIdx.x / tiles;
+    const uint32_t tile = block % tiles, chunk = block / tiles;
     const Chunk    c = chunk_rows(offsets, s.rows, sets, chunk);
     if(c.len <= 0) return;
     const int64_t col = static_cast<int64_t>(tile) * kStatCols + side * 8;
@@ -237,15 +285,33 @@ __global__ __launch_bounds__(256) void token_stats_kernel(TokenSource s, const i
     if constexpr(SUM) colsum[chunk * s.cols + at] = (lsum[0][i] + lsum[1][i]) + (lsum[2][i] + lsum[3][i]);
 }
 
+template <typename T, bool SUM> __global__ __launch_bounds__(256) void token_stats_kernel(const BothArgs p)
+{
+    __shared__ StatsLds<SUM> lds;
+    stats_body<T, SUM>(p, blockIdx.x, lds);
+}
+// of two matrices, `a` first
+template <typename TA, typename TB> __global__ __launch_bounds__(256) void token_stats_pair_kernel(const BothArgs a, const BothArgs b)
+{
+    __shared__ StatsLds<false> lds;
+    const uint32_t n = a.chunks * a.stat_tiles;
+    if(blockIdx.x < n) stats_body<TA, false>(a, blockIdx.x, lds);
+    else               stats_body<TB, false>(b, blockIdx.x - n, lds);
+}
+
 // Scales and inverse scales of the rows (workgroups behind `col_blocks`) and of the sets' columns: sixteen threads fold a column's chunks,
 // every sixteenth each, then their results in order (one thread a column took 35 us for 128 chunks).
-template <bool SUM>
-__global__ __launch_bounds__(256) void token_scales_kernel(const int32_t* offsets, int64_t rows, int64_t cols, int64_t sets, int64_t col_blocks, int col_tiles, const uint32_t* rowpart,
-                                                           const uint32_t* colmax, const float* colsum, float* row_scale, float* row_inv, float* col_scale, float* col_inv, float* sum_out)
+template <bool SUM> __device__ __forceinline__ void scales_body(const BothArgs& p, uint32_t block, uint32_t (&lmax)[16][16], float (&lsum)[16][16])
 {
-    if(blockIdx.x >= col_blocks)
+    const int32_t* offsets = p.offsets;
+    const int64_t  rows = p.s.rows, cols = p.s.cols, sets = p.sets, col_blocks = p.col_blocks;
+    const int      col_tiles = static_cast<int>(p.stat_tiles);
+    const uint32_t *rowpart = p.rowpart, *colmax = p.colmax;
+    const float*    colsum = p.colsum;
+    float *         row_scale = p.row_scale, *row_inv = p.row_inv, *col_scale = p.col_scale, *col_inv = p.col_inv, *sum_out = p.sum_out;
+    if(block >= col_blocks)
     {
-        const int64_t r = (static_cast<int64_t>(blockIdx.x) - col_blocks) * 256 + threadIdx.x;
+        const int64_t r = (static_cast<int64_t>(block) - col_blocks) * 256 + threadIdx.x;
         if(r >= rows || (offsets && r >= offsets[sets])) return;
         uint32_t m = 0u;
         for(int t0 = 0; t0 < col_tiles; t0 += 8)
@@ -261,10 +327,8 @@ __global__ __launch_bounds__(256) void token_scales_kernel(const int32_t* offset
         row_inv[r]   = cs.inv;
         return;
     }
-    __shared__ uint32_t lmax[16][16];
-    __shared__ float    lsum[16][16];
     const int     side = threadIdx.x % 16, part = threadIdx.x / 16;
-    const int64_t tiles = (cols + 15) / 16, e = blockIdx.x / tiles, c = blockIdx.x % tiles * 16 + side, cc = c < cols ? c : cols - 1;
+    const int64_t tiles = (cols + 15) / 16, e = block / tiles, c = block % tiles * 16 + side, cc = c < cols ? c : cols - 1;
     const SetRows s = set_rows(offsets, rows, sets, e);
     const int64_t first = set_start(offsets, s, e) / kCodePad, end = first + code_pad(s.len) / kCodePad;
     uint32_t      m = 0u;
@@ -303,50 +367,64 @@ __global__ __launch_bounds__(256) void token_scales_kernel(const int32_t* offset
     if constexpr(SUM) sum_out[e * cols + c] = sum;
 }
 
+template <bool SUM> __global__ __launch_bounds__(256) void token_scales_kernel(const BothArgs p)
+{
+    __shared__ uint32_t lmax[16][16];
+    __shared__ float    lsum[16][16];
+    scales_body<SUM>(p, blockIdx.x, lmax, lsum);
+}
+__global__ __launch_bounds__(256) void token_scales_pair_kernel(const BothArgs a, const BothArgs b)
+{
+    __shared__ uint32_t lmax[16][16];
+    __shared__ float    lsum[16][16];
+    const bool first = blockIdx.x < a.scale_blocks;
+    scales_body<false>(first ? a : b, first ? blockIdx.x : blockIdx.x - a.scale_blocks, lmax, lsum);
+}
+
 // (Both passes walk the matrix row after row, the second one from its end: what the first one read last still lies in front of the memory.)
 // 128 positions x 64 columns a workgroup: a thread has four rows of eight columns, whose codes along the columns leave as words of four rows.
-template <typename T, int RND>
-__global__ __launch_bounds__(256) void token_codes_kernel(TokenSource s, const int32_t* offsets, int64_t sets, uint32_t tiles, uint64_t seed, uint64_t offset,
-                                                          const float* row_inv, const float* col_inv, int8_t* q, int8_t* qT)
+template <typename T, int RND> __device__ __forceinline__ void codes_body(const BothArgs& p, uint32_t back, uint64_t seed, uint64_t offset, uint32_t (&lds)[64 * 33])
 {
-    __shared__ uint32_t lds[64 * 33];
-    const uint32_t back = gridDim.x - 1 - blockIdx.x, tile = back % tiles;
-    const Chunk    c = chunk_rows(offsets, s.rows, sets, back / tiles);
+    const TokenSource& s = p.s;
+    const int32_t*     offsets = p.offsets;
+    const int64_t      sets = p.sets;
+    const float *      row_inv = p.row_inv, *col_inv = p.col_inv;
+    int8_t *           q = p.q, *qT = p.qT;
+    const uint32_t     tile = back % p.code_tiles;
+    const Chunk        c = chunk_rows(offsets, s.rows, sets, back / p.code_tiles);
     if(c.len <= 0) return;
     const int     cg = threadIdx.x % 8, rq = threadIdx.x / 8;
     const int64_t col0 = static_cast<int64_t>(tile) * 64, col = col0 + cg * 8, per_row = (s.cols + 7) / 8, qcols = code_pad(s.cols);
-    float         ci[8];
-#pragma unroll
-    for(int j = 0; j < 8; ++j) ci[j] = col + j < s.cols ? col_inv[c.set * s.cols + col + j] : 0.0f;
-    uint32_t w[8];
-#pragma unroll
-    for(int j = 0; j < 8; ++j) w[j] = 0u;
+    // (all loads before the first store, which might change what they read as far as the compiler knows)
+    Row8<T> v[4];
+    float   rf[4], ci[8];
 #pragma unroll
     for(int i = 0; i < 4; ++i)
     {
-        if(rq * 4 + i >= c.len) break;
-        const int64_t r = c.row0 + rq * 4 + i, from = source_row(s, r);
-        Row8<T>       v;
-        float         e[8];
-        load8(static_cast<const T*>(s.x) + (from < 0 ? 0 : from) * s.ld, col, from < 0 ? 0 : s.cols, v);
-        v.decode(e);
-        uint4 blk = make_uint4(0, 0, 0, 0);
-        if constexpr(RND == kStochastic) blk = philox_group(seed, offset, static_cast<uint64_t>(r * per_row + col / 8));
-        uint32_t    b[2];
-        const float ri = row_inv[r];
-        float       er[8];
-#pragma unroll
-        for(int j = 0; j < 8; ++j)
-        {
-            er[j] = ri == 0.0f ? 0.0f : e[j];
-            e[j]  = ci[j] == 0.0f ? 0.0f : e[j];
-        }
-        quantize_group<float, RND>(er, ri, 127, blk, b);
-        *reinterpret_cast<uint2*>(q + r * qcols + col) = make_uint2(b[0], b[1]);
-#pragma unroll
-        for(int j = 0; j < 8; ++j)
-            w[j] |= (static_cast<uint32_t>(quantize_code<RND>(e[j], ci[j], 127, philox_draw16(blk, j))) & 0xFFu) << (8 * i);
+        const bool    in = rq * 4 + i < c.len;
+        const int64_t r = c.row0 + (in ? rq * 4 + i : 0), from = in ? source_row(s, r) : -1;
+        load8(static_cast<const T*>(s.x) + (from < 0 ? 0 : from) * s.ld, col, from < 0 ? 0 : s.cols, v[i]);
+        rf[i] = code_factor<RND>(row_inv[r]);
     }
+#pragma unroll
+    for(int j = 0; j < 8; ++j) ci[j] = code_factor<RND>(col + j < s.cols ? col_inv[c.set * s.cols + col + j] : 0.0f);
+    uint32_t k[4][8], w[8];
+#pragma unroll
+    for(int i = 0; i < 4; ++i)
+    {
+        const int64_t r = c.row0 + rq * 4 + i;
+        float         e[8];
+        uint32_t      u[4];
+        v[i].decode(e);
+        draws8<RND>(seed, offset, r * per_row + col / 8, u);
+        if(rq * 4 + i < c.len) *reinterpret_cast<uint2*>(q + r * qcols + col) = codes8<RND>(e, rf[i], u);
+        k[i][0] = code_word<RND, 0>(e[0], ci[0], u); k[i][1] = code_word<RND, 1>(e[1], ci[1], u);
+        k[i][2] = code_word<RND, 2>(e[2], ci[2], u); k[i][3] = code_word<RND, 3>(e[3], ci[3], u);
+        k[i][4] = code_word<RND, 4>(e[4], ci[4], u); k[i][5] = code_word<RND, 5>(e[5], ci[5], u);
+        k[i][6] = code_word<RND, 6>(e[6], ci[6], u); k[i][7] = code_word<RND, 7>(e[7], ci[7], u);
+    }
+#pragma unroll
+    for(int j = 0; j < 8; ++j) w[j] = pack_codes<RND>(k[0][j], k[1][j], k[2][j], k[3][j]);
 #pragma unroll
     for(int j = 0; j < 8; ++j) lds[(cg * 8 + j) * 33 + rq] = w[j];
     __syncthreads();
@@ -360,6 +438,19 @@ __global__ __launch_bounds__(256) void token_codes_kernel(TokenSource s, const i
         const uint32_t* at = lds + cc * 33 + seg * 4;
         if(col0 + cc < s.cols) *reinterpret_cast<uint4*>(out + (col0 + cc) * ldt + seg * 16) = make_uint4(at[0], at[1], at[2], at[3]);
     }
+}
+
+template <typename T, int RND> __global__ __launch_bounds__(256) void token_codes_kernel(const BothArgs p, uint64_t seed, uint64_t offset)
+{
+    __shared__ uint32_t lds[64 * 33];
+    codes_body<T, RND>(p, gridDim.x - 1 - blockIdx.x, seed, offset, lds);
+}
+template <typename TA, typename TB> __global__ __launch_bounds__(256) void token_codes_pair_kernel(const BothArgs a, const BothArgs b)
+{
+    __shared__ uint32_t lds[64 * 33];
+    const uint32_t      n = a.chunks * a.code_tiles, back = gridDim.x - 1 - blockIdx.x;
+    if(back < n) codes_body<TA, kNearest>(a, back, 0, 0, lds);
+    else         codes_body<TB, kNearest>(b, back - n, 0, 0, lds);
 }
 
 struct BothWorkspace { size_t rowpart, row_inv, col_inv, colmax, colsum, total; };
@@ -377,26 +468,49 @@ BothWorkspace both_workspace(int64_t rows, int64_t cols, int64_t sets, bool offs
     return w;
 }
 
-template <typename T, int RND>
-hipError_t launch_both(const TokenSource& s, int64_t sets, const int32_t* offsets, uint64_t seed, uint64_t offset, float* row_scale, int8_t* q, float* col_scale, int8_t* qT,
-                       float* colsum, void* workspace, hipStream_t st)
+BothArgs both_args(const TokenMatrix& m, const TokenBoth& o)
 {
-    const BothWorkspace w = both_workspace(s.rows, s.cols, sets, offsets != nullptr);
-    uint8_t* const      base = static_cast<uint8_t*>(workspace);
-    uint32_t*           rowpart = reinterpret_cast<uint32_t*>(base + w.rowpart);
-    uint32_t*           cm = reinterpret_cast<uint32_t*>(base + w.colmax);
-    float *             ri = reinterpret_cast<float*>(base + w.row_inv), *ci = reinterpret_cast<float*>(base + w.col_inv), *sm = reinterpret_cast<float*>(base + w.colsum);
-    const unsigned      chunks = static_cast<unsigned>(code_positions(s.rows, sets, offsets != nullptr) / kCodePad);
-    const unsigned      tiles = static_cast<unsigned>((s.cols + kStatCols - 1) / kStatCols);
-    if(colsum) token_stats_kernel<T, true><<<chunks * tiles, 256, 0, st>>>(s, offsets, sets, tiles, rowpart, cm, sm);
-    else       token_stats_kernel<T, false><<<chunks * tiles, 256, 0, st>>>(s, offsets, sets, tiles, rowpart, cm, sm);
-    const int64_t  col_blocks = sets * ((s.cols + 15) / 16);
-    const unsigned blocks = static_cast<unsigned>(col_blocks + (s.rows + 255) / 256);
-    if(colsum) token_scales_kernel<true><<<blocks, 256, 0, st>>>(offsets, s.rows, s.cols, sets, col_blocks, static_cast<int>(tiles), rowpart, cm, sm, row_scale, ri, col_scale, ci, colsum);
-    else       token_scales_kernel<false><<<blocks, 256, 0, st>>>(offsets, s.rows, s.cols, sets, col_blocks, static_cast<int>(tiles), rowpart, cm, nullptr, row_scale, ri, col_scale, ci, nullptr);
-    const unsigned wide = static_cast<unsigned>(code_pad(s.cols) / 64);
-    token_codes_kernel<T, RND><<<chunks * wide, 256, 0, st>>>(s, offsets, sets, wide, seed, offset, ri, ci, q, qT);
+    BothArgs             a{};
+    const BothWorkspace  w = both_workspace(m.rows, m.cols, o.sets, o.offsets != nullptr);
+    uint8_t* const       base = static_cast<uint8_t*>(o.workspace);
+    a.s          = TokenSource{m.x, m.x_rows, m.cols, m.ld, m.rows, m.source, m.group};
+    a.offsets    = o.offsets;
+    a.sets       = o.sets;
+    a.chunks     = static_cast<uint32_t>(code_positions(m.rows, o.sets, o.offsets != nullptr) / kCodePad);
+    a.stat_tiles = static_cast<uint32_t>((m.cols + kStatCols - 1) / kStatCols);
+    a.code_tiles = static_cast<uint32_t>(code_pad(m.cols) / 64);
+    a.col_blocks = static_cast<uint32_t>(o.sets * ((m.cols + 15) / 16));
+    a.scale_blocks = a.col_blocks + static_cast<uint32_t>((m.rows + 255) / 256);
+    a.rowpart   = reinterpret_cast<uint32_t*>(base + w.rowpart);
+    a.colmax    = reinterpret_cast<uint32_t*>(base + w.colmax);
+    a.colsum    = reinterpret_cast<float*>(base + w.colsum);
+    a.row_inv   = reinterpret_cast<float*>(base + w.row_inv);
+    a.col_inv   = reinterpret_cast<float*>(base + w.col_inv);
+    a.row_scale = o.row_scale;
+    a.col_scale = o.col_scale;
+    a.sum_out   = o.colsum;
+    a.q         = o.q;
+    a.qT        = o.qT;
+    return a;
+}
+template <typename T, int RND> hipError_t launch_both(const BothArgs& a, uint64_t seed, uint64_t offset, hipStream_t st)
+{
+    if(a.sum_out)
+    {
+        token_stats_kernel<T, true><<<a.chunks * a.stat_tiles, 256, 0, st>>>(a);
+        token_scales_kernel<true><<<a.scale_blocks, 256, 0, st>>>(a);
+    }
+    else
+    {
+        token_stats_kernel<T, false><<<a.chunks * a.stat_tiles, 256, 0, st>>>(a);
+        token_scales_kernel<false><<<a.scale_blocks, 256, 0, st>>>(a);
+    }
+    token_codes_kernel<T, RND><<<a.chunks * a.code_tiles, 256, 0, st>>>(a, seed, offset);
     return hipGetLastError();
+}
+template <typename F> hipError_t with_type(int dtype, F&& f)
+{
+    return dtype == kF16 ? f(_Float16{}) : dtype == kBF16 ? f(__bf16{}) : f(float{});
 }
 
 }  // namespace
@@ -406,24 +520,36 @@ size_t token_both_workspace_bytes(int64_t rows, int64_t cols, int64_t sets, bool
 hipError_t launch_token_quantize(const TokenMatrix& m, const int32_t* count, int rnd, uint64_t seed, uint64_t offset, float* scale, int8_t* q, hipStream_t st)
 {
     const TokenSource s{m.x, m.x_rows, m.cols, m.ld, m.rows, m.source, m.group};
-    auto typed = [&](auto tag) {
+    return with_type(m.dtype, [&](auto tag) {
         typedef decltype(tag) T;
         if(rnd == kStochastic) return launch_rows<T, kStochastic>(s, count, seed, offset, scale, q, st);
         return launch_rows<T, kNearest>(s, count, seed, offset, scale, q, st);
-    };
-    return m.dtype == kF16 ? typed(_Float16{}) : m.dtype == kBF16 ? typed(__bf16{}) : typed(float{});
+    });
 }
 
-hipError_t launch_token_quantize_both(const TokenMatrix& m, int64_t sets, const int32_t* offsets, int rnd, uint64_t seed, uint64_t offset, float* row_scale, int8_t* q,
-                                      float* col_scale, int8_t* qT, float* colsum, void* workspace, hipStream_t st)
+hipError_t launch_token_quantize_both(const TokenMatrix& m, const TokenBoth& o, int rnd, uint64_t seed, uint64_t offset, hipStream_t st)
 {
-    const TokenSource s{m.x, m.x_rows, m.cols, m.ld, m.rows, m.source, m.group};
-    auto typed = [&](auto tag) {
+    const BothArgs a = both_args(m, o);
+    return with_type(m.dtype, [&](auto tag) {
         typedef decltype(tag) T;
-        if(rnd == kStochastic) return launch_both<T, kStochastic>(s, sets, offsets, seed, offset, row_scale, q, col_scale, qT, colsum, workspace, st);
-        return launch_both<T, kNearest>(s, sets, offsets, seed, offset, row_scale, q, col_scale, qT, colsum, workspace, st);
-    };
-    return m.dtype == kF16 ? typed(_Float16{}) : m.dtype == kBF16 ? typed(__bf16{}) : typed(float{});
+        return rnd == kStochastic ? launch_both<T, kStochastic>(a, seed, offset, st) : launch_both<T, kNearest>(a, seed, offset, st);
+    });
+}
+
+// Each pass of the two matrices in one launch.  (The launches of one beside the other's: what a small matrix's take is latency.)
+hipError_t launch_token_quantize_pair(const TokenMatrix& m, const TokenBoth& o, const TokenMatrix& m2, const TokenBoth& o2, hipStream_t st)
+{
+    const BothArgs a = both_args(m, o), b = both_args(m2, o2);
+    return with_type(m.dtype, [&](auto tag) {
+        typedef decltype(tag) TA;
+        return with_type(m2.dtype, [&](auto tag2) {
+            typedef decltype(tag2) TB;
+            token_stats_pair_kernel<TA, TB><<<a.chunks * a.stat_tiles + b.chunks * b.stat_tiles, 256, 0, st>>>(a, b);
+            token_scales_pair_kernel<<<a.scale_blocks + b.scale_blocks, 256, 0, st>>>(a, b);
+            token_codes_pair_kernel<TA, TB><<<a.chunks * a.code_tiles + b.chunks * b.code_tiles, 256, 0, st>>>(a, b);
+            return hipGetLastError();
+        });
+    });
 }
 
 }  // namespace qsync

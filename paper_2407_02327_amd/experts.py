@@ -179,17 +179,19 @@ class _CodeLinear:
         self.db = e(*((sets, N) if routed else (N,))) if bias else None
         self.ws_x = _scratch(max(Q.qsync_token_quantize_both_workspace_bytes(rows, c, sets, routed) for c in (N, K)), device)
         self.ws_w = _scratch(Q.qsync_token_quantize_both_workspace_bytes(sets * N, K, sets, False), device)
-        self.ws_bwd = _scratch(max(Q.qsync_token_linear_workspace_bytes(rows, K, N, sets), Q.qsync_token_wgrad_workspace_bytes(rows, N, K, sets)),
-                               device)
+        self.ws_bwd = _scratch(Q.qsync_token_linear_bwd_workspace_bytes(rows, N, K, sets), device)
+
+    def _weights(self, w) -> torch.Tensor:
+        if not isinstance(w, torch.Tensor) or w.shape != self.dw_shape:
+            raise ValueError(f"w: {list(self.dw_shape)} expected")
+        w = w.flatten(0, -2) if w.dim() > 2 and w.is_contiguous() else w
+        _check_packed(w, self.sets * self.N, self.K, _ANY_FLOAT, self.device, "w")
+        return w
 
     def convert_w(self, w: torch.Tensor, stream=None) -> None:
         """The codes of the weights, which `forward` and `backward` use until the next conversion."""
         _on_device(self.device)
-        shape = tuple(self.dw_shape)
-        if not isinstance(w, torch.Tensor) or tuple(w.shape) != shape:
-            raise ValueError(f"w: {list(shape)} expected")
-        w = w.flatten(0, -2) if w.is_contiguous() else w
-        _check_packed(w, self.sets * self.N, self.K, _ANY_FLOAT, self.device, "w")
+        w = self._weights(w)
         rows, K = self.sets * self.N, self.K
         if self.training:
             Q.qsync_token_quantize_both(w, rows, K, K, None, 1, rows, self.sets, None, Q.ROUND_NEAREST, 0, 0, self.sw, self.wq, self.swc, self.wqT,
@@ -198,14 +200,22 @@ class _CodeLinear:
             Q.qsync_token_quantize(w, rows, K, K, None, 1, rows, None, Q.ROUND_NEAREST, 0, 0, self.sw, self.wq, stream)
         self._converted = True
 
-    def _forward(self, x, x_rows, ld, source, group, n, offsets, stream):
-        if not self._converted:
+    def _forward(self, x, x_rows, ld, w, source, group, n, offsets, stream):
+        if w is not None and (not self.training or not n):
+            self.convert_w(w, stream)
+            w = None
+        if w is None and not self._converted:
             raise RuntimeError("forward without weights: w, or convert_w before it")
         if not n:      # (a tensor without elements has no address)
             pass
         elif self.training:
-            Q.qsync_token_quantize_both(x, x_rows, self.K, ld, source, group, n, self.sets, offsets, Q.ROUND_NEAREST, 0, 0, self.sx, self.xq,
-                                        self.sxc, self.xqT, None, self.ws_x, stream)
+            if w is not None:
+                Q.qsync_token_convert(x, x_rows, self.K, ld, source, group, n, self.sets, offsets, self.sx, self.xq, self.sxc, self.xqT,
+                                      self._weights(w), self.N, self.sw, self.wq, self.swc, self.wqT, self.ws_x, self.ws_w, stream)
+                self._converted = True
+            else:
+                Q.qsync_token_quantize_both(x, x_rows, self.K, ld, source, group, n, self.sets, offsets, Q.ROUND_NEAREST, 0, 0, self.sx, self.xq,
+                                            self.sxc, self.xqT, None, self.ws_x, stream)
             Q.qsync_token_linear_fwd(n, self.N, self.K, self.sets, offsets, self.xq, self.sx, self.wq, self.sw, self.bias, self.y, self.ws, stream)
         else:
             Q.qsync_token_linear(x, x_rows, self.K, ld, source, group, n, self.N, self.sets, offsets, self.wq, self.sw, self.bias, self.y, self.sx,
@@ -224,8 +234,10 @@ class _CodeLinear:
         if self.dy_round == Q.ROUND_STOCHASTIC:
             self.offset += n * ((N + 7) // 8)
         if n:
-            Q.qsync_token_linear_fwd(n, K, N, sets, offsets, self.dyq, self.sdy, self.wqT, self.swc, None, self.dx, self.ws_bwd, stream)
-        Q.qsync_token_linear_wgrad(n, N, K, sets, offsets, at(self.dyqT), self.sdyc, at(self.xqT), self.sxc, self.dw, self.ws_bwd, stream)
+            Q.qsync_token_linear_bwd(n, N, K, sets, offsets, self.dyq, self.sdy, self.wqT, self.swc, self.dyqT, self.sdyc, self.xqT, self.sxc, self.dx,
+                                     self.dw, self.ws_bwd, stream)
+        else:
+            Q.qsync_token_linear_wgrad(0, N, K, sets, offsets, self.dw, self.sdyc, self.dw, self.sxc, self.dw, self.ws_bwd, stream)
         return self.dx if n == self.rows else self.dx[:n], self.dw, self.db
 
     def _check_backward(self) -> None:
@@ -248,10 +260,8 @@ class TokenLinear(_CodeLinear):
         """x [n <= rows, K], rows at any stride; w [N, K], or None: the weights that `convert_w` was given last.  `backward` reads neither."""
         _on_device(self.device)
         ld = _check_rows(x, self.rows, self.K, self.device, "x")
-        if w is not None:
-            self.convert_w(w, stream)
-        n = x.shape[0]
-        y = self._forward(x, n, ld, None, 1, n, None, stream)
+        n = len(x)
+        y = self._forward(x, n, ld, w, None, 1, n, None, stream)
         if self.training:
             self._saved = n
         return y
@@ -286,9 +296,7 @@ class ExpertLinear(_CodeLinear):
         ld = _check_rows(x, have, self.K, self.device, "x")
         if x.shape[0] != have:
             raise ValueError(f"x has {x.shape[0]} rows, {have} expected")
-        if w is not None:
-            self.convert_w(w, stream)
-        y = self._forward(x, have, ld, route.source if self.gather else None, route.k if self.gather else 1, n, route.offsets, stream)
+        y = self._forward(x, have, ld, w, route.source if self.gather else None, route.k if self.gather else 1, n, route.offsets, stream)
         if self.training:
             self._saved = (route, route.sorts, n)
         return y

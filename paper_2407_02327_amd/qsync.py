@@ -92,10 +92,14 @@ SIGNATURES = {
                                        _vp]),
     "qsync_token_quantize_both_workspace_bytes": (_sz, [_i64, _i64, _i64, _i]),
     "qsync_token_linear_fwd": (_i, [_i64, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _vp, _sz, _vp]),
+    "qsync_token_convert": (_i, [_vp, _i, _i64, _i64, _i64, _vp, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i64, _vp, _vp, _vp, _vp, _vp,
+                                 _sz, _vp, _sz, _vp]),
     "qsync_token_linear": (_i, [_vp, _i, _i64, _i64, _i64, _vp, _i64, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _i, _vp, _vp, _vp, _sz, _vp]),
     "qsync_token_linear_workspace_bytes": (_sz, [_i64, _i64, _i64, _i64]),
     "qsync_token_linear_wgrad": (_i, [_i64, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _i, _vp, _sz, _vp]),
     "qsync_token_wgrad_workspace_bytes": (_sz, [_i64, _i64, _i64, _i64]),
+    "qsync_token_linear_bwd": (_i, [_i64, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _vp, _i, _vp, _sz, _vp]),
+    "qsync_token_linear_bwd_workspace_bytes": (_sz, [_i64, _i64, _i64, _i64]),
     "qsync_expert_sort": (_i, [_vp, _i, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _sz, _vp]),
     "qsync_expert_sort_workspace_bytes": (_sz, [_i64, _i64]),
     "qsync_expert_gather": (_i, [_vp, _i, _i64, _i64, _i64, _vp, _i64, _i64, _vp, _vp, _vp]),
@@ -392,6 +396,12 @@ def qsync_token_quantize_both(x, x_rows, cols, ld, source_opt, group, rows, sets
                                       col_scale, qT, colsum_opt, workspace, workspace, stream)
 
 
+def qsync_token_convert(x, x_rows, K, ld, source_opt, group, rows, sets, offsets_opt, sx, xq, sxc, xqT, w, N, sw, wq, swc, wqT, ws_x, ws_w,
+                        stream=None) -> None:
+    _native.qsync_token_convert(x, x, x_rows, K, ld, source_opt, group, rows, sets, offsets_opt, sx, xq, sxc, xqT, w, w, N, sw, wq, swc, wqT,
+                                ws_x, ws_x, ws_w, ws_w, stream)
+
+
 def qsync_token_linear_workspace_bytes(rows: int, N: int, K: int, sets: int) -> int:
     return lib.qsync_token_linear_workspace_bytes(rows, N, K, sets)
 
@@ -411,6 +421,15 @@ def qsync_token_wgrad_workspace_bytes(rows: int, N: int, K: int, sets: int) -> i
 
 def qsync_token_linear_wgrad(rows, N, K, sets, offsets_opt, dyqT, sdy, xqT, sx, dw, workspace, stream=None) -> None:
     _native.qsync_token_linear_wgrad(rows, N, K, sets, offsets_opt, dyqT, sdy, xqT, sx, dw, dw, workspace, workspace, stream)
+
+
+def qsync_token_linear_bwd_workspace_bytes(rows: int, N: int, K: int, sets: int) -> int:
+    return lib.qsync_token_linear_bwd_workspace_bytes(rows, N, K, sets)
+
+
+def qsync_token_linear_bwd(rows, N, K, sets, offsets_opt, dyq, sdy, wqT, swc, dyqT, sdyc, xqT, sxc, dx, dw, workspace, stream=None) -> None:
+    _native.qsync_token_linear_bwd(rows, N, K, sets, offsets_opt, dyq, sdy, wqT, swc, dyqT, sdyc, xqT, sxc, dx, dx, dw, dw, workspace, workspace,
+                                   stream)
 
 
 def qsync_expert_sort_workspace_bytes(entries: int, experts: int) -> int:

@@ -32,10 +32,14 @@ BOTH = Call(lib.qsync_token_quantize_both, "x xdt x_rows cols ld source group ro
             [_at(1), Q.F16, 4, 100, 101, _at(2), 2, 8, 3, _at(3), 0, 1, 2, _at(4), _at(5), _at(6), _at(7), _at(8), _at(9), BIG, None])
 FWD = Call(lib.qsync_token_linear_fwd, "rows N K sets offsets a sa b sb bias y ydt ws ws_bytes stream",
            [40, 30, 20, 3, _at(1), _at(2), _at(3), _at(4), _at(5), _at(6), _at(7), Q.BF16, _at(8), BIG, None])
+CONVERT = Call(lib.qsync_token_convert, "x xdt x_rows cols ld source group rows sets offsets scale q col_scale qT w wdt N sw wq swc wqT ws ws_bytes ws_w ws_w_bytes stream",
+               [_at(1), Q.BF16, 4, 100, 101, _at(2), 2, 8, 3, _at(3), _at(4), _at(5), _at(6), _at(7), _at(8), Q.F32, 30, _at(9), _at(10), _at(11), _at(12), _at(13), BIG, _at(14), BIG, None])
 SERVE = Call(lib.qsync_token_linear, "x xdt x_rows cols ld source group rows N sets offsets b sb bias y ydt scale q ws ws_bytes stream",
              [_at(1), Q.BF16, 4, 100, 101, _at(2), 2, 8, 30, 3, _at(3), _at(4), _at(5), _at(6), _at(7), Q.F16, _at(8), _at(9), _at(10), BIG, None])
 WGRAD = Call(lib.qsync_token_linear_wgrad, "rows N K sets offsets a sa b sb y ydt ws ws_bytes stream",
              [40, 30, 20, 3, _at(1), _at(2), _at(3), _at(4), _at(5), _at(7), Q.F32, _at(8), BIG, None])
+GRADS = Call(lib.qsync_token_linear_bwd, "rows N K sets offsets a sa b sb dyT sdc xT sxc dx dxdt dw dwdt ws ws_bytes stream",
+             [40, 30, 20, 3, _at(1), _at(2), _at(3), _at(4), _at(5), _at(6), _at(7), _at(8), _at(9), _at(10), Q.F16, _at(11), Q.F32, _at(12), BIG, None])
 SORT = Call(lib.qsync_expert_sort, "ids idt tokens group experts offsets source slot ws ws_bytes stream",
             [_at(1), Q.I64, 40, 2, 8, _at(2), _at(3), _at(4), _at(5), BIG, None])
 GATHER = Call(lib.qsync_expert_gather, "x xdt x_rows cols ld source group rows count y stream", [_at(1), Q.F16, 4, 100, 100, _at(2), 2, 8, _at(3), _at(4), None])
@@ -44,18 +48,18 @@ BWD = Call(lib.qsync_expert_combine_bwd, "x xdt tokens cols ld z zdt rows ldz sl
            [_at(1), Q.F16, 4, 100, 100, _at(2), Q.F32, 8, 100, _at(3), 2, _at(4), _at(5), Q.BF16, _at(6), None])
 
 
-@pytest.mark.parametrize("call, required", [(ROWS, "x scale q"), (BOTH, "x scale q col_scale qT"), (SERVE, "x b sb y scale q"), (FWD, "a sa b sb y"), (WGRAD, "a sa b sb y"), (SORT, "ids offsets source slot"),
-                                            (GATHER, "x source count y"), (COMBINE, "x slot y"), (BWD, "x slot z")], ids="rows both serve fwd wgrad sort gather combine bwd".split())
+@pytest.mark.parametrize("call, required", [(ROWS, "x scale q"), (BOTH, "x scale q col_scale qT"), (CONVERT, "x scale q col_scale qT w sw wq swc wqT"), (SERVE, "x b sb y scale q"), (FWD, "a sa b sb y"), (WGRAD, "a sa b sb y"), (GRADS, "a sa b sb dyT sdc xT sxc dx dw"), (SORT, "ids offsets source slot"),
+                                            (GATHER, "x source count y"), (COMBINE, "x slot y"), (BWD, "x slot z")], ids="rows both convert serve fwd wgrad bwd sort gather combine combine_bwd".split())
 def test_what_is_required(call, required):
     assert call.but() in OK_OR_NO_GPU
     for name in required.split():
         assert call.but(**{name: NULL}) == Q.ERR_NULL, name
-    for name in set(call.names) & {"xdt", "ydt", "idt", "zdt", "dzdt"}:
+    for name in set(call.names) & {"xdt", "ydt", "idt", "zdt", "dzdt", "wdt", "dxdt", "dwdt"}:
         for bad in (Q.I8, 6, -1) + ((Q.F32, Q.F16, Q.BF16) if name == "idt" else (Q.I32, Q.I64)):
             assert call.but(**{name: bad}) == Q.ERR_BAD_ENUM, (name, bad)
 
 
-@pytest.mark.parametrize("call", [ROWS, BOTH, SERVE, GATHER, COMBINE, BWD], ids="rows both serve gather combine bwd".split())
+@pytest.mark.parametrize("call", [ROWS, BOTH, CONVERT, SERVE, GATHER, COMBINE, BWD], ids="rows both convert serve gather combine bwd".split())
 def test_matrices(call):
     for shape in (dict(rows=-1), dict(cols=-1), dict(ld=99), dict(group=0), dict(rows=1 << 50, cols=1 << 50, ld=1 << 50)):
         assert call.but(**shape) == Q.ERR_BAD_SHAPE, shape
@@ -70,7 +74,8 @@ def test_matrices(call):
         assert call.but(**{name: ctypes.c_void_p(value.value + 2)}) == Q.ERR_ALIGN, name
 
 
-@pytest.mark.parametrize("call, out, inputs", [(ROWS, "q", "x"), (BOTH, "q", "x"), (BOTH, "qT", "x"), (SERVE, "q", "x"), (SERVE, "scale", "x"), (SERVE, "y", "x"), (SERVE, "y", "q"), (GATHER, "y", "x"), (COMBINE, "y", "x"), (BWD, "dz", "x"), (BWD, "dz", "z")])
+@pytest.mark.parametrize("call, out, inputs", [(ROWS, "q", "x"), (BOTH, "q", "x"), (BOTH, "qT", "x"), (CONVERT, "q", "x"), (CONVERT, "q", "w"), (CONVERT, "wqT", "x"), (CONVERT, "wq", "w"), (CONVERT, "ws_w", "ws"),
+                                               (SERVE, "q", "x"), (SERVE, "scale", "x"), (SERVE, "y", "x"), (SERVE, "y", "q"), (GATHER, "y", "x"), (COMBINE, "y", "x"), (BWD, "dz", "x"), (BWD, "dz", "z")])
 def test_outputs_do_not_overlap_inputs(call, out, inputs):
     source = dict(zip(call.names, call.values))[inputs]
     assert call.but(**{out: source}) == Q.ERR_UNSUPPORTED
@@ -89,6 +94,15 @@ def test_quantizers():
     need = Q.qsync_token_quantize_both_workspace_bytes(8, 100, 3, True)
     assert need > 0 and BOTH.but(ws_bytes=need - 1) == Q.ERR_WORKSPACE and BOTH.but(ws=NULL) == Q.ERR_WORKSPACE and BOTH.but(ws=_at(9, 8)) == Q.ERR_ALIGN
     assert BOTH.but(rows=0, sums=NULL) == Q.OK
+
+
+def test_convert():
+    need_x, need_w = Q.qsync_token_quantize_both_workspace_bytes(8, 100, 3, True), Q.qsync_token_quantize_both_workspace_bytes(90, 100, 3, False)
+    assert CONVERT.but(ws_bytes=need_x - 1) == Q.ERR_WORKSPACE and CONVERT.but(ws_w_bytes=need_w - 1) == Q.ERR_WORKSPACE
+    assert CONVERT.but(ws_bytes=need_x, ws_w_bytes=need_w) in OK_OR_NO_GPU and CONVERT.but(ws_w=_at(14, 8)) == Q.ERR_ALIGN
+    assert CONVERT.but(N=-1) == Q.ERR_BAD_SHAPE and CONVERT.but(sets=0) == Q.ERR_UNSUPPORTED and CONVERT.but(N=1 << 23) == Q.ERR_UNSUPPORTED
+    assert CONVERT.but(wqT=_at(12, 8)) == Q.ERR_ALIGN and CONVERT.but(w=_at(8, 2)) == Q.ERR_ALIGN
+    assert CONVERT.but(rows=0) in OK_OR_NO_GPU and CONVERT.but(N=0) in OK_OR_NO_GPU and CONVERT.but(rows=0, N=0) == Q.OK
 
 
 def test_serving():
@@ -137,6 +151,18 @@ def test_products(call):
     # the products run with any room, and without
     assert call.but(ws=NULL, ws_bytes=0) in OK_OR_NO_GPU and call.but(ws_bytes=0) in OK_OR_NO_GPU and call.but(ws=_at(8, 8)) == Q.ERR_ALIGN
     assert Q.qsync_token_linear_workspace_bytes(200, 128, 16384, 1) > 0 and Q.qsync_token_wgrad_workspace_bytes(16384, 128, 200, 1) > 0
+
+
+def test_both_gradients():
+    for name in ("rows", "N", "K"):
+        assert GRADS.but(**{name: -1}) == Q.ERR_BAD_SHAPE and GRADS.but(**{name: 1 << 24}) == Q.ERR_UNSUPPORTED
+        assert GRADS.but(**{name: 0}) in OK_OR_NO_GPU
+    assert GRADS.but(rows=0, N=0) == Q.OK and GRADS.but(sets=513) == Q.ERR_UNSUPPORTED and GRADS.but(offsets=NULL) == Q.ERR_UNSUPPORTED
+    for name in ("a", "b", "dyT", "xT"):
+        value = dict(zip(GRADS.names, GRADS.values))[name]
+        assert GRADS.but(**{name: ctypes.c_void_p(value.value + 8)}) == Q.ERR_ALIGN, name
+        assert GRADS.but(dx=value) == Q.ERR_UNSUPPORTED and GRADS.but(dw=value) == Q.ERR_UNSUPPORTED, name
+    assert GRADS.but(dx=_at(11)) == Q.ERR_UNSUPPORTED and GRADS.but(ws=NULL, ws_bytes=0) in OK_OR_NO_GPU and GRADS.but(ws=_at(12, 8)) == Q.ERR_ALIGN
 
 
 def test_sort():

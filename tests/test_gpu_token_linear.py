@@ -263,6 +263,49 @@ def test_weight_gradients(rows, sets, offsets, N, K, dtype):
         assert_within(dw[e], want, bound + rounded(want, dtype), f"set {e}")
 
 
+@pytest.mark.parametrize("rows, N, K, sets, offsets", [(300, 200, 130, 1, None), (2187, 1001, 777, 1, None), (5, 40, 30, 1, None), (700, 90, 300, 4, [0, 100, 100, 690, 695]),
+                                                       (3000, 520, 264, 30, [100 * i - (i % 3) * 7 for i in range(31)]), (9, 16, 16, 3, [0, 0, 0, 0]), (9000, 1100, 1500, 1, None)])
+@pytest.mark.parametrize("x_dtype, w_dtype", [(F16, F32), (F32, BF16), (BF16, F16)])
+def test_calls_that_join_two(rows, N, K, sets, offsets, x_dtype, w_dtype):
+    """Conversion of both operands, and both gradients, in one call each: the bits of the separate calls, whatever the buffers held."""
+    say("token linear, joined calls", rows, N, K, sets, x_dtype)
+    given = None if offsets is None else torch.tensor(offsets, dtype=torch.int32, device="cuda")
+    n, routed = rows if offsets is None else offsets[-1], offsets is not None
+    x, w, dy = values(rows, K, x_dtype, 17, pad=3), values(sets * N, K, w_dtype, 18).contiguous(), values(rows, N, x_dtype, 19)
+    xq, sx, xqT, sxc, _ = quantize_both(x, sets, given, Q.ROUND_NEAREST, sums=False)
+    wq, sw, wqT, swc, _ = quantize_both(w, sets, None, Q.ROUND_NEAREST, sums=False)
+    dq, sd, dqT, sdc, _ = quantize_both(dy, sets, given, Q.ROUND_STOCHASTIC)
+    like = [torch.full_like(t, 77 if t.dtype == torch.int8 else -7) for t in (sx, xq, sxc, xqT, sw, wq, swc, wqT)]
+    ws = [torch.empty(Q.qsync_token_quantize_both_workspace_bytes(*a), dtype=torch.uint8, device="cuda").random_() for a in ((rows, K, sets, routed), (sets * N, K, sets, False))]
+    Q.qsync_token_convert(x, rows, K, x.stride(0), None, 1, rows, sets, given, *like[:4], w, N, *like[4:], *ws)
+    torch.cuda.synchronize()
+    for a, b in zip(like, (sx, xq, sxc, xqT, sw, wq, swc, wqT)):
+        assert torch.equal(a, b)
+    room = torch.empty(Q.qsync_token_linear_bwd_workspace_bytes(rows, N, K, sets) + 16, dtype=torch.uint8, device="cuda").random_()
+    out = []
+    for joined in (False, True):
+        dx, dw = torch.full((rows, K), 7.0, dtype=x_dtype, device="cuda"), torch.full((sets, N, K), 7.0, device="cuda")
+        if joined:
+            Q.qsync_token_linear_bwd(rows, N, K, sets, given, dq, sd, wqT, swc, dqT, sdc, xqT, sxc, dx, dw, room)
+        else:
+            Q.qsync_token_linear_fwd(rows, K, N, sets, given, dq, sd, wqT, swc, None, dx, room)
+            Q.qsync_token_linear_wgrad(rows, N, K, sets, given, dqT, sdc, xqT, sxc, dw, room)
+        torch.cuda.synchronize()
+        out.append((dx, dw))
+    assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1]) and (out[1][0][n:] == 7.0).all()
+
+
+def test_an_empty_contraction():
+    """No features to sum over: the bias, and zeros."""
+    one, codes = torch.ones(4, device="cuda"), torch.zeros(256, dtype=torch.int8, device="cuda")
+    y, dx, dw = (torch.full((4, 3), 7.0, device="cuda") for _ in range(3))
+    Q.qsync_token_linear_fwd(4, 3, 0, 1, None, codes, one, codes, one, one, y, None)
+    Q.qsync_token_linear_wgrad(0, 4, 3, 1, None, codes, one, codes, one, dw, None)
+    Q.qsync_token_linear_bwd(4, 0, 3, 1, None, codes, one, codes, one, codes, one, codes, one, dx, dw, None)
+    torch.cuda.synchronize()
+    assert (y == 1.0).all() and not dx.any() and not dw.any()
+
+
 def test_accumulators_at_their_largest():
     """All codes 127 over a contraction whose sums need 25 bits and more: exact until the conversion to 32 bits."""
     M, N, K = 70, 90, 130000
