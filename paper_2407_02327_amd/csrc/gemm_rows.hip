@@ -59,6 +59,21 @@ __global__ __launch_bounds__(64 * kRowsWaves) void gemm_rows_kernel(const GemmKe
 #pragma unroll
     for(int f = 0; f < MF * NF; ++f) acc[f] = vec{0, 0, 0, 0};
     const int      row = lane % 16, quad = lane / 16;
+    // (the epilogue's scales and biases are requested in front of everything)
+    [[maybe_unused]] float row_scale = 0.0f, cs[4] = {}, cb[4] = {};
+    if constexpr(TOKEN)
+        if(wave < MF * NF)
+        {
+            const int64_t m = m0 + wave % MF * 16 + row, n = n0 + wave / MF * 16 + quad * 4;
+            row_scale = p.row_scale[m < p.M ? m : p.M - 1];
+#pragma unroll
+            for(int e = 0; e < 4; ++e)
+            {
+                const int64_t c = n + e < p.N ? n + e : p.N - 1;
+                cs[e] = p.col_scale[c];
+                cb[e] = p.col_bias ? p.col_bias[c] : 0.0f;
+            }
+        }
     const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t*)mine));
     const uint32_t frag = static_cast<uint32_t>(row * 64 + ((quad ^ ((row >> 2) & 3)) * 16));
 #pragma unroll
@@ -90,11 +105,17 @@ __global__ __launch_bounds__(64 * kRowsWaves) void gemm_rows_kernel(const GemmKe
 
     const int64_t m = m0 + wave % MF * 16 + row, n = n0 + wave / MF * 16 + quad * 4;
     if(m >= p.M || n >= p.N) return;
-    const float alpha = TOKEN ? (p.row_scale ? p.row_scale[m] : 1.0f) : *(p.s0 ? p.s0 : &g_one) * *(p.s1 ? p.s1 : &g_one);
+    const float alpha = TOKEN ? row_scale : *(p.s0 ? p.s0 : &g_one) * *(p.s1 ? p.s1 : &g_one);
     float       fs[4], bs[4];
 #pragma unroll
     for(int e = 0; e < 4; ++e)
     {
+        if constexpr(TOKEN)
+        {
+            fs[e] = alpha * cs[e];
+            bs[e] = cb[e];
+            continue;
+        }
         const int64_t c = n + e < p.N ? n + e : p.N - 1;
         fs[e] = p.col_scale ? alpha * p.col_scale[c] : alpha;
         bs[e] = p.col_bias ? p.col_bias[c] : 0.0f;

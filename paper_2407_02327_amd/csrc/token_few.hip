@@ -13,9 +13,14 @@ namespace qsync {
 
 namespace {
 
-constexpr int kFewWaves = 8, kFewStages = 8, kFewRows = 16, kFewStageBytes = kFewWaves * kFewStages * 1024, kFewHeld = 8;
-constexpr int kFewLds = 156 * 1024;
-__host__ __device__ constexpr int64_t few_lds(int64_t rows, int64_t kb) { return kFewStageBytes + rows * (kb + 16); }
+constexpr int kFewWaves = 8, kFewRows = 16, kFewHeld = 8;
+constexpr int kFewLds = 96 * 1024;      // (at most 64 KB of stages, 16 KB of codes and their padding)
+int64_t few_lds(int64_t rows, int64_t kb, int stages) { return kFewWaves * stages * 1024 + rows * (kb + 16); }
+
+// What every workgroup quantizes for itself has to stay small, and the workgroups few enough to run at once.  One launch / two, us, binary16: 1 row
+// 1024x4096 6.6 / 7.4, 4096x4096 8.2 / 8.3, 300x16384 9.8 / 13.0; 4 rows 4096x1024 5.5 / 7.3, 4096x4096 9.2 / 8.8; 16 rows 1024x1024 6.6 / 7.0, 1024x4096
+// 11.1 / 7.0; 1 row 16384x1024 12.2 / 9.6.
+constexpr int64_t kFewElements = 16384, kFewColumns = 4096;
 
 struct FewArgs
 {
@@ -27,15 +32,16 @@ struct FewArgs
     int           rows, ydt;
 };
 
-template <typename T> __global__ __launch_bounds__(64 * kFewWaves) void token_few_kernel(const FewArgs p)
+// STAGES: turns of a wavefront in flight, no more than there are (short contractions: more workgroups on a unit).
+template <typename T, int STAGES> __global__ __launch_bounds__(64 * kFewWaves) void token_few_kernel(const FewArgs p)
 {
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     __shared__ uint32_t top[kFewWaves];
     __shared__ float    scales[kFewRows];
     const int     lane = threadIdx.x % kWaveSize, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x / kWaveSize));
     const int64_t n0 = static_cast<int64_t>(blockIdx.x) * 16, kb = code_pad(p.K);
-    uint8_t* const mine = lds + wave * (kFewStages * 1024);
-    uint8_t* const codes = lds + kFewStageBytes;
+    uint8_t* const mine = lds + wave * (STAGES * 1024);
+    uint8_t* const codes = lds + kFewWaves * STAGES * 1024;
     const int      pitch = static_cast<int>(kb) + 16;      // (sixteen rows' chunks meet all banks)
 
     // Weights: four lanes read 64 consecutive bytes of a column's row; the 16-byte chunks land XOR-swizzled.
@@ -44,7 +50,7 @@ template <typename T> __global__ __launch_bounds__(64 * kFewWaves) void token_fe
     const int      all = static_cast<int>(kb / 64), turns = all > wave ? (all - wave + kFewWaves - 1) / kFewWaves : 0;
     auto issue = [&](int t) {
         __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src + (static_cast<int64_t>(t) * kFewWaves + wave) * 64),
-                                         (__attribute__((address_space(3))) void*)(mine + t % kFewStages * 1024), 16, 0, 0);
+                                         (__attribute__((address_space(3))) void*)(mine + t % STAGES * 1024), 16, 0, 0);
     };
     // (the columns' scales and biases, by the wavefront that needs them: in front of everything, their latency is nobody's)
     float sb[4] = {}, bias[4] = {};
@@ -88,7 +94,7 @@ template <typename T> __global__ __launch_bounds__(64 * kFewWaves) void token_fe
             if(i * step < groups) load(g0 + i * step, v[i]);      // (the same for all lanes)
         if(!requested)      // (behind the first rows' loads: what waits for those does not wait for the weights)
         {
-            for(int t = 0; t < kFewStages && t < turns; ++t) issue(t);
+            for(int t = 0; t < STAGES && t < turns; ++t) issue(t);
             requested = true;
         }
 #pragma unroll
@@ -143,13 +149,13 @@ template <typename T> __global__ __launch_bounds__(64 * kFewWaves) void token_fe
     v4i32 acc = {0, 0, 0, 0};
     for(int t = 0; t < turns; ++t)
     {   // (every wavefront by itself: its loads, its slice of LDS)
-        wait_tiles<1, kFewStages - 1>(turns - 1 - t);
+        wait_tiles<1, STAGES - 1>(turns - 1 - t);
         v4i32 a, b;
-        frag_read<0>(b, frag + static_cast<uint32_t>(t % kFewStages * 1024));
+        frag_read<0>(b, frag + static_cast<uint32_t>(t % STAGES * 1024));
         frag_read<0>(a, code0 + static_cast<uint32_t>(t * (kFewWaves * 64)));
         asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(a), "+v"(b)::"memory");
         __builtin_amdgcn_sched_barrier(0);
-        if(t + kFewStages < turns) issue(t + kFewStages);      // (into the stage just read)
+        if(t + STAGES < turns) issue(t + STAGES);      // (into the stage just read)
         acc = I8Traits::mfma(b, a, acc);
         __builtin_amdgcn_sched_barrier(0);
     }
@@ -171,26 +177,31 @@ template <typename T> __global__ __launch_bounds__(64 * kFewWaves) void token_fe
     }
 }
 
-template <typename T> hipError_t launch_few(const FewArgs& a, hipStream_t st)
+template <typename T, int STAGES> hipError_t launch_stages(const FewArgs& a, hipStream_t st)
 {
     static bool attr_set[16] = {};      // per instantiation and device; benign if set twice
     int         dev = 0;
     const bool  known = hipGetDevice(&dev) == hipSuccess && dev >= 0 && dev < 16;
     if(!known || !attr_set[dev])
     {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&token_few_kernel<T>), hipFuncAttributeMaxDynamicSharedMemorySize, kFewLds);
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&token_few_kernel<T, STAGES>), hipFuncAttributeMaxDynamicSharedMemorySize, kFewLds);
         if(e != hipSuccess) return e;
         if(known) attr_set[dev] = true;
     }
-    token_few_kernel<T><<<static_cast<unsigned>((a.N + 15) / 16), 64 * kFewWaves, static_cast<size_t>(few_lds(a.rows, code_pad(a.K))), st>>>(a);
+    token_few_kernel<T, STAGES><<<static_cast<unsigned>((a.N + 15) / 16), 64 * kFewWaves, static_cast<size_t>(few_lds(a.rows, code_pad(a.K), STAGES)), st>>>(a);
     return hipGetLastError();
+}
+template <typename T> hipError_t launch_few(const FewArgs& a, hipStream_t st)
+{
+    const int64_t turns = (code_pad(a.K) / 64 + kFewWaves - 1) / kFewWaves;
+    return turns <= 2 ? launch_stages<T, 2>(a, st) : turns <= 4 ? launch_stages<T, 4>(a, st) : launch_stages<T, 8>(a, st);
 }
 
 }  // namespace
 
 hipError_t launch_token_few(const TokenMatrix& m, const TokenProduct& p, bool* taken, hipStream_t st)
 {
-    *taken = p.sets == 1 && !p.offsets && !m.source && p.rows <= kFewRows && p.K > 0 && few_lds(p.rows, code_pad(p.K)) <= kFewLds;
+    *taken = p.sets == 1 && !p.offsets && !m.source && p.rows <= kFewRows && p.K > 0 && p.rows * code_pad(p.K) <= kFewElements && p.N <= kFewColumns;
     if(!*taken) return hipSuccess;
     const FewArgs a{m.x, p.B, p.sb, p.bias, p.C, p.K, m.ld, p.N, static_cast<int>(p.rows), p.c_dtype};
     return m.dtype == kF16 ? launch_few<_Float16>(a, st) : m.dtype == kBF16 ? launch_few<__bf16>(a, st) : launch_few<float>(a, st);

@@ -287,7 +287,10 @@ template <bool WGRAD> int64_t most_tiles(const TokenProduct& p, int BM, int BN)
 template <bool WGRAD> int64_t blocks_of(const TokenProduct& p, int BM, int BN)
 {
     const int64_t tiles = most_tiles<WGRAD>(p, BM, BN);
-    return WGRAD ? (tiles + kNumXcd - 1) / kNumXcd * kNumXcd + (p.sets % kNumXcd ? tiles / p.sets * kNumXcd : 0) : tiles + kNumXcd + (BM == 256 ? 3 * kRest : 0);
+    if(!WGRAD) return tiles + kNumXcd + (BM == 256 ? 3 * kRest : 0);
+    if(!p.offsets || p.sets > kFewSets) return (tiles + kNumXcd - 1) / kNumXcd * kNumXcd;
+    const int64_t one = tiles / p.sets, left = p.sets % kNumXcd * (one / kNumXcd + 1);
+    return kNumXcd * (p.sets / kNumXcd * one + (left < one ? left : one));
 }
 int wgrad_group(const TokenProduct& p) { return p.offsets && p.sets <= kFewSets ? 4 : kGroupM; }
 
@@ -332,7 +335,9 @@ GemmPlan product_plan(bool wgrad, int64_t rows, int64_t M, int64_t N, int64_t K,
     return plan;
 }
 
-constexpr int64_t kPairBlocks = 4 * kNumCu * 2;
+// Workgroups (64 tiles of both gradients) up to which they share a launch; us, joined / apart: 300x200x100 of 3 sets 6.7 / 9.7, 2048x2048x1024 15.7 / 21.8,
+// 1500x3000x700 18.9 / 29.8, 4000x1000x500 of 16 sets 25.0 / 32.9; 4096x1024x2048 (2576 workgroups) 34.4 / 32.6.
+constexpr int64_t kPairBlocks = 8 * kNumCu, kPairBlocksSets = 16 * kNumCu;
 template <bool WGRAD> hipError_t launch_product(const TokenProduct& p, void* workspace, size_t workspace_bytes, hipStream_t st)
 {
     const GemmPlan plan = product_plan(WGRAD, p.rows, p.M, p.N, p.K, p.sets, p.offsets != nullptr);
@@ -382,7 +387,7 @@ hipError_t launch_token_gradients(const TokenProduct& x, const TokenProduct& w, 
 {
     const GemmPlan px = product_plan(false, x.rows, x.M, x.N, x.K, x.sets, x.offsets != nullptr), pw = product_plan(true, w.rows, w.M, w.N, w.K, w.sets, w.offsets != nullptr);
     const int64_t  first = (blocks_of<false>(x, 64, 64) + kNumXcd - 1) / kNumXcd * kNumXcd, all = first + blocks_of<true>(w, 64, 64);
-    if(px.tile >= 1 && px.splits == 1 && pw.tile >= 1 && pw.splits == 1 && all <= kPairBlocks && !token_rows_takes(x))
+    if(px.tile >= 1 && px.splits == 1 && pw.tile >= 1 && pw.splits == 1 && all <= (x.offsets ? kPairBlocksSets : kPairBlocks) && !token_rows_takes(x))
     {
         constexpr int lds = 2 * (64 + 64) * kRowBytes + kColumnBytes<64> + 64 * 4;
         static bool   set[kMaxDevices] = {};
