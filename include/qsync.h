@@ -729,7 +729,8 @@ size_t qsync_distill_topk_workspace_bytes(int ldt, int64_t rows, int64_t cols);
  * outputs and no access outside of the buffers.
  * Codes along the rows (of the columns, transposed) hold, set after set, a packed matrix [cols][rows of the set rounded up to 128]; the
  * buffer has qsync_token_code_rows(rows, sets, offsets != NULL) * cols bytes.
- * Limits: rows <= 2^23, cols <= 2^20, sets 1..512 (QSYNC_ERR_UNSUPPORTED beyond).  x is of QSYNC_F32, QSYNC_F16 or QSYNC_BF16 at any
+ * Limits: rows <= 2^23, cols <= 2^20, sets 1..512, and of codes along the rows sets * cols <= 2^27 and 2^36 codes (QSYNC_ERR_UNSUPPORTED
+ * beyond).  x is of QSYNC_F32, QSYNC_F16 or QSYNC_BF16 at any
  * element's alignment; codes, and the workspace, are 16-byte aligned.  Outputs do not overlap inputs.
  */
 int64_t qsync_token_code_cols(int64_t cols);
@@ -797,8 +798,8 @@ int qsync_token_linear(const void* x, int xdt, int64_t x_rows, int64_t K, int64_
                        int ydt, float* sx, void* xq, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
- * qsync_token_linear_wgrad - dW[e,n,k] = (sum over the rows m of set e of dyqT[n,m] xqT[k,m]) * (sdy[e,n] * sx[e,k]), on codes along the rows
- * (qsync_token_quantize_both) of dY [rows, N] and X [rows, K].  dw out, [sets, N, K] of dwdt; zeros for a set without rows.
+ * qsync_token_linear_wgrad - dW[e,n,k] = (sum over the rows m of set e of dyqT[n,m] xqT[k,m]) * (sdy[e,n] * sx[e,k]), the sum in int32 (which wraps
+ * mod 2^32: never for sets of up to 133144 rows), on codes along the rows (qsync_token_quantize_both) of dY [rows, N] and X [rows, K].  dw out, [sets, N, K] of dwdt; zeros for a set without rows.
  * offsets_opt NULL: one set.  workspace: qsync_token_wgrad_workspace_bytes(rows, N, K, sets) bytes, as above.
  */
 int qsync_token_linear_wgrad(int64_t rows, int64_t N, int64_t K, int64_t sets, const int32_t* offsets_opt, const void* dyqT,

@@ -1167,11 +1167,13 @@ int token_matrix(const void* x, int xdt, int64_t x_rows, int64_t cols, int64_t l
     if(rows == 0 || cols == 0) return 1;
     return elements_aligned(x, xdt) && elements_aligned(source, QSYNC_I32) ? QSYNC_OK : QSYNC_ERR_ALIGN;
 }
-int token_sets(int64_t rows, int64_t sets, const int32_t* offsets)
+int token_sets(int64_t rows, int64_t cols, int64_t sets, const int32_t* offsets)
 {
     if(sets < 0) return QSYNC_ERR_BAD_SHAPE;
     if(sets < 1 || sets > kMaxSets) return QSYNC_ERR_UNSUPPORTED;
-    return offsets || rows % sets == 0 ? QSYNC_OK : QSYNC_ERR_BAD_SHAPE;
+    if(!offsets && rows % sets != 0) return QSYNC_ERR_BAD_SHAPE;
+    // (threads that a grid can count: of the columns' scales, of the codes)
+    return sets * cols > (int64_t(1) << 27) || qsync_token_code_rows(rows, sets, offsets != nullptr) * qsync_token_code_cols(cols) > (int64_t(1) << 36) ? QSYNC_ERR_UNSUPPORTED : QSYNC_OK;
 }
 int token_product(int64_t rows, int64_t N, int64_t K, int64_t sets, const int32_t* offsets, const void* a, const float* sa, const void* b, const float* sb, const float* bias,
                   const void* c, int cdt)
@@ -1218,7 +1220,7 @@ int qsync_token_quantize_both(const void* x, int xdt, int64_t x_rows, int64_t co
     if(!row_scale || !q || !col_scale || !qT) return QSYNC_ERR_NULL;
     int rc = token_matrix(x, xdt, x_rows, cols, ld, source_opt, group, rows, rnd);
     if(rc < 0) return rc;
-    const int sc = token_sets(rows, sets, offsets_opt);
+    const int sc = token_sets(rows, cols, sets, offsets_opt);
     if(sc != QSYNC_OK) return sc;
     if(rc == 1)
     {   // no rows: no scale is set by any; the sums are zeros
@@ -1246,7 +1248,8 @@ int qsync_token_convert(const void* x, int xdt, int64_t x_rows, int64_t K, int64
     if(rx < 0) return rx;
     const int rw = token_matrix(w, wdt, wrows, K, K, nullptr, 1, wrows, QSYNC_ROUND_NEAREST);
     if(rw < 0) return rw;
-    const int sc = token_sets(rows, sets, offsets_opt);
+    int sc = token_sets(rows, K, sets, offsets_opt);
+    if(sc == QSYNC_OK) sc = token_sets(wrows, K, sets, nullptr);
     if(sc != QSYNC_OK) return sc;
     // an operand without elements: the other by itself
     if(rx == 1)

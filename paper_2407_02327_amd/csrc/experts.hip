@@ -366,7 +366,7 @@ constexpr int64_t kManyRows = 4096;      // workgroups of one row a thread from 
 // rows (of 256 >> side_log2 a workgroup) over the grid's y and z: neither may count more than 65535
 dim3 rows_over_grid(const RowGrid& g, int64_t rows, int per_thread = 1)
 {
-    const int64_t each = static_cast<int64_t>(256 >> g.side_log2) * per_thread, blocks = (rows + each - 1) / each, z = blocks < 128 ? 1 : 128;
+    const int64_t each = static_cast<int64_t>(256 >> g.side_log2) * per_thread, blocks = (rows + each - 1) / each, z = blocks < 256 ? 1 : 256;
     return dim3(static_cast<unsigned>(g.blocks_x), static_cast<unsigned>((blocks + z - 1) / z), static_cast<unsigned>(z));
 }
 

@@ -17,6 +17,7 @@ typedef float    v16f32 __attribute__((ext_vector_type(16)));
 typedef float    v4f32 __attribute__((ext_vector_type(4)));
 typedef _Float16 v8f16 __attribute__((ext_vector_type(8)));
 typedef unsigned v4u32 __attribute__((ext_vector_type(4)));
+typedef v4u32    v4u32_any __attribute__((aligned(2)));
 
 constexpr int kRowBytes   = 128;  // K bytes per tile row and per LDS row
 constexpr int kChunks     = 8;    // 16-byte chunks per LDS row
@@ -514,6 +515,13 @@ __device__ __forceinline__ void store_tile(const GemmKernelArgs& p, typename TR:
                 const v4u32   val = *reinterpret_cast<const v4u32*>(stg + (r + lr0) * PITCH + seg * 16);
                 const int64_t row = row0 + r, left = row < p.M ? p.N - col : 0;      // valid elements from here on (may be <= 0)
                 const int64_t at  = row * p.N + col;
+                // (memory takes 16 bytes at any element's address: 2187x1001x777 with fp32 output 13.4 -> 9.2 us)
+                if constexpr(TOKEN)
+                    if(left >= EPV)
+                    {
+                        __builtin_nontemporal_store(val, reinterpret_cast<v4u32_any*>(dst_base + at * OS));
+                        continue;
+                    }
 #pragma unroll
                 for(int e = 0; e < EPV; ++e)
                 {

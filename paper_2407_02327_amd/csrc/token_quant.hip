@@ -188,7 +188,9 @@ __device__ __forceinline__ Chunk chunk_rows(const int32_t* offsets, int64_t rows
 // a workgroup has sixteen rows at a time and, with all eight of a lane's loads requested before the first is used, 32 to 64 KB in flight.
 // With 512 columns, a row a wavefront and one load in flight a chunk took 30 us whatever its size.
 // rowpart [column tiles][rows], colpart [chunks][cols]: maxima, sums
-constexpr int kStatCols = 128;
+// A matrix of few such workgroups goes in quarters of a chunk (2187x1001 fp32 with sums, 144 of them: 8.5 -> 6.3 us).
+constexpr int      kStatCols = 128, kStatRows = 32;
+constexpr uint32_t kStatFew  = 1024;
 __device__ __forceinline__ uint32_t max_of_16(uint32_t v)
 {
     auto step = [&](auto ctrl) { v = max(v, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), decltype(ctrl)::value, 0xF, 0xF, false))); };
@@ -203,17 +205,18 @@ struct BothArgs      // one matrix's part in the three passes
     TokenSource    s;
     const int32_t* offsets;
     int64_t        sets;
-    uint32_t       chunks, stat_tiles, code_tiles, scale_blocks, col_blocks;      // (scale_blocks: of rows and columns, those of the columns first)
+    uint32_t       chunks, pieces, stat_tiles, code_tiles, scale_blocks, col_blocks;      // (pieces: of a chunk in the first pass; scale_blocks: of rows and columns, those of the columns first)
     uint32_t *     rowpart, *colmax;
     float *        colsum, *row_scale, *row_inv, *col_scale, *col_inv, *sum_out;
     int8_t *       q, *qT;
+    __host__ __device__ uint32_t stat_blocks() const { return chunks * pieces * stat_tiles; }
 };
 template <bool SUM> struct StatsLds
 {
     uint32_t lmax[4][kStatCols];
     float    lsum[SUM ? 4 : 1][SUM ? kStatCols : 1];
 };
-template <typename T, bool SUM> __device__ __forceinline__ void stats_body(const BothArgs& p, uint32_t block, StatsLds<SUM>& lds)
+template <typename T, bool SUM, int R> __device__ __forceinline__ void stats_body(const BothArgs& p, uint32_t block, StatsLds<SUM>& lds)
 {
     const TokenSource& s = p.s;
     const int32_t*     offsets = p.offsets;
@@ -224,11 +227,23 @@ template <typename T, bool SUM> __device__ __forceinline__ void stats_body(const
     auto&              lmax = lds.lmax;
     [[maybe_unused]] auto& lsum = lds.lsum;
     const int     lane = threadIdx.x % 64, wave = threadIdx.x / 64, side = threadIdx.x % 16, down = threadIdx.x / 16;
-    const uint32_t tile = block % tiles, chunk = block / tiles;
-    const Chunk    c = chunk_rows(offsets, s.rows, sets, chunk);
-    if(c.len <= 0) return;
+    const uint32_t tile = block % tiles, piece = block / tiles;
+    Chunk          c = chunk_rows(offsets, s.rows, sets, piece / (kCodePad / R));
+    const int      skip = static_cast<int>(piece % (kCodePad / R)) * R;
+    c.row0 += skip;
+    c.len = min(c.len - skip, R);
     const int64_t col = static_cast<int64_t>(tile) * kStatCols + side * 8;
-    constexpr int N = kCodePad / 16;
+    if(c.len <= 0)
+    {   // (a piece behind its chunk's rows is folded like the others)
+        const int64_t at = static_cast<int64_t>(tile) * kStatCols + threadIdx.x;
+        if(threadIdx.x < kStatCols && at < s.cols)
+        {
+            colmax[piece * s.cols + at] = 0u;
+            if constexpr(SUM) colsum[piece * s.cols + at] = 0.0f;
+        }
+        return;
+    }
+    constexpr int N = R / 16;
     Row8<T>       v[N];
     bool          there[N];
 #pragma unroll
@@ -281,22 +296,23 @@ template <typename T, bool SUM> __device__ __forceinline__ void stats_body(const
     const int     i  = threadIdx.x;
     const int64_t at = static_cast<int64_t>(tile) * kStatCols + i;
     if(i >= kStatCols || at >= s.cols) return;
-    colmax[chunk * s.cols + at] = max(max(lmax[0][i], lmax[1][i]), max(lmax[2][i], lmax[3][i]));
-    if constexpr(SUM) colsum[chunk * s.cols + at] = (lsum[0][i] + lsum[1][i]) + (lsum[2][i] + lsum[3][i]);
+    colmax[piece * s.cols + at] = max(max(lmax[0][i], lmax[1][i]), max(lmax[2][i], lmax[3][i]));
+    if constexpr(SUM) colsum[piece * s.cols + at] = (lsum[0][i] + lsum[1][i]) + (lsum[2][i] + lsum[3][i]);
 }
 
-template <typename T, bool SUM> __global__ __launch_bounds__(256) void token_stats_kernel(const BothArgs p)
+// R: rows of a workgroup, all of a chunk's or a quarter (BothArgs::pieces)
+template <typename T, bool SUM, int R> __global__ __launch_bounds__(256) void token_stats_kernel(const BothArgs p)
 {
     __shared__ StatsLds<SUM> lds;
-    stats_body<T, SUM>(p, blockIdx.x, lds);
+    stats_body<T, SUM, R>(p, blockIdx.x, lds);
 }
 // of two matrices, `a` first
-template <typename TA, typename TB> __global__ __launch_bounds__(256) void token_stats_pair_kernel(const BothArgs a, const BothArgs b)
+template <typename TA, typename TB, int R> __global__ __launch_bounds__(256) void token_stats_pair_kernel(const BothArgs a, const BothArgs b)
 {
     __shared__ StatsLds<false> lds;
-    const uint32_t n = a.chunks * a.stat_tiles;
-    if(blockIdx.x < n) stats_body<TA, false>(a, blockIdx.x, lds);
-    else               stats_body<TB, false>(b, blockIdx.x - n, lds);
+    const uint32_t n = a.stat_blocks();
+    if(blockIdx.x < n) stats_body<TA, false, R>(a, blockIdx.x, lds);
+    else               stats_body<TB, false, R>(b, blockIdx.x - n, lds);
 }
 
 // Scales and inverse scales of the rows (workgroups behind `col_blocks`) and of the sets' columns: sixteen threads fold a column's chunks,
@@ -330,7 +346,7 @@ template <bool SUM> __device__ __forceinline__ void scales_body(const BothArgs& 
     const int     side = threadIdx.x % 16, part = threadIdx.x / 16;
     const int64_t tiles = (cols + 15) / 16, e = block / tiles, c = block % tiles * 16 + side, cc = c < cols ? c : cols - 1;
     const SetRows s = set_rows(offsets, rows, sets, e);
-    const int64_t first = set_start(offsets, s, e) / kCodePad, end = first + code_pad(s.len) / kCodePad;
+    const int64_t first = set_start(offsets, s, e) / kCodePad * p.pieces, end = first + code_pad(s.len) / kCodePad * p.pieces;
     uint32_t      m = 0u;
     float         sum = 0.0f;
     for(int64_t k0 = first + part; k0 < end; k0 += 64)
@@ -462,9 +478,11 @@ BothWorkspace both_workspace(int64_t rows, int64_t cols, int64_t sets, bool offs
     w.rowpart = 0;
     w.row_inv = w.rowpart + up(tiles * rows * 4);
     w.col_inv = w.row_inv + up(static_cast<size_t>(rows) * 4);
+    // (what is enough for some number of rows is enough for fewer: partial results of fewer chunks in more pieces)
+    const size_t few = (kStatFew + tiles) / tiles * (kCodePad / kStatRows), parts = chunks * tiles < kStatFew ? chunks * (kCodePad / kStatRows) : chunks > few ? chunks : few;
     w.colmax  = w.col_inv + up(static_cast<size_t>(sets) * cols * 4);
-    w.colsum  = w.colmax + up(chunks * cols * 4);
-    w.total   = w.colsum + up(chunks * cols * 4);
+    w.colsum  = w.colmax + up(parts * cols * 4);
+    w.total   = w.colsum + up(parts * cols * 4);
     return w;
 }
 
@@ -478,6 +496,7 @@ BothArgs both_args(const TokenMatrix& m, const TokenBoth& o)
     a.sets       = o.sets;
     a.chunks     = static_cast<uint32_t>(code_positions(m.rows, o.sets, o.offsets != nullptr) / kCodePad);
     a.stat_tiles = static_cast<uint32_t>((m.cols + kStatCols - 1) / kStatCols);
+    a.pieces     = a.chunks * a.stat_tiles < kStatFew ? kCodePad / kStatRows : 1;
     a.code_tiles = static_cast<uint32_t>(code_pad(m.cols) / 64);
     a.col_blocks = static_cast<uint32_t>(o.sets * ((m.cols + 15) / 16));
     a.scale_blocks = a.col_blocks + static_cast<uint32_t>((m.rows + 255) / 256);
@@ -495,14 +514,17 @@ BothArgs both_args(const TokenMatrix& m, const TokenBoth& o)
 }
 template <typename T, int RND> hipError_t launch_both(const BothArgs& a, uint64_t seed, uint64_t offset, hipStream_t st)
 {
+    const unsigned blocks = a.stat_blocks();
     if(a.sum_out)
     {
-        token_stats_kernel<T, true><<<a.chunks * a.stat_tiles, 256, 0, st>>>(a);
+        if(a.pieces > 1) token_stats_kernel<T, true, kStatRows><<<blocks, 256, 0, st>>>(a);
+        else             token_stats_kernel<T, true, kCodePad><<<blocks, 256, 0, st>>>(a);
         token_scales_kernel<true><<<a.scale_blocks, 256, 0, st>>>(a);
     }
     else
     {
-        token_stats_kernel<T, false><<<a.chunks * a.stat_tiles, 256, 0, st>>>(a);
+        if(a.pieces > 1) token_stats_kernel<T, false, kStatRows><<<blocks, 256, 0, st>>>(a);
+        else             token_stats_kernel<T, false, kCodePad><<<blocks, 256, 0, st>>>(a);
         token_scales_kernel<false><<<a.scale_blocks, 256, 0, st>>>(a);
     }
     token_codes_kernel<T, RND><<<a.chunks * a.code_tiles, 256, 0, st>>>(a, seed, offset);
@@ -539,12 +561,14 @@ hipError_t launch_token_quantize_both(const TokenMatrix& m, const TokenBoth& o, 
 // Each pass of the two matrices in one launch.  (The launches of one beside the other's: what a small matrix's take is latency.)
 hipError_t launch_token_quantize_pair(const TokenMatrix& m, const TokenBoth& o, const TokenMatrix& m2, const TokenBoth& o2, hipStream_t st)
 {
-    const BothArgs a = both_args(m, o), b = both_args(m2, o2);
+    BothArgs a = both_args(m, o), b = both_args(m2, o2);
+    a.pieces = b.pieces = a.pieces > 1 && b.pieces > 1 ? a.pieces : 1;
     return with_type(m.dtype, [&](auto tag) {
         typedef decltype(tag) TA;
         return with_type(m2.dtype, [&](auto tag2) {
             typedef decltype(tag2) TB;
-            token_stats_pair_kernel<TA, TB><<<a.chunks * a.stat_tiles + b.chunks * b.stat_tiles, 256, 0, st>>>(a, b);
+            if(a.pieces > 1) token_stats_pair_kernel<TA, TB, kStatRows><<<a.stat_blocks() + b.stat_blocks(), 256, 0, st>>>(a, b);
+            else             token_stats_pair_kernel<TA, TB, kCodePad><<<a.stat_blocks() + b.stat_blocks(), 256, 0, st>>>(a, b);
             token_scales_pair_kernel<<<a.scale_blocks + b.scale_blocks, 256, 0, st>>>(a, b);
             token_codes_pair_kernel<TA, TB><<<a.chunks * a.code_tiles + b.chunks * b.code_tiles, 256, 0, st>>>(a, b);
             return hipGetLastError();

@@ -94,6 +94,8 @@ def test_quantizers():
     need = Q.qsync_token_quantize_both_workspace_bytes(8, 100, 3, True)
     assert need > 0 and BOTH.but(ws_bytes=need - 1) == Q.ERR_WORKSPACE and BOTH.but(ws=NULL) == Q.ERR_WORKSPACE and BOTH.but(ws=_at(9, 8)) == Q.ERR_ALIGN
     assert BOTH.but(rows=0, sums=NULL) == Q.OK
+    huge = dict(x_rows=1 << 23, rows=1 << 23, ws_bytes=1 << 62)                    # (more than a grid's threads count)
+    assert BOTH.but(cols=1 << 14, ld=1 << 14, **huge) == Q.ERR_UNSUPPORTED and BOTH.but(cols=1 << 19, ld=1 << 19, sets=512) == Q.ERR_UNSUPPORTED
 
 
 def test_convert():
