@@ -719,8 +719,9 @@ size_t qsync_distill_topk_workspace_bytes(int ldt, int64_t rows, int64_t cols);
  * Codes of a slice v (a row, or a column within a set of rows) with a = max |v|:
  *   a < 2^-100: scale 1, codes 0.   a not finite: scale NaN, codes 0 (what takes part in its products is NaN, nothing else is).
  *   otherwise scale = a / 127, inverse = 127 / a (one fp32 division each), code = clamp(round(v * inverse), -127, 127).
- * round: to nearest even, or stochastic as in qsync_quantize, where the element (row, col) has the draw col % 8 of the Philox block
- * offset + row * ceil(cols / 8) + col / 8; a call consumes rows * ceil(cols / 8) counters.
+ * round: to nearest even, or stochastic as in qsync_quantize (floor(x), and 1 more where u < floor((x - floor(x)) * 2^16), the difference in
+ * fp32), where the element (row, col) has the draw col % 8 of the Philox block offset + row * ceil(cols / 8) + col / 8; a call consumes
+ * rows * ceil(cols / 8) counters.
  *
  * Rows of codes are padded with zeros to qsync_token_code_cols(cols) = cols rounded up to a multiple of 128.
  * Sets of rows: with offsets_opt (device, sets + 1 int32, ascending from 0), set e has the rows offsets[e] .. offsets[e+1]-1 and rows from

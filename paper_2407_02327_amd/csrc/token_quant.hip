@@ -51,25 +51,29 @@ template <typename T> __device__ __forceinline__ uint32_t max8(const Row8<T>& v,
 // Codes in as few vector operations as they take (with the general quantizer's,
 // about twice as many, the vector unit is as busy as the memory).  A slice's own inverse keeps its products within 127 and a rounding:
 //   nearest: adding 1.5 2^23 leaves the integer, to nearest even, in the low byte of the sum;
-//   stochastic: t = floor(x inv 2^16), clamped, + 65535 - u has the code in byte 2 (2^16 in one factor with the inverse: it moves the exponent only).
-// The factor of a slice that is not finite is 0, and the product by the rule that zero times anything is zero.
-template <int RND> __device__ __forceinline__ float code_factor(float inv) { return RND == kStochastic ? inv * 65536.0f : inv; }
-template <int RND, int J> __device__ __forceinline__ uint32_t code_word(float x, float factor, const uint32_t (&not_u)[4])
+//   stochastic: floor(v) likewise, and 1 more where u < floor(fl(v - floor(v)) 2^16), the carry of that + 65535 - u into bit 16.  (The difference is
+//   rounded to 32 bits, as the oracle's is: floor(v 2^16) would be four operations less, and another code for one negative v above -1/2 in 2^25.)
+// The inverse of a slice that is not finite is 0, and the product by the rule that zero times anything is zero.
+template <int RND, int J> __device__ __forceinline__ uint32_t code_word(float x, float inv, const uint32_t (&not_u)[4])
 {
     float v;
-    asm("v_mul_legacy_f32 %0, %1, %2" : "=v"(v) : "v"(x), "v"(factor));
-    if constexpr(RND == kStochastic) return add_half<J % 2>(clamped_fixed_point(v, 127), not_u[J / 2]);
-    else                             return __float_as_uint(v + 12582912.0f);
+    asm("v_mul_legacy_f32 %0, %1, %2" : "=v"(v) : "v"(x), "v"(inv));
+    if constexpr(RND == kStochastic)
+    {
+        v = __builtin_amdgcn_fmed3f(v, -127.0f, 127.0f);
+        const float down = floorf(v), part = v - down;
+        return add_half<1>(static_cast<int>(__float_as_uint(down + 12582912.0f)), add_half<J % 2>(static_cast<int>(static_cast<uint32_t>(part * 65536.0f)), not_u[J / 2]));
+    }
+    else return __float_as_uint(v + 12582912.0f);
 }
-template <int RND> __device__ __forceinline__ uint32_t pack_codes(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+__device__ __forceinline__ uint32_t pack_codes(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
 {
-    if constexpr(RND == kStochastic) return __builtin_amdgcn_perm(b, a, 0x0C0C0602u) | __builtin_amdgcn_perm(d, c, 0x06020C0Cu);
-    else                             return __builtin_amdgcn_perm(b, a, 0x0C0C0400u) | __builtin_amdgcn_perm(d, c, 0x04000C0Cu);
+    return __builtin_amdgcn_perm(b, a, 0x0C0C0400u) | __builtin_amdgcn_perm(d, c, 0x04000C0Cu);
 }
 template <int RND> __device__ __forceinline__ uint2 codes8(const float (&e)[8], float f, const uint32_t (&u)[4])
 {
-    return make_uint2(pack_codes<RND>(code_word<RND, 0>(e[0], f, u), code_word<RND, 1>(e[1], f, u), code_word<RND, 2>(e[2], f, u), code_word<RND, 3>(e[3], f, u)),
-                      pack_codes<RND>(code_word<RND, 4>(e[4], f, u), code_word<RND, 5>(e[5], f, u), code_word<RND, 6>(e[6], f, u), code_word<RND, 7>(e[7], f, u)));
+    return make_uint2(pack_codes(code_word<RND, 0>(e[0], f, u), code_word<RND, 1>(e[1], f, u), code_word<RND, 2>(e[2], f, u), code_word<RND, 3>(e[3], f, u)),
+                      pack_codes(code_word<RND, 4>(e[4], f, u), code_word<RND, 5>(e[5], f, u), code_word<RND, 6>(e[6], f, u), code_word<RND, 7>(e[7], f, u)));
 }
 // the complements of the draws of a block of eight elements
 template <int RND> __device__ __forceinline__ void draws8(uint64_t seed, uint64_t offset, int64_t group, uint32_t (&not_u)[4])
@@ -123,13 +127,12 @@ __global__ __launch_bounds__(256) void token_rows_kernel(TokenSource s, const in
     const CodeScale cs = code_scale(m);
     if(t == 0) scale[r] = cs.scale;
     int8_t* out = q + r * groups * 8;
-    const float f = code_factor<RND>(cs.inv);
-    auto        put = [&](const Row8<T>& w, int64_t g) {
+    auto put = [&](const Row8<T>& w, int64_t g) {
         float    e[8];
         uint32_t u[4];
         w.decode(e);
         draws8<RND>(seed, offset, r * per_row + g, u);
-        *reinterpret_cast<uint2*>(out + g * 8) = codes8<RND>(e, f, u);
+        *reinterpret_cast<uint2*>(out + g * 8) = codes8<RND>(e, cs.inv, u);
     };
 #pragma unroll
     for(int i = 0; i < V; ++i)
@@ -420,10 +423,10 @@ template <typename T, int RND> __device__ __forceinline__ void codes_body(const 
         const bool    in = rq * 4 + i < c.len;
         const int64_t r = c.row0 + (in ? rq * 4 + i : 0), from = in ? source_row(s, r) : -1;
         load8(static_cast<const T*>(s.x) + (from < 0 ? 0 : from) * s.ld, col, from < 0 ? 0 : s.cols, v[i]);
-        rf[i] = code_factor<RND>(row_inv[r]);
+        rf[i] = row_inv[r];
     }
 #pragma unroll
-    for(int j = 0; j < 8; ++j) ci[j] = code_factor<RND>(col + j < s.cols ? col_inv[c.set * s.cols + col + j] : 0.0f);
+    for(int j = 0; j < 8; ++j) ci[j] = col + j < s.cols ? col_inv[c.set * s.cols + col + j] : 0.0f;
     uint32_t k[4][8], w[8];
 #pragma unroll
     for(int i = 0; i < 4; ++i)
@@ -440,7 +443,7 @@ template <typename T, int RND> __device__ __forceinline__ void codes_body(const 
         k[i][6] = code_word<RND, 6>(e[6], ci[6], u); k[i][7] = code_word<RND, 7>(e[7], ci[7], u);
     }
 #pragma unroll
-    for(int j = 0; j < 8; ++j) w[j] = pack_codes<RND>(k[0][j], k[1][j], k[2][j], k[3][j]);
+    for(int j = 0; j < 8; ++j) w[j] = pack_codes(k[0][j], k[1][j], k[2][j], k[3][j]);
 #pragma unroll
     for(int j = 0; j < 8; ++j) lds[(cg * 8 + j) * 33 + rq] = w[j];
     __syncthreads();

@@ -510,3 +510,19 @@ def test_offsets_that_pass_32_bits():
     xq, sx = R.codes(f64(x[at]), 1)
     want, bound = R.product(xq, sx, *R.codes(f64(w), 1))
     assert_within(y[at], want, bound + rounded(want, F16), "rows")
+
+
+def test_fractions_that_32_bits_round():
+    """Negative products above -1/2 whose distance to the floor below takes more than 24 bits, at the draws where that decides: the oracle's
+    codes.  (A column of 127 is every row's largest, so that the products are the values themselves.)"""
+    rows, cols = 64, 1032
+    u = R.draws(rows, cols, SEED, OFFSET).astype(np.float64)
+    x = np.full((rows, cols), 127.0, np.float32)
+    x[:, 8:] = (-((65536 - u[:, 8:]) / 65536)).astype(np.float32)                       # the border itself, and one step of 2^-25 on either side
+    x[1::3, 8:] = np.nextafter(x[1::3, 8:], np.float32(-2))
+    x[2::3, 8:] = np.nextafter(x[2::3, 8:], np.float32(2))
+    q, s, qT, sc, _ = quantize_both(torch.from_numpy(x).cuda(), 1, None, Q.ROUND_STOCHASTIC)
+    down = np.floor(x)
+    oracle = np.clip(down + (u < ((x - down).astype(np.float32) * np.float32(65536.0)).astype(np.uint32)), -127, 127)
+    equal(q[:, :cols], oracle, "codes")
+    check_rows(q, s, x, R.draws(rows, cols, SEED, OFFSET), "rows")

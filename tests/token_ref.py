@@ -30,7 +30,7 @@ def codes(x: np.ndarray, axis: int, u=None):
         q = np.rint(v)
     else:
         down = np.floor(v)
-        q = down + (u < np.floor((v.astype(np.float64) - down) * 65536.0))
+        q = down + (u < np.floor((v - down).astype(np.float32) * np.float32(65536.0)))      # (the difference in 32 bits, as in the oracle)
     return np.clip(q, -127, 127).astype(np.int64), np.squeeze(scale, axis)
 
 
