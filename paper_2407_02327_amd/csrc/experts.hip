@@ -138,34 +138,66 @@ __global__ __launch_bounds__(kSortThreads) void expert_place_kernel(const I* ids
 }
 
 // ---- rows ------------------------------------------------------------------------------------------------------------------------
-// Eight columns a thread; a workgroup's 256 threads are 256 / side rows (or tokens) of `side` threads, as many as a row has vectors up to 256, and
-// longer rows take several workgroups: whatever the shape, a thread does little, and a launch has as many threads as there is data.
+// A thread has V columns, 16 bytes of the input (in the backward pass eight, whatever the type: 3333x1001 fp32, three rows each, 23.5 us, by fours 25.8); a workgroup's 256 threads are 256 / side rows (or tokens) of
+// `side` threads, as many as a row has vectors up to 256, and longer rows take several workgroups: whatever the shape, a thread does little, and
+// a launch has as many threads as there is data.
 struct RowGrid { int side_log2, blocks_x; };
-RowGrid row_grid(int64_t cols, int least)
+RowGrid row_grid(int64_t cols, int V, int least)
 {
-    const int64_t vectors = (cols + 7) / 8;
+    const int64_t vectors = (cols + V - 1) / V;
     int           log2 = least;
     while(log2 < 8 && (int64_t(1) << log2) < vectors) ++log2;
     return {log2, static_cast<int>((vectors + (1 << log2) - 1) >> log2)};
 }
-template <typename T> __device__ __forceinline__ void load_tail(const T* row, int64_t c, int64_t cols, Row8<T>& v)
+template <typename T, int V> struct RowPart
 {
-    if(c + 8 <= cols) v.load(row + c);
-    else
+    static constexpr int N = RowType<T>::N;
+    row_v4u32 w[V / N];
+    __device__ __forceinline__ void load(const T* row, int64_t c, int64_t cols)      // zeros behind the last column
     {
-        float e[8];
+        if(c + V <= cols)
 #pragma unroll
-        for(int i = 0; i < 8; ++i) e[i] = c + i < cols ? row_element(row + c + i) : 0.0f;
-        v.encode(e);
+            for(int i = 0; i < V / N; ++i) w[i] = row_load(row + c + i * N);
+        else
+        {
+            float e[V];
+#pragma unroll
+            for(int i = 0; i < V; ++i) e[i] = c + i < cols ? row_element(row + c + i) : 0.0f;
+            encode(e);
+        }
     }
-}
-__device__ __forceinline__ void store_tail(void* base, int dtype, int64_t at, int64_t c, int64_t cols, float (&v)[8])
-{
-    if(c + 8 <= cols) row8_store<false>(base, dtype, at + c, v);
-    else
+    __device__ __forceinline__ void decode(float (&v)[V]) const
+    {
 #pragma unroll
-        for(int i = 0; i < 8; ++i)
+        for(int i = 0; i < V / N; ++i) row_decode<T>(w[i], v + i * N);
+    }
+    __device__ __forceinline__ void encode(const float (&v)[V])
+    {
+#pragma unroll
+        for(int i = 0; i < V / N; ++i)
+        {
+            float e[N];
+#pragma unroll
+            for(int j = 0; j < N; ++j) e[j] = v[i * N + j];
+            w[i] = RowType<T>::pack(e);
+        }
+    }
+    __device__ __forceinline__ void store(T* p) const
+    {
+#pragma unroll
+        for(int i = 0; i < V / N; ++i) row_store(p + i * N, w[i]);
+    }
+};
+template <int V> __device__ __forceinline__ void store_part(void* base, int dtype, int64_t at, int64_t c, int64_t cols, float (&v)[V])
+{
+    if(c + V > cols)
+    {
+#pragma unroll
+        for(int i = 0; i < V; ++i)
             if(c + i < cols) element_store(base, dtype, at + c + i, v[i]);
+    }
+    else if constexpr(V == 8) row8_store<false>(base, dtype, at + c, v);
+    else                      vector_store<float, false>(base, dtype, at + c, v);
 }
 
 // rows[r] = x[source[r] / group]; a place outside of x: NaN.  A thread has U rows, their loads requested together (65536 rows of 1024 bfloat16: one
@@ -174,24 +206,25 @@ template <typename T, int U>
 __global__ __launch_bounds__(256) void expert_gather_kernel(const T* x, int64_t x_rows, int64_t cols, int64_t ld, const int32_t* source, int group, const int32_t* count, int64_t rows, T* y,
                                                             int side_log2)
 {
+    constexpr int V = RowType<T>::N;
     const int     side = threadIdx.x & ((1 << side_log2) - 1), at_once = 256 >> side_log2;
     const int64_t r0 = (static_cast<int64_t>(blockIdx.y) * gridDim.z + blockIdx.z) * at_once * U + (threadIdx.x >> side_log2);
-    const int64_t c = ((static_cast<int64_t>(blockIdx.x) << side_log2) + side) * 8, n = min(rows, static_cast<int64_t>(*count));
+    const int64_t c = ((static_cast<int64_t>(blockIdx.x) << side_log2) + side) * V, n = min(rows, static_cast<int64_t>(*count));
     if(c >= cols) return;
     int32_t i[U];
-    Row8<T> v[U];
+    RowPart<T, V> v[U];
 #pragma unroll
     for(int u = 0; u < U; ++u) i[u] = r0 + u * at_once < n ? source[r0 + u * at_once] : -1;
 #pragma unroll
     for(int u = 0; u < U; ++u)
     {
         const bool ok = i[u] >= 0 && i[u] / group < x_rows;
-        load_tail(x + (ok ? i[u] / group : 0) * ld, c, ok ? cols : 0, v[u]);
+        v[u].load(x + (ok ? i[u] / group : 0) * ld, c, ok ? cols : 0);
         if(!ok)
         {
-            float e[8];
+            float e[V];
 #pragma unroll
-            for(int j = 0; j < 8; ++j) e[j] = __uint_as_float(0x7FC00000u);
+            for(int j = 0; j < V; ++j) e[j] = __uint_as_float(0x7FC00000u);
             v[u].encode(e);
         }
     }
@@ -201,13 +234,13 @@ __global__ __launch_bounds__(256) void expert_gather_kernel(const T* x, int64_t 
         const int64_t r = r0 + u * at_once;
         if(r >= n) break;
         T* out = y + r * cols;
-        if(c + 8 <= cols) v[u].store(out + c);
+        if(c + V <= cols) v[u].store(out + c);
         else
         {
-            float e[8];
+            float e[V];
             v[u].decode(e);
 #pragma unroll
-            for(int j = 0; j < 8; ++j)
+            for(int j = 0; j < V; ++j)
                 if(c + j < cols) out[c + j] = static_cast<T>(e[j]);
         }
     }
@@ -218,18 +251,19 @@ template <typename T, int U>
 __global__ __launch_bounds__(256) void expert_combine_kernel(const T* z, int64_t rows, int64_t cols, int64_t ld, const int32_t* slot, int64_t tokens, int group, const float* weight, void* y, int ydt,
                                                              int side_log2)
 {
+    constexpr int V = RowType<T>::N;
     const int     side = threadIdx.x & ((1 << side_log2) - 1);
     const int64_t t = static_cast<int64_t>(blockIdx.y) * gridDim.z * (256 >> side_log2) + blockIdx.z * (256 >> side_log2) + (threadIdx.x >> side_log2);
-    const int64_t c = ((static_cast<int64_t>(blockIdx.x) << side_log2) + side) * 8;
+    const int64_t c = ((static_cast<int64_t>(blockIdx.x) << side_log2) + side) * V;
     if(t >= tokens || c >= cols) return;
-    float sum[8];
+    float sum[V];
 #pragma unroll
-    for(int j = 0; j < 8; ++j) sum[j] = 0.0f;
+    for(int j = 0; j < V; ++j) sum[j] = 0.0f;
     for(int j0 = 0; j0 < group; j0 += U)
     {
-        Row8<T> v[U];
-        float   w[U];
-        bool    ok[U];
+        RowPart<T, V> v[U];
+        float         w[U];
+        bool          ok[U];
 #pragma unroll
         for(int u = 0; u < U; ++u)
         {
@@ -237,19 +271,19 @@ __global__ __launch_bounds__(256) void expert_combine_kernel(const T* z, int64_t
             const int32_t r = slot[at];
             ok[u] = j0 + u < group && r >= 0 && r < rows;
             w[u]  = weight ? weight[at] : 1.0f;
-            load_tail(z + (ok[u] ? r : 0) * ld, c, ok[u] ? cols : 0, v[u]);
+            v[u].load(z + (ok[u] ? r : 0) * ld, c, ok[u] ? cols : 0);
         }
 #pragma unroll
         for(int u = 0; u < U; ++u)
             if(ok[u])
             {
-                float e[8];
+                float e[V];
                 v[u].decode(e);
 #pragma unroll
-                for(int j = 0; j < 8; ++j) sum[j] = fmaf(w[u], e[j], sum[j]);
+                for(int j = 0; j < V; ++j) sum[j] = fmaf(w[u], e[j], sum[j]);
             }
     }
-    store_tail(y, ydt, t * cols, c, cols, sum);
+    store_part<V>(y, ydt, t * cols, c, cols, sum);
 }
 
 // A token's gradient is read once for all its rows: `side` threads (64 at least, so that whole wavefronts share a token) walk its columns with
@@ -258,6 +292,7 @@ template <typename T, typename U, bool DOT, bool DZ>
 __global__ __launch_bounds__(256) void expert_combine_bwd_kernel(const T* dy, int64_t tokens, int64_t cols, int64_t lddy, const U* z, int64_t rows, int64_t ldz, const int32_t* slot, int group,
                                                                  const float* weight, void* dz, int dzdt, float* dweight, int side_log2)
 {
+    constexpr int    V = 8;
     __shared__ float part[4][4];
     const int     threads = 1 << side_log2, side = threadIdx.x & (threads - 1), wave = threadIdx.x / 64;
     const int64_t t = (static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x) * (256 >> side_log2) + (threadIdx.x >> side_log2);
@@ -276,32 +311,32 @@ __global__ __launch_bounds__(256) void expert_combine_bwd_kernel(const T* dy, in
             w[u]   = weight ? weight[at] : 1.0f;
             dot[u] = 0.0f;
         }
-        for(int64_t c = side * 8; c < cols; c += threads * 8)
+        for(int64_t c = side * V; c < cols; c += threads * V)
         {
-            Row8<T> g;
-            Row8<U> v[4];
-            load_tail(dy + tt * lddy, c, cols, g);
+            RowPart<T, V> g;
+            RowPart<U, V> v[4];
+            g.load(dy + tt * lddy, c, cols);
             if constexpr(DOT)
 #pragma unroll
-                for(int u = 0; u < 4; ++u) load_tail(z + (r[u] < 0 ? 0 : r[u]) * ldz, c, r[u] < 0 ? 0 : cols, v[u]);
-            float d[8];
+                for(int u = 0; u < 4; ++u) v[u].load(z + (r[u] < 0 ? 0 : r[u]) * ldz, c, r[u] < 0 ? 0 : cols);
+            float d[V];
             g.decode(d);
 #pragma unroll
             for(int u = 0; u < 4; ++u)
                 if(r[u] >= 0)
                 {
-                    float e[8];
+                    float e[V];
                     if constexpr(DOT)
                     {
                         v[u].decode(e);
 #pragma unroll
-                        for(int j = 0; j < 8; ++j) dot[u] = c + j < cols ? fmaf(d[j], e[j], dot[u]) : dot[u];
+                        for(int j = 0; j < V; ++j) dot[u] = c + j < cols ? fmaf(d[j], e[j], dot[u]) : dot[u];
                     }
                     if constexpr(DZ)
                     {
 #pragma unroll
-                        for(int j = 0; j < 8; ++j) e[j] = w[u] * d[j];
-                        store_tail(dz, dzdt, r[u] * cols, c, cols, e);
+                        for(int j = 0; j < V; ++j) e[j] = w[u] * d[j];
+                        store_part<V>(dz, dzdt, r[u] * cols, c, cols, e);
                     }
                 }
         }
@@ -372,7 +407,7 @@ dim3 rows_over_grid(const RowGrid& g, int64_t rows, int per_thread = 1)
 
 hipError_t launch_expert_gather(const void* x, int dtype, int64_t x_rows, int64_t cols, int64_t ld, const int32_t* source, int group, int64_t rows, const int32_t* count, void* y, hipStream_t st)
 {
-    const RowGrid g = row_grid(cols, 3);
+    const RowGrid g = row_grid(cols, dtype == kF32 ? 4 : 8, 3);
     auto typed = [&](auto tag) {
         typedef decltype(tag) T;
         if(rows * g.blocks_x >= kManyRows * (256 >> g.side_log2))
@@ -386,7 +421,7 @@ hipError_t launch_expert_gather(const void* x, int dtype, int64_t x_rows, int64_
 
 hipError_t launch_expert_combine(const void* z, int zdt, int64_t rows, int64_t cols, int64_t ld, const int32_t* slot, int64_t tokens, int group, const float* weight, void* y, int ydt, hipStream_t st)
 {
-    const RowGrid g = row_grid(cols, 3);
+    const RowGrid g = row_grid(cols, zdt == kF32 ? 4 : 8, 3);
     auto typed = [&](auto tag) {
         typedef decltype(tag) T;
         // (8192 tokens of 1024 bfloat16, eight rows each: by fours 37.4 us, by eights 40.1; of 4096, two each: by fours 48.8, by twos 40.2)
@@ -400,7 +435,7 @@ hipError_t launch_expert_combine(const void* z, int zdt, int64_t rows, int64_t c
 hipError_t launch_expert_combine_bwd(const void* dy, int dydt, int64_t tokens, int64_t cols, int64_t lddy, const void* z, int zdt, int64_t rows, int64_t ldz, const int32_t* slot, int group,
                                      const float* weight, void* dz, int dzdt, float* dweight, hipStream_t st)
 {
-    const int     side_log2 = row_grid(cols, 6).side_log2;
+    const int     side_log2 = row_grid(cols, 8, 6).side_log2;
     const int64_t blocks = (tokens + (256 >> side_log2) - 1) / (256 >> side_log2), x = blocks < 65536 ? blocks : 65536;
     const dim3    grid(static_cast<unsigned>(x), static_cast<unsigned>((blocks + x - 1) / x));
     auto typed = [&](auto tag, auto ztag) {
