@@ -32,7 +32,7 @@ HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-cont
 # gemm_f32_kernel has no such reads, but a lambda that is left as a call puts all it captures there (128 tile 8 -> 150 us).
 NO_SPILL = {"gemm_mfma.hip": ("gemm_nt_kernel", "gemm_nt_pair_kernel", "gemm_nt_persistent_kernel"),
             "conv3x3.hip": ("conv3x3_kernel",), "gemm_rows.hip": ("gemm_rows_kernel",),
-            "gemm_f32.hip": ("gemm_f32_kernel",), "token_gemm.hip": ("token_gemm_kernel", "token_split_kernel", "token_pair_kernel"),
+            "gemm_f32.hip": ("gemm_f32_kernel",), "token_gemm.hip": ("token_gemm_kernel", "token_split_kernel", "token_pair_kernel", "token_set_rows_kernel"),
             "token_few.hip": ("token_few_kernel",)}
 
 

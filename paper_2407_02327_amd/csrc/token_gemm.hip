@@ -5,9 +5,11 @@
 // A workgroup's tile is a tile of one set's product, computed as any other product's (gemm_tile.h: direct loads to LDS, 16x16 matrix
 // instructions), with the rows' scales beside the columns' in LDS for the epilogue.  The host knows how many tiles there may be at most, from the sizes; which there
 // are is read from the offsets by the workgroups, and those behind the last one end at once.
+#include "gemm_rows.h"
 #include "gemm_tile.h"
 #include "row_ops.h"
 #include "token_ops.h"
+#include <algorithm>
 
 namespace qsync {
 
@@ -205,6 +207,22 @@ template <bool VEC> __global__ __launch_bounds__(256) void token_reduce_kernel(c
         for(int e = 0; e < W; ++e) element_store(c, cdt, i + e, v[e]);
 }
 
+// A set's kernel arguments in the forward form
+__device__ __forceinline__ GemmKernelArgs forward_args(const TokenProduct& p, int64_t set, const SetRows& s)
+{
+    GemmKernelArgs a{};
+    a.N = p.N;
+    a.c_is_f16 = p.c_dtype == kF16 ? 1 : p.c_dtype == kBF16 ? 2 : 0;
+    a.Kb = code_pad(p.K);
+    a.A = reinterpret_cast<const uint8_t*>(p.A) + s.first * a.Kb;
+    a.B = reinterpret_cast<const uint8_t*>(p.B) + set * p.N * a.Kb;
+    a.M = s.len;
+    a.C = static_cast<uint8_t*>(p.C) + s.first * p.N * (p.c_dtype == kF32 ? 4 : 2);
+    a.row_scale = a.Kb ? p.sa + s.first : nullptr;
+    a.col_scale = a.Kb ? p.sb + set * p.N : nullptr;
+    a.col_bias  = p.bias ? p.bias + set * p.N : nullptr;
+    return a;
+}
 template <int BM, int BN, int WGM, int WGN, int ST, bool WGRAD>
 __device__ __forceinline__ void product_body(const TokenProduct& p, uint32_t block, int group_m)
 {
@@ -216,33 +234,23 @@ __device__ __forceinline__ void product_body(const TokenProduct& p, uint32_t blo
     }
     else if(!set_tile<BM, BN, QUARTERS>(p, block, group_m, t)) return;
     const SetRows s{uniform64(t.rows.first), uniform64(t.rows.len)};
-    GemmKernelArgs a{};
-    const int64_t  os = p.c_dtype == kF32 ? 4 : 2;
-    a.N        = p.N;
-    a.c_is_f16 = p.c_dtype == kF16 ? 1 : p.c_dtype == kBF16 ? 2 : 0;
+    GemmKernelArgs a;
     if constexpr(WGRAD)
     {
         const int64_t start = set_start(p.offsets, s, t.set);
+        a = GemmKernelArgs{};
+        a.N        = p.N;
+        a.c_is_f16 = p.c_dtype == kF16 ? 1 : p.c_dtype == kBF16 ? 2 : 0;
         a.A = reinterpret_cast<const uint8_t*>(p.A) + start * p.M;
         a.B = reinterpret_cast<const uint8_t*>(p.B) + start * p.N;
         a.M = p.M;
         a.Kb = code_pad(s.len);
-        a.C  = static_cast<uint8_t*>(p.C) + t.set * p.M * p.N * os;
+        a.C  = static_cast<uint8_t*>(p.C) + t.set * p.M * p.N * (p.c_dtype == kF32 ? 4 : 2);
         // (a set without rows has no scales worth the name: zeros)
         a.row_scale = s.len ? p.sa + t.set * p.M : nullptr;
         a.col_scale = s.len ? p.sb + t.set * p.N : nullptr;
     }
-    else
-    {
-        a.Kb = code_pad(p.K);
-        a.A = reinterpret_cast<const uint8_t*>(p.A) + s.first * a.Kb;
-        a.B = reinterpret_cast<const uint8_t*>(p.B) + t.set * p.N * a.Kb;
-        a.M = s.len;
-        a.C = static_cast<uint8_t*>(p.C) + s.first * p.N * os;
-        a.row_scale = a.Kb ? p.sa + s.first : nullptr;
-        a.col_scale = a.Kb ? p.sb + t.set * p.N : nullptr;
-        a.col_bias  = p.bias ? p.bias + t.set * p.N : nullptr;
-    }
+    else a = forward_args(p, t.set, s);
     if constexpr(QUARTERS)
         if(t.quarter >= 0)
         {
@@ -257,6 +265,14 @@ template <int BM, int BN, int WGM, int WGN, int ST, bool WGRAD>
 __global__ __launch_bounds__(64 * WGM * WGN, 2) void token_gemm_kernel(const TokenProduct p, int group_m)
 {
     product_body<BM, BN, WGM, WGN, ST, WGRAD>(p, blockIdx.x, group_m);
+}
+// Sets of few rows whose 64 x 64 tiles leave units idle: a workgroup's wavefronts share the contraction.
+template <int MF, int NF> __global__ __launch_bounds__(64 * kRowsWaves) void token_set_rows_kernel(const TokenProduct p)
+{
+    SetTile t;
+    if(!set_tile<16 * MF, 16 * NF, false>(p, blockIdx.x, kGroupM, t)) return;
+    const GemmKernelArgs a = forward_args(p, t.set, SetRows{uniform64(t.rows.first), uniform64(t.rows.len)});
+    gemm_rows_tile<I8Traits, MF, NF, true>(a, static_cast<int64_t>(t.tm) * (16 * MF), static_cast<int64_t>(t.tn) * (16 * NF));
 }
 // Data and weight gradient side by side: each of them alone leaves units idle, and pays its own launch, first loads and drain.
 template <int BM, int BN, int WGM, int WGN, int ST>
@@ -338,6 +354,28 @@ GemmPlan product_plan(bool wgrad, int64_t rows, int64_t M, int64_t N, int64_t K,
 // Workgroups (64 tiles of both gradients) up to which they share a launch; us, joined / apart: 300x200x100 of 3 sets 6.7 / 9.7, 2048x2048x1024 15.7 / 21.8,
 // 1500x3000x700 18.9 / 29.8, 4000x1000x500 of 16 sets 25.0 / 32.9; 4096x1024x2048 (2576 workgroups) 34.4 / 32.6.
 constexpr int64_t kPairBlocks = 8 * kNumCu, kPairBlocksSets = 16 * kNumCu;
+template <int MF, int NF> hipError_t launch_set_rows(const TokenProduct& p, hipStream_t st)
+{
+    static bool      set[kMaxDevices] = {};
+    const hipError_t e = allow_lds(&token_set_rows_kernel<MF, NF>, kRowsLds<MF, NF>, set);
+    if(e != hipSuccess) return e;
+    token_set_rows_kernel<MF, NF><<<static_cast<unsigned>(blocks_of<false>(p, 16 * MF, 16 * NF)), 64 * kRowsWaves, kRowsLds<MF, NF>, st>>>(p);
+    return hipGetLastError();
+}
+// Row fragments of a workgroup (1: with one of columns, 4: with two), 0: the tiles are faster.  A 64 tile walks K alone, 0.45 us per 128 bytes, up to
+// 512 of them at once; here a workgroup takes 0.37 us (0.95) for 512 bytes, with two of them on a unit (one).  us, bfloat16, tile / 1 / 4:
+//   16 rows of 8 sets, 1024 x 4096 17.5 / 7.5 / 8.5; 128 of 8 17.7 / 11.0 / 10.6; 200 of 4, 256 x 8192 30.3 / 7.4 / 15.1; 2000 of 4, 200 x 4096 17.8 / 19.2 / 10.6;
+//   64 of 16, 1024 x 1024 7.5 / 8.5 / 10.0; 256 of 8, 2048 x 2048 11.4 / 20.8 / 15.4; 512 of 8, 1024 x 4096 18.1 / 24.9 / 18.8.
+int set_rows_fragments(const TokenProduct& p)
+{
+    if(!p.offsets || p.K == 0) return 0;
+    const double kt = static_cast<double>(code_pad(p.K) / kRowBytes), sets = static_cast<double>(p.sets < p.rows ? p.sets : p.rows);
+    auto         tiles = [&](int bm, int bn) { return std::max(static_cast<double>(p.rows) / bm + sets / 2, sets) * static_cast<double>((p.N + bn - 1) / bn); };
+    const double tile = 2.0 + std::max(1.0, tiles(64, 64) / 512.0) * (1.5 + 0.45 * kt);
+    const double one = 2.0 + std::max(1.0, tiles(16, 16) / 512.0) * (2.5 + 0.37 * kt / 4), four = 2.0 + std::max(1.0, tiles(64, 32) / 256.0) * (2.5 + 0.95 * kt / 4);
+    return std::min(one, four) > 0.9 * tile ? 0 : one < four ? 1 : 4;
+}
+
 template <bool WGRAD> hipError_t launch_product(const TokenProduct& p, void* workspace, size_t workspace_bytes, hipStream_t st)
 {
     const GemmPlan plan = product_plan(WGRAD, p.rows, p.M, p.N, p.K, p.sets, p.offsets != nullptr);
@@ -378,6 +416,9 @@ size_t token_product_workspace_bytes(bool wgrad, int64_t rows, int64_t M, int64_
 hipError_t launch_token_product(const TokenProduct& p, bool wgrad, void* workspace, size_t workspace_bytes, hipStream_t st)
 {
     if(wgrad) return launch_product<true>(p, workspace, workspace_bytes, st);
+    const int fragments = set_rows_fragments(p);
+    if(fragments == 1) return launch_set_rows<1, 1>(p, st);
+    if(fragments == 4) return launch_set_rows<4, 2>(p, st);
     bool             taken;
     const hipError_t e = launch_token_rows(p, &taken, st);
     return taken || e != hipSuccess ? e : launch_product<false>(p, workspace, workspace_bytes, st);
@@ -387,7 +428,7 @@ hipError_t launch_token_gradients(const TokenProduct& x, const TokenProduct& w, 
 {
     const GemmPlan px = product_plan(false, x.rows, x.M, x.N, x.K, x.sets, x.offsets != nullptr), pw = product_plan(true, w.rows, w.M, w.N, w.K, w.sets, w.offsets != nullptr);
     const int64_t  first = (blocks_of<false>(x, 64, 64) + kNumXcd - 1) / kNumXcd * kNumXcd, all = first + blocks_of<true>(w, 64, 64);
-    if(px.tile >= 1 && px.splits == 1 && pw.tile >= 1 && pw.splits == 1 && all <= (x.offsets ? kPairBlocksSets : kPairBlocks) && !token_rows_takes(x))
+    if(px.tile >= 1 && px.splits == 1 && pw.tile >= 1 && pw.splits == 1 && all <= (x.offsets ? kPairBlocksSets : kPairBlocks) && !token_rows_takes(x) && !set_rows_fragments(x))
     {
         constexpr int lds = 2 * (64 + 64) * kRowBytes + kColumnBytes<64> + 64 * 4;
         static bool   set[kMaxDevices] = {};

@@ -217,7 +217,7 @@ SETS = [(40, 5, [0, 3, 3, 20, 40, 40]), (700, 3, [0, 1, 650, 690]), (2000, 16, [
 
 
 @pytest.mark.parametrize("rows, sets, offsets", SETS)
-@pytest.mark.parametrize("N, K, dtype", [(33, 70, F32), (264, 1024, BF16), (1024, 300, F16)])
+@pytest.mark.parametrize("N, K, dtype", [(33, 70, F32), (264, 1024, BF16), (1024, 300, F16), (100, 4100, F16), (96, 9000, F32)])
 def test_products_of_sets(rows, sets, offsets, N, K, dtype):
     """Each set with weights of its own; rows that belong to none stay as they were."""
     say("token product of sets", rows, sets, N, K, dtype)
