@@ -754,7 +754,8 @@ int qsync_token_quantize(const void* x, int xdt, int64_t x_rows, int64_t cols, i
  * qsync_token_quantize_both - codes with a scale for each row, and codes with a scale for each column of each set, from two reads of x
  * (stochastic: from the same draws).  The first are an operand of the forward pass or the data gradient, the second of the weight
  * gradient; of weights ([sets * N, K], offsets_opt NULL) the second are the operand of the data gradient.
- * row_scale rows floats, q as above; col_scale [sets, cols] floats, qT as described above; a column of an empty set has scale 1.
+ * row_scale rows floats, q as above; col_scale [sets, cols] floats, qT as described above; a column of an empty set has scale 1.  Without rows
+ * at all only the sums are written (zeros); the products do not read the scales of nothing.
  * colsum_opt  out, [sets, cols] floats or NULL: the sums of the columns (a bias gradient), in fp32 in an order that depends on the sizes
  *             and offsets alone.
  * workspace   at least qsync_token_quantize_both_workspace_bytes(rows, cols, sets, offsets_opt != NULL) bytes, no contents needed.

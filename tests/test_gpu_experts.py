@@ -313,3 +313,82 @@ def test_rows_that_pass_32_bits():
     del dz, rows
     want = (x[-10:].double() ** 2).sum(1)
     assert ((dweight[-10:].double() - want[:, None]).abs() <= cols * U * want[:, None]).all()
+
+
+def test_calls_out_of_their_order_are_refused():
+    route, other = ExpertRoute(20, 2, 3, 16), ExpertRoute(20, 2, 4)
+    op = ExpertLinear(40, 24, 16, 3, gather=False)
+    ids, x = ids_of(20, 2, 3, 70), values(40, 16, F16, 71)
+    for r in (route, other):
+        r.sort(ids)
+    with pytest.raises(RuntimeError, match="weights"):
+        op.forward(x, route)
+    with pytest.raises(ValueError, match="experts"):
+        op.forward(x, other, w=torch.zeros(3, 24, 16, device="cuda"))
+    w, dy = values(72, 16, F32, 72).view(3, 24, 16), values(40, 24, F16, 73)
+    op.forward(x, route, w=w)
+    for bad, error in ((dy[:39], ValueError), (dy.t(), ValueError), (dy.double(), ValueError), (dy.cpu(), ValueError)):
+        with pytest.raises(error):
+            op.backward(bad)
+    with pytest.raises(ValueError, match="w:"):
+        op.forward(x, route, w=w[:2])
+    with pytest.raises(ValueError, match="x"):
+        op.forward(x[:20], route)
+    with pytest.raises(ValueError, match="cols"):
+        other.gather(x[:20])
+    with pytest.raises(ValueError, match="expected, not"):
+        route.gather(values(20, 16, F32, 74))
+    with pytest.raises(RuntimeError, match="combine"):
+        route.combine_backward(x[:20])
+    with pytest.raises(ValueError, match="weight"):
+        route.combine(x, torch.ones(20, 2, device="cuda", dtype=torch.float64))
+    with pytest.raises(RuntimeError, match="training"):
+        ExpertRoute(20, 2, 3, 16, training=False).gather_backward(x)
+    op.backward(dy)
+    route.sort(ids)
+    with pytest.raises(RuntimeError, match="another batch"):
+        op.backward(dy)
+
+
+def test_serving_in_graphs():
+    """A few tokens to their experts and back, and through a token linear, captured and replayed over other tokens, ids and numbers of rows an
+    expert; two graphs that share the operators' buffers."""
+    from paper_2407_02327_amd.experts import TokenLinear
+    T, k, E, C, F = 8, 2, 4, 256, 512
+    route, up = ExpertRoute(T, k, E, C, training=False), ExpertLinear(T * k, F, C, E, training=False)
+    down, last = ExpertLinear(T * k, C, F, E, gather=False, training=False), TokenLinear(T, 130, C, training=False)
+    up.convert_w(values(E * F, C, F32, 80).view(E, F, C) / 64), down.convert_w(values(E * C, F, F32, 81).view(E, C, F) / 64), last.convert_w(values(130, C, F32, 82))
+    x, ids, weight = values(T, C, F16, 83).clamp(-4, 4), ids_of(T, k, E, 84), torch.rand(T, k, device="cuda")
+    for t in (up.y, down.y):
+        t.zero_()
+
+    def step(n):
+        route.sort(ids[:n])
+        y = route.combine(down.forward(up.forward(x[:n], route).relu(), route), weight[:n])
+        return y, last.forward(y)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(T), step(1)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graphs = []
+    for n in (T, 1):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            out = step(n)
+        graphs.append((n, g, out))
+    for replay in range(3):
+        x.copy_(values(T, C, F16, 85 + replay).clamp(-4, 4))
+        ids.copy_(ids_of(T, k, E, 90 + replay, outside=0.2 * replay))
+        for n, g, out in graphs:
+            say("serving graph", replay, n)
+            want = [t.clone() for t in step(n)]
+            for t in out:
+                t.zero_()
+            torch.cuda.synchronize()
+            g.replay()
+            torch.cuda.synchronize()
+            for a, b in zip(out, want):
+                assert torch.equal(bits(a), bits(b)), (replay, n)
