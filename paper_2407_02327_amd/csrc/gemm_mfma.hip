@@ -655,6 +655,7 @@ hipError_t launch_gemm_f32(const GemmProblem& p, const GemmPlan& plan, void* wor
 
 static thread_local int g_tile_override = -1;     // set by tests and tuning runs only; per calling thread
 void set_gemm_tile_override(int tile) { g_tile_override = (tile >= 0 && tile < kNumTiles) ? tile : -1; }
+bool gemm_tile_pinned() { return g_tile_override >= 0; }
 static thread_local int g_persistent_mode = -1;   // 1: whenever eligible; anything else: never (the default, see launch_gemm)
 void set_gemm_persistent_mode(int mode) { g_persistent_mode = (mode == 0 || mode == 1) ? mode : -1; }
 

@@ -249,6 +249,7 @@ GemmPlan plan_gemm(int prec, int64_t M, int64_t N, int64_t K, int force_tile = -
                    bool allow_split = true, bool tn = false);
 // tile >= 0 pins the tile shape of every later plan (tests, tuning); -1 returns the choice to the planner.
 void set_gemm_tile_override(int tile);
+bool gemm_tile_pinned();      // by the call above
 // 1: launch the persistent 256x256 kernel whenever a problem is eligible; anything else: never (the default)
 void set_gemm_persistent_mode(int mode);
 // GemmProblem with conv_H > 0, not tn, checked by launch_gemm: input tile kept in LDS (conv3x3.hip); *taken is false, and nothing

@@ -331,22 +331,33 @@ template <int BM, int BN, int WGM, int WGN, int ST, bool WGRAD> hipError_t launc
 }
 
 // Tile and K splits: of one set, as of any other product of its size; of several, without splits, no wider than their rows on average.
-GemmPlan product_plan(bool wgrad, int64_t rows, int64_t M, int64_t N, int64_t K, int64_t sets, bool offsets)
+GemmPlan product_plan(bool wgrad, int64_t rows, int64_t M, int64_t N, int64_t K, int64_t sets, bool offsets, int cdt)
 {
-    const int64_t share = (rows + sets - 1) / sets;
+    const int64_t share = (rows + sets - 1) / sets, k = code_pad(wgrad ? share : K);
+    // Few K tiles and more outputs than a round of 256 tiles: two 128 tiles on a unit, of which one multiplies while the other stores.  Rows of C in whole
+    // lines only (256 / 128 tile, us; fp32: 8192x4096x128 42 / 28, 16 sets of 1024x4096, 256 deep 73 / 59, weight gradient 8192x8192 of 128 78 / 52, of 4
+    // sets 4096x4096 of 256 69 / 59; bfloat16: 16384x8192x128 76 / 70, 8192x4096x256 27 / 24; not: fp32 6000x3333x128 38 / 42, 8192x4096x1024 61 / 69,
+    // bfloat16 4096x4096x128 12 / 13, weight gradient of 32 sets 2048x2048 of 128 79 / 80).
+    auto stores = [&](int64_t m) {
+        const int64_t tiles = (m + 255) / 256 * ((N + 255) / 256);
+        if(gemm_tile_pinned() || N * (cdt == kF32 ? 4 : 2) % 128 != 0) return false;
+        return cdt == kF32 ? tiles > kNumCu && k <= (wgrad ? 256 : 384) : tiles >= 2 * kNumCu && k <= 256 && (!wgrad || !offsets);
+    };
     if(!offsets)
     {
-        const int64_t m = wgrad ? M : rows, k = code_pad(wgrad ? rows : K);
+        const int64_t m = wgrad ? M : rows;
         GemmPlan      plan = plan_gemm(8, m, N, k, -1, -1, true);
+        if(plan.tile == 0 && plan.splits == 1 && stores(m)) plan.tile = 1;
         // Operands beyond what the caches in front of the memory hold for them: the 256 tile, which reads half as much, in K splits instead of the
         // 128 tile without (us, operands from memory: 1024x4096 of 16384 112 -> 83, 2048x2048 of 16384 95 -> 81, 1400x1400 of 16384 73 -> 54;
         // below, 1024x4096 of 8192 47 -> 59, 1024x1024 of 16384 34 -> 40)
-        if(plan.tile == 1 && plan.splits == 1 && (m + N) * k >= (int64_t(44) << 20)) plan = plan_gemm(8, m, N, k, 0, 0, true);
+        else if(plan.tile == 1 && plan.splits == 1 && (m + N) * k >= (int64_t(44) << 20)) plan = plan_gemm(8, m, N, k, 0, 0, true);
         return plan;
     }
-    GemmPlan      plan = plan_gemm(8, wgrad ? M * sets : rows, N, code_pad(wgrad ? share : K), -1, -1, false);
+    const int64_t all = wgrad ? M * sets : rows;
+    GemmPlan      plan = plan_gemm(8, all, N, k, -1, -1, false);
     const int64_t m = wgrad ? M : share;
-    plan.tile = plan.tile == 0 && m < 192 ? 1 : plan.tile;
+    plan.tile = plan.tile == 0 && (m < 192 || stores(all)) ? 1 : plan.tile;
     plan.tile = plan.tile == 1 && m < 96 ? 2 : plan.tile;
     return plan;
 }
@@ -378,7 +389,7 @@ int set_rows_fragments(const TokenProduct& p)
 
 template <bool WGRAD> hipError_t launch_product(const TokenProduct& p, void* workspace, size_t workspace_bytes, hipStream_t st)
 {
-    const GemmPlan plan = product_plan(WGRAD, p.rows, p.M, p.N, p.K, p.sets, p.offsets != nullptr);
+    const GemmPlan plan = product_plan(WGRAD, p.rows, p.M, p.N, p.K, p.sets, p.offsets != nullptr, p.c_dtype);
     const int64_t  M = WGRAD ? p.M : p.rows, kt = code_pad(WGRAD ? p.rows : p.K) / kRowBytes;
     SplitArgs      sp{workspace, 1, 0};
     // (sums of integers: with less room there are fewer splits, and the same results)
@@ -410,7 +421,7 @@ template <bool WGRAD> hipError_t launch_product(const TokenProduct& p, void* wor
 size_t token_product_workspace_bytes(bool wgrad, int64_t rows, int64_t M, int64_t N, int64_t K, int64_t sets)
 {
     if(sets != 1) return 0;
-    return product_plan(wgrad, rows, M, N, K, 1, false).workspace;
+    return product_plan(wgrad, rows, M, N, K, 1, false, kF32).workspace;      // (the type moves tiles of unsplit products only)
 }
 
 hipError_t launch_token_product(const TokenProduct& p, bool wgrad, void* workspace, size_t workspace_bytes, hipStream_t st)
@@ -426,7 +437,7 @@ hipError_t launch_token_product(const TokenProduct& p, bool wgrad, void* workspa
 
 hipError_t launch_token_gradients(const TokenProduct& x, const TokenProduct& w, void* workspace, size_t workspace_bytes, hipStream_t st)
 {
-    const GemmPlan px = product_plan(false, x.rows, x.M, x.N, x.K, x.sets, x.offsets != nullptr), pw = product_plan(true, w.rows, w.M, w.N, w.K, w.sets, w.offsets != nullptr);
+    const GemmPlan px = product_plan(false, x.rows, x.M, x.N, x.K, x.sets, x.offsets != nullptr, x.c_dtype), pw = product_plan(true, w.rows, w.M, w.N, w.K, w.sets, w.offsets != nullptr, w.c_dtype);
     const int64_t  first = (blocks_of<false>(x, 64, 64) + kNumXcd - 1) / kNumXcd * kNumXcd, all = first + blocks_of<true>(w, 64, 64);
     if(px.tile >= 1 && px.splits == 1 && pw.tile >= 1 && pw.splits == 1 && all <= (x.offsets ? kPairBlocksSets : kPairBlocks) && !token_rows_takes(x) && !set_rows_fragments(x))
     {

@@ -212,6 +212,52 @@ def test_room_does_not_change_results(M, N, K, dtype):
         assert torch.equal(y, out[0][0]) and torch.equal(dw, out[0][1])
 
 
+@pytest.mark.parametrize("rows, N, K, offsets, dtype", [(4200, 4096, 100, None, F32), (8200, 4096, 256, None, BF16), (4200, 4096, 300, [0, 1500, 1500, 4133], F32),
+                                                        (8200, 4096, 128, [0, 257, 5000, 8190], F16)])
+def test_many_outputs_of_short_contractions(rows, N, K, offsets, dtype):
+    """Forward and weight gradient (K rows a set), on each tile and the one of the rule: the same bits, and some of the rows against the formula."""
+    say("token product, short contraction", rows, N, K, offsets, dtype)
+    g = torch.Generator(device="cuda").manual_seed(26)
+    sets = len(offsets) - 1 if offsets else 1
+    at = [0, rows] if offsets is None else offsets
+    a, b = random_codes(rows, K, g), random_codes(sets * N, K, g)
+    sa, sb = torch.rand(rows, generator=g, device="cuda") * 1e-3, torch.rand(sets, N, generator=g, device="cuda") * 1e-2
+    off = None if offsets is None else torch.tensor(offsets, dtype=torch.int32, device="cuda")
+    M = rows // sets
+    woff = None if offsets is None else torch.tensor([K * i for i in range(sets + 1)], dtype=torch.int32, device="cuda")
+    positions = Q.qsync_token_code_rows(K * sets, sets, offsets is not None)
+    c, d = torch.zeros(positions * M, dtype=torch.int8, device="cuda"), torch.zeros(positions * N, dtype=torch.int8, device="cuda")
+    for e in range(sets):      # set e: a packed matrix [.., pad(K)] from position pad(K e) + 128 e on
+        start = (R.pad(K * e) + 128 * e) if offsets else 0
+        c[start * M:(start + R.pad(K)) * M] = random_codes(M, K, g).flatten()
+        d[start * N:(start + R.pad(K)) * N] = random_codes(N, K, g).flatten()
+    sc, sd = torch.rand(sets, M, generator=g, device="cuda") * 1e-3, torch.rand(sets, N, generator=g, device="cuda") * 1e-2
+    out = []
+    try:
+        for tile in (-1, 0, 1, 2):
+            Q.qsync_debug_set_gemm_tile(tile)
+            y, dw = torch.full((rows, N), 7.0, dtype=dtype, device="cuda"), torch.full((sets, M, N), 7.0, dtype=dtype, device="cuda")
+            Q.qsync_token_linear_fwd(rows, N, K, sets, off, a, sa, b, sb, None, y, None)
+            Q.qsync_token_linear_wgrad(K * sets, M, N, sets, woff, c, sc, d, sd, dw, None)
+            torch.cuda.synchronize()
+            out.append((y, dw))
+    finally:
+        Q.qsync_debug_set_gemm_tile(-1)
+    for y, dw in out[1:]:
+        assert torch.equal(y, out[0][0]) and torch.equal(dw, out[0][1])
+    y, dw = out[0]
+    assert (y[at[-1]:] == 7.0).all()
+    for e, (i, j) in enumerate(zip(at[:-1], at[1:])):
+        some = sorted({i, (i + j) // 2, j - 1}) if j > i else []
+        if some:
+            want, bound = R.product(f64(a)[some], sa.cpu().numpy()[some], f64(b[e * N:(e + 1) * N]), sb.cpu().numpy()[e])
+            assert_within(y[some], want, bound + rounded(want, dtype), f"y of set {e}")
+        some, start = [0, 255, 256, M // 2, M - 1], (R.pad(K * e) + 128 * e) if offsets else 0
+        rows_of = lambda t, n: f64(t[start * n:(start + R.pad(K)) * n]).reshape(n, R.pad(K))
+        want, bound = R.product(rows_of(c, M)[some], sc.cpu().numpy()[e][some], rows_of(d, N), sd.cpu().numpy()[e])
+        assert_within(dw[e][some], want, bound + rounded(want, dtype), f"dw of set {e}")
+
+
 SETS = [(40, 5, [0, 3, 3, 20, 40, 40]), (700, 3, [0, 1, 650, 690]), (2000, 16, [0] + [125 * i - 60 for i in range(1, 16)] + [1990]), (6, 64, [0] * 30 + [2] * 20 + [6] * 15),
         (900, 1, [0, 900]), (513, 2, [0, 256, 513]), (5, 2, [0, 0, 0]), (4000, 7, [0, 600, 600, 1300, 2500, 2501, 3100, 4000])]
 
