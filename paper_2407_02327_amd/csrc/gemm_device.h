@@ -394,7 +394,10 @@ __device__ __forceinline__ void store_tile(const GemmKernelArgs& p, typename TR:
         constexpr int LPR = WTN / EPV;                           // lanes per output row in the store phase
         constexpr int RPI = 64 / LPR;                            // rows per store instruction
         static_assert(64 % LPR == 0 && (FPP * R) % RPI == 0, "store instructions cover whole rows");
-        const bool    vec = (p.N * OS) % 16 == 0 && (reinterpret_cast<uintptr_t>(dst_base) & 15) == 0;
+        // TOKEN: rows that do not lie in whole lines leave by ordinary stores, which the L2 joins; streamed ones reach memory as parts of lines
+        // (fp32 8192x3332x128 44 -> 25 us, 8192x4097x128 52 -> 32, bfloat16 29 -> 22 and 33 -> 24)
+        constexpr int LINE = TOKEN && !RAW ? 128 : 16;
+        const bool    vec = (p.N * OS) % LINE == 0 && (reinterpret_cast<uintptr_t>(dst_base) & (LINE - 1)) == 0;
         const int     seg = lane % LPR, lr0 = lane / LPR;
         const int64_t col = wcol0 + seg * EPV;
         __syncthreads();                                  // all wavefronts are done reading the stages
@@ -509,19 +512,27 @@ __device__ __forceinline__ void store_tile(const GemmKernelArgs& p, typename TR:
                 }
                 continue;
             }
+            if constexpr(TOKEN)
+            {   // (memory takes 16 bytes at any element's address: 2187x1001x777 with fp32 output 13.4 -> 9.2 us)
+                uint8_t*      dst = dst_base + (row0 * p.N + col) * OS;
+                const int64_t step = RPI * p.N * OS, left = p.N - col;      // valid elements from here on (may be <= 0)
+#pragma unroll 8
+                for(int r = 0; r < FPP * R; r += RPI, dst += step)
+                {
+                    const uint8_t* const from = stg + (r + lr0) * PITCH + seg * 16;
+                    if(row0 + r >= p.M) continue;
+                    if(left >= EPV) *reinterpret_cast<v4u32_any*>(dst) = *reinterpret_cast<const v4u32*>(from);
+                    else
+                        for(int e = 0; e < static_cast<int>(left); ++e) reinterpret_cast<out_t*>(dst)[e] = reinterpret_cast<const out_t*>(from)[e];
+                }
+                continue;
+            }
 #pragma unroll 1
             for(int r = 0; r < FPP * R; r += RPI)
             {
                 const v4u32   val = *reinterpret_cast<const v4u32*>(stg + (r + lr0) * PITCH + seg * 16);
                 const int64_t row = row0 + r, left = row < p.M ? p.N - col : 0;      // valid elements from here on (may be <= 0)
                 const int64_t at  = row * p.N + col;
-                // (memory takes 16 bytes at any element's address: 2187x1001x777 with fp32 output 13.4 -> 9.2 us)
-                if constexpr(TOKEN)
-                    if(left >= EPV)
-                    {
-                        __builtin_nontemporal_store(val, reinterpret_cast<v4u32_any*>(dst_base + at * OS));
-                        continue;
-                    }
 #pragma unroll
                 for(int e = 0; e < EPV; ++e)
                 {

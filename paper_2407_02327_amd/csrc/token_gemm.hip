@@ -334,13 +334,13 @@ template <int BM, int BN, int WGM, int WGN, int ST, bool WGRAD> hipError_t launc
 GemmPlan product_plan(bool wgrad, int64_t rows, int64_t M, int64_t N, int64_t K, int64_t sets, bool offsets, int cdt)
 {
     const int64_t share = (rows + sets - 1) / sets, k = code_pad(wgrad ? share : K);
-    // Few K tiles and more outputs than a round of 256 tiles: two 128 tiles on a unit, of which one multiplies while the other stores.  Rows of C in whole
-    // lines only (256 / 128 tile, us; fp32: 8192x4096x128 42 / 28, 16 sets of 1024x4096, 256 deep 73 / 59, weight gradient 8192x8192 of 128 78 / 52, of 4
-    // sets 4096x4096 of 256 69 / 59; bfloat16: 16384x8192x128 76 / 70, 8192x4096x256 27 / 24; not: fp32 6000x3333x128 38 / 42, 8192x4096x1024 61 / 69,
-    // bfloat16 4096x4096x128 12 / 13, weight gradient of 32 sets 2048x2048 of 128 79 / 80).
+    // Few K tiles and more outputs than a round of 256 tiles: two 128 tiles on a unit, of which one multiplies while the other stores (256 / 128 tile, us;
+    // fp32: 8192x4096x128 42 / 28, 8192x3333x128 31 / 26, 16 sets of 1024x4096, 256 deep 73 / 59, 8 of 1024x2777, 384 deep 35 / 29, weight gradient
+    // 8192x8192 of 128 78 / 52, of 4 sets 4096x4096 of 256 69 / 59; bfloat16: 16384x8192x128 76 / 70, 8192x4096x256 27 / 24; not: fp32 8192x4096x1024
+    // 61 / 69, bfloat16 4096x4096x128 12 / 13, weight gradient of 32 sets 2048x2048 of 128 79 / 80).
     auto stores = [&](int64_t m) {
         const int64_t tiles = (m + 255) / 256 * ((N + 255) / 256);
-        if(gemm_tile_pinned() || N * (cdt == kF32 ? 4 : 2) % 128 != 0) return false;
+        if(gemm_tile_pinned()) return false;
         return cdt == kF32 ? tiles > kNumCu && k <= (wgrad ? 256 : 384) : tiles >= 2 * kNumCu && k <= 256 && (!wgrad || !offsets);
     };
     if(!offsets)
