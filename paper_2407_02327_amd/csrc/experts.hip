@@ -141,6 +141,9 @@ __global__ __launch_bounds__(kSortThreads) void expert_place_kernel(const I* ids
 // A thread has V columns, 16 bytes of the input (in the backward pass eight, whatever the type: 3333x1001 fp32, three rows each, 23.5 us, by fours 25.8); a workgroup's 256 threads are 256 / side rows (or tokens) of
 // `side` threads, as many as a row has vectors up to 256, and longer rows take several workgroups: whatever the shape, a thread does little, and
 // a launch has as many threads as there is data.
+// The last vector of a row that is no whole number of them starts V elements in front of the row's end: what two threads have in common they both
+// leave, alike, and no thread walks single elements (rows of V elements and more).
+__device__ __forceinline__ int64_t vector_start(int64_t c, int64_t cols, int V) { return c + V > cols && cols >= V ? cols - V : c; }
 struct RowGrid { int side_log2, blocks_x; };
 RowGrid row_grid(int64_t cols, int V, int least)
 {
@@ -209,8 +212,8 @@ __global__ __launch_bounds__(256) void expert_gather_kernel(const T* x, int64_t 
     constexpr int V = RowType<T>::N;
     const int     side = threadIdx.x & ((1 << side_log2) - 1), at_once = 256 >> side_log2;
     const int64_t r0 = (static_cast<int64_t>(blockIdx.y) * gridDim.z + blockIdx.z) * at_once * U + (threadIdx.x >> side_log2);
-    const int64_t c = ((static_cast<int64_t>(blockIdx.x) << side_log2) + side) * V, n = min(rows, static_cast<int64_t>(*count));
-    if(c >= cols) return;
+    const int64_t c0 = ((static_cast<int64_t>(blockIdx.x) << side_log2) + side) * V, c = vector_start(c0, cols, V), n = min(rows, static_cast<int64_t>(*count));
+    if(c0 >= cols) return;
     int32_t i[U];
     RowPart<T, V> v[U];
 #pragma unroll
@@ -254,8 +257,8 @@ __global__ __launch_bounds__(256) void expert_combine_kernel(const T* z, int64_t
     constexpr int V = RowType<T>::N;
     const int     side = threadIdx.x & ((1 << side_log2) - 1);
     const int64_t t = static_cast<int64_t>(blockIdx.y) * gridDim.z * (256 >> side_log2) + blockIdx.z * (256 >> side_log2) + (threadIdx.x >> side_log2);
-    const int64_t c = ((static_cast<int64_t>(blockIdx.x) << side_log2) + side) * V;
-    if(t >= tokens || c >= cols) return;
+    const int64_t c0 = ((static_cast<int64_t>(blockIdx.x) << side_log2) + side) * V, c = vector_start(c0, cols, V);
+    if(t >= tokens || c0 >= cols) return;
     float sum[V];
 #pragma unroll
     for(int j = 0; j < V; ++j) sum[j] = 0.0f;
@@ -311,8 +314,9 @@ __global__ __launch_bounds__(256) void expert_combine_bwd_kernel(const T* dy, in
             w[u]   = weight ? weight[at] : 1.0f;
             dot[u] = 0.0f;
         }
-        for(int64_t c = side * V; c < cols; c += threads * V)
+        for(int64_t c0 = side * V; c0 < cols; c0 += threads * V)
         {
+            const int64_t c = vector_start(c0, cols, V);
             RowPart<T, V> g;
             RowPart<U, V> v[4];
             g.load(dy + tt * lddy, c, cols);
@@ -330,7 +334,7 @@ __global__ __launch_bounds__(256) void expert_combine_bwd_kernel(const T* dy, in
                     {
                         v[u].decode(e);
 #pragma unroll
-                        for(int j = 0; j < V; ++j) dot[u] = c + j < cols ? fmaf(d[j], e[j], dot[u]) : dot[u];
+                        for(int j = 0; j < V; ++j) dot[u] = c + j >= c0 && c + j < cols ? fmaf(d[j], e[j], dot[u]) : dot[u];
                     }
                     if constexpr(DZ)
                     {

@@ -247,7 +247,8 @@ class _CodeLinear:
 
 
 class TokenLinear(_CodeLinear):
-    """y = x w^T + b in 8-bit integers, with a scale for each token of x and each channel of w."""
+    """y = x w^T + b in 8-bit integers, with a scale for each token of x and each channel of w.  Sums are of 32 bits, as `QLinear`'s: exact for
+    contractions of up to 133144, over K, N and, in the weight gradient, the rows of a set."""
 
     def __init__(self, rows: int, N: int, K: int, x_dtype=torch.float16, y_dtype=None, dx_dtype=None, dw_dtype=torch.float32,
                  dy_round: int = Q.ROUND_STOCHASTIC, philox_seed: int = 0, bias: bool = True, training: bool = True, device="cuda"):
