@@ -336,7 +336,7 @@ GemmPlan product_plan(bool wgrad, int64_t rows, int64_t M, int64_t N, int64_t K,
     const int64_t share = (rows + sets - 1) / sets, k = code_pad(wgrad ? share : K);
     // Few K tiles and more outputs than a round of 256 tiles: two 128 tiles on a unit, of which one multiplies while the other stores (256 / 128 tile, us;
     // fp32: 8192x4096x128 42 / 28, 8192x3333x128 31 / 26, 16 sets of 1024x4096, 256 deep 73 / 59, 8 of 1024x2777, 384 deep 35 / 29, weight gradient
-    // 8192x8192 of 128 78 / 52, of 4 sets 4096x4096 of 256 69 / 59; bfloat16: 16384x8192x128 76 / 70, 8192x4096x256 27 / 24; not: fp32 8192x4096x1024
+    // 8192x8192 of 128 78 / 52, of 4 sets 4096x4096 of 256 69 / 59; bfloat16: 16384x8192x128 76 / 70, 8192x4096x256 27 / 24, but 32768x4096x128 71 / 76; not: fp32 8192x4096x1024
     // 61 / 69, bfloat16 4096x4096x128 12 / 13, weight gradient of 32 sets 2048x2048 of 128 79 / 80).
     auto stores = [&](int64_t m) {
         const int64_t tiles = (m + 255) / 256 * ((N + 255) / 256);

@@ -95,6 +95,13 @@ def test_rows_there_and_back(tokens, k, experts, cols, dtype, other, outside):
     assert_within(dx, terms.sum(1), k * U * np.abs(terms).sum(1) + rounded(terms.sum(1), dtype) + 2.0 ** -149, "tokens' gradient")
 
 
+@pytest.mark.parametrize("cols", [*range(1, 19), 31, 33, 63, 65, 255, 257, 2047, 2049, 2055])
+@pytest.mark.parametrize("dtype, other", [(F16, F32), (BF16, BF16), (F32, F16)])
+def test_rows_of_any_width(cols, dtype, other):
+    """A row's last vector overlaps the one before it: nothing is counted twice, nothing beside the row is written."""
+    test_rows_there_and_back(9, 3, 4, cols, dtype, other, 0.25)
+
+
 def test_route_gradients_against_differences():
     tokens, k, experts, cols = 6, 2, 3, 5
     route = ExpertRoute(tokens, k, experts, cols, dtype=F32)
