@@ -782,8 +782,8 @@ int qsync_token_convert(const void* x, int xdt, int64_t x_rows, int64_t K, int64
  * xq [rows, code_cols(K)], sx rows floats; wq [sets, N, code_cols(K)], sw [sets, N] floats; bias_opt [sets, N] floats or NULL.
  * offsets_opt NULL: one set (QSYNC_ERR_UNSUPPORTED otherwise).
  * y   out, packed [rows, N] of ydt (QSYNC_F32, QSYNC_F16 or QSYNC_BF16), rounded once.
- * workspace   qsync_token_linear_workspace_bytes(rows, N, K, sets) bytes, 16-byte aligned, no contents needed.  With less, or none, the
- *             contraction is split into fewer pieces: slower, the same bits.
+ * workspace   qsync_token_linear_workspace_bytes(rows, N, K, sets) bytes, 16-byte aligned, no contents needed; enough for fewer rows, too.  With
+ *             less, or none, the contraction is split into fewer pieces: slower, the same bits.
  */
 int qsync_token_linear_fwd(int64_t rows, int64_t N, int64_t K, int64_t sets, const int32_t* offsets_opt, const void* xq, const float* sx,
                            const void* wq, const float* sw, const float* bias_opt, void* y, int ydt, void* workspace,

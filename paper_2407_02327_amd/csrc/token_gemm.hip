@@ -330,7 +330,9 @@ template <int BM, int BN, int WGM, int WGN, int ST, bool WGRAD> hipError_t launc
     return hipGetLastError();
 }
 
-// Tile and K splits: of one set, as of any other product of its size; of several, without splits, no wider than their rows on average.
+// Tile and K splits: of one set, as of any other product of its size, the rows rounded up to a fragment's (so that few plans say what any number of
+// rows may need); of several, without splits, no wider than their rows on average.
+constexpr int64_t kPlanRows = 16;
 GemmPlan product_plan(bool wgrad, int64_t rows, int64_t M, int64_t N, int64_t K, int64_t sets, bool offsets, int cdt)
 {
     const int64_t share = (rows + sets - 1) / sets, k = code_pad(wgrad ? share : K);
@@ -345,7 +347,7 @@ GemmPlan product_plan(bool wgrad, int64_t rows, int64_t M, int64_t N, int64_t K,
     };
     if(!offsets)
     {
-        const int64_t m = wgrad ? M : rows;
+        const int64_t m = wgrad ? M : (rows + kPlanRows - 1) / kPlanRows * kPlanRows;
         GemmPlan      plan = plan_gemm(8, m, N, k, -1, -1, true);
         if(plan.tile == 0 && plan.splits == 1 && stores(m)) plan.tile = 1;
         // Operands beyond what the caches in front of the memory hold for them: the 256 tile, which reads half as much, in K splits instead of the
@@ -418,10 +420,31 @@ template <bool WGRAD> hipError_t launch_product(const TokenProduct& p, void* wor
 
 }  // namespace
 
+// The largest need of any number of rows up to this one: fewer rows have fewer tiles, and those more splits.  (An operator of 8192 rows, 4096 outputs,
+// 14336 deep, none of whose 8192 rows' tiles are split: with 64 rows and room for none 57 us, with room for their 8 splits 21; 400 rows 79, 55.)
 size_t token_product_workspace_bytes(bool wgrad, int64_t rows, int64_t M, int64_t N, int64_t K, int64_t sets)
 {
     if(sets != 1) return 0;
-    return product_plan(wgrad, rows, M, N, K, 1, false, kF32).workspace;      // (the type moves tiles of unsplit products only)
+    // (the type moves tiles of unsplit products only)
+    auto splits = [&](int64_t r) { return static_cast<size_t>(product_plan(wgrad, r, M, N, wgrad ? r : K, 1, false, kF32).splits); };
+    // (Splits fill the units, with one workgroup of the 256 tile, two of the 128 or four of the 64 tile on each: none where an output has more than half as
+    // many tiles as there are places, which is more than kNumCu / 2 of the 256 tile.)
+    const int64_t tiles_n = (N + 255) / 256, tiles_m = kNumCu / 2 / tiles_n;
+    if(wgrad)
+    {
+        if((M + 255) / 256 > tiles_m) return 0;
+        size_t most = 1;
+        for(int64_t r = kCodePad; r < rows + kCodePad; r += kCodePad) most = std::max(most, splits(r));      // (a plan knows the K tiles)
+        return most > 1 ? most * M * N * 4 : 0;
+    }
+    const int64_t last = std::min(rows, tiles_m * 256);
+    size_t        need = 0;      // rows times splits
+    for(int64_t r = std::min(last, kPlanRows); r > 0; r = r < last ? std::min(last, r + kPlanRows) : 0)
+    {
+        const size_t s = splits(r);
+        if(s > 1) need = std::max(need, s * r);
+    }
+    return need * N * 4;
 }
 
 hipError_t launch_token_product(const TokenProduct& p, bool wgrad, void* workspace, size_t workspace_bytes, hipStream_t st)

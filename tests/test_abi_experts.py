@@ -228,3 +228,22 @@ def test_classes_refuse_calls():
         experts.backward(x)
     with pytest.raises(RuntimeError, match="forward"):
         TokenLinear(4, 8, 8, training=False, device="cpu").backward(x)
+
+
+@pytest.mark.parametrize("N, K", [(1024, 8192), (4096, 14336), (14336, 4096), (128, 4096), (1, 200_000), (64, 2048), (1000, 3000), (2048, 16384), (300, 60_000)])
+def test_room_for_many_rows_is_enough_for_fewer(N, K):
+    """The products' K splits, too: an operator built for a prompt is called with a few rows."""
+    sizes = [*range(1, 70), 100, 127, 128, 129, 200, 255, 400, 511, 512, 513, 700, 1000, 1024, 1100, 1500, 1600, 2000, 2047, 2048, 2049, 3000, 4095, 4096, 8192, 16384,
+             20_000, 40_000, 100_000, 1 << 18]
+    queries = [Q.qsync_token_wgrad_workspace_bytes, Q.qsync_token_linear_bwd_workspace_bytes] + ([Q.qsync_token_linear_workspace_bytes] if K <= 1 << 20 else [])
+    for query in queries:
+        need = [query(rows, N, K, 1) for rows in sizes]
+        assert need == sorted(need), query.__name__
+        assert need[-1] <= 64 << 20      # (what fills the units: one 256 x 256 sum each)
+
+
+def test_room_of_a_large_operator():
+    """Sizes whose calls of a few rows are planned in pieces, at the least two."""
+    assert Q.qsync_token_linear_workspace_bytes(8192, 4096, 14336, 1) >= Q.qsync_token_linear_workspace_bytes(64, 4096, 14336, 1) >= 2 * 64 * 4096 * 4
+    assert Q.qsync_token_linear_workspace_bytes(16384, 1024, 8192, 1) >= Q.qsync_token_linear_workspace_bytes(1600, 1024, 8192, 1) >= 2 * 1600 * 1024 * 4
+    assert Q.qsync_token_linear_bwd_workspace_bytes(4096, 14336, 4096, 1) >= Q.qsync_token_linear_bwd_workspace_bytes(200, 14336, 4096, 1) >= 2 * 200 * 4096 * 4

@@ -572,3 +572,39 @@ def test_fractions_that_32_bits_round():
     oracle = np.clip(down + (u < ((x - down).astype(np.float32) * np.float32(65536.0)).astype(np.uint32)), -127, 127)
     equal(q[:, :cols], oracle, "codes")
     check_rows(q, s, x, R.draws(rows, cols, SEED, OFFSET), "rows")
+
+
+@pytest.mark.parametrize("N, K", [(1024, 8192), (520, 14336)])
+def test_fewer_rows_than_an_operator_was_built_for(N, K):
+    """What an operator of those rows returns, bit for bit, and no less room for it."""
+    large = TokenLinear(8192, N, K, x_dtype=BF16, training=False)
+    w = values(N, K, BF16, 149).contiguous()
+    large.convert_w(w)
+    for n in (1, 8, 64, 400, 1500):
+        say("token linear, fewer rows", N, K, n)
+        x = values(n, K, BF16, 150 + n)
+        small = TokenLinear(n, N, K, x_dtype=BF16, training=False)
+        small.convert_w(w)
+        have, need = large.ws.numel(), small.ws.numel()
+        assert have >= need
+        a, b = small.forward(x), large.forward(x)
+        assert torch.equal(a, b)
+        some = [0, n // 2, n - 1]
+        want, bound = R.product(*R.codes(f64(x)[some], 1), *R.codes(f64(w), 1))
+        assert_within(b[some], want, bound + rounded(want, BF16), f"{n} rows")
+
+
+def test_gradients_of_fewer_rows_than_an_operator_was_built_for():
+    N, K = 3000, 520
+    large, w = TokenLinear(20000, N, K, x_dtype=F16), values(3000, 520, F32, 151).contiguous()
+    for n in (5, 200, 2100):
+        say("token linear, fewer rows' gradients", n)
+        x, dy = values(n, K, F16, 152 + n), values(n, N, F16, 153 + n)
+        small, out = TokenLinear(n, N, K, x_dtype=F16), []
+        have, need = large.ws_bwd.numel(), small.ws_bwd.numel()
+        assert have >= need
+        for op in (small, large):
+            op.offset = 0
+            out.append([t.clone() for t in (op.forward(x, w=w), *op.backward(dy))])
+        for a, b in zip(*out):
+            assert torch.equal(a, b)
