@@ -353,7 +353,7 @@ GemmPlan product_plan(bool wgrad, int64_t rows, int64_t M, int64_t N, int64_t K,
         // Operands beyond what the caches in front of the memory hold for them: the 256 tile, which reads half as much, in K splits instead of the
         // 128 tile without (us, operands from memory: 1024x4096 of 16384 112 -> 83, 2048x2048 of 16384 95 -> 81, 1400x1400 of 16384 73 -> 54;
         // below, 1024x4096 of 8192 47 -> 59, 1024x1024 of 16384 34 -> 40)
-        else if(plan.tile == 1 && plan.splits == 1 && (m + N) * k >= (int64_t(44) << 20)) plan = plan_gemm(8, m, N, k, 0, 0, true);
+        else if(!gemm_tile_pinned() && plan.tile == 1 && plan.splits == 1 && (m + N) * k >= (int64_t(44) << 20)) plan = plan_gemm(8, m, N, k, 0, 0, true);
         return plan;
     }
     const int64_t all = wgrad ? M * sets : rows;

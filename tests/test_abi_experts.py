@@ -247,3 +247,16 @@ def test_room_of_a_large_operator():
     assert Q.qsync_token_linear_workspace_bytes(8192, 4096, 14336, 1) >= Q.qsync_token_linear_workspace_bytes(64, 4096, 14336, 1) >= 2 * 64 * 4096 * 4
     assert Q.qsync_token_linear_workspace_bytes(16384, 1024, 8192, 1) >= Q.qsync_token_linear_workspace_bytes(1600, 1024, 8192, 1) >= 2 * 1600 * 1024 * 4
     assert Q.qsync_token_linear_bwd_workspace_bytes(4096, 14336, 4096, 1) >= Q.qsync_token_linear_bwd_workspace_bytes(200, 14336, 4096, 1) >= 2 * 200 * 4096 * 4
+
+
+def test_room_follows_a_pinned_tile():
+    """1024 x 4096, 16384 deep: four pieces on the 256 tile, the rule's choice; the 128 tile fills the units with two."""
+    piece = 1024 * 4096 * 4
+    rooms = {}
+    try:
+        for tile in (-1, 0, 1):
+            Q.qsync_debug_set_gemm_tile(tile)
+            rooms[tile] = Q.qsync_token_wgrad_workspace_bytes(16384, 1024, 4096, 1), Q.qsync_token_linear_workspace_bytes(1024, 4096, 16384, 1)
+    finally:
+        Q.qsync_debug_set_gemm_tile(-1)
+    assert all(r == 4 * piece for r in rooms[-1] + rooms[0]) and all(r <= 2 * piece for r in rooms[1])
