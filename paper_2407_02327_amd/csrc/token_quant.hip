@@ -561,10 +561,19 @@ hipError_t launch_token_quantize_both(const TokenMatrix& m, const TokenBoth& o, 
     });
 }
 
-// Each pass of the two matrices in one launch.  (The launches of one beside the other's: what a small matrix's take is latency.)
+// Each pass of the two matrices in one launch.  (The launches of one beside the other's: what a small matrix's take is latency.)  One after the other where
+// both together have more threads than a grid counts (2^32; the rest would not run, and no error would say so): columns' scales, 2^31 of one matrix at
+// 2^27 columns of all the sets, and codes, 2^31 at 2^36 of them.
+constexpr int64_t kGridBlocks = (int64_t(1) << 32) / 256;
 hipError_t launch_token_quantize_pair(const TokenMatrix& m, const TokenBoth& o, const TokenMatrix& m2, const TokenBoth& o2, hipStream_t st)
 {
     BothArgs a = both_args(m, o), b = both_args(m2, o2);
+    auto     codes = [](const BothArgs& p) { return static_cast<int64_t>(p.chunks) * p.code_tiles; };
+    if(static_cast<int64_t>(a.scale_blocks) + b.scale_blocks >= kGridBlocks || codes(a) + codes(b) >= kGridBlocks)
+    {
+        const hipError_t e = launch_token_quantize_both(m, o, kNearest, 0, 0, st);
+        return e != hipSuccess ? e : launch_token_quantize_both(m2, o2, kNearest, 0, 0, st);
+    }
     a.pieces = b.pieces = a.pieces > 1 && b.pieces > 1 ? a.pieces : 1;
     return with_type(m.dtype, [&](auto tag) {
         typedef decltype(tag) TA;

@@ -608,3 +608,37 @@ def test_gradients_of_fewer_rows_than_an_operator_was_built_for():
             out.append([t.clone() for t in (op.forward(x, w=w), *op.backward(dy))])
         for a, b in zip(*out):
             assert torch.equal(a, b)
+
+
+def test_two_operands_beyond_a_grid():
+    """Columns of 128 sets whose scales, of one operand as many as the interface allows, would be more workgroups for both than a launch counts."""
+    sets, K = 128, 1 << 20
+    say("token convert, two operands of 2^27 columns")
+    g = torch.Generator(device="cuda").manual_seed(154)
+    x, w = (torch.randn(sets, K, generator=g, device="cuda", dtype=F16) for _ in range(2))
+    offsets = torch.arange(sets + 1, dtype=torch.int32, device="cuda")
+    out = []
+    for joined in (True, False):
+        dst = []
+        for routed in (True, False):
+            dst += [torch.empty(sets, device="cuda"), torch.empty(sets, K, dtype=torch.int8, device="cuda"), torch.empty(sets, K, device="cuda"),
+                    torch.empty(Q.qsync_token_code_rows(sets, sets, routed) * K, dtype=torch.int8, device="cuda")]
+        ws = [torch.empty(Q.qsync_token_quantize_both_workspace_bytes(sets, K, sets, routed), dtype=torch.uint8, device="cuda") for routed in (True, False)]
+        if joined:
+            Q.qsync_token_convert(x, sets, K, K, None, 1, sets, sets, offsets, *dst[:4], w, 1, *dst[4:], *ws)
+        else:
+            Q.qsync_token_quantize_both(x, sets, K, K, None, 1, sets, sets, offsets, Q.ROUND_NEAREST, 0, 0, *dst[:4], None, ws[0])
+            Q.qsync_token_quantize_both(w, sets, K, K, None, 1, sets, sets, None, Q.ROUND_NEAREST, 0, 0, *dst[4:], None, ws[1])
+        torch.cuda.synchronize()
+        out.append(dst)
+    for i, (a, b) in enumerate(zip(*out)):
+        if i == 3:      # (a set has one row; the stretch behind each set's belongs to none)
+            for e in range(sets):
+                start = (R.pad(e) + 128 * e) * K
+                assert torch.equal(a[start:start + 128 * K], b[start:start + 128 * K]), e
+        else:
+            assert torch.equal(a, b), i
+    for t, scale in ((x, out[0][2]), (w, out[0][6])):      # (64-bit quotients of 11-bit values by 127 are near no border of 32 bits)
+        assert torch.equal(scale, torch.where(t == 0, 1.0, t.double().abs() / 127).float())
+    del out, dst, ws
+    torch.cuda.empty_cache()
