@@ -610,6 +610,69 @@ def test_gradients_of_fewer_rows_than_an_operator_was_built_for():
             assert torch.equal(a, b)
 
 
+SERVED = [(16, 64), (1, 1), (33, 130), (1000, 700), (4096, 640), (130, 1024), (50, 1500), (300, 2048), (1000, 4096), (48, 5400), (17, 8190), (130, 16384), (4097, 200)]
+
+
+@pytest.mark.parametrize("rows", [1, 2, 3, 4, 5, 8, 9, 15, 16])
+@pytest.mark.parametrize("N, K", SERVED)
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_every_row_of_a_serving_call(rows, N, K, dtype):
+    """A handful of rows in one launch, one row among them, at every depth of its stages and at the ends of its rule (16384 codes, 4096 columns): each
+    row against the formula, and the bits of the two calls; then with a last row that is not finite."""
+    say("token linear, every row of one call", rows, N, K, dtype)
+    x, w = values(rows, K, dtype, 146, pad=3), values(N, K, F32, 147).contiguous()
+    bias = torch.randn(N, generator=torch.Generator(device="cuda").manual_seed(148), device="cuda")
+    wq, sw = quantize(w, Q.ROUND_NEAREST)
+    ws = torch.empty(Q.qsync_token_linear_workspace_bytes(rows, N, K, 1) + 16, dtype=torch.uint8, device="cuda").random_()
+    wc = R.codes(f64(w), 1)
+    for last in (None, float("nan")):
+        if last is not None:
+            x[rows - 1, K - 1] = last
+        xq, sx = quantize(x, Q.ROUND_NEAREST)
+        a, b = torch.full((rows, N), 7.0, dtype=dtype, device="cuda"), torch.full((rows, N), 7.0, dtype=dtype, device="cuda")
+        Q.qsync_token_linear_fwd(rows, N, K, 1, None, xq, sx, wq, sw, bias, a, ws)
+        Q.qsync_token_linear(x, rows, K, x.stride(0), None, 1, rows, N, 1, None, wq, sw, bias, b, torch.empty_like(sx), torch.empty_like(xq), ws)
+        torch.cuda.synchronize()
+        finite = rows if last is None else rows - 1
+        assert torch.isnan(b[finite:]).all() and torch.isnan(a[finite:]).all()
+        assert torch.equal(a[:finite], b[:finite])
+        if finite:
+            want, bound = R.product(*R.codes(f64(x)[:finite], 1), *wc, f64(bias))
+            assert_within(b[:finite], want, bound + rounded(want, dtype), "y")
+
+
+@pytest.mark.parametrize("M, N, K", [(300, 257, 9000), (130, 1030, 4200), (1000, 4098, 16384), (1024, 4096, 16384), (600, 520, 33000)])
+@pytest.mark.parametrize("tile", [-1, 0, 1, 2])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_pieces_of_every_tile(M, N, K, tile, dtype):
+    """Contractions in pieces on the tile of the rule (the 256 tile for 16384 deep) and on each of the others, outputs that are no whole tiles: forward and
+    weight gradient, some rows against the formula, and all of them bit for bit as without pieces."""
+    say("token product in pieces", M, N, K, tile, dtype)
+    g = torch.Generator(device="cuda").manual_seed(116)
+    a, b = random_codes(M, K, g), random_codes(N, K, g)
+    sa, sb, bias = (torch.rand(M, generator=g, device="cuda") * 1e-3, torch.rand(N, generator=g, device="cuda") * 1e-2, torch.randn(N, generator=g, device="cuda"))
+    out = []
+    try:
+        Q.qsync_debug_set_gemm_tile(tile)
+        forward, wgrad = Q.qsync_token_linear_workspace_bytes(M, N, K, 1), Q.qsync_token_wgrad_workspace_bytes(K, M, N, 1)
+        for pieces in (False, True):
+            ws = torch.empty(max(forward, wgrad), dtype=torch.uint8, device="cuda").random_() if pieces else None
+            y, dw = torch.full((M, N), 7.0, dtype=dtype, device="cuda"), torch.full((M, N), 7.0, dtype=dtype, device="cuda")
+            Q.qsync_token_linear_fwd(M, N, K, 1, None, a, sa, b, sb, bias, y, ws)
+            Q.qsync_token_linear_wgrad(K, M, N, 1, None, a, sa, b, sb, dw, ws)
+            torch.cuda.synchronize()
+            out.append((y, dw))
+    finally:
+        Q.qsync_debug_set_gemm_tile(-1)
+    assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
+    some = sorted({0, 1, 63, 64, 127, 128, M // 2, min(255, M - 1), min(256, M - 1), M - 2, M - 1})
+    codes, scales, b64, sb64 = f64(a[some]), sa.cpu().numpy()[some], f64(b), sb.cpu().numpy()
+    want, bound = R.product(codes, scales, b64, sb64, f64(bias))
+    assert_within(out[1][0][some], want, bound + rounded(want, dtype), "y")
+    want, bound = R.product(codes, scales, b64, sb64)
+    assert_within(out[1][1][some], want, bound + rounded(want, dtype), "dw")
+
+
 def test_two_operands_beyond_a_grid():
     """Columns of 128 sets whose scales, of one operand as many as the interface allows, would be more workgroups for both than a launch counts."""
     sets, K = 128, 1 << 20
