@@ -1291,8 +1291,9 @@ int qsync_token_linear_fwd(int64_t rows, int64_t N, int64_t K, int64_t sets, con
     if(rows == 0 || N == 0) return QSYNC_OK;
     if(workspace && !aligned16(workspace)) return QSYNC_ERR_ALIGN;
     if(!apart(y, rows * N * dtype_bytes(ydt), xq, rows * qsync_token_code_cols(K))) return QSYNC_ERR_UNSUPPORTED;
-    return hip_status(launch_token_product(TokenProduct{static_cast<const int8_t*>(xq), static_cast<const int8_t*>(wq), sx, sw, bias_opt, y, ydt, rows, rows, N, K, sets,
-                                                        offsets_opt}, false, workspace, workspace_bytes, static_cast<hipStream_t>(stream)));
+    const TokenProduct p{static_cast<const int8_t*>(xq), static_cast<const int8_t*>(wq), sx, sw, bias_opt, y, ydt, rows, rows, N, K, sets, offsets_opt};
+    if(!token_product_countable(p, false)) return QSYNC_ERR_UNSUPPORTED;
+    return hip_status(launch_token_product(p, false, workspace, workspace_bytes, static_cast<hipStream_t>(stream)));
 }
 
 int qsync_token_linear(const void* x, int xdt, int64_t x_rows, int64_t K, int64_t ld, const int32_t* source_opt, int64_t group, int64_t rows, int64_t N, int64_t sets,
@@ -1310,6 +1311,7 @@ int qsync_token_linear(const void* x, int xdt, int64_t x_rows, int64_t K, int64_
     if(!apart(xq, qb, x, xb) || !apart(sx, rows * 4, x, xb) || !apart(y, yb, x, xb) || !apart(y, yb, xq, qb)) return QSYNC_ERR_UNSUPPORTED;
     const TokenMatrix  m{x, xdt, x_rows, K, ld, rows, source_opt, static_cast<int>(group)};
     const TokenProduct p{static_cast<const int8_t*>(xq), static_cast<const int8_t*>(wq), sx, sw, bias_opt, y, ydt, rows, rows, N, K, sets, offsets_opt};
+    if(!token_product_countable(p, false)) return QSYNC_ERR_UNSUPPORTED;
     const hipStream_t  st = static_cast<hipStream_t>(stream);
     bool               taken;
     hipError_t         e = launch_token_few(m, p, &taken, st);
@@ -1331,8 +1333,9 @@ int qsync_token_linear_wgrad(int64_t rows, int64_t N, int64_t K, int64_t sets, c
     if(!count_ok(sets * N, K)) return QSYNC_ERR_BAD_SHAPE;
     if(N == 0 || K == 0) return QSYNC_OK;
     if(workspace && !aligned16(workspace)) return QSYNC_ERR_ALIGN;
-    return hip_status(launch_token_product(TokenProduct{static_cast<const int8_t*>(dyqT), static_cast<const int8_t*>(xqT), sdy, sx, nullptr, dw, dwdt, rows, N, K, rows, sets,
-                                                        offsets_opt}, true, workspace, workspace_bytes, static_cast<hipStream_t>(stream)));
+    const TokenProduct p{static_cast<const int8_t*>(dyqT), static_cast<const int8_t*>(xqT), sdy, sx, nullptr, dw, dwdt, rows, N, K, rows, sets, offsets_opt};
+    if(!token_product_countable(p, true)) return QSYNC_ERR_UNSUPPORTED;
+    return hip_status(launch_token_product(p, true, workspace, workspace_bytes, static_cast<hipStream_t>(stream)));
 }
 
 size_t qsync_token_linear_bwd_workspace_bytes(int64_t rows, int64_t N, int64_t K, int64_t sets)
@@ -1362,6 +1365,7 @@ int qsync_token_linear_bwd(int64_t rows, int64_t N, int64_t K, int64_t sets, con
     if(!apart(dx, xb, dw, wb)) return QSYNC_ERR_UNSUPPORTED;
     const TokenProduct x{static_cast<const int8_t*>(dyq), static_cast<const int8_t*>(wqT), sdy, swc, nullptr, dx, dxdt, rows, rows, K, N, sets, offsets_opt};
     const TokenProduct w{static_cast<const int8_t*>(dyqT), static_cast<const int8_t*>(xqT), sdyc, sxc, nullptr, dw, dwdt, rows, N, K, rows, sets, offsets_opt};
+    if(!token_product_countable(x, false) || !token_product_countable(w, true)) return QSYNC_ERR_UNSUPPORTED;
     const hipStream_t  st = static_cast<hipStream_t>(stream);
     if(rows == 0 || N == 0 || K == 0)
     {

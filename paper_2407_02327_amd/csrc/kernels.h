@@ -181,6 +181,7 @@ struct TokenProduct
     const int32_t* offsets;
 };
 size_t token_product_workspace_bytes(bool wgrad, int64_t rows, int64_t M, int64_t N, int64_t K, int64_t sets);      // (of up to that many rows; with less: fewer K splits)
+bool token_product_countable(const TokenProduct& p, bool wgrad);      // whether a grid counts its tiles, the largest at least: the launches below need it
 hipError_t launch_token_product(const TokenProduct& p, bool wgrad, void* workspace, size_t workspace_bytes, hipStream_t st);
 // The data gradient x (forward form) and the weight gradient w of one operator, in one launch where both are small.
 hipError_t launch_token_gradients(const TokenProduct& x, const TokenProduct& w, void* workspace, size_t workspace_bytes, hipStream_t st);

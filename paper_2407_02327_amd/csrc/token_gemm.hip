@@ -314,7 +314,6 @@ template <int BM, int BN, int WGM, int WGN, int ST, bool WGRAD> hipError_t launc
 {
     constexpr int lds = ST * (BM + BN) * kRowBytes + kColumnBytes<BN> + BM * 4;
     const int64_t tiles = most_tiles<WGRAD>(p, BM, BN);
-    if(tiles * sp.splits >= int64_t(1) << 22) return hipErrorInvalidValue;      // (threads that a grid can count)
     static bool set[2][kMaxDevices] = {};
     if(sp.splits > 1)
     {
@@ -389,9 +388,22 @@ int set_rows_fragments(const TokenProduct& p)
     return std::min(one, four) > 0.9 * tile ? 0 : one < four ? 1 : 4;
 }
 
+// The plan of a product, on a larger tile where its own has more threads than a grid counts (2^32).
+template <bool WGRAD> bool countable(const TokenProduct& p, int tile)
+{
+    constexpr int side[3] = {256, 128, 64}, threads[3] = {512, 512, 256};
+    return blocks_of<WGRAD>(p, side[tile], side[tile]) < (int64_t(1) << 32) / threads[tile];
+}
+template <bool WGRAD> GemmPlan countable_plan(const TokenProduct& p)
+{
+    GemmPlan plan = product_plan(WGRAD, p.rows, p.M, p.N, p.K, p.sets, p.offsets != nullptr, p.c_dtype);
+    while(plan.tile > 0 && !countable<WGRAD>(p, plan.tile)) --plan.tile;
+    return plan;
+}
+
 template <bool WGRAD> hipError_t launch_product(const TokenProduct& p, void* workspace, size_t workspace_bytes, hipStream_t st)
 {
-    const GemmPlan plan = product_plan(WGRAD, p.rows, p.M, p.N, p.K, p.sets, p.offsets != nullptr, p.c_dtype);
+    const GemmPlan plan = countable_plan<WGRAD>(p);
     const int64_t  M = WGRAD ? p.M : p.rows, kt = code_pad(WGRAD ? p.rows : p.K) / kRowBytes;
     SplitArgs      sp{workspace, 1, 0};
     // (sums of integers: with less room there are fewer splits, and the same results)
@@ -446,6 +458,8 @@ size_t token_product_workspace_bytes(bool wgrad, int64_t rows, int64_t M, int64_
     }
     return need * N * 4;
 }
+
+bool token_product_countable(const TokenProduct& p, bool wgrad) { return wgrad ? countable<true>(p, 0) : countable<false>(p, 0); }
 
 hipError_t launch_token_product(const TokenProduct& p, bool wgrad, void* workspace, size_t workspace_bytes, hipStream_t st)
 {

@@ -260,3 +260,15 @@ def test_room_follows_a_pinned_tile():
     finally:
         Q.qsync_debug_set_gemm_tile(-1)
     assert all(r == 4 * piece for r in rooms[-1] + rooms[0]) and all(r <= 2 * piece for r in rooms[1])
+
+
+def test_products_of_more_tiles_than_a_grid_counts():
+    """Refused as such, before anything is launched; what fits on larger tiles is not."""
+    wide = dict(rows=1 << 23, N=1 << 20)                                           # 2^27 tiles of 256 x 256
+    assert FWD.but(**wide) == Q.ERR_UNSUPPORTED and FWD.but(offsets=NULL, sets=1, **wide) == Q.ERR_UNSUPPORTED
+    assert FWD.but(rows=1 << 20, N=1 << 16) in OK_OR_NO_GPU                        # 2^20
+    assert SERVE.but(x_rows=1 << 22, **wide) == Q.ERR_UNSUPPORTED
+    assert WGRAD.but(sets=512, N=1, K=1 << 20) in OK_OR_NO_GPU and WGRAD.but(sets=512, N=70, K=1 << 20) in OK_OR_NO_GPU      # 2^21
+    assert WGRAD.but(sets=512, N=1280, K=1 << 20) == Q.ERR_UNSUPPORTED             # 2^21 x 5
+    assert GRADS.but(sets=512, N=1280, K=1 << 20, dw=_at(4000)) == Q.ERR_UNSUPPORTED
+    assert GRADS.but(rows=1 << 23, N=1, K=1 << 20, dx=_at(40), dw=_at(4000)) == Q.ERR_UNSUPPORTED      # (the data gradient's)

@@ -673,6 +673,17 @@ def test_pieces_of_every_tile(M, N, K, tile, dtype):
     assert_within(out[1][1][some], want, bound + rounded(want, dtype), "dw")
 
 
+def test_tiles_of_many_wide_sets():
+    """Gradients of 512 sets without rows, 2^20 columns wide: 2^23 tiles of 64 x 64, all of them zeros."""
+    sets, K = 512, 1 << 20
+    say("token weight gradient, 2^23 tiles")
+    offsets, dw = torch.zeros(sets + 1, dtype=torch.int32, device="cuda"), torch.full((sets, 1, K), 7.0, dtype=BF16, device="cuda")
+    some = torch.zeros(256, dtype=torch.int8, device="cuda")      # (no row's code or scale is read)
+    Q.qsync_token_linear_wgrad(0, 1, K, sets, offsets, some, offsets.view(F32), some, offsets.view(F32), dw, None)
+    torch.cuda.synchronize()
+    assert not dw.any()
+
+
 def test_two_operands_beyond_a_grid():
     """Columns of 128 sets whose scales, of one operand as many as the interface allows, would be more workgroups for both than a launch counts."""
     sets, K = 128, 1 << 20
