@@ -21,6 +21,15 @@ int64_t few_lds(int64_t rows, int64_t kb, int stages) { return kFewWaves * stage
 // 1024x4096 6.6 / 7.4, 4096x4096 8.2 / 8.3, 300x16384 9.8 / 13.0; 4 rows 4096x1024 5.5 / 7.3, 4096x4096 9.2 / 8.8; 16 rows 1024x1024 6.6 / 7.0, 1024x4096
 // 11.1 / 7.0; 1 row 16384x1024 12.2 / 9.6.
 constexpr int64_t kFewElements = 16384, kFewColumns = 4096;
+// wavefronts that share a row: 1, 2, 4 or 8; and whether the longest row of any number of them fits the registers that hold it
+__host__ __device__ constexpr int few_share(int rows) { return rows > 4 ? 1 : rows > 2 ? 2 : rows == 2 ? 4 : 8; }
+constexpr bool few_held()
+{
+    for(int rows = 1; rows <= kFewRows; ++rows)
+        if(kFewElements / rows / 8 > kFewHeld * few_share(rows) * kWaveSize) return false;
+    return true;
+}
+static_assert(few_held(), "a row's vectors stay in registers between its maximum and its codes");
 
 struct FewArgs
 {
@@ -62,8 +71,7 @@ template <typename T, int STAGES> __global__ __launch_bounds__(64 * kFewWaves) v
             sb[e]   = p.sw[c];
             bias[e] = p.bias ? p.bias[c] : 0.0f;
         }
-    // Rows: 1, 2, 4 or 8 wavefronts share one
-    const int share = p.rows > 4 ? 1 : p.rows > 2 ? 2 : p.rows == 2 ? 4 : 8, at_once = kFewWaves / share, part = wave % share;
+    const int share = few_share(p.rows), at_once = kFewWaves / share, part = wave % share;
     const int groups = static_cast<int>(kb / 8), step = share * 64;
     Row8<T>   v[kFewHeld];
     bool      requested = false;
@@ -100,12 +108,6 @@ template <typename T, int STAGES> __global__ __launch_bounds__(64 * kFewWaves) v
 #pragma unroll
         for(int i = 0; i < kFewHeld; ++i)
             if(i * step < groups) fold(v[i]);
-        for(int g = g0 + kFewHeld * step; g < groups; g += step)
-        {
-            Row8<T> d;
-            load(g, d);
-            fold(d);
-        }
 #pragma unroll
         for(int off = 32; off >= 1; off >>= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), off)));
         if(share > 1)
@@ -131,12 +133,6 @@ template <typename T, int STAGES> __global__ __launch_bounds__(64 * kFewWaves) v
 #pragma unroll
             for(int i = 0; i < kFewHeld; ++i)
                 if(i * step < groups && g0 + i * step < groups) put(v[i], g0 + i * step);
-            for(int g = g0 + kFewHeld * step; g < groups; g += step)
-            {
-                Row8<T> d;
-                load(g, d);
-                put(d, g);
-            }
         }
     }
     wg_barrier();
