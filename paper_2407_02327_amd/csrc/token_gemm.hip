@@ -102,14 +102,22 @@ template <int BM, int BN, bool QUARTERS> __device__ __forceinline__ bool set_til
     return false;
 }
 // Weight gradient: every set has the same tiles, but as long a contraction as it has rows.  An XCD takes a contiguous share of all tiles, or, with
-// few sets, an eighth of every set's, the longest sets first (16 sets of different size one after the other by XCD: half of the chip waits for the
-// two longest, 16384 rows, 4096 x 1024 in 142 us, by eighths 124).
-constexpr int kFewSets = 23;
+// few sets of many tiles, an eighth of every set's, the longest sets first (16 sets of different size one after the other by XCD: half of the chip waits for the
+// two longest, 16384 rows, 4096 x 1024 in 142 us, by eighths 124).  Eighths read every set's operands into all L2s, which costs where sets are alike or small.
+// Share / eighths, bfloat16, us: 16384 rows, 1024 x 4096 4 sets 88 / 79, 8 98 / 70, 16 104 / 82, 23 118 / 100, 24 99 / 100, 32 125 / 119, 40 121 / 142, 64 168 / 215, 16 alike
+// of 1024 x 2048 39 / 45; fewer tiles: 16384, 512 x 1024, 16 sets 19 / 22, 8192, 256 x 512, 8 sets 7.8 / 11.8, 4096, 128 x 256, 16 sets 4.3 / 5.2.  Over 213 draws of 2 to 64
+// sets, 128 to 4096 either way, alike to very different: this rule is 1.3 % behind the faster one on average (28 % at most), up to 23 sets whatever their tiles
+// 5.9 % (58 %), shares alone 3.0 % (a factor of 2), eighths alone 12.9 %.
+__host__ __device__ constexpr bool by_eighths(bool offsets, int64_t sets, int64_t tiles, int BM)
+{
+    const int64_t least = BM == 256 ? 1 : BM == 128 ? 48 : 96, all = BM == 64 ? 2 * kNumCu : kNumCu;
+    return offsets && sets <= 23 && tiles >= least && sets * tiles >= all;
+}
 template <int BM, int BN> __device__ __forceinline__ bool set_tile_wgrad(const TokenProduct& p, uint32_t block, int group_m, SetTile& t)
 {
     const int tiles_m = static_cast<int>((p.M + BM - 1) / BM), tiles_n = static_cast<int>((p.N + BN - 1) / BN), tiles = tiles_m * tiles_n;
     t.quarter = -1;
-    if(!p.offsets || p.sets > kFewSets)
+    if(!by_eighths(p.offsets != nullptr, p.sets, tiles, BM))
     {
         const int64_t item = item_of_xcd(block, static_cast<int64_t>(tiles) * p.sets);
         if(item < 0) return false;
@@ -304,11 +312,11 @@ template <bool WGRAD> int64_t blocks_of(const TokenProduct& p, int BM, int BN)
 {
     const int64_t tiles = most_tiles<WGRAD>(p, BM, BN);
     if(!WGRAD) return tiles + kNumXcd + (BM == 256 ? 3 * kRest : 0);
-    if(!p.offsets || p.sets > kFewSets) return (tiles + kNumXcd - 1) / kNumXcd * kNumXcd;
+    if(!by_eighths(p.offsets != nullptr, p.sets, tiles / p.sets, BM)) return (tiles + kNumXcd - 1) / kNumXcd * kNumXcd;
     const int64_t one = tiles / p.sets, left = p.sets % kNumXcd * (one / kNumXcd + 1);
     return kNumXcd * (p.sets / kNumXcd * one + (left < one ? left : one));
 }
-int wgrad_group(const TokenProduct& p) { return p.offsets && p.sets <= kFewSets ? 4 : kGroupM; }
+int wgrad_group(const TokenProduct& p, int BM, int BN) { return by_eighths(p.offsets != nullptr, p.sets, most_tiles<true>(p, BM, BN) / p.sets, BM) ? 4 : kGroupM; }
 
 template <int BM, int BN, int WGM, int WGN, int ST, bool WGRAD> hipError_t launch_tiles(const TokenProduct& p, const SplitArgs& sp, hipStream_t st)
 {
@@ -325,7 +333,7 @@ template <int BM, int BN, int WGM, int WGN, int ST, bool WGRAD> hipError_t launc
     const hipError_t e = allow_lds(&token_gemm_kernel<BM, BN, WGM, WGN, ST, WGRAD>, lds, set[1]);
     if(e != hipSuccess) return e;
     const int64_t blocks = blocks_of<WGRAD>(p, BM, BN);
-    token_gemm_kernel<BM, BN, WGM, WGN, ST, WGRAD><<<static_cast<unsigned>(blocks), 64 * WGM * WGN, lds, st>>>(p, WGRAD ? wgrad_group(p) : kGroupM);
+    token_gemm_kernel<BM, BN, WGM, WGN, ST, WGRAD><<<static_cast<unsigned>(blocks), 64 * WGM * WGN, lds, st>>>(p, WGRAD ? wgrad_group(p, BM, BN) : kGroupM);
     return hipGetLastError();
 }
 
@@ -482,7 +490,7 @@ hipError_t launch_token_gradients(const TokenProduct& x, const TokenProduct& w, 
         static bool   set[kMaxDevices] = {};
         const hipError_t e = allow_lds(&token_pair_kernel<64, 64, 2, 2, 2>, lds, set);
         if(e != hipSuccess) return e;
-        token_pair_kernel<64, 64, 2, 2, 2><<<static_cast<unsigned>(all), 64 * 4, lds, st>>>(x, w, static_cast<uint32_t>(first), kGroupM, wgrad_group(w));
+        token_pair_kernel<64, 64, 2, 2, 2><<<static_cast<unsigned>(all), 64 * 4, lds, st>>>(x, w, static_cast<uint32_t>(first), kGroupM, wgrad_group(w, 64, 64));
         return hipGetLastError();
     }
     const hipError_t e = launch_token_product(x, false, workspace, workspace_bytes, st);

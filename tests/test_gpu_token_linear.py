@@ -673,6 +673,34 @@ def test_pieces_of_every_tile(M, N, K, tile, dtype):
     assert_within(out[1][1][some], want, bound + rounded(want, dtype), "dw")
 
 
+@pytest.mark.parametrize("rows, N, K, sets", [(700, 700, 600, 5), (2500, 1100, 1500, 4), (1500, 900, 1030, 23), (3000, 2100, 2000, 6), (3000, 1030, 1028, 24), (400, 2100, 2000, 8)])
+@pytest.mark.parametrize("tile", [-1, 0, 1, 2])
+def test_weight_gradients_of_few_large_sets(rows, N, K, sets, tile):
+    """Sets of different and of no rows whose tiles are dealt out by eighths, and those next to them that are not; on each tile."""
+    say("token weight gradient, sets of many tiles", rows, N, K, sets, tile)
+    g = torch.Generator().manual_seed(160)
+    cuts = sorted((torch.rand(sets - 1, generator=g) ** 2 * (rows - 9)).long().tolist())
+    cuts[1 if sets > 4 else 0] = cuts[0]                       # (a set without rows)
+    bounds = [0, *sorted(cuts), rows - 9]
+    q = {c: torch.randint(-127, 128, (rows - 9, c), generator=g).numpy() for c in (N, K)}
+    sides = []
+    for cols in (N, K):
+        flat = np.full(Q.qsync_token_code_rows(rows, sets, True) * cols, 99, np.int8)
+        for start, m in R.transposed_layout(q[cols], bounds, True).values():
+            flat[start:start + m.size] = m.reshape(-1)
+        sides.append((torch.from_numpy(flat).cuda(), torch.rand(sets, cols, generator=g).cuda() * 1e-2))
+    dw = torch.full((sets, N, K), 7.0, device="cuda")
+    try:
+        Q.qsync_debug_set_gemm_tile(tile)
+        Q.qsync_token_linear_wgrad(rows, N, K, sets, torch.tensor(bounds, dtype=torch.int32, device="cuda"), *sides[0], *sides[1], dw, None)
+        torch.cuda.synchronize()
+    finally:
+        Q.qsync_debug_set_gemm_tile(-1)
+    for e, (i, j) in enumerate(zip(bounds[:-1], bounds[1:])):
+        want, bound = R.product(q[N][i:j].T, sides[0][1][e].cpu().numpy(), q[K][i:j].T, sides[1][1][e].cpu().numpy())
+        assert_within(dw[e], want, bound + rounded(want, F32), f"set {e}")
+
+
 def test_tiles_of_many_wide_sets():
     """Gradients of 512 sets without rows, 2^20 columns wide: 2^23 tiles of 64 x 64, all of them zeros."""
     sets, K = 512, 1 << 20
