@@ -731,9 +731,8 @@ size_t qsync_distill_topk_workspace_bytes(int ldt, int64_t rows, int64_t cols);
  * Codes along the rows (of the columns, transposed) hold, set after set, a packed matrix [cols][rows of the set rounded up to 128]; the
  * buffer has qsync_token_code_rows(rows, sets, offsets != NULL) * cols bytes.
  * Limits: rows <= 2^23, cols <= 2^20, sets 1..512, of codes along the rows sets * cols <= 2^27 and 2^36 codes, and fewer than 2^23 - 256 tiles
- * of 256 x 256 outputs of a product, a set's rows in tiles of their own (QSYNC_ERR_UNSUPPORTED
- * beyond).  x is of QSYNC_F32, QSYNC_F16 or QSYNC_BF16 at any
- * element's alignment; codes, and the workspace, are 16-byte aligned.  Outputs do not overlap inputs.
+ * of 256 x 256 outputs of a product, a set's rows in tiles of their own (QSYNC_ERR_UNSUPPORTED beyond).  x is of QSYNC_F32, QSYNC_F16 or
+ * QSYNC_BF16 at any element's alignment; codes, and the workspace, are 16-byte aligned.  Outputs do not overlap inputs.
  */
 int64_t qsync_token_code_cols(int64_t cols);
 int64_t qsync_token_code_rows(int64_t rows, int64_t sets, int with_offsets);

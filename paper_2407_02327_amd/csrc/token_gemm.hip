@@ -358,8 +358,9 @@ GemmPlan product_plan(bool wgrad, int64_t rows, int64_t M, int64_t N, int64_t K,
         GemmPlan      plan = plan_gemm(8, m, N, k, -1, -1, true);
         if(plan.tile == 0 && plan.splits == 1 && stores(m)) plan.tile = 1;
         // Operands beyond what the caches in front of the memory hold for them: the 256 tile, which reads half as much, in K splits instead of the
-        // 128 tile without (us, operands from memory: 1024x4096 of 16384 112 -> 83, 2048x2048 of 16384 95 -> 81, 1400x1400 of 16384 73 -> 54;
-        // below, 1024x4096 of 8192 47 -> 59, 1024x1024 of 16384 34 -> 40)
+        // 128 tile without (weight gradients, 128 tile / 256 in pieces, us, operands from memory: 80 Mi 1024x4096 of 16384 rows 114 / 81, 64 Mi 2048x2048 of 16384
+        // 111 / 78, 50 Mi 1024x4096 of 10240 73 / 62, 45 Mi of 9216 65 / 58; below, 40 Mi of 8192 57 / 55, 35 Mi of 7168 50 / 52, 32 Mi 2048x2048 of 8192 51 / 54, 24 Mi of 6144
+        // 37 / 49; operands found in the caches: 80 Mi 80 / 75, 40 Mi 46 / 52)
         else if(!gemm_tile_pinned() && plan.tile == 1 && plan.splits == 1 && (m + N) * k >= (int64_t(44) << 20)) plan = plan_gemm(8, m, N, k, 0, 0, true);
         return plan;
     }
