@@ -166,7 +166,7 @@ class _CodeLinear:
         self.wq, self.sw = e(sets * N, pad(K), dt=i8), e(sets * N)
         self.bias = torch.zeros(*((sets, N) if routed else (N,)), dtype=torch.float32, device=device) if bias else None
         self.y = e(rows, N, dt=y_dtype)
-        self.ws = _scratch(Q.qsync_token_linear_workspace_bytes(rows, N, K, sets), device)
+        self.ws = _scratch(0 if routed else Q.qsync_token_linear_workspace_bytes(rows, N, K, sets), device)      # (of K splits, which the experts' have none of)
         self._converted, self._saved = False, None
         if not training:
             return
@@ -179,7 +179,7 @@ class _CodeLinear:
         self.db = e(*((sets, N) if routed else (N,))) if bias else None
         self.ws_x = _scratch(max(Q.qsync_token_quantize_both_workspace_bytes(rows, c, sets, routed) for c in (N, K)), device)
         self.ws_w = _scratch(Q.qsync_token_quantize_both_workspace_bytes(sets * N, K, sets, False), device)
-        self.ws_bwd = _scratch(Q.qsync_token_linear_bwd_workspace_bytes(rows, N, K, sets), device)
+        self.ws_bwd = _scratch(0 if routed else Q.qsync_token_linear_bwd_workspace_bytes(rows, N, K, sets), device)
 
     def _weights(self, w) -> torch.Tensor:
         if not isinstance(w, torch.Tensor) or w.shape != self.dw_shape:

@@ -272,3 +272,9 @@ def test_products_of_more_tiles_than_a_grid_counts():
     assert WGRAD.but(sets=512, N=1280, K=1 << 20) == Q.ERR_UNSUPPORTED             # 2^21 x 5
     assert GRADS.but(sets=512, N=1280, K=1 << 20, dw=_at(4000)) == Q.ERR_UNSUPPORTED
     assert GRADS.but(rows=1 << 23, N=1, K=1 << 20, dx=_at(40), dw=_at(4000)) == Q.ERR_UNSUPPORTED      # (the data gradient's)
+
+
+def test_experts_keep_no_room_for_pieces():
+    """One expert's rows lie where the route says, too, and such contractions are not split."""
+    one, linear = (c(8192, 64, 4096, *extra, device="cpu") for c, extra in ((ExpertLinear, (1,)), (TokenLinear, ())))
+    assert one.ws.numel() <= 256 and one.ws_bwd.numel() <= 256 < min(linear.ws.numel(), linear.ws_bwd.numel())
